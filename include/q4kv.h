@@ -125,6 +125,46 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
                 const int32_t *seq_len_before, int32_t num_agents, int32_t chunk_len, int32_t layer_begin,
                 int32_t layer_end, void *hip_stream);
 
+/* What a model does to the heads of Q and K between a layer's projections and the cache (Sec. 3.6 names the models).  For
+ * every head row x of k_dim elements:
+ *   norm      elements i < norm_dim become x_i * weight[i] / sqrt(mean of x_j^2 over j < norm_dim + eps); the others stay.
+ *             q_weight and k_weight are device binary32 [layers of the call][norm_dim]; NULL: no norm on Q (on K)
+ *   rotation  of the elements rot_begin .. rot_begin + rot_dim - 1, after the norm: pair (y_i, y_j) of a token at position p
+ *             becomes (y_i c - y_j s, y_j c + y_i s) with c = cos_table[p][n], s = sin_table[p][n] (device binary32
+ *             [table_len][rot_dim / 2]) for the n-th pair: n and n + rot_dim / 2 inside the span, or with `neighbours` != 0
+ *             2n and 2n + 1.  rot_dim == 0: none, the tables are not read.
+ * norm_dim and rot_begin are multiples of 8, rot_dim of 16, both spans lie inside k_dim and may overlap; weights and tables
+ * are 16-byte aligned.  Results are those of binary64 arithmetic rounded once to binary16 (but for a result within about
+ * 2^-50 of itself of a rounding border). */
+typedef struct {
+    const float *q_weight, *k_weight;
+    const float *cos_table, *sin_table;
+    int32_t norm_dim; /* 0 where neither Q nor K is normed */
+    float eps;        /* >= 0 */
+    int32_t rot_begin, rot_dim, neighbours, table_len;
+} q4kv_head_form;
+
+/* q4kv_append behind that: one pass from the projections of new tokens to their queries and cache rows.
+ *   q, k_new, v_new  device, [layers of the call][num_agents][chunk_len] token rows, each token's heads contiguous
+ *                    ([num_q_heads][k_dim], [num_kv_heads][k_dim], [num_kv_heads][v_dim]); *_stride elements from one token
+ *                    row to the next, so that the three may be parts of one fused projection.  Strides are multiples of 8
+ *                    and no smaller than a row, pointers 16-byte aligned.  v_new must be NULL when spec->v_aliases_k.
+ *                    in_format: 0 binary16, 1 bfloat16 (a q4kv_param_format, of all three); values must be finite and, as
+ *                    prepared, inside the binary16 range
+ *   q_out            device out, binary16 [layers][num_agents][chunk_len][num_q_heads][k_dim], 16-byte aligned: what
+ *                    q4kv_batched_attention takes as q.  May not overlap the inputs.
+ *   positions        device int32 [num_agents][chunk_len], or NULL: seq_len_before[a] + c for token c of agent a
+ * V rows are quantized as they are.  Block tables, seq_len_before and skipped tokens as for q4kv_append (a token that finds no
+ * slot still gets its query); with a rotation, a token whose position is outside [0, table_len) is skipped whole: neither its
+ * query nor its rows are written.  The cache gets the bits that q4kv_append makes of the same prepared rows.  Rows of more than
+ * 1,024 elements -> Q4KV_ESHAPE. */
+int q4kv_norm_rope_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const q4kv_head_form *form,
+                          const void *q, const void *k_new, const void *v_new, int32_t in_format, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, uint16_t *q_out, const int32_t *block_table,
+                          int32_t max_blocks, const int32_t *seq_len_before, const int32_t *positions,
+                          int32_t num_agents, int32_t chunk_len, int32_t layer_begin, int32_t layer_end,
+                          void *hip_stream);
+
 /* Sec. 3.4, second half of update_and_fetch, and Sec. 3.6 (GQA grouping, causal chunk masks):
  * out = softmax(sm_scale * q K_hat^T) V_hat per agent, layer and query head, directly on the Q4
  * pools (nothing is dequantized to memory).
@@ -264,9 +304,20 @@ int q4kv_export_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_poo
 int q4kv_import_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const int32_t *block_ids,
                        int32_t num_blocks, const void *image, size_t image_bytes, void *hip_stream);
 
+/* Copies blocks inside the pools: block dst_ids[i] of every layer, K and V, codes and parameters, becomes a copy of block
+ * src_ids[i].  What a fork's last block and the moves of a compaction need (q4kv_block_pool_fork, _truncate, _compact hand out
+ * the pairs), with nothing in between.
+ *   src_ids, dst_ids  device, int32 [num_pairs]; a pair with an id outside [0, pool.num_blocks) or of one id twice is skipped.
+ *                     A block may be the source of any number of pairs; one that is the destination of two pairs, or of one
+ *                     and the source of another, holds afterwards a mixture of their bytes.
+ * Enqueues on hip_stream, allocates nothing.  At most 65,535 layers. */
+int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const int32_t *src_ids,
+                     const int32_t *dst_ids, int32_t num_pairs, void *hip_stream);
+
 /* Sec. 3.1 "Block Pool with Per-Agent Isolation", host side: which 256-token block of the device pools belongs to
  * which agent.  Pure bookkeeping in HOST memory (no device call): a block id is either free or in exactly one agent's
- * list, so two agents can never share or overwrite a block (the paper's namespace isolation); the list order is the
+ * list, so two agents can never share or overwrite a block (the paper's namespace isolation) -- unless the caller forks an
+ * agent, whose full blocks parent and child then both list and neither writes to (below); the list order is the
  * token order, i.e. a row of the block table the attention calls read.  Eviction is the caller's sequence
  * lru_victim -> q4kv_export_blocks -> (file) -> release; a restore is reserve -> q4kv_import_blocks into whatever blocks
  * were free.  Agent ids are caller-chosen non-negative numbers.  Every call locks the pool (thread-safe).
@@ -280,7 +331,23 @@ int q4kv_import_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_poo
  *   table_row     the same as a block-table row: ids, then `fill` up to max_blocks; Q4KV_ERANGE if it owns more
  *   touch         mark the agent most recently used;  pin(1): never a victim while it is in a running batch
  *   lru_victim    the unpinned agent with at least one block that was used least recently, or -1
- *   free_blocks   length of the free list;  owner: the agent id that owns a block, or -1 */
+ *   free_blocks   length of the free list;  owner: the agent id that owns a block (the smallest of those that share it), or -1
+ * Agents that share a prefix:
+ *   fork          a new agent `child` that has the first `tokens` cached tokens of `parent`: it lists the parent's
+ *                 tokens / 256 full blocks too and, where tokens are left over, a free block of its own that must become a
+ *                 copy of the parent's: *copy_from and *copy_to (host) get that pair for q4kv_copy_blocks, or -1.  Returns the
+ *                 number of blocks the child lists; Q4KV_EINVAL if the child is known already or the parent is not,
+ *                 Q4KV_ERANGE if the parent has not that many blocks, Q4KV_ENOSPACE (nothing changed)
+ *   truncate      the agent keeps its first `tokens` tokens: blocks behind them are freed (shared ones when nobody else lists
+ *                 them).  A block that stays in part and is shared is replaced by a free one, with its pair in *copy_from and
+ *                 *copy_to (else -1).  Returns the number of blocks it still lists; errors as for fork
+ *   compact       moves blocks to lower ids until the blocks in use are the lowest ones, but for those of pinned agents, which
+ *                 stay; lists change at once, and the pairs in copy_from[], copy_to[] (host, [cap]) are to be given to ONE call of
+ *                 q4kv_copy_blocks (no block is in both) before any of the blocks is used.  Returns the number of pairs;
+ *                 Q4KV_ERANGE when there are more than cap (nothing changed).  cap == 0: only counts
+ *   shares        agents that list a block (0: free)
+ * release frees a shared block with the last agent that lists it, and returns the number of blocks freed.  A block is shared
+ * only while it is full of tokens that all its agents have, so appending behind one's tokens never writes into it. */
 typedef struct q4kv_block_pool q4kv_block_pool;
 q4kv_block_pool *q4kv_block_pool_create(int32_t num_blocks);
 void q4kv_block_pool_destroy(q4kv_block_pool *pool);
@@ -293,6 +360,12 @@ int32_t q4kv_block_pool_pin(q4kv_block_pool *pool, int64_t agent_id, int32_t pin
 int64_t q4kv_block_pool_lru_victim(q4kv_block_pool *pool);
 int32_t q4kv_block_pool_free_blocks(q4kv_block_pool *pool);
 int64_t q4kv_block_pool_owner(q4kv_block_pool *pool, int32_t block_id);
+int32_t q4kv_block_pool_fork(q4kv_block_pool *pool, int64_t parent_id, int64_t child_id, int64_t tokens, int32_t *copy_from,
+                             int32_t *copy_to);
+int32_t q4kv_block_pool_truncate(q4kv_block_pool *pool, int64_t agent_id, int64_t tokens, int32_t *copy_from,
+                                 int32_t *copy_to);
+int32_t q4kv_block_pool_compact(q4kv_block_pool *pool, int32_t *copy_from, int32_t *copy_to, int32_t cap);
+int32_t q4kv_block_pool_shares(q4kv_block_pool *pool, int32_t block_id);
 
 /* Measurement helper, no part of the method: a kernel that only reads.  Reads the first
  * floor(bytes / 16384) * 16384 bytes of the device buffer `src` (16-byte aligned) exactly once, in the launch

@@ -18,6 +18,8 @@ EXPORTS = ["q4kv_quantize", "q4kv_dequantize", "q4kv_quantize_fmt", "q4kv_dequan
            "q4kv_block_pool_create", "q4kv_block_pool_destroy", "q4kv_block_pool_reserve", "q4kv_block_pool_release",
            "q4kv_block_pool_blocks", "q4kv_block_pool_table_row", "q4kv_block_pool_touch", "q4kv_block_pool_pin",
            "q4kv_block_pool_lru_victim", "q4kv_block_pool_free_blocks", "q4kv_block_pool_owner",
+           "q4kv_block_pool_fork", "q4kv_block_pool_truncate", "q4kv_block_pool_compact", "q4kv_block_pool_shares",
+           "q4kv_copy_blocks", "q4kv_norm_rope_append",
            "q4kv_last_error",
            "q4kv_version"]
 
@@ -41,6 +43,13 @@ PARAMS_F16, PARAMS_BF16 = 0, 1   # q4kv_param_format: type of the stored scale a
 class _CPool(C.Structure):
     """q4kv_pool"""
     _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p), ("bias", C.c_void_p), ("num_blocks", C.c_int32)]
+
+
+class _CHeadForm(C.Structure):
+    """q4kv_head_form"""
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("cos_table", C.c_void_p), ("sin_table", C.c_void_p),
+                ("norm_dim", C.c_int32), ("eps", C.c_float), ("rot_begin", C.c_int32), ("rot_dim", C.c_int32),
+                ("neighbours", C.c_int32), ("table_len", C.c_int32)]
 
 
 _lib = None
@@ -97,6 +106,13 @@ def lib():
         l.q4kv_block_pool_free_blocks.argtypes = [vp]
         l.q4kv_block_pool_owner.restype = i64
         l.q4kv_block_pool_owner.argtypes = [vp, i32]
+        l.q4kv_block_pool_fork.argtypes = [vp, i64, i64, i64, C.POINTER(i32), C.POINTER(i32)]
+        l.q4kv_block_pool_truncate.argtypes = [vp, i64, i64, C.POINTER(i32), C.POINTER(i32)]
+        l.q4kv_block_pool_compact.argtypes = [vp, C.POINTER(i32), C.POINTER(i32), i32]
+        l.q4kv_block_pool_shares.argtypes = [vp, i32]
+        l.q4kv_copy_blocks.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), vp, vp, i32, vp]
+        l.q4kv_norm_rope_append.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), C.POINTER(_CHeadForm), vp, vp, vp,
+                                            i32, i64, i64, i64, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp]
         l.q4kv_last_error.restype = C.c_char_p
         l.q4kv_version.restype = C.c_int
         _lib = l
@@ -150,8 +166,45 @@ class Pool:
             self.scale.fill_(nan_bits)
             self.bias.fill_(nan_bits)
 
+    @classmethod
+    def of(cls, codes, scale, bias):
+        """A pool around arrays that the caller has: int32 codes, int16 bits of scale and bias, shaped as above."""
+        lead = tuple(codes.shape[:-1])
+        if not (codes.dim() == 5 and tuple(scale.shape[:-1]) == lead == tuple(bias.shape[:-1]) and
+                scale.shape[-1] * 8 == codes.shape[-1] == bias.shape[-1] * 8):
+            raise ValueError(f"codes {tuple(codes.shape)}, scale {tuple(scale.shape)} and bias {tuple(bias.shape)} are no pool")
+        for t, kind, name in ((codes, torch.int32, "codes"), (scale, torch.int16, "scale"), (bias, torch.int16, "bias")):
+            _dev(t, kind, name)
+        p = cls.__new__(cls)
+        p.dim, p.num_blocks, p.codes, p.scale, p.bias = codes.shape[-1] * 8, codes.shape[1], codes, scale, bias
+        return p
+
     def c(self):
         return _CPool(self.codes.data_ptr(), self.scale.data_ptr(), self.bias.data_ptr(), self.num_blocks)
+
+
+class HeadForm:
+    """q4kv_head_form: what happens to a head of Q and K before it is used.  q_weight / k_weight: float32
+    [layers of the call][norm_dim] on the GPU or None; cos / sin: float32 [positions][rot_dim / 2] on the GPU or None."""
+
+    def __init__(self, norm_dim=0, q_weight=None, k_weight=None, eps=1e-6, rot_begin=0, rot_dim=0, neighbours=False, cos=None,
+                 sin=None):
+        self.norm_dim, self.q_weight, self.k_weight, self.eps = norm_dim, q_weight, k_weight, eps
+        self.rot_begin, self.rot_dim, self.neighbours, self.cos, self.sin = rot_begin, rot_dim, neighbours, cos, sin
+
+    def c(self, layers):
+        for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+            if t is not None and tuple(t.shape) != (layers, self.norm_dim):
+                raise ValueError(f"{name}: {tuple(t.shape)} instead of {(layers, self.norm_dim)}")
+        table_len = 0
+        if self.rot_dim:
+            if self.cos is None or self.sin is None or self.cos.shape != self.sin.shape or self.cos.dim() != 2 or \
+                    self.cos.shape[1] * 2 != self.rot_dim:
+                raise ValueError(f"cos and sin: one shape, [positions][{self.rot_dim // 2}]")
+            table_len = self.cos.shape[0]
+        return _CHeadForm(_dev(self.q_weight, torch.float32, "q_weight"), _dev(self.k_weight, torch.float32, "k_weight"),
+                          _dev(self.cos, torch.float32, "cos"), _dev(self.sin, torch.float32, "sin"), self.norm_dim, self.eps,
+                          self.rot_begin, self.rot_dim, 1 if self.neighbours else 0, table_len)
 
 
 class BlockPool:
@@ -209,6 +262,33 @@ class BlockPool:
 
     def owner(self, block_id):
         return lib().q4kv_block_pool_owner(self._h, block_id)
+
+    def fork(self, parent_id, child_id, tokens):
+        """The pairs (source block, destination block) that q4kv_copy_blocks is to copy: none or one."""
+        return self._with_pair(lib().q4kv_block_pool_fork, parent_id, child_id, tokens)
+
+    def truncate(self, agent_id, tokens):
+        """As fork()."""
+        return self._with_pair(lib().q4kv_block_pool_truncate, agent_id, tokens)
+
+    def _with_pair(self, call, *args):
+        src, dst = C.c_int32(-1), C.c_int32(-1)
+        self._ok(call(self._h, *args, C.byref(src), C.byref(dst)))
+        return [] if dst.value < 0 else [(src.value, dst.value)]
+
+    def compact(self):
+        """The pairs that one call of q4kv_copy_blocks is to copy before any block is used again."""
+        cap = lib().q4kv_block_pool_compact(self._h, None, None, 0)
+        while self._ok(cap) > 0:
+            src, dst = (C.c_int32 * cap)(), (C.c_int32 * cap)()
+            n = lib().q4kv_block_pool_compact(self._h, src, dst, cap)
+            if n != -3:                       # else another thread has freed blocks in between: more to move
+                return list(zip(src, dst))[:self._ok(n)]
+            cap = lib().q4kv_block_pool_compact(self._h, None, None, 0)
+        return []
+
+    def shares(self, block_id):
+        return self._ok(lib().q4kv_block_pool_shares(self._h, block_id))
 
 
 def q4kv_version():
@@ -299,6 +379,64 @@ def q4kv_append(spec, kpool, vpool, k_new, v_new, block_table, seq_len_before, l
                              _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
                              _dev(seq_len_before, torch.int32, "seq_len_before"), A, Cn, layer_begin, layer_end,
                              _stream()))
+
+
+def _token_rows(t, heads, dim, name):
+    """[layers][agents][chunk][heads][dim] with contiguous tokens a fixed stride apart -> that stride in elements."""
+    if t.dim() != 5 or t.shape[3] != heads or t.shape[4] != dim or not t.is_cuda:
+        raise TypeError(f"{name}: need [layers][agents][chunk][{heads}][{dim}] on the GPU, got {tuple(t.shape)} on {t.device}")
+    Lr, A, Cn = t.shape[:3]
+    # the stride of an axis of one element means nothing: the first axis that has more gives the distance of two tokens
+    stride, rows = None, 1
+    for size, step in ((Cn, t.stride(2)), (A, t.stride(1)), (Lr, t.stride(0))):
+        if size > 1:
+            if stride is None and step % rows == 0:
+                stride = step // rows
+            if stride is None or step != stride * rows:
+                raise TypeError(f"{name}: tokens are not a fixed stride apart (strides {t.stride()})")
+        rows *= size
+    if (dim > 1 and t.stride(4) != 1) or (heads > 1 and t.stride(3) != dim):
+        raise TypeError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
+    return heads * dim if stride is None else stride
+
+
+def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table, seq_len_before, positions=None,
+                          layer_begin=0, layer_end=None, q_out=None):
+    """q / k_new / v_new: fp16 or bf16 [layers_in_call][A][C][heads][dim], possibly parts of one fused projection (tokens a fixed
+    stride apart); form: HeadForm.  Returns the prepared queries, fp16 [layers_in_call][A][C][q_heads][k_dim]."""
+    layer_end = spec.num_layers if layer_end is None else layer_end
+    Lr, A, Cn = q.shape[:3]
+    strides = [_token_rows(q, spec.num_q_heads, spec.k_dim, "q"), _token_rows(k_new, spec.num_kv_heads, spec.k_dim, "k_new"),
+               0 if v_new is None else _token_rows(v_new, spec.num_kv_heads, spec.v_dim, "v_new")]
+    for t, name in ((q, "q"), (k_new, "k_new"), (v_new, "v_new")):
+        if t is not None and (t.dtype != q.dtype or t.shape[:3] != q.shape[:3] or t.dtype not in (torch.float16, torch.bfloat16)):
+            raise TypeError(f"{name}: fp16 or bf16, of one type and leading shape with q, got {t.dtype} {tuple(t.shape)}")
+    if Lr != layer_end - layer_begin:
+        raise ValueError(f"{Lr} layers of projections for {layer_end - layer_begin} layers")
+    if q_out is None:
+        q_out = torch.empty((Lr, A, Cn, spec.num_q_heads, spec.k_dim), dtype=torch.float16, device=q.device)
+    if positions is not None and tuple(positions.shape) != (A, Cn):
+        raise ValueError(f"positions: {tuple(positions.shape)} instead of {(A, Cn)}")
+    kp, cform = kpool.c(), form.c(Lr)
+    vp = None if spec.v_aliases_k else vpool.c()
+    _check(lib().q4kv_norm_rope_append(
+        C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), C.byref(cform), q.data_ptr(), k_new.data_ptr(),
+        None if v_new is None else v_new.data_ptr(), 1 if q.dtype == torch.bfloat16 else 0, *strides,
+        _dev(q_out, torch.float16, "q_out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
+        _dev(seq_len_before, torch.int32, "seq_len_before"), _dev(positions, torch.int32, "positions"), A, Cn, layer_begin,
+        layer_end, _stream()))
+    return q_out
+
+
+def q4kv_copy_blocks(spec, kpool, vpool, src_ids, dst_ids):
+    """Block dst_ids[i] becomes a copy of block src_ids[i], every layer, K and V; ids: int32 tensors on the GPU."""
+    if src_ids.numel() != dst_ids.numel():
+        raise ValueError(f"{src_ids.numel()} sources for {dst_ids.numel()} destinations")
+    kp = kpool.c()
+    vp = None if spec.v_aliases_k else vpool.c()
+    _check(lib().q4kv_copy_blocks(C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp),
+                                  _dev(src_ids, torch.int32, "src_ids"), _dev(dst_ids, torch.int32, "dst_ids"),
+                                  src_ids.numel(), _stream()))
 
 
 def q4kv_default_split_tokens(spec, num_agents, q_len, max_seq_len, layers_in_call):

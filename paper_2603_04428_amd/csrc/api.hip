@@ -277,6 +277,66 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
     return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "append launch: %s", hipGetErrorString(e));
 }
 
+int q4kv_norm_rope_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const q4kv_head_form *form,
+                          const void *q, const void *k_new, const void *v_new, int32_t in_format, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, uint16_t *q_out, const int32_t *block_table,
+                          int32_t max_blocks, const int32_t *seq_len_before, const int32_t *positions,
+                          int32_t num_agents, int32_t chunk_len, int32_t layer_begin, int32_t layer_end, void *hip_stream)
+{
+    int rc = check_spec(spec);
+    if (rc) return rc;
+    if ((rc = check_pool(k, "K"))) return rc;
+    if (spec->v_aliases_k) {
+        if (v || v_new) return fail(Q4KV_EINVAL, "v and v_new must be NULL when v_aliases_k");
+    } else {
+        if ((rc = check_pool(v, "V"))) return rc;
+        if (v->num_blocks != k->num_blocks) return fail(Q4KV_EINVAL, "K and V pools differ in num_blocks");
+    }
+    if (!form) return fail(Q4KV_EINVAL, "form is NULL");
+    if (spec->k_dim > q4kv::head_append_max_dim() || (v && spec->v_dim > q4kv::head_append_max_dim()))
+        return fail(Q4KV_ESHAPE, "rows of more than %d elements", q4kv::head_append_max_dim());
+    if (in_format != Q4KV_PARAMS_F16 && in_format != Q4KV_PARAMS_BF16)
+        return fail(Q4KV_EINVAL, "in_format %d is neither 0 (binary16) nor 1 (bfloat16)", in_format);
+    const q4kv_head_form &f = *form;
+    const bool norm = f.q_weight || f.k_weight;
+    if (f.norm_dim < 0 || f.norm_dim > spec->k_dim || f.norm_dim % 8 || (norm && f.norm_dim == 0))
+        return fail(Q4KV_ESHAPE, "norm_dim %d must be a multiple of 8 up to k_dim, and positive where there are weights", f.norm_dim);
+    if (norm && !(f.eps >= 0.0f)) return fail(Q4KV_EINVAL, "eps must not be negative");
+    if (f.rot_dim < 0 || f.rot_begin < 0 || f.rot_dim > spec->k_dim || f.rot_begin > spec->k_dim - f.rot_dim || f.rot_begin % 8 ||
+        f.rot_dim % 16)
+        return fail(Q4KV_ESHAPE, "rotated span [%d, +%d): a multiple of 8 and one of 16, inside k_dim", f.rot_begin, f.rot_dim);
+    if (!aligned16(f.q_weight) || !aligned16(f.k_weight)) return fail(Q4KV_EINVAL, "weights must be 16-byte aligned");
+    if (f.rot_dim > 0) {
+        if (!f.cos_table || !f.sin_table) return fail(Q4KV_EINVAL, "a rotation without its tables");
+        if (!aligned16(f.cos_table) || !aligned16(f.sin_table)) return fail(Q4KV_EINVAL, "tables must be 16-byte aligned");
+        if (f.table_len < 0) return fail(Q4KV_EINVAL, "table_len < 0");
+    }
+    if (layer_begin < 0 || layer_end > spec->num_layers || layer_begin > layer_end)
+        return fail(Q4KV_EINVAL, "bad layer range [%d, %d)", layer_begin, layer_end);
+    if (num_agents < 0 || chunk_len < 0 || max_blocks <= 0) return fail(Q4KV_EINVAL, "negative count");
+    if (num_agents == 0 || chunk_len == 0 || layer_begin == layer_end) return Q4KV_OK;
+    if (chunk_len > Q4KV_MAX_CHUNK_LEN)
+        return fail(Q4KV_ERANGE, "chunk_len %d is beyond %d tokens: append it in pieces", chunk_len, Q4KV_MAX_CHUNK_LEN);
+    if (num_agents > 65535 || layer_end - layer_begin > 65535)
+        return fail(Q4KV_ERANGE, "at most 65,535 agents and layers in one call");
+    if (!q || !k_new || (v && !v_new) || !q_out || !block_table || !seq_len_before) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out))
+        return fail(Q4KV_EINVAL, "q, k_new, v_new and q_out must be 16-byte aligned");
+    const int64_t q_row = (int64_t)spec->num_q_heads * spec->k_dim, k_row = (int64_t)spec->num_kv_heads * spec->k_dim;
+    const int64_t v_row = (int64_t)spec->num_kv_heads * spec->v_dim;
+    if (q_stride < q_row || k_stride < k_row || (v && v_stride < v_row) || q_stride % 8 || k_stride % 8 || (v && v_stride % 8))
+        return fail(Q4KV_ESHAPE, "token strides %lld, %lld, %lld: multiples of 8, no smaller than a token's row", (long long)q_stride,
+                    (long long)k_stride, (long long)v_stride);
+    // workgroups along the first axis: at most one per token and head
+    if ((int64_t)chunk_len * (spec->num_q_heads + 2 * (int64_t)spec->num_kv_heads) > 0x7fffffffLL)
+        return fail(Q4KV_ERANGE, "more than 2^31 rows per agent in one call: append it in pieces");
+    const q4kv::HeadAppendArgs a = {spec, k, v, form, q, k_new, v_new, q_stride, k_stride, v_stride, q_out, block_table,
+                                    seq_len_before, positions, in_format, max_blocks, num_agents, chunk_len, layer_begin,
+                                    layer_end, compute_units()};
+    const hipError_t e = q4kv::launch_head_append(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "append launch: %s", hipGetErrorString(e));
+}
+
 int32_t q4kv_default_split_tokens(const q4kv_spec *spec, int32_t num_agents, int32_t q_len, int32_t max_seq_len,
                                   int32_t num_layers_in_call)
 {
@@ -582,6 +642,27 @@ int q4kv_import_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_poo
 {
     return block_image_common(spec, k, v, block_ids, num_blocks, const_cast<void *>(image), image_bytes, false,
                               hip_stream);
+}
+
+int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const int32_t *src_ids,
+                     const int32_t *dst_ids, int32_t num_pairs, void *hip_stream)
+{
+    int rc = check_spec(spec);
+    if (rc) return rc;
+    if ((rc = check_pool(k, "K"))) return rc;
+    if (spec->v_aliases_k) {
+        if (v) return fail(Q4KV_EINVAL, "v must be NULL when v_aliases_k");
+    } else {
+        if ((rc = check_pool(v, "V"))) return rc;
+        if (v->num_blocks != k->num_blocks) return fail(Q4KV_EINVAL, "K and V pools differ in num_blocks");
+    }
+    if (num_pairs < 0) return fail(Q4KV_EINVAL, "num_pairs < 0");
+    if (num_pairs == 0) return Q4KV_OK;
+    if (!src_ids || !dst_ids) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (q4kv::image_record_bytes(*spec) >= (1u << 31)) return fail(Q4KV_ESHAPE, "a block of one layer must be below 2^31 bytes");
+    if (spec->num_layers > 65535) return fail(Q4KV_ERANGE, "at most 65,535 layers");
+    const hipError_t e = q4kv::launch_block_copy(*spec, *k, v, src_ids, dst_ids, num_pairs, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "copy launch: %s", hipGetErrorString(e));
 }
 
 int q4kv_read_probe(const void *src, size_t bytes, uint32_t *sink, void *hip_stream)

@@ -1,0 +1,297 @@
+// From a layer's projections to its queries and cache rows in one pass (Sec. 3.4, the first half of update_and_fetch, with
+// what a model does to a head in front of it): per head of Q and K
+//     y_i = x_i w_i / sqrt(mean_{i < norm_dim} x_i^2 + eps)        for i < norm_dim, y_i = x_i behind it or without weights
+//     (y_i, y_j) -> (y_i c - y_j s, y_j c + y_i s)                 for the pairs (i, j) of the rotated span, c and s of the
+//                                                                  token's position from the caller's tables
+// rounded once to binary16; Q goes out, K and the rows of V (as they are) are quantized into the agents' blocks as q4kv_append
+// does.  Done in three passes (norm and rotate Q, the same for K, append) the rows of K travel twice more.
+//
+// What bounds it is memory: 2 bytes in per element of Q, K and V, 2 out for Q and 0.5625 for K and V.  A lane takes 8
+// consecutive elements (16 bytes), a row of up to 512 elements LPR lanes, a wider one two passes of a wave; a row of 192 leaves
+// a quarter of its 32 lanes idle.
+//
+// All arithmetic in front of the rounding is binary64: codes come from roundings, so a result on the other side of a border
+// moves a cache value by a whole scale (a fifteenth of its group's range), and with binary32 about one element in 2,000 is
+// rounded differently.  The vector ALUs do binary64 multiply-adds at the rate of binary32 ones.  Products of a weight and a
+// table entry have 48 bits and are exact; they are taken once per (lane, token) and serve all heads the lane visits.
+#include "q4_device.h"
+#include "q4kv_internal.h"
+#include "quantize_octet.h"
+
+namespace q4kv {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct HeadSection { // Q, K or V
+    const uint16_t *x;
+    int64_t token_stride;  // elements from a token's row to the next token's
+    const float *weight;   // [layers in call][norm_dim] or null
+    int heads, dim, splits; // splits: workgroups that share the heads
+};
+
+struct HeadAppendParams {
+    HeadSection sec[3];
+    uint16_t *q_out;
+    uint32_t *codes[2];
+    uint16_t *scale[2], *bias[2];
+    const float *cos, *sin;
+    const int32_t *block_table, *seq_len_before, *positions;
+    double eps;
+    int norm_dim, rot_begin, rot_dim, neighbours, table_len;
+    int agents, chunk, max_blocks, num_blocks, layer_begin;
+    int tokens_log2; // tokens of a workgroup's rows
+    uint32_t token_chunks;
+};
+
+// binary64 to binary16 in one rounding: what lies below the upper word's 20 fraction bits is folded into the last of them
+// (round to odd), the rest is exact in binary32, and only the conversion to binary16 rounds
+__device__ __forceinline__ half_t half_once(double d)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, d);
+    const uint32_t hi = (uint32_t)(u >> 32) | ((uint32_t)u != 0u ? 1u : 0u);
+    return (half_t)(float)__builtin_bit_cast(double, (uint64_t)hi << 32);
+}
+
+template <bool IN_BF>
+__device__ __forceinline__ void widen(const uint4 &raw, float (&x)[8])
+{
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = IN_BF ? __builtin_bit_cast(float, w[i] << 16) : half_bits_to_float((uint16_t)(w[i] & 0xffffu));
+        x[2 * i + 1] = IN_BF ? __builtin_bit_cast(float, w[i] & 0xffff0000u) : half_bits_to_float((uint16_t)(w[i] >> 16));
+    }
+}
+
+// LPR: lanes of a row (a power of two); CPL: passes over a row.  BF: type of the stored parameters, IN_BF: of the projections.
+template <int LPR, int CPL, bool BF, bool IN_BF>
+__global__ __launch_bounds__(kThreads) void head_append_kernel(HeadAppendParams p)
+{
+    constexpr int ROWS = kThreads / LPR; // rows of a workgroup: 2^tokens_log2 tokens of as many heads as that leaves
+    const int in_row = threadIdx.x % LPR, row = threadIdx.x / LPR;
+    const int a = blockIdx.y, li = blockIdx.z;
+    int split = (int)(blockIdx.x / p.token_chunks), which = 0;
+    const uint32_t token_chunk = blockIdx.x - (uint32_t)split * p.token_chunks;
+    while (split >= p.sec[which].splits) split -= p.sec[which++].splits; // the splits of all sections are the grid's extent
+    const HeadSection s = p.sec[which];
+    const int tokens = 1 << p.tokens_log2, heads_step = ROWS >> p.tokens_log2;
+    const int c = (int)token_chunk * tokens + (row & (tokens - 1));
+    if (c >= p.chunk) return; // the whole row leaves
+
+    const int t = p.seq_len_before[a] + c;
+    const int pos = p.positions ? p.positions[(int64_t)a * p.chunk + c] : t;
+    if (p.rot_dim > 0 && (pos < 0 || pos >= p.table_len)) return;
+    int64_t dst0 = -1; // row of head 0 in the pool
+    if (which > 0) {
+        const int bi = t / kBlockTokens;
+        if (t < 0 || bi >= p.max_blocks) return;
+        const int blk = p.block_table[(int64_t)a * p.max_blocks + bi];
+        if (blk < 0 || blk >= p.num_blocks) return;
+        dst0 = (((int64_t)(p.layer_begin + li) * p.num_blocks + blk) * s.heads) * kBlockTokens + t % kBlockTokens;
+    }
+    const int64_t token = ((int64_t)li * p.agents + a) * p.chunk + c;
+    const uint16_t *src = s.x + token * s.token_stride;
+    const bool prepared = which < 2;
+    const bool normed = prepared && s.weight != nullptr;
+
+    // what a chunk of eight elements is multiplied with: y = (x ca + x' cb) / rms, x' its partners in the rotation
+    double ca[CPL][8], cb[CPL][8];
+    int partner[CPL]; // element the partners begin at; < 0: the chunk is not rotated
+    bool front[CPL];  // under the norm
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+        const int d = 8 * (in_row + LPR * i), r = d - p.rot_begin;
+        front[i] = normed && d < p.norm_dim;
+        partner[i] = -1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ca[i][e] = 1.0;
+            cb[i][e] = 0.0;
+        }
+        if (!prepared || d >= s.dim) continue;
+        float w[8], wp[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = wp[e] = 1.0f;
+        const float *weight = s.weight + (int64_t)li * p.norm_dim;
+        if (front[i]) __builtin_memcpy(w, __builtin_assume_aligned(weight + d, 16), 32);
+        const bool rotated = r >= 0 && r < p.rot_dim;
+        if (rotated) {
+            const int half_span = p.rot_dim / 2;
+            float cs[8], sn[8];
+            const float *cos = p.cos + (int64_t)pos * half_span, *sin = p.sin + (int64_t)pos * half_span;
+            if (p.neighbours) {
+                partner[i] = d;
+                float c4[4], s4[4];
+                __builtin_memcpy(c4, __builtin_assume_aligned(cos + r / 2, 16), 16);
+                __builtin_memcpy(s4, __builtin_assume_aligned(sin + r / 2, 16), 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    cs[e] = c4[e / 2];
+                    sn[e] = (e & 1) ? s4[e / 2] : -s4[e / 2];
+                    wp[e] = w[e ^ 1];
+                }
+            } else {
+                const bool upper = r >= half_span;
+                const int at = upper ? r - half_span : r;
+                partner[i] = upper ? d - half_span : d + half_span;
+                __builtin_memcpy(cs, __builtin_assume_aligned(cos + at, 16), 32);
+                __builtin_memcpy(sn, __builtin_assume_aligned(sin + at, 16), 32);
+                if (normed && partner[i] < p.norm_dim) __builtin_memcpy(wp, __builtin_assume_aligned(weight + partner[i], 16), 32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sn[e] = upper ? sn[e] : -sn[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ca[i][e] = (double)w[e] * (double)cs[e];
+                cb[i][e] = (double)wp[e] * (double)sn[e];
+            }
+        } else if (front[i]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ca[i][e] = (double)w[e];
+        }
+    }
+
+    const int G = s.dim / kGroup;
+    for (int h = split * heads_step + (row >> p.tokens_log2); h < s.heads; h += s.splits * heads_step) {
+        const uint16_t *x_row = src + (int64_t)h * s.dim;
+        uint4 raw[CPL], other[CPL];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            const int d = 8 * (in_row + LPR * i);
+            raw[i] = other[i] = make_uint4(0, 0, 0, 0);
+            if (d < s.dim) raw[i] = *reinterpret_cast<const uint4 *>(x_row + d);
+            if (partner[i] >= 0) other[i] = *reinterpret_cast<const uint4 *>(x_row + partner[i]);
+        }
+        double inv = 1.0;
+        if (normed) {
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                if (!front[i]) continue;
+                float x[8];
+                widen<IN_BF>(raw[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)x[e], (double)x[e], sum);
+            }
+#pragma unroll
+            for (int off = LPR / 2; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, LPR);
+            inv = 1.0 / sqrt(sum / (double)p.norm_dim + p.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            const int chunk = in_row + LPR * i;
+            if (8 * chunk >= s.dim) continue; // whole octets: dim is a multiple of 64
+            uint32_t out[4];
+            if (front[i] || partner[i] >= 0) {
+                float x[8], y[8];
+                widen<IN_BF>(raw[i], x);
+                widen<IN_BF>(other[i], y);
+                // of a pair under the norm one half may lie behind it (norm_dim inside the rotated span)
+                const double own = front[i] ? inv : 1.0;
+                const double theirs = partner[i] >= 0 && normed && (p.neighbours ? 8 * chunk : partner[i]) < p.norm_dim ? inv : 1.0;
+                half_t o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const double mine = (double)x[e] * ca[i][e] * own;
+                    const float xp = p.neighbours ? y[e ^ 1] : y[e];
+                    o[e] = half_once(partner[i] >= 0 ? __builtin_fma((double)xp * theirs, cb[i][e], mine) : mine);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = half2_to_bits(half2_t{o[2 * e], o[2 * e + 1]});
+            } else if (IN_BF) {
+                float x[8];
+                widen<IN_BF>(raw[i], x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = half2_to_bits(half2_t{(half_t)x[2 * e], (half_t)x[2 * e + 1]});
+            } else {
+                out[0] = raw[i].x; out[1] = raw[i].y; out[2] = raw[i].z; out[3] = raw[i].w;
+            }
+            const uint4 y8 = make_uint4(out[0], out[1], out[2], out[3]);
+            if (which == 0) {
+                *reinterpret_cast<uint4 *>(p.q_out + (token * s.heads + h) * s.dim + 8 * chunk) = y8;
+            } else {
+                const int sub = threadIdx.x & 7, pool = which - 1;
+                uint16_t sb, bb;
+                const uint32_t word = quantize_octet<BF>(y8, sub, &sb, &bb);
+                const int64_t dst = dst0 + (int64_t)h * kBlockTokens;
+                p.codes[pool][dst * (s.dim / 8) + chunk] = word;
+                if (sub < 2) (sub == 0 ? p.scale[pool] : p.bias[pool])[dst * G + chunk / 8] = sub == 0 ? sb : bb;
+            }
+        }
+    }
+}
+
+template <int LPR, int CPL>
+hipError_t launch_rows(const HeadAppendParams &p, bool bf, bool in_bf, dim3 grid, hipStream_t stream)
+{
+    const auto kernel = bf ? (in_bf ? head_append_kernel<LPR, CPL, true, true> : head_append_kernel<LPR, CPL, true, false>)
+                           : (in_bf ? head_append_kernel<LPR, CPL, false, true> : head_append_kernel<LPR, CPL, false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+} // namespace
+
+int head_append_max_dim() { return 1024; }
+
+hipError_t launch_head_append(const HeadAppendArgs &a, hipStream_t stream)
+{
+    const q4kv_spec &s = *a.spec;
+    HeadAppendParams p;
+    p.sec[0] = HeadSection{static_cast<const uint16_t *>(a.q), a.q_stride, a.form->q_weight, s.num_q_heads, s.k_dim, 1};
+    p.sec[1] = HeadSection{static_cast<const uint16_t *>(a.k_new), a.k_stride, a.form->k_weight, s.num_kv_heads, s.k_dim, 1};
+    p.sec[2] = HeadSection{static_cast<const uint16_t *>(a.v_new), a.v_stride, nullptr, a.v ? s.num_kv_heads : 0, s.v_dim, a.v ? 1 : 0};
+    p.q_out = a.q_out;
+    const q4kv_pool *const pools[2] = {a.k, a.v ? a.v : a.k};
+    for (int i = 0; i < 2; ++i) {
+        p.codes[i] = pools[i]->codes;
+        p.scale[i] = pools[i]->scale;
+        p.bias[i] = pools[i]->bias;
+    }
+    p.cos = a.form->cos_table;
+    p.sin = a.form->sin_table;
+    p.block_table = a.block_table;
+    p.seq_len_before = a.seq_len_before;
+    p.positions = a.positions;
+    p.eps = a.form->eps;
+    p.norm_dim = a.form->norm_dim;
+    p.rot_begin = a.form->rot_begin;
+    p.rot_dim = a.form->rot_dim;
+    p.neighbours = a.form->neighbours;
+    p.table_len = a.form->table_len;
+    p.agents = a.num_agents;
+    p.chunk = a.chunk_len;
+    p.max_blocks = a.max_blocks;
+    p.num_blocks = a.k->num_blocks;
+    p.layer_begin = a.layer_begin;
+    const int layers = a.layer_end - a.layer_begin;
+    const int dim = a.v && s.v_dim > s.k_dim ? s.v_dim : s.k_dim;
+    const int lanes = dim <= 64 ? 8 : dim <= 128 ? 16 : dim <= 256 ? 32 : 64;
+    const int rows = kThreads / lanes;
+    p.tokens_log2 = 0;
+    while ((1 << p.tokens_log2) < rows && (1 << p.tokens_log2) < a.chunk_len) ++p.tokens_log2;
+    const int tokens = 1 << p.tokens_log2, heads_step = rows / tokens;
+    p.token_chunks = (uint32_t)((a.chunk_len + tokens - 1) / tokens);
+    // A lane visits several heads of its token, with the same weights and table entries in its registers, as soon as the launch
+    // keeps eight workgroups per compute unit without it.
+    const int64_t columns = (int64_t)p.token_chunks * a.num_agents * layers;
+    int total = 0;
+    for (HeadSection &sec : p.sec) {
+        if (sec.heads == 0) continue;
+        const int steps = (sec.heads + heads_step - 1) / heads_step;
+        int per = 1;
+        while (per < 8 && per * 2 <= steps && columns * (steps / (per * 2)) >= 8 * (int64_t)a.compute_units) per *= 2;
+        sec.splits = (steps + per - 1) / per;
+        total += sec.splits;
+    }
+    const dim3 grid(p.token_chunks * (unsigned)total, (unsigned)a.num_agents, (unsigned)layers);
+    const bool bf = s.param_format == Q4KV_PARAMS_BF16, in_bf = a.in_format == Q4KV_PARAMS_BF16;
+    if (dim <= 64) return launch_rows<8, 1>(p, bf, in_bf, grid, stream);
+    if (dim <= 128) return launch_rows<16, 1>(p, bf, in_bf, grid, stream);
+    if (dim <= 256) return launch_rows<32, 1>(p, bf, in_bf, grid, stream);
+    if (dim <= 512) return launch_rows<64, 1>(p, bf, in_bf, grid, stream);
+    return launch_rows<64, 2>(p, bf, in_bf, grid, stream);
+}
+
+} // namespace q4kv

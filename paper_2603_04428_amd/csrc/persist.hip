@@ -57,6 +57,50 @@ __global__ __launch_bounds__(kCopyThreads) void image_copy_kernel(ImageParams p)
     }
 }
 
+// Copies of blocks inside the pools (a fork's last block, the moves of a compaction): (layer, pair) records as above, their
+// pieces read from the source block and written to the destination block.  Only moves bytes: floor = 2 * bytes at the rate
+// of a copy.  A workgroup takes kCopyUnit bytes of one record, kCopyLoads independent 16-byte loads per lane before the
+// first store, and nothing is carried between workgroups, so that a single pair on a few layers already fills the chip.
+constexpr int kCopyLoads = 4;
+constexpr int kCopyUnit = kCopyLoads * kChunkBytes;
+
+struct BlockCopyParams {
+    unsigned char *pool[kPieces];
+    uint32_t piece_bytes[kPieces], piece_off[kPieces];
+    uint32_t record_bytes;
+    const int32_t *src, *dst;
+    int pieces, num_pairs, pool_blocks;
+};
+
+__global__ __launch_bounds__(kCopyThreads) void block_copy_kernel(BlockCopyParams p)
+{
+    typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+    const uint32_t off0 = blockIdx.x * kCopyUnit + threadIdx.x * 16;
+    for (int i = blockIdx.y; i < p.num_pairs; i += gridDim.y) {
+        const int src = p.src[i], dst = p.dst[i];
+        if (src < 0 || src >= p.pool_blocks || dst < 0 || dst >= p.pool_blocks || src == dst) continue;
+        u4_t data[kCopyLoads];
+        unsigned char *to[kCopyLoads];
+#pragma unroll
+        for (int j = 0; j < kCopyLoads; ++j) {
+            const uint32_t off = off0 + j * kChunkBytes;
+            to[j] = nullptr;
+            if (off >= p.record_bytes) continue;
+            int piece = 0;
+#pragma unroll
+            for (int k = 1; k < kPieces; ++k)
+                if (k < p.pieces && off >= p.piece_off[k]) piece = k;
+            unsigned char *base = p.pool[piece] + (off - p.piece_off[piece]);
+            const long long layer = (long long)blockIdx.z * p.pool_blocks;
+            data[j] = *reinterpret_cast<const u4_t *>(base + (layer + src) * p.piece_bytes[piece]);
+            to[j] = base + (layer + dst) * p.piece_bytes[piece];
+        }
+#pragma unroll
+        for (int j = 0; j < kCopyLoads; ++j)
+            if (to[j]) __builtin_nontemporal_store(data[j], reinterpret_cast<u4_t *>(to[j]));
+    }
+}
+
 } // namespace
 
 size_t image_record_bytes(const q4kv_spec &s)
@@ -119,6 +163,34 @@ hipError_t launch_image_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+hipError_t launch_block_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_pool *v, const int32_t *src_ids,
+                             const int32_t *dst_ids, int num_pairs, hipStream_t stream)
+{
+    BlockCopyParams p;
+    const uint32_t rows = (uint32_t)s.num_kv_heads * kBlockTokens;
+    const q4kv_pool *const pools[2] = {&k, v ? v : &k};
+    const int dims[2] = {s.k_dim, s.v_dim};
+    uint32_t off = 0;
+    for (int i = 0; i < kPieces; ++i) {
+        const q4kv_pool &pool = *pools[i / 3];
+        const uint32_t codes = rows * (dims[i / 3] / 8) * 4, params = rows * (dims[i / 3] / kGroup) * 2;
+        p.pool[i] = i % 3 == 0 ? reinterpret_cast<unsigned char *>(pool.codes)
+                               : reinterpret_cast<unsigned char *>(i % 3 == 1 ? pool.scale : pool.bias);
+        p.piece_bytes[i] = i % 3 == 0 ? codes : params;
+        p.piece_off[i] = off;
+        if (i < 3 || v) off += p.piece_bytes[i];
+    }
+    p.pieces = v ? kPieces : 3;
+    p.record_bytes = off;
+    p.src = src_ids;
+    p.dst = dst_ids;
+    p.num_pairs = num_pairs;
+    p.pool_blocks = k.num_blocks;
+    const dim3 grid((p.record_bytes + kCopyUnit - 1) / kCopyUnit, (unsigned)(num_pairs < 65535 ? num_pairs : 65535), (unsigned)s.num_layers);
+    hipLaunchKernelGGL(block_copy_kernel, grid, dim3(kCopyThreads), 0, stream, p);
+    return hipGetLastError();
 }
 
 } // namespace q4kv

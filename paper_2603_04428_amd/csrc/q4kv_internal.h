@@ -19,6 +19,20 @@ hipError_t launch_append(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_p
                          const int32_t *seq_len_before, int num_agents, int chunk_len, int layer_begin, int layer_end,
                          int compute_units, hipStream_t stream);
 
+// head_append.hip: the arguments of q4kv_norm_rope_append (v, v_new: null when the V rows alias the K rows)
+struct HeadAppendArgs {
+    const q4kv_spec *spec;
+    const q4kv_pool *k, *v;
+    const q4kv_head_form *form;
+    const void *q, *k_new, *v_new;
+    int64_t q_stride, k_stride, v_stride;
+    uint16_t *q_out;
+    const int32_t *block_table, *seq_len_before, *positions;
+    int in_format, max_blocks, num_agents, chunk_len, layer_begin, layer_end, compute_units;
+};
+int head_append_max_dim();
+hipError_t launch_head_append(const HeadAppendArgs &a, hipStream_t stream);
+
 constexpr int kFineRecords = 2; // bit that is turned round in the signature of a plan made for more records (csrc/api.hip)
 
 struct AttentionArgs {
@@ -83,6 +97,11 @@ size_t image_record_bytes(const q4kv_spec &s);
 hipError_t launch_image_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_pool *v, const int32_t *block_ids,
                              int num_blocks, void *image, bool to_image, int workgroups_when_on_device,
                              hipStream_t stream);
+
+// copies block src_ids[i] to dst_ids[i] on every layer (v: null when V aliases K); num_pairs > 0, one (layer, block) record
+// below 2^31 bytes, at most 65,535 layers
+hipError_t launch_block_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_pool *v, const int32_t *src_ids,
+                             const int32_t *dst_ids, int num_pairs, hipStream_t stream);
 
 // read_probe.hip: reads bytes / 16,384 * 16,384 bytes of `src` once; `sink` is one device word that may be written
 hipError_t launch_read_probe(const void *src, size_t bytes, uint32_t *sink, int workgroups, hipStream_t stream);

@@ -1,0 +1,184 @@
+"""Forking, truncating and compacting agents in the host-side block pool, against a plain Python model and against what
+sharing must keep: a block that several agents list is full of tokens that all of them have.  No GPU needed."""
+import random
+
+import pytest
+
+from paper_2603_04428_amd import binding as b
+
+
+def test_fork_shares_full_blocks_and_copies_the_rest():
+    p = b.BlockPool(10)
+    p.reserve(1, 700)                                                    # blocks 0, 1, 2
+    assert p.fork(1, 5, 600) == [(2, 3)] and p.blocks(5) == [0, 1, 3]
+    assert [p.shares(i) for i in range(5)] == [2, 2, 1, 1, 0] and p.free_blocks() == 6
+    assert p.fork(5, 0, 512) == [] and p.blocks(0) == [0, 1]             # whole blocks only: nothing to copy
+    assert p.shares(0) == 3 and p.owner(0) == 0 and p.owner(3) == 5
+    assert p.fork(1, 7, 0) == [] and p.blocks(7) == []
+    assert p.fork(1, 8, 100) == [(0, 4)] and p.blocks(8) == [4]          # a partial copy of a shared block
+    assert p.reserve(0, 513) == 3 and p.blocks(0) == [0, 1, 5]           # grows behind what it shares
+    assert p.release(0) == 1 and p.owner(0) == 1                         # its own block; the others still list the rest
+    assert p.release(1) == 1 and p.owner(0) == 5 and p.shares(0) == 1
+    assert p.release(5) == 3 and p.release(8) == 1 and p.release(7) == 0
+    assert p.free_blocks() == 10 and all(p.shares(i) == 0 and p.owner(i) == -1 for i in range(10))
+
+
+def test_fork_refusals_change_nothing():
+    p = b.BlockPool(3)
+    p.reserve(1, 700)
+    for args, code in (((1, 1, 10), -1), ((1, -2, 10), -1), ((9, 2, 0), -1), ((1, 2, -1), -1), ((1, 2, 769), -3), ((1, 2, 700), -6)):
+        with pytest.raises(b.Q4KVError) as e:
+            p.fork(*args)
+        assert e.value.code == code
+        with pytest.raises(b.Q4KVError):
+            p.blocks(2)
+    assert p.free_blocks() == 0 and [p.shares(i) for i in range(3)] == [1, 1, 1]
+    assert p.fork(1, 2, 768) == []                                       # no block needed: fits
+    with pytest.raises(b.Q4KVError):
+        p.fork(1, 2, 0)                                                  # known already
+    l = b.lib()
+    assert l.q4kv_block_pool_fork(None, 1, 2, 0, None, None) == -1 and l.q4kv_block_pool_fork(p._h, 1, 3, 0, None, None) == -1
+    assert l.q4kv_block_pool_truncate(p._h, 1, 0, None, None) == -1 and l.q4kv_block_pool_compact(p._h, None, None, 3) == -1
+    assert l.q4kv_block_pool_shares(p._h, 3) == -1 and l.q4kv_block_pool_shares(p._h, -1) == -1
+
+
+def test_truncate_frees_and_gives_up_a_shared_partial_block():
+    p = b.BlockPool(6)
+    p.reserve(1, 1000)                                                   # 0 .. 3
+    p.fork(1, 2, 1024)
+    assert p.truncate(2, 300) == [(1, 4)] and p.blocks(2) == [0, 4]
+    assert [p.shares(i) for i in range(6)] == [2, 1, 1, 1, 1, 0]
+    assert p.truncate(2, 290) == [] and p.blocks(2) == [0, 4]            # already its own
+    assert p.truncate(1, 256) == [] and p.free_blocks() == 4 and p.blocks(1) == [0]
+    assert p.truncate(1, 0) == [] and p.blocks(1) == [] and p.shares(0) == 1
+    with pytest.raises(b.Q4KVError) as e:
+        p.truncate(2, 513)
+    assert e.value.code == -3
+    q = b.BlockPool(2)
+    q.reserve(1, 300)
+    q.fork(1, 2, 512)
+    with pytest.raises(b.Q4KVError) as e:
+        q.truncate(2, 100)                                               # block 1 stays with agent 1: none is free
+    assert e.value.code == b.BlockPool.ENOSPACE and q.blocks(2) == [0, 1] and q.shares(1) == 2
+    q.truncate(1, 256)
+    assert q.truncate(2, 200) == [(0, 1)] and q.blocks(2) == [1]         # the block it gives up is the one it gets
+
+
+def test_compact_moves_down_around_pinned_blocks():
+    p = b.BlockPool(12)
+    for a in range(4):
+        p.reserve(a, 3 * 256)
+    p.fork(3, 9, 512)
+    p.release(0)
+    p.release(1)                                                         # 0 .. 5 free, 6 .. 11 in use
+    p.pin(2)                                                             # 6, 7, 8 stay
+    assert b.lib().q4kv_block_pool_compact(p._h, None, None, 0) == 3
+    src, dst = (b.C.c_int32 * 2)(), (b.C.c_int32 * 2)()
+    assert b.lib().q4kv_block_pool_compact(p._h, src, dst, 2) == -3 and p.blocks(3) == [9, 10, 11]
+    assert p.compact() == [(11, 0), (10, 1), (9, 2)]
+    assert p.blocks(3) == [2, 1, 0] and p.blocks(9) == [2, 1] and p.blocks(2) == [6, 7, 8]
+    assert p.shares(2) == 2 and p.owner(2) == 3 and p.shares(9) == 0
+    assert p.reserve(7, 1) == 1 and p.blocks(7) == [3]                   # the free list follows
+    p.pin(2, False)
+    assert p.compact() == [(8, 4), (7, 5)] and p.blocks(2) == [6, 5, 4] and p.compact() == []
+
+
+def test_random_operations_against_a_model():
+    rng = random.Random(17)
+    N = 48
+    p = b.BlockPool(N)
+    lists, tokens, free = {}, {}, set(range(N))                          # tokens: cached per agent, in its blocks
+    content = {}                                                         # block -> what its 256 slots hold
+    serial = 0
+
+    def write(a, n):                                                     # the agent appends n tokens
+        nonlocal serial
+        for _ in range(n):
+            t = tokens[a]
+            blk = lists[a][t // 256]
+            assert sum(blk in x for x in lists.values()) == 1            # nobody else reads what it writes into
+            content[blk][t % 256] = serial
+            history[a].append(serial)
+            serial += 1
+            tokens[a] += 1
+
+    def copied(pairs):
+        assert not {s for s, _ in pairs} & {d for _, d in pairs}
+        for s, d in pairs:
+            content[d] = list(content[s])
+
+    history = {}
+    for step in range(1500):
+        op, a = rng.random(), rng.randrange(8)
+        if op < 0.35:
+            n = rng.choice([1, 30, 256, 300])
+            want = tokens.get(a, 0) + n
+            need = -(-want // 256) - len(lists.get(a, []))
+            if need > len(free):
+                with pytest.raises(b.Q4KVError):
+                    p.reserve(a, want)
+                continue
+            p.reserve(a, want)
+            lists.setdefault(a, [])
+            tokens.setdefault(a, 0)
+            history.setdefault(a, [])
+            for _ in range(max(0, need)):
+                blk = min(free)
+                free.remove(blk)
+                lists[a].append(blk)
+                content[blk] = [None] * 256
+            write(a, n)
+        elif op < 0.55 and a in lists:
+            child = rng.randrange(8)
+            n = rng.choice([tokens[a], tokens[a] // 256 * 256, rng.randint(0, tokens[a])])
+            if child in lists or (n % 256 and not free):
+                with pytest.raises(b.Q4KVError):
+                    p.fork(a, child, n)
+                continue
+            pairs = p.fork(a, child, n)
+            lists[child] = lists[a][:n // 256]
+            if n % 256:
+                blk = min(free)
+                free.remove(blk)
+                assert pairs == [(lists[a][n // 256], blk)]
+                lists[child].append(blk)
+            else:
+                assert pairs == []
+            copied(pairs)
+            tokens[child], history[child] = n, history[a][:n]
+        elif op < 0.7 and a in lists:
+            n = rng.randint(0, tokens[a])
+            try:
+                pairs = p.truncate(a, n)
+            except b.Q4KVError as e:
+                assert e.code == b.BlockPool.ENOSPACE and not free
+                continue
+            gone = lists[a][-(-n // 256):]
+            lists[a] = lists[a][:-(-n // 256)]
+            free |= {x for x in gone if not any(x in y for y in lists.values())}
+            if pairs:
+                assert pairs[0][0] == lists[a][-1] and pairs[0][1] == min(free)
+                free.remove(pairs[0][1])
+                lists[a][-1] = pairs[0][1]
+            copied(pairs)
+            tokens[a], history[a] = n, history[a][:n]
+        elif op < 0.8 and a in lists:
+            mine = lists.pop(a)
+            gone = {x for x in mine if not any(x in y for y in lists.values())}
+            assert p.release(a) == len(gone)
+            free |= gone
+            del tokens[a], history[a]
+        elif op < 0.9:
+            pairs = p.compact()
+            copied(pairs)
+            move = dict(pairs)
+            lists = {k: [move.get(x, x) for x in v] for k, v in lists.items()}
+            free = set(range(N)) - {x for v in lists.values() for x in v}
+            assert free == set(range(N - len(free), N))                  # the lowest ids are the ones in use
+        for k, v in lists.items():
+            assert p.blocks(k) == v
+            assert [content[v[t // 256]][t % 256] for t in range(tokens[k])] == history[k]
+        assert p.free_blocks() == len(free)
+        for blk in range(N):
+            users = [k for k, v in lists.items() if blk in v]
+            assert p.shares(blk) == len(users) and p.owner(blk) == (min(users) if users else -1)

@@ -1,0 +1,122 @@
+"""Refusals of the entry points behind forked agents, found on the host before anything is launched (fake pointers)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2603_04428_amd import binding as b
+
+
+def _err():
+    return b.lib().q4kv_last_error().decode()
+
+
+def _pool(nb=4):
+    return b._CPool(0x1000, 0x2000, 0x3000, nb)
+
+
+def test_copy_blocks_argument_errors():
+    l, spec = b.lib(), b.make_spec(2, 4, 2, 128)
+
+    def call(spec=spec, kp=_pool(), vp=_pool(), src=0x4000, dst=0x5000, n=3):
+        return l.q4kv_copy_blocks(C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), src, dst, n, None)
+
+    assert call(n=0, src=None, dst=None) == 0
+    assert call(n=-1) == -1 and "num_pairs" in _err()
+    assert call(src=None) == -1 and call(dst=None) == -1
+    assert call(vp=None) == -1 and call(vp=_pool(5)) == -1
+    assert call(kp=b._CPool(0x1004, 0x2000, 0x3000, 4)) == -1 and "aligned" in _err()
+    assert call(spec=b.make_spec(2, 16, 1, 576, 512, True)) == -1 and "NULL" in _err()
+    assert call(spec=b.make_spec(2, 1 << 16, 1 << 16, 256)) == -2 and "2^31" in _err()
+    assert call(spec=b.make_spec(1 << 17, 4, 2, 128)) == -3
+    assert call(spec=b.make_spec(2, 5, 2, 128)) == -2
+
+
+def _form(**kw):
+    f = dict(q_weight=0x10000, k_weight=0x20000, cos_table=0x30000, sin_table=0x40000, norm_dim=128, eps=1e-6, rot_begin=0, rot_dim=128,
+             neighbours=0, table_len=100)
+    f.update(kw)
+    return b._CHeadForm(**f)
+
+
+def test_norm_rope_append_argument_errors():
+    l, spec = b.lib(), b.make_spec(2, 4, 2, 128)
+
+    def call(spec=spec, kp=_pool(), vp=_pool(), form=_form(), q=0x50000, k=0x60000, v=0x70000, fmt=1, qs=1024, ks=1024, vs=1024, out=0x80000,
+             bt=0x90000, mb=4, sl=0xA0000, pos=None, A=2, Cn=8, lb=0, le=2):
+        return l.q4kv_norm_rope_append(C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), None if form is None else C.byref(form),
+                                       q, k, v, fmt, qs, ks, vs, out, bt, mb, sl, pos, A, Cn, lb, le, None)
+
+    assert call(Cn=0) == 0 and call(A=0) == 0 and call(lb=1, le=1) == 0        # nothing to do
+    assert call(form=None) == -1 and "form" in _err()
+    assert call(fmt=2) == -1 and "in_format" in _err()
+    for bad in (dict(norm_dim=12), dict(norm_dim=136), dict(norm_dim=0), dict(norm_dim=-8), dict(rot_dim=24), dict(rot_dim=144),
+                dict(rot_begin=8), dict(rot_begin=4, rot_dim=16), dict(rot_begin=-8, rot_dim=16), dict(rot_dim=-16)):
+        assert call(form=_form(**bad)) == -2, bad
+    for bad in (dict(eps=-1.0), dict(eps=float("nan")), dict(cos_table=None), dict(sin_table=0x40004), dict(k_weight=0x20008),
+                dict(table_len=-1)):
+        assert call(form=_form(**bad)) == -1, bad
+    assert call(form=_form(q_weight=None, k_weight=None, norm_dim=0, rot_dim=0, cos_table=None, sin_table=None), Cn=0) == 0
+    for bad in (dict(qs=504), dict(ks=248), dict(vs=248), dict(qs=1028), dict(ks=260), dict(vs=-1024)):
+        assert call(**bad) == -2 and "stride" in _err(), bad
+    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(bt=None), dict(sl=None), dict(q=0x50008), dict(k=0x60002),
+                dict(v=0x70004), dict(out=0x80008), dict(le=3), dict(lb=-1), dict(A=-1), dict(Cn=-1), dict(mb=0), dict(vp=None),
+                dict(vp=_pool(5))):
+        assert call(**bad) == -1, bad
+    assert call(Cn=(1 << 20) + 1) == -3 and "chunk_len" in _err()
+    assert call(A=65536) == -3
+    assert call(spec=b.make_spec(2, 4, 2, 1088)) == -2 and "1024" in _err()
+    assert call(spec=b.make_spec(2, 4, 2, 128, 2048), vs=4096) == -2
+    latent = b.make_spec(2, 16, 1, 576, 512, True)
+    assert call(spec=latent) == -1 and "NULL" in _err()
+    assert call(spec=latent, vp=None, v=None, qs=16 * 576, ks=576, vs=0, form=_form(norm_dim=512, rot_begin=512, rot_dim=64), Cn=0) == 0
+
+
+def test_token_strides_of_projections():
+    def rows(t, heads=2, dim=64):
+        t = torch.empty(0).new_empty(0) if t is None else t
+        return b._token_rows(t, heads, dim, "x")
+
+    class OnGpu:  # shapes and strides of a tensor that says it lies on the GPU
+        def __init__(self, t):
+            self.t, self.is_cuda, self.shape, self.device = t, True, t.shape, "cuda"
+
+        def dim(self):
+            return self.t.dim()
+
+        def stride(self, i=None):
+            return self.t.stride() if i is None else self.t.stride(i)
+
+    whole = torch.empty(3, 2, 5, 512)
+    part = whole[..., 128:256].unflatten(-1, (2, 64))
+    assert rows(OnGpu(part)) == 512
+    assert rows(OnGpu(torch.empty(3, 2, 5, 2, 64))) == 128
+    assert rows(OnGpu(part[:1, :1, :1])) == 128                          # one token: any stride says the same
+    assert rows(OnGpu(part[:, :, :1][:, :1])) == 2 * 5 * 512             # one token per layer
+    assert rows(OnGpu(part[:, :1, :1][:1])) == 128
+    assert rows(OnGpu(torch.empty(0, 2, 5, 2, 64))) == 128
+    for bad in (part.transpose(0, 1), part[:, :, ::2], torch.empty(3, 2, 5, 64, 2).transpose(3, 4), part.flip(2)[:, :, :, :1],
+                torch.empty(3, 2, 5, 2, 128)[..., ::2]):
+        with pytest.raises(TypeError):
+            rows(OnGpu(bad))
+    with pytest.raises(TypeError):
+        rows(part)                                                       # not on the GPU
+
+
+def test_pool_around_arrays_and_head_forms_check_their_shapes():
+    codes, par = torch.zeros(1, 2, 1, 256, 8, dtype=torch.int32), torch.zeros(1, 2, 1, 256, 1, dtype=torch.int16)
+    with pytest.raises(ValueError):
+        b.Pool.of(codes, par, par[:, :1])
+    with pytest.raises(ValueError):
+        b.Pool.of(codes[0], par[0], par[0])
+    with pytest.raises(TypeError):
+        b.Pool.of(codes, par, par)                                       # not on the GPU
+    w = torch.ones(2, 64)
+    with pytest.raises(ValueError):
+        b.HeadForm(norm_dim=64, q_weight=w).c(3)
+    with pytest.raises(ValueError):
+        b.HeadForm(rot_dim=64, cos=torch.ones(10, 16), sin=torch.ones(10, 16)).c(1)
+    with pytest.raises(ValueError):
+        b.HeadForm(rot_dim=64, cos=torch.ones(10, 32)).c(1)
+    c = b.HeadForm().c(1)
+    assert c.q_weight is None and c.rot_dim == 0 and c.table_len == 0

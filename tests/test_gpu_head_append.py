@@ -1,0 +1,228 @@
+"""q4kv_norm_rope_append against its formula in 64 bits, bit for bit: queries are the binary64 result rounded once to
+binary16 (numpy rounds once), cache rows are what the CPU oracle quantizes of rows prepared in the same way.  A result
+within 2^-48 of itself of a rounding border could differ; the inputs here hold none (a chance of 1e-9 per test)."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2603_04428_amd import binding as b
+from tests.gpu_util import DEV, bits
+
+pytestmark = pytest.mark.gpu
+
+BASE = 10000.0
+
+
+def tables(n, rot):
+    angle = np.arange(n)[:, None] * BASE ** (-np.arange(rot // 2) * 2.0 / max(rot, 1))
+    return np.cos(angle).astype(np.float32), np.sin(angle).astype(np.float32)
+
+
+def prepared(x, pos, weight, f, cos, sin):
+    """x [L][A][C][H][D] float64, pos [A][C]; the definition, element pair by element pair."""
+    y = x.copy()
+    if weight is not None:
+        n = f["norm_dim"]
+        y[..., :n] *= weight[:, None, None, None].astype(np.float64) / np.sqrt((x[..., :n] ** 2).mean(-1, keepdims=True) + float(np.float32(f["eps"])))
+    r0, rot = f["rot_begin"], f["rot_dim"]
+    z = y.copy()
+    for i in range(rot // 2):
+        p, q = (r0 + 2 * i, r0 + 2 * i + 1) if f["neighbours"] else (r0 + i, r0 + i + rot // 2)
+        c, s = cos[pos, i].astype(np.float64)[None, :, :, None], sin[pos, i].astype(np.float64)[None, :, :, None]
+        z[..., p] = y[..., p] * c - y[..., q] * s
+        z[..., q] = y[..., q] * c + y[..., p] * s
+    return z.astype(np.float16)
+
+
+class Problem:
+    """Projections, tables and poisoned pools on both sides."""
+
+    def __init__(self, L, Hq, Hkv, dk, dv, alias, before, C, norm=0, norm_q=True, norm_k=True, rot=(0, 0), neighbours=False, in_bf=False,
+                 fused=False, fmt=0, positions=None, table_len=None, seed=0, spread=1.0, layer_begin=0, num_layers=None):
+        rng = np.random.default_rng(seed)
+        A = len(before)
+        self.L, self.A, self.C, self.lb = L, A, C, layer_begin
+        self.spec = b.make_spec(num_layers or layer_begin + L, Hq, Hkv, dk, dv, alias, param_format=fmt)
+        self.ospec = oracle.make_spec(num_layers or layer_begin + L, Hq, Hkv, dk, dv, alias, param_format=fmt)
+        kind = torch.bfloat16 if in_bf else torch.float16
+        widths = [Hq * dk, Hkv * dk] + ([] if alias else [Hkv * dv])
+        x = torch.from_numpy(rng.standard_normal((L, A, C, sum(widths))) * spread).to(kind)
+        parts = x.split(widths, -1) if fused else [t.contiguous() for t in x.split(widths, -1)]
+        heads = [t.unflatten(-1, (h, -1)) for t, h in zip(parts, (Hq, Hkv, Hkv))]
+        on_gpu = x.to(DEV)
+        gparts = on_gpu.split(widths, -1) if fused else [t.contiguous() for t in on_gpu.split(widths, -1)]
+        self.g = [t.unflatten(-1, (h, -1)) for t, h in zip(gparts, (Hq, Hkv, Hkv))] + ([None] if alias else [])
+        self.h = [t.double().numpy() for t in heads] + ([None] if alias else [])
+        self.f = dict(norm_dim=norm, eps=1e-5, rot_begin=rot[0], rot_dim=rot[1], neighbours=neighbours)
+        weights = [(1 + 0.2 * rng.standard_normal((L, norm))).astype(np.float32) if norm and on else None for on in (norm_q, norm_k)]
+        self.w = weights
+        self.before = np.array(before, np.int32)
+        self.pos = self.before[:, None] + np.arange(C) if positions is None else positions
+        n = table_len or int(self.pos.max(initial=0)) + 1
+        self.cos, self.sin = tables(n, rot[1])
+        dev = lambda a: None if a is None else torch.from_numpy(a).to(DEV)  # noqa: E731
+        self.form = b.HeadForm(q_weight=dev(weights[0]), k_weight=dev(weights[1]), cos=dev(self.cos) if rot[1] else None,
+                               sin=dev(self.sin) if rot[1] else None, **self.f)
+        self.positions = None if positions is None else torch.from_numpy(positions.astype(np.int32)).to(DEV)
+        pages = [max(0, n + C + 255) // 256 for n in before]
+        ids = rng.permutation(sum(pages) + 2).astype(np.int32)
+        self.table = np.full((A, max(max(pages), 1)), ids[-1], np.int32)
+        at = 0
+        for a, n in enumerate(pages):
+            self.table[a, :n] = ids[at:at + n]
+            at += n
+        nb, nan = len(ids), 0x7FC0 if fmt else 0x7E00
+        self.kp, self.vp = b.Pool(self.spec, dk, nb, DEV, True), None if alias else b.Pool(self.spec, dv, nb, DEV, True)
+        self.okp = oracle.Pool(self.ospec, dk, nb, fill=nan)
+        self.ovp = None if alias else oracle.Pool(self.ospec, dv, nb, fill=nan)
+
+    def call(self, q_out=None, table=None, before=None):
+        return b.q4kv_norm_rope_append(self.spec, self.kp, self.vp, self.form, *self.g,
+                                       torch.from_numpy(self.table if table is None else table).to(DEV),
+                                       torch.from_numpy(self.before if before is None else before).to(DEV), self.positions, self.lb, self.lb + self.L, q_out)
+
+    def want_rows(self):
+        pos = np.clip(self.pos, 0, len(self.cos) - 1)
+        q = prepared(self.h[0], pos, self.w[0], self.f, self.cos, self.sin)
+        k = prepared(self.h[1], pos, self.w[1], self.f, self.cos, self.sin)
+        return q, k, None if self.h[2] is None else self.h[2].astype(np.float16)
+
+    def check_pools(self):
+        for got, want in ((self.kp, self.okp), (self.vp, self.ovp)):
+            if got is not None:
+                for name in ("codes", "scale", "bias"):
+                    assert np.array_equal(bits(getattr(got, name)), getattr(want, name)), name
+
+    def check(self):
+        q_out = self.call()
+        q, k, v = self.want_rows()
+        oracle.append(self.ospec, self.okp, self.ovp, k, v, self.table, self.before, self.lb, self.lb + self.L)
+        torch.cuda.synchronize()
+        assert np.array_equal(bits(q_out), q.view(np.uint16))
+        self.check_pools()
+
+
+CASES = {
+    # one token each, the smallest rows
+    "step_64": dict(L=1, Hq=4, Hkv=1, dk=64, dv=64, alias=False, before=(0, 255, 256), C=1, norm=64, rot=(0, 32)),
+    # a decode step from a fused bfloat16 projection, norm and rotation over the whole head
+    "step_256_fused": dict(L=2, Hq=16, Hkv=8, dk=256, dv=256, alias=False, before=(700, 3, 511, 0, 1024), C=1, norm=256, rot=(0, 256), in_bf=True, fused=True),
+    # rotation alone, odd chunk over a page border, bfloat16 parameters
+    "turn_128": dict(L=2, Hq=8, Hkv=2, dk=128, dv=128, alias=False, before=(250, 0, 300), C=37, rot=(0, 128), fused=True, fmt=1),
+    # the last 64 of 192 rotated as neighbours, values narrower than keys
+    "per_head": dict(L=1, Hq=3, Hkv=3, dk=192, dv=128, alias=False, before=(5, 900), C=9, rot=(128, 64), neighbours=True, in_bf=True),
+    # keys narrower than values
+    "wide_values": dict(L=1, Hq=2, Hkv=1, dk=64, dv=320, alias=False, before=(17,), C=5, norm=64, rot=(32, 16)),
+    # a shared latent: norm over 512, rotation behind it, K only
+    "latent": dict(L=2, Hq=16, Hkv=1, dk=576, dv=512, alias=True, before=(0, 100, 256), C=21, norm=512, norm_q=False, rot=(512, 64), neighbours=True, fmt=1),
+    # nothing to prepare: the bits of q4kv_append
+    "plain": dict(L=1, Hq=2, Hkv=2, dk=128, dv=64, alias=False, before=(30, 260), C=70),
+    # the norm ends inside the rotated span (pairs with one half under it)
+    "norm_cuts_rotation": dict(L=1, Hq=2, Hkv=2, dk=128, dv=128, alias=False, before=(1, 2), C=6, norm=72, rot=(16, 96)),
+    "norm_cuts_neighbours": dict(L=1, Hq=2, Hkv=2, dk=128, dv=128, alias=False, before=(1, 2), C=6, norm=72, rot=(16, 96), neighbours=True),
+    # norm on one side only, wide and tiny values
+    "norm_q_only": dict(L=1, Hq=4, Hkv=2, dk=128, dv=128, alias=False, before=(9,), C=11, norm=128, norm_k=False, rot=(0, 64), spread=100.0),
+    "tiny": dict(L=1, Hq=4, Hkv=2, dk=64, dv=64, alias=False, before=(9,), C=11, norm=64, norm_q=False, rot=(0, 64), spread=1e-4),
+    # widest rows
+    "wide_1024": dict(L=1, Hq=2, Hkv=1, dk=1024, dv=1024, alias=False, before=(0, 255), C=3, norm=1024, rot=(0, 1024)),
+    # long chunks of several agents: a lane visits several heads
+    "prefill": dict(L=1, Hq=16, Hkv=8, dk=256, dv=256, alias=False, before=(0, 77, 1000), C=700, norm=256, rot=(0, 256), in_bf=True, fused=True),
+    "prefill_64": dict(L=3, Hq=8, Hkv=1, dk=64, dv=64, alias=False, before=(0, 77, 1000), C=1031, norm=64, rot=(0, 32), fused=True),
+    # far positions of a few tokens, layers 1 and 2 of four
+    "far": dict(L=2, Hq=4, Hkv=2, dk=128, dv=128, alias=False, before=(3, 4), C=4, norm=128, rot=(0, 128), layer_begin=1, num_layers=4,
+                positions=np.array([[0, 131071, 65536, 7], [99999, 2, 131070, 1]])),
+}
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_matches_the_formula_in_64_bits(name):
+    Problem(seed=sum(map(ord, name)), **CASES[name]).check()
+
+
+def test_without_norm_and_rotation_it_is_the_append():
+    p = Problem(1, 2, 2, 128, 64, False, (30, 260), 70, seed=3)
+    q_out = p.call()
+    kp, vp = b.Pool(p.spec, 128, p.kp.num_blocks, DEV, True), b.Pool(p.spec, 64, p.kp.num_blocks, DEV, True)
+    b.q4kv_append(p.spec, kp, vp, p.g[1], p.g[2], torch.from_numpy(p.table).to(DEV), torch.from_numpy(p.before).to(DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(q_out, p.g[0])
+    for x, y in ((p.kp, kp), (p.vp, vp)):
+        assert torch.equal(x.codes, y.codes) and torch.equal(x.scale, y.scale) and torch.equal(x.bias, y.bias)
+
+
+def test_rows_of_zeros_and_equal_values():
+    p = Problem(1, 2, 1, 64, 64, False, (0,), 4, norm=64, rot=(0, 64), seed=4)
+    for g, h in zip(p.g, p.h):
+        g[:, :, 1], h[:, :, 1] = 0, 0
+        g[:, :, 2], h[:, :, 2] = -1.5, -1.5
+    p.check()
+
+
+def test_skipped_tokens_leave_everything_as_it_was():
+    """Positions outside the tables: nothing is written.  No slot (table too short, bad block id, negative length): the query is."""
+    L, A, C = 1, 4, 3
+    p = Problem(L, 2, 1, 64, 64, False, (0, 510, 20, 5), C, rot=(0, 64), seed=5,
+                positions=np.array([[0, -1, 2], [8, 9, 10], [30, 31, 32], [1, 40, 3]]), table_len=32)
+    table = p.table[:, :2].copy()          # agent 1: tokens 510, 511 fit, 512 does not
+    table[2, 0] = p.kp.num_blocks          # agent 2: a block id outside the pool
+    before = p.before.copy()
+    before[3] = -2                         # agent 3: tokens -2, -1 have no slot, token 0 has
+    q_out = torch.full((L, A, C, 2, 64), 7.0, dtype=torch.float16, device=DEV)
+    p.call(q_out, table, before)
+    q, k, v = p.want_rows()
+    whole = np.array([[1, 0, 1], [1, 1, 1], [1, 1, 0], [1, 0, 1]], bool)   # position inside [0, 32)
+    slots = {(0, 0): 0, (0, 2): 2, (1, 0): 510, (1, 1): 511, (3, 2): 0}
+    for (a, c), t in slots.items():
+        oracle.append(p.ospec, p.okp, p.ovp, k[:, a:a + 1, c:c + 1], v[:, a:a + 1, c:c + 1], table[a:a + 1], np.array([t], np.int32))
+    torch.cuda.synchronize()
+    want = np.where(whole[None, :, :, None, None], q, np.float16(7.0))
+    assert np.array_equal(bits(q_out), want.view(np.uint16))
+    p.check_pools()
+
+
+def test_on_a_side_stream_and_captured():
+    p = Problem(1, 4, 2, 128, 128, False, (12, 250), 10, norm=128, rot=(0, 128), seed=6, in_bf=True, fused=True)
+    q, k, v = p.want_rows()
+    oracle.append(p.ospec, p.okp, p.ovp, k, v, p.table, p.before)
+    table, before = torch.from_numpy(p.table).to(DEV), torch.from_numpy(p.before).to(DEV)
+    q_out = torch.zeros((1, 2, 10, 4, 128), dtype=torch.float16, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def call():
+        b.q4kv_norm_rope_append(p.spec, p.kp, p.vp, p.form, *p.g, table, before, q_out=q_out)
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    assert np.array_equal(bits(q_out), q.view(np.uint16))
+    p.check_pools()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        q_out.zero_()
+        for pool in (p.kp, p.vp):
+            pool.codes.fill_(-1)
+            pool.scale.fill_(0x7E00)
+            pool.bias.fill_(0x7E00)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(bits(q_out), q.view(np.uint16))
+        p.check_pools()
+
+
+def test_types_and_shapes_that_do_not_fit_are_refused():
+    p = Problem(1, 4, 2, 128, 128, False, (0,), 2, seed=7)
+    table, before = torch.from_numpy(p.table).to(DEV), torch.from_numpy(p.before).to(DEV)
+
+    def call(q=p.g[0], k=p.g[1], v=p.g[2], **kw):
+        return b.q4kv_norm_rope_append(p.spec, p.kp, p.vp, p.form, q, k, v, table, before, **kw)
+    for bad in (dict(q=p.g[0].float()), dict(k=p.g[1].bfloat16()), dict(v=p.g[2][:, :, :1]), dict(q=p.g[0].cpu()),
+                dict(k=p.g[1].transpose(3, 4).contiguous().transpose(3, 4)), dict(q_out=torch.empty(1, dtype=torch.float32, device=DEV))):
+        with pytest.raises(TypeError):
+            call(**bad)
+    with pytest.raises(ValueError):
+        call(positions=torch.zeros((2, 2), dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        call(layer_begin=1)
