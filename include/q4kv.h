@@ -242,6 +242,33 @@ int q4kv_batched_attention_planned(const q4kv_spec *spec, const q4kv_pool *k, co
                                    int32_t layer_begin, int32_t layer_end, void *workspace, size_t workspace_bytes,
                                    void *hip_stream);
 
+/* Decode attention (q_len == 1) of agents that share prefixes: q4kv_batched_attention on global layers, with the tokens that
+ * a group of agents has in common read once for all of them (Sec. 3.4, the decode loop of a batch; q4kv_block_pool_fork makes such
+ * agents).  With ten agents behind a common prompt of 8,192 tokens the cache that a step reads is a seventh.
+ *   group_begin  device int32 [num_groups + 1]: group g is agents group_begin[g] .. group_begin[g + 1] - 1; ascending.  Agents
+ *                outside all groups share nothing.  Bounds that fall are read as the largest one in front of them, and bounds
+ *                outside [0, num_agents] as the nearest in it.
+ *   prefix_len   device int32 [num_groups]: the first prefix_len[g] tokens are the same for all agents of group g.  They are read
+ *                through the block-table row of the group's FIRST agent, which must list them, in whole 64-token tiles (what is
+ *                left of the last one is read through every agent's own row, as are its further tokens), and no further than
+ *                max_seq_len.  A row sees the first seq_len[a] tokens as ever, also where that is less than prefix_len.
+ *   num_groups   0: nobody shares anything, the two arrays may be NULL.  No more than num_agents
+ *   workspace    device scratch of at least q4kv_shared_prefix_workspace_bytes(...) bytes, 16-byte aligned; contents before and
+ *                after the call are unspecified.  Calls that overlap in time need one each.
+ * All other arguments, block ids outside the pool, rows that see no token (zeros) and run-to-run identical bits as for
+ * q4kv_batched_attention; the order of a row's sum is another one, so the bits are in general not that call's.  At most 512
+ * agents (more -> Q4KV_ERANGE).  Head shapes: k_dim == v_dim of 64, 128 or 256, or 192 and 128; at most 16 query heads per KV
+ * head; no shared latent (Q4KV_ESHAPE). */
+int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const uint16_t *q,
+                                 uint16_t *out, const int32_t *block_table, int32_t max_blocks, const int32_t *seq_len,
+                                 int32_t num_agents, const int32_t *group_begin, const int32_t *prefix_len,
+                                 int32_t num_groups, int32_t max_seq_len, float sm_scale, int32_t layer_begin,
+                                 int32_t layer_end, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace q4kv_shared_prefix_attention needs for these arguments, whatever the groups.  0 on bad arguments. */
+size_t q4kv_shared_prefix_workspace_bytes(const q4kv_spec *spec, int32_t num_agents, int32_t max_seq_len,
+                                          int32_t num_layers_in_call);
+
 /* For callers that cannot allocate device memory or have none to hand over -- code recording a HIP graph, tight
  * serving loops that call once per layer, harnesses that forbid hipMalloc: q4kv_batched_attention with the decode
  * path's workspace (tile plan and partial results) taken from a fixed array of Q4KV_STATIC_SCRATCH_BYTES bytes that

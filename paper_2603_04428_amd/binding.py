@@ -19,7 +19,7 @@ EXPORTS = ["q4kv_quantize", "q4kv_dequantize", "q4kv_quantize_fmt", "q4kv_dequan
            "q4kv_block_pool_blocks", "q4kv_block_pool_table_row", "q4kv_block_pool_touch", "q4kv_block_pool_pin",
            "q4kv_block_pool_lru_victim", "q4kv_block_pool_free_blocks", "q4kv_block_pool_owner",
            "q4kv_block_pool_fork", "q4kv_block_pool_truncate", "q4kv_block_pool_compact", "q4kv_block_pool_shares",
-           "q4kv_copy_blocks", "q4kv_norm_rope_append",
+           "q4kv_copy_blocks", "q4kv_norm_rope_append", "q4kv_shared_prefix_attention", "q4kv_shared_prefix_workspace_bytes",
            "q4kv_last_error",
            "q4kv_version"]
 
@@ -113,6 +113,10 @@ def lib():
         l.q4kv_copy_blocks.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), vp, vp, i32, vp]
         l.q4kv_norm_rope_append.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), C.POINTER(_CHeadForm), vp, vp, vp,
                                             i32, i64, i64, i64, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp]
+        l.q4kv_shared_prefix_attention.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), vp, vp, vp, i32, vp, i32, vp, vp,
+                                                   i32, i32, C.c_float, i32, i32, vp, C.c_size_t, vp]
+        l.q4kv_shared_prefix_workspace_bytes.restype = C.c_size_t
+        l.q4kv_shared_prefix_workspace_bytes.argtypes = [C.POINTER(Spec), i32, i32, i32]
         l.q4kv_last_error.restype = C.c_char_p
         l.q4kv_version.restype = C.c_int
         _lib = l
@@ -476,6 +480,37 @@ def q4kv_batched_attention(spec, kpool, vpool, q, block_table, seq_len, max_seq_
         _check(lib().q4kv_batched_attention_windows(*common, windows, *tail))
     else:
         _check(lib().q4kv_batched_attention(*common, int(window), *tail))
+    return out
+
+
+def q4kv_shared_prefix_workspace_bytes(spec, num_agents, max_seq_len, layers_in_call):
+    return lib().q4kv_shared_prefix_workspace_bytes(C.byref(spec), num_agents, max_seq_len, layers_in_call)
+
+
+def q4kv_shared_prefix_attention(spec, kpool, vpool, q, block_table, seq_len, group_begin, prefix_len, max_seq_len, sm_scale,
+                                 layer_begin=0, layer_end=None, out=None, workspace=None):
+    """Decode attention of agents in groups that share a prefix: q fp16 [layers_in_call][A][1][q_heads][k_dim]; group_begin int32
+    [groups + 1] and prefix_len int32 [groups] on the GPU (both None: nobody shares).  workspace: uint8 tensor on the GPU of
+    q4kv_shared_prefix_workspace_bytes(...) bytes, or None: allocated."""
+    layer_end = spec.num_layers if layer_end is None else layer_end
+    Lr, A = q.shape[0], q.shape[1]
+    if q.shape[2] != 1:
+        raise ValueError(f"{q.shape[2]} query tokens per agent: this is a decode call")
+    groups = 0 if prefix_len is None else prefix_len.numel()
+    if groups and (group_begin is None or group_begin.numel() != groups + 1):
+        raise ValueError(f"{groups} groups need {groups + 1} bounds")
+    if out is None:
+        out = torch.empty((Lr, A, 1, spec.num_q_heads, spec.v_dim), dtype=torch.float16, device=q.device)
+    if workspace is None:
+        need = q4kv_shared_prefix_workspace_bytes(spec, max(A, 1), max_seq_len, max(Lr, 1))
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    kp, vp = kpool.c(), None if vpool is None else vpool.c()
+    _check(lib().q4kv_shared_prefix_attention(
+        C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), _dev(q, torch.float16, "q"),
+        _dev(out, torch.float16, "out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
+        _dev(seq_len, torch.int32, "seq_len"), A, _dev(group_begin, torch.int32, "group_begin"),
+        _dev(prefix_len, torch.int32, "prefix_len"), groups, max_seq_len, float(sm_scale), layer_begin, layer_end,
+        workspace.data_ptr(), workspace.numel(), _stream()))
     return out
 
 

@@ -496,6 +496,57 @@ int q4kv_batched_attention_windows(const q4kv_spec *spec, const q4kv_pool *k, co
                             hip_stream);
 }
 
+size_t q4kv_shared_prefix_workspace_bytes(const q4kv_spec *spec, int32_t num_agents, int32_t max_seq_len, int32_t num_layers_in_call)
+{
+    if (check_spec(spec) != Q4KV_OK) return 0;
+    if (num_agents <= 0 || max_seq_len < 0 || num_layers_in_call <= 0) {
+        fail(Q4KV_EINVAL, "bad counts");
+        return 0;
+    }
+    size_t acc_at, ml_at;
+    return q4kv::prefix_workspace_bytes(*spec, num_agents, max_seq_len, num_layers_in_call, compute_units(), acc_at, ml_at);
+}
+
+int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const uint16_t *q,
+                                 uint16_t *out, const int32_t *block_table, int32_t max_blocks, const int32_t *seq_len,
+                                 int32_t num_agents, const int32_t *group_begin, const int32_t *prefix_len,
+                                 int32_t num_groups, int32_t max_seq_len, float sm_scale, int32_t layer_begin,
+                                 int32_t layer_end, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_spec(spec);
+    if (rc) return rc;
+    if (!q4kv::prefix_supported(*spec))
+        return fail(Q4KV_ESHAPE, "no shared-prefix kernel for k_dim=%d v_dim=%d n_rep=%d alias=%d", spec->k_dim, spec->v_dim,
+                    spec->num_q_heads / spec->num_kv_heads, spec->v_aliases_k);
+    if ((rc = check_pool(k, "K")) || (rc = check_pool(v, "V"))) return rc;
+    if (v->num_blocks != k->num_blocks) return fail(Q4KV_EINVAL, "K and V pools differ in num_blocks");
+    if (layer_begin < 0 || layer_end > spec->num_layers || layer_begin > layer_end)
+        return fail(Q4KV_EINVAL, "bad layer range [%d, %d)", layer_begin, layer_end);
+    if (num_agents < 0 || num_groups < 0 || max_blocks <= 0 || max_seq_len < 0) return fail(Q4KV_EINVAL, "bad counts");
+    if (num_agents > q4kv::prefix_max_agents() || num_groups > num_agents)
+        return fail(Q4KV_ERANGE, "at most %d agents in one call, in no more groups than agents: got %d in %d", q4kv::prefix_max_agents(),
+                    num_agents, num_groups);
+    if ((int64_t)max_seq_len > (int64_t)max_blocks * 256)
+        return fail(Q4KV_ERANGE, "max_seq_len %d exceeds max_blocks*256 = %lld", max_seq_len, (long long)max_blocks * 256);
+    if (num_agents == 0 || layer_begin == layer_end) return Q4KV_OK;
+    if (!q || !out || !block_table || !seq_len || (num_groups > 0 && (!group_begin || !prefix_len)))
+        return fail(Q4KV_EINVAL, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out)) return fail(Q4KV_EINVAL, "q and out must be 16-byte aligned");
+    const int layers = layer_end - layer_begin;
+    if (q4kv::prefix_tiles(*spec, num_agents, num_groups, max_seq_len, layers) > 0x7fffffffLL)
+        return fail(Q4KV_ERANGE, "more than 2^31 tiles in one call: split the layer range");
+    if ((int64_t)layers * num_agents * spec->num_q_heads * (spec->v_dim / 4) > 0x7fffffffLL * 256)
+        return fail(Q4KV_ERANGE, "more rows than a launch can have: split the layer range");
+    size_t acc_at, ml_at;
+    const size_t need = q4kv::prefix_workspace_bytes(*spec, num_agents, max_seq_len, layers, compute_units(), acc_at, ml_at);
+    if (!workspace || workspace_bytes < need || !aligned16(workspace))
+        return fail(Q4KV_EWORKSPACE, "workspace needs %zu bytes (16-byte aligned), got %zu", need, workspace_bytes);
+    const q4kv::PrefixArgs a = {spec, k, v, q, out, block_table, seq_len, group_begin, prefix_len, max_blocks, num_agents, num_groups,
+                                max_seq_len, layer_begin, layers, compute_units(), sm_scale, workspace};
+    const hipError_t e = q4kv::launch_prefix_attention(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "attention launch: %s", hipGetErrorString(e));
+}
+
 // Device address of `scratch` on the current device, looked up once per device (threads that race here store the
 // same value).  nullptr with the error message set when the runtime cannot resolve it.
 static void *static_scratch()

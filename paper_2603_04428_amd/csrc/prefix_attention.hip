@@ -1,0 +1,1124 @@
+// Decode attention of agents that share a prefix (forked from one parent: their block-table rows begin with the same blocks):
+//   out[l][a][h] = softmax(sm * q K_hat^T) V_hat   over all of the agent's tokens, as in decode_attention.hip,
+// with the tokens that a group of agents shares read and unpacked once for the query rows of all of them.
+//
+// A group's first prefix_len tokens are one unit per (layer, KV head) with (agents of the group) * n_rep query rows; what lies
+// behind them is one unit per (layer, KV head, agent) with n_rep rows.  A row's softmax over the two parts (and over the ranges
+// that several workers take of a unit) is joined from their un-normalised sums, maxima and denominators:
+//   m = max m_i,  out = sum_i 2^(m_i - m) acc_i / sum_i 2^(m_i - m) l_i.
+//
+// One pass over each unit's cache, 64 tokens at a time, per wave (no synchronisation inside the tile loop):
+//  * code words and parameters travel HBM -> LDS directly (global_load_lds, 16 bytes a lane) into a ring of tile buffers; the K
+//    part of a buffer is asked for again as soon as the scores of its tile are taken, the rest when its values are summed, so
+//    that kRing - 1/2 tiles are on their way while one is worked on.  Rows lie swizzled in LDS: 16-byte chunk c of token t at
+//    chunk c ^ f(t), which spreads both kinds of reads below over all banks; the transfer fetches permuted chunks of one row.
+//  * scores, transposed: S^T[t][row] = sum_g s[t,g] (C_g Q_g^T)[t][row] + (b Qsum^T)[t][row]: two v_mfma_f32_16x16x32_f16 per 16
+//    tokens, group and 16 rows, operand A a code word masked in place (nibbles are binary16 subnormals), the scale applied to
+//    the binary32 results; the bias term is one 16x16x16 instruction over the groups, group sums of q split in two binary16
+//    parts.
+//  * output, transposed: O^T[e][row] = sum_t c[t,e] (p[row,t] s[t,g(e)]) + sum_t b[t,g(e)] p[row,t]: the transposing 4-bit LDS read
+//    gives a lane 16 tokens of one element, masks unpack 8 of them into operand A; the lane that received S^T of (row, four
+//    tokens of each 16) supplies their p s as operand B, so probabilities never leave their registers.
+// Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
+#include <algorithm>
+
+#include "q4_device.h"
+#include "q4kv_internal.h"
+
+namespace q4kv {
+namespace {
+
+template <int V> struct Int { static constexpr int value = V; };
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kCols = 16;          // query rows of a column tile
+constexpr int kMaxAgents = 512;    // agents of a call: their lengths and tile counts are kept in LDS
+constexpr int kSoloTiles = 16;     // tiles per wave from which the waves of a workgroup take ranges of their own
+constexpr int kLeastTiles = 4;     // smallest range of a workgroup: a tile per wave
+constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kOneTermBits = 0x37D7;   // binary16 0.49: largest value scale for which one binary16 term of p s keeps the tolerance
+constexpr uint32_t kLiftScaleBits = 0x5BE0; // binary16 252: 2^8 times that is still below 65504
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+typedef int int2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) int2_t *lds_int2_ptr;
+typedef uint32_t uint2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) short4_t *lds_short4_ptr;
+typedef const __attribute__((address_space(3))) uint2_t *lds_uint2_ptr;
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+struct PrefixParams {
+    const uint32_t *k_codes, *v_codes;
+    const uint16_t *k_scale, *k_bias, *v_scale, *v_bias;
+    const uint16_t *q;
+    uint16_t *out;
+    const int32_t *block_table, *seq_len, *group_begin, *prefix_len;
+    int32_t *plan;
+    float *part_acc, *part_ml;
+    int num_agents, num_groups, max_blocks, num_blocks, kv_heads, q_heads, n_rep, layer_begin, layers, max_seq_len;
+    int slots;    // records reserved per row for the prefix, and as many for the agent's own tokens
+    int row_tile; // rows of a prefix unit: 16 * CT
+    float score_scale;
+};
+
+// What the merge needs to know of the plan, written by workgroup 0: header, then per agent the tiles in front of its own part,
+// where that part begins (in tiles; the tiles of the prefix it shares), the tiles in front of its group's units, and the
+// group's first agent.
+constexpr int kHeader = 4; // [0] tiles per worker  [1] tiles of a (layer, KV head)  [2] tiles of its prefix units
+__host__ __device__ constexpr int plan_ints(int agents) { return kHeader + 4 * agents + 1; }
+
+// ---------------------------------------------------------------------------------------------- the plan
+
+// The tiles of a (layer, KV head): all prefix units (group by group, row tile by row tile), then the agents' own parts.  Every
+// workgroup works it out for itself, in LDS.
+struct Plan {
+    int own[kMaxAgents + 1];   // tiles of the agents in front of an agent
+    int group[kMaxAgents + 1]; // tiles of the prefix units of the groups in front of a group
+    int len[kMaxAgents];       // visible tokens of an agent
+    int start[kMaxAgents];     // tile its own part begins with
+    int begin[kMaxAgents + 1]; // first agent of a group
+    int wave_sum[2][kWaves];
+};
+
+__device__ __forceinline__ int tiles_of(int tokens) { return (tokens + kWave - 1) / kWave; }
+
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false); // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false); // row_bcast15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false); // row_bcast31 into rows 2 and 3
+    return v;
+}
+
+// inclusive maximum over the lanes of values that are not negative
+__device__ __forceinline__ int wave_scan_max(int v)
+{
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
+    return v;
+}
+
+// the last index of 0 .. count - 1 whose entry is at most x (entries do not fall; entry 0 is at most x)
+__device__ __forceinline__ int last_at_most(const int *pre, int count, int x)
+{
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (pre[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ void make_plan(const PrefixParams &p, Plan &pl)
+{
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    constexpr int EACH = kMaxAgents / kThreads; // agents (and groups) of a thread
+    const int A = p.num_agents, G = p.num_groups;
+    int n[EACH], shared_tiles[EACH], first[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int a = tid * EACH + i;
+        n[i] = a < A ? min(max(p.seq_len[a], 0), p.max_seq_len) : 0;
+        shared_tiles[i] = a < G ? min(max(p.prefix_len[a], 0), p.max_seq_len) / kWave : 0;
+        if (a < A) pl.len[a] = n[i];
+        first[i] = a < G ? min(max(p.group_begin[a], 0), A) : 0;
+    }
+    // bounds that fall are raised to the ones in front of them: groups never overlap, whatever the caller wrote
+    int top = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) first[i] = top = max(top, first[i]);
+    const int raised = wave_scan_max(top);
+    if (lane == kWave - 1) pl.wave_sum[0][wave] = raised;
+    __syncthreads();
+    top = __shfl_up(raised, 1, kWave);
+    if (lane == 0) top = 0;
+    for (int w = 0; w < wave; ++w) top = max(top, pl.wave_sum[0][w]);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (tid * EACH + i < G) pl.begin[tid * EACH + i] = max(top, first[i]);
+    if (tid == kThreads - 1) pl.begin[G] = G > 0 ? max(max(top, first[EACH - 1]), min(max(p.group_begin[G], 0), A)) : 0;
+    __syncthreads();
+    // a group of one agent shares nothing
+    int group_tiles[EACH], own_tiles[EACH], group_sum = 0, own_sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int g = tid * EACH + i;
+        group_tiles[i] = 0;
+        if (g < G) {
+            const int agents = pl.begin[g + 1] - pl.begin[g];
+            if (agents < 2) shared_tiles[i] = 0;
+            group_tiles[i] = shared_tiles[i] * (agents < 2 ? 0 : (agents * p.n_rep + p.row_tile - 1) / p.row_tile);
+            pl.group[g] = shared_tiles[i]; // for the agents, until the sums are taken
+        }
+        group_sum += group_tiles[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int a = tid * EACH + i;
+        own_tiles[i] = 0;
+        if (a < A) {
+            int start = 0;
+            if (G > 0 && a >= pl.begin[0]) {
+                const int g = last_at_most(pl.begin, G, a);
+                if (a < pl.begin[g + 1]) start = pl.group[g];
+            }
+            pl.start[a] = start;
+            own_tiles[i] = max(0, tiles_of(n[i]) - start);
+        }
+        own_sum += own_tiles[i];
+    }
+    const int group_incl = wave_scan(group_sum), own_incl = wave_scan(own_sum);
+    if (lane == kWave - 1) {
+        pl.wave_sum[0][wave] = group_incl;
+        pl.wave_sum[1][wave] = own_incl;
+    }
+    __syncthreads();
+    int group_at = group_incl - group_sum, own_at = own_incl - own_sum;
+    for (int w = 0; w < wave; ++w) {
+        group_at += pl.wave_sum[0][w];
+        own_at += pl.wave_sum[1][w];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int a = tid * EACH + i;
+        if (a <= G) pl.group[a] = group_at;
+        if (a <= A) pl.own[a] = own_at;
+        group_at += group_tiles[i];
+        own_at += own_tiles[i];
+    }
+    if (tid == kThreads - 1) { // counts of exactly kMaxAgents
+        if (G == kMaxAgents) pl.group[G] = group_at;
+        if (A == kMaxAgents) pl.own[A] = own_at;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void write_plan(const PrefixParams &p, const Plan &pl, int per)
+{
+    const int A = p.num_agents, G = p.num_groups;
+    if (threadIdx.x == 0) {
+        p.plan[0] = per;
+        p.plan[1] = pl.group[G] + pl.own[A];
+        p.plan[2] = pl.group[G];
+    }
+    for (int a = threadIdx.x; a < A; a += kThreads) {
+        const int g = G > 0 && a >= pl.begin[0] ? last_at_most(pl.begin, G, a) : 0;
+        p.plan[kHeader + a] = pl.own[a];
+        p.plan[kHeader + A + 1 + a] = pl.start[a];
+        p.plan[kHeader + 2 * A + 1 + a] = pl.group[g];
+        p.plan[kHeader + 3 * A + 1 + a] = pl.begin[g];
+    }
+    if (threadIdx.x == 0) p.plan[kHeader + A] = pl.own[A];
+}
+
+// ---------------------------------------------------------------------------------------------- tiles in LDS
+
+__device__ __forceinline__ half8_t words_to_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_bit_cast(half8_t, make_uint4(a, b, c, d));
+}
+
+__device__ __forceinline__ half8_t code_operand(uint32_t w)
+{
+    const uint32_t w8 = w >> 8;
+    return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
+}
+
+__device__ __forceinline__ float half_of(uint32_t pair, int hi)
+{
+    return half_bits_to_float((uint16_t)(hi ? pair >> 16 : pair & 0xffffu));
+}
+
+__device__ __forceinline__ float xor16_max(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float xor32_max(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float xor16_sum(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float xor32_sum(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// Code rows of one width in LDS: UNITS chunks of 16 bytes per row, chunk c of token t at place c ^ swizzle(t).  A row is 8, 16,
+// 24 or 32 banks long: with the swizzle the 16 rows 16 j .. 16 j + 15 (a set of the scores) and the 16 rows 16 j + 4 q + r of one q
+// (a slot of the values) each spread one chunk per row over all 64 banks, as far as rows of 64 elements allow.
+template <int DIM>
+struct Rows {
+    static constexpr int BYTES = DIM / 2;          // of a row
+    static constexpr int UNITS = DIM / 32;
+    static constexpr int LOADS = kWave * BYTES / 1024; // 1 KiB transfers of a tile
+    __device__ __forceinline__ static constexpr int swizzle(int t)
+    {
+        if constexpr (UNITS == 8) return ((t >> 1) & 7) ^ (2 * ((t >> 4) & 3));
+        else if constexpr (UNITS == 4) return ((t >> 2) & 3) ^ ((t >> 4) & 3);
+        else return ((t >> 3) ^ (t >> 4)) & 1;
+    }
+    // byte offset in the tile's rows that lane `lane` fetches in transfer i, less 1024 i
+    __device__ __forceinline__ static uint32_t source(int i, int lane)
+    {
+        const int u = i * kWave + lane, t = u / UNITS, c = (u % UNITS) ^ swizzle(t);
+        return (uint32_t)((t * UNITS + c - i * kWave) * 16);
+    }
+    // which of the first SOURCES transfers has the same offsets
+    static constexpr int SOURCES = LOADS < 4 ? LOADS : UNITS == 6 ? 3 : 4;
+    static constexpr int source_of(int i) { return UNITS == 6 ? i % 3 : i < 4 ? i : (i - 4) ^ 1; }
+    // for the rows 16 j + col of set j: what the swizzle adds to that of j == 0 and group g, and the offset behind the exclusive or
+    static constexpr int set_xor(int j, int g)
+    {
+        if constexpr (UNITS == 8) return 2 * (g ^ j);
+        else if constexpr (UNITS == 4) return (2 * g) ^ j;
+        else return j & 1;
+    }
+    static constexpr int group_offset(int g) { return UNITS == 6 ? 32 * g : 0; }
+};
+
+template <int DK, int DV>
+struct Shape {
+    static constexpr int GK = DK / kGroup, GV = DV / kGroup;
+    static constexpr int K_BYTES = kWave * DK / 2, V_BYTES = kWave * DV / 2;
+    static constexpr int PARAM_UNITS = 16 * (GK + GV);                      // chunks of K scale, K bias, V scale, V bias of a tile
+    static constexpr int PARAM_LOADS = (PARAM_UNITS + kWave - 1) / kWave;
+    static constexpr int P_BYTES = PARAM_LOADS * 1024;
+    static constexpr int TILE_BYTES = K_BYTES + V_BYTES + P_BYTES;
+    static constexpr int WAVES_PER_SIMD = 1;
+    static constexpr int RING = DK == 256 ? 2 : DK == 192 ? 3 : 4;
+    static constexpr int WAVE_BYTES = RING * TILE_BYTES;
+    static constexpr int ROW_PITCH = DV + 4;                                // floats of a row of sums in LDS
+    // offsets of the parameter arrays in a tile's parameters
+    static constexpr int KS_AT = 0, KB_AT = 128 * GK, VS_AT = 256 * GK, VB_AT = 256 * GK + 128 * GV;
+};
+
+// up to four transfers of 1 KiB from consecutive KiB of global memory to consecutive KiB of LDS
+template <int N>
+__device__ __forceinline__ void transfer(uint32_t lds, const void *src, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3)
+{
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(lds), "s"(src), "v"(o0) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024" ::"s"(lds),
+                     "s"(src), "v"(o0), "v"(o1)
+                     : "memory");
+    else if constexpr (N == 3)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:2048" ::"s"(lds),
+                     "s"(src), "v"(o0), "v"(o1), "v"(o2)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072" ::"s"(lds),
+                     "s"(src), "v"(o0), "v"(o1), "v"(o2), "v"(o3)
+                     : "memory");
+}
+// the code rows of a tile
+template <int DIM>
+__device__ __forceinline__ void transfer_rows(uint32_t lds, const unsigned char *src, const uint32_t (&from)[Rows<DIM>::SOURCES])
+{
+    typedef Rows<DIM> R;
+#pragma unroll
+    for (int i = 0; i < R::LOADS; i += 4) {
+        const uint32_t o0 = from[R::source_of(i)], o1 = from[R::source_of(i + 1 < R::LOADS ? i + 1 : i)];
+        const uint32_t o2 = from[R::source_of(i + 2 < R::LOADS ? i + 2 : i)], o3 = from[R::source_of(i + 3 < R::LOADS ? i + 3 : i)];
+        if (R::LOADS - i >= 4) transfer<4>(lds + i * 1024, src + i * 1024, o0, o1, o2, o3);
+        else if (R::LOADS - i == 3) transfer<3>(lds + i * 1024, src + i * 1024, o0, o1, o2, o3);
+        else if (R::LOADS - i == 2) transfer<2>(lds + i * 1024, src + i * 1024, o0, o1, o2, o3);
+        else transfer<1>(lds + i * 1024, src + i * 1024, o0, o1, o2, o3);
+    }
+}
+// the same from an address per lane
+__device__ __forceinline__ void transfer_from(uint32_t lds, uint64_t address)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_for_all_but()
+{
+    static_assert(N <= 63, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// A unit, or the part of it that a worker takes.
+struct Part {
+    int li, kvh;       // layer in call, KV head
+    int agent, agents; // the agents whose rows read it: first, number
+    int row0, rows;    // rows of this unit: row0 .. row0 + rows - 1 of those agents' rows
+    int tile, count;   // the part: first tile (of the agent's tokens), number of tiles
+    int slot, slots;   // the part's record among the unit's
+    int which;         // 0: prefix, 1: own tokens
+    int whole_row;     // 1: there is nothing else to join, the rows' outputs are final
+};
+
+__device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, int x, int x1, int per, int worker)
+{
+    Part u;
+    const int group_tiles = pl.group[p.num_groups], head_tiles = group_tiles + pl.own[p.num_agents];
+    const int lk = x / head_tiles;
+    int r = x - lk * head_tiles, tiles, unit0;
+    u.li = lk / p.kv_heads;
+    u.kvh = lk - u.li * p.kv_heads;
+    if (r < group_tiles) {
+        const int g = last_at_most(pl.group, p.num_groups, r);
+        u.agent = pl.begin[g];
+        u.agents = pl.begin[g + 1] - u.agent;
+        tiles = pl.start[u.agent];
+        r -= pl.group[g];
+        const int rt = r / tiles;
+        r -= rt * tiles;
+        u.row0 = rt * p.row_tile;
+        u.rows = min(p.row_tile, u.agents * p.n_rep - u.row0);
+        u.tile = r;
+        u.which = 0;
+    } else {
+        r -= group_tiles;
+        u.agent = last_at_most(pl.own, p.num_agents, r);
+        u.agents = 1;
+        tiles = pl.own[u.agent + 1] - pl.own[u.agent];
+        r -= pl.own[u.agent];
+        u.row0 = 0;
+        u.rows = p.n_rep;
+        u.tile = r + pl.start[u.agent];
+        u.which = 1;
+    }
+    u.count = min(tiles - r, x1 - x);
+    unit0 = x - r;
+    const int first = unit0 / per;
+    u.slot = worker - first;
+    u.slots = (unit0 + tiles - 1) / per - first + 1;
+    u.whole_row = u.which == 1 && u.slots == 1 && pl.start[u.agent] == 0;
+    u.li = uniform(u.li); u.kvh = uniform(u.kvh); u.agent = uniform(u.agent); u.agents = uniform(u.agents);
+    u.row0 = uniform(u.row0); u.rows = uniform(u.rows); u.tile = uniform(u.tile); u.count = uniform(u.count);
+    u.slot = uniform(u.slot); u.slots = uniform(u.slots); u.which = uniform(u.which); u.whole_row = uniform(u.whole_row);
+    return u;
+}
+
+// the place of row `row` of a part: (layer, agent, query head)
+__device__ __forceinline__ int64_t row_index(const PrefixParams &p, const Part &u, int row, int &agent)
+{
+    const int idx = u.row0 + row, in_group = idx / p.n_rep;
+    agent = u.agent + in_group;
+    return ((int64_t)u.li * p.num_agents + agent) * p.q_heads + u.kvh * p.n_rep + (idx - in_group * p.n_rep);
+}
+
+// CT: column tiles of 16 rows of the prefix units.  BF: scale and bias are stored as bfloat16.
+template <int DK, int DV, int CTP, bool BF>
+__global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void prefix_attention_kernel(const PrefixParams p)
+{
+    typedef Shape<DK, DV> S;
+    constexpr int GK = S::GK, GV = S::GV;
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_lds[kWaves * S::WAVE_BYTES];
+    __shared__ Plan plan;
+    __shared__ float ml_lds[kWaves][CTP * kCols][2];
+
+    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
+    make_plan(p, plan);
+    const int head_tiles = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]);
+    const int total = head_tiles * p.kv_heads * p.layers; // the host keeps this below 2^31
+    const int workgroups = gridDim.x;
+    int per = (total + workgroups * kWaves - 1) / (workgroups * kWaves);
+    const bool solo = per >= kSoloTiles;
+    if (!solo) per = max(kLeastTiles, (total + workgroups - 1) / workgroups);
+    if (blockIdx.x == 0) write_plan(p, plan, per);
+    const int worker = solo ? (int)blockIdx.x * kWaves + wave : (int)blockIdx.x;
+    const long long begin = (long long)worker * per;
+    if (begin >= total) return; // a whole workgroup, or a wave on its own
+    const int x1 = (int)min((long long)total, begin + per);
+
+    unsigned char *const region = tiles_lds + wave * S::WAVE_BYTES;
+    const uint32_t region_at = (uint32_t)(uintptr_t)(lds_ptr_t)region;
+    const int col = lane % 16, qk = lane / 16;
+
+    // what a lane fetches of a tile's rows and parameters
+    uint32_t k_src[Rows<DK>::SOURCES], v_src[Rows<DV>::SOURCES];
+#pragma unroll
+    for (int i = 0; i < Rows<DK>::SOURCES; ++i) k_src[i] = Rows<DK>::source(i, lane);
+#pragma unroll
+    for (int i = 0; i < Rows<DV>::SOURCES; ++i) v_src[i] = Rows<DV>::source(i, lane);
+    uint64_t param_src[S::PARAM_LOADS];
+    bool param_of_v[S::PARAM_LOADS];
+#pragma unroll
+    for (int i = 0; i < S::PARAM_LOADS; ++i) {
+        const int u = min(i * kWave + lane, S::PARAM_UNITS - 1); // (behind the last: that one again)
+        const bool of_v = u >= 16 * GK;
+        const int in_pool = of_v ? u - 16 * GK : u, units = 8 * (of_v ? GV : GK);
+        const uint16_t *base = of_v ? (in_pool < units ? p.v_scale : p.v_bias) : (in_pool < units ? p.k_scale : p.k_bias);
+        param_src[i] = (uint64_t)(uintptr_t)base + 16 * (in_pool < units ? in_pool : in_pool - units);
+        param_of_v[i] = of_v;
+    }
+    // where it reads them: row `col` of set 0 for the scores, row 16 (col / 4) + 4 qk + col % 4 for the values
+    const uint32_t k_at = region_at + col * Rows<DK>::BYTES + (((qk >> 1) ^ Rows<DK>::swizzle(col)) << 4) + (qk & 1) * 8;
+    const int v_row = 16 * (col / 4) + 4 * qk + col % 4;
+    const uint32_t v_at = region_at + S::K_BYTES + v_row * Rows<DV>::BYTES + (Rows<DV>::swizzle(v_row) << 4);
+
+    auto run_part = [&](auto column_tiles, const Part &u) __attribute__((always_inline)) {
+        constexpr int CT = decltype(column_tiles)::value;
+        constexpr bool kTight = CT * (GK + GV) >= 16; // registers for everything only if loads from LDS do not move far ahead
+        const int step = solo ? 1 : kWaves;
+        const int first = solo ? 0 : wave;                                       // tiles of the part that are this wave's:
+        const int mine = u.count > first ? (u.count - first + step - 1) / step : 0; // first, first + step, ...
+        const int64_t unit_row = ((int64_t)(p.layer_begin + u.li) * p.num_blocks * p.kv_heads + u.kvh) * kBlockTokens;
+        const int32_t *const table = p.block_table + (int64_t)u.agent * p.max_blocks;
+        // block ids of 64 blocks from table_base on, one per lane
+        int table_base = (u.tile + first) / 4;
+        auto fetch_table = [&]() { return table_base + lane < p.max_blocks ? table[table_base + lane] : -1; };
+        int table_ids = fetch_table();
+        auto block_of = [&](int t) __attribute__((always_inline)) { // wave-uniform
+            const int b = t / 4;
+            if (__builtin_expect(b >= table_base + kWave, 0)) {
+                table_base = b;
+                table_ids = fetch_table();
+            }
+            return __builtin_amdgcn_readlane(table_ids, b - table_base);
+        };
+        uint32_t reachable_bufs = 0; // bit: the block id of the tile in that buffer is inside the pool
+        auto row_of = [&](int t, int buf) __attribute__((always_inline)) {
+            const int blk = block_of(t);
+            const bool inside = blk >= 0 && blk < p.num_blocks;
+            reachable_bufs = (reachable_bufs & ~(1u << buf)) | (inside ? 1u << buf : 0u);
+            // the loads of a tile whose id is outside the pool go to block 0; all they bring is masked
+            return unit_row + (int64_t)(inside ? blk : 0) * (p.kv_heads * kBlockTokens) + (t % 4) * kWave;
+        };
+        auto issue_k = [&](int t, int buf) __attribute__((always_inline)) {
+            const unsigned char *src = reinterpret_cast<const unsigned char *>(p.k_codes) + row_of(t, buf) * Rows<DK>::BYTES;
+            const uint32_t dst = region_at + buf * S::TILE_BYTES;
+            transfer_rows<DK>(dst, src, k_src);
+        };
+        auto issue_rest = [&](int t, int buf) __attribute__((always_inline)) { // parameters, then V
+            const int64_t row = row_of(t, buf);
+            const uint32_t dst = region_at + buf * S::TILE_BYTES + S::K_BYTES;
+#pragma unroll
+            for (int i = 0; i < S::PARAM_LOADS; ++i)
+                transfer_from(dst + S::V_BYTES + i * 1024, param_src[i] + (uint64_t)row * (2 * GK != 2 * GV && param_of_v[i] ? 2 * GV : 2 * GK));
+            const unsigned char *src = reinterpret_cast<const unsigned char *>(p.v_codes) + row * Rows<DV>::BYTES;
+            transfer_rows<DV>(dst, src, v_src);
+        };
+        // Of the transfers behind what is waited for, `ahead` tiles' (the tiles behind the current one that have been asked for) may
+        // still be on their way; loads complete in order.
+        constexpr int K_LOADS = Rows<DK>::LOADS, V_LOADS = Rows<DV>::LOADS, ALL = K_LOADS + V_LOADS + S::PARAM_LOADS;
+        auto wait_scores = [&](int ahead) __attribute__((always_inline)) { // K and parameters of the current tile
+            if (S::RING >= 4 && ahead >= 3) wait_for_all_but<(V_LOADS + 3 * ALL > 63 ? 0 : V_LOADS + 3 * ALL)>();
+            else if (S::RING >= 3 && ahead >= 2) wait_for_all_but<V_LOADS + 2 * ALL>();
+            else if (ahead >= 1) wait_for_all_but<V_LOADS + ALL>();
+            else wait_for_all_but<V_LOADS>();
+        };
+        auto wait_values = [&](int ahead) __attribute__((always_inline)) { // V of the current tile; K of RING tiles on may have been asked for
+            if (S::RING >= 4 && ahead >= 4) wait_for_all_but<(3 * ALL + K_LOADS > 63 ? 0 : 3 * ALL + K_LOADS)>();
+            else if (S::RING >= 4 && ahead >= 3) wait_for_all_but<3 * ALL>();
+            else if (S::RING == 3 && ahead >= 3) wait_for_all_but<2 * ALL + K_LOADS>();
+            else if (S::RING >= 3 && ahead >= 2) wait_for_all_but<2 * ALL>();
+            else if (S::RING == 2 && ahead >= 2) wait_for_all_but<ALL + K_LOADS>();
+            else if (ahead >= 1) wait_for_all_but<ALL>();
+            else wait_for_all_but<0>();
+        };
+
+        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0): the counts below start from nothing, and all reads of LDS are done
+        for (int i = 0; i < S::RING; ++i)
+            if (i < mine) {
+                issue_k(u.tile + first + i * step, i);
+                issue_rest(u.tile + first + i * step, i);
+            }
+
+        // ---- the rows: query operand (element order of code_operand, odd elements / 16 because their codes arrive 16 times
+        // larger), group sums of q, visible tokens
+        half8_t qop[CT][GK][2];
+        half4_t qsop[CT];
+        int n_row[CT], n_min = 0x7fffffff, n_max = 0;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            int agent;
+            const int64_t row = row_index(p, u, min(16 * ct + col, u.rows - 1), agent);
+            n_row[ct] = plan.len[agent];
+            n_min = min(n_min, n_row[ct]);
+            n_max = max(n_max, n_row[ct]);
+            const uint16_t *qrow = p.q + row * DK + 16 * qk;
+            float qs[GK];
+#pragma unroll
+            for (int g = 0; g < GK; ++g) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint4 raw = *reinterpret_cast<const uint4 *>(qrow + g * kGroup + 8 * r);
+                    const half2_t e01 = bits_to_half2(raw.x), e23 = bits_to_half2(raw.y);
+                    const half2_t e45 = bits_to_half2(raw.z), e67 = bits_to_half2(raw.w);
+                    const half_t sixteenth = (half_t)0.0625f;
+                    qop[ct][g][r] = half8_t{e01.x, e45.x, e01.y * sixteenth, e45.y * sixteenth,
+                                            e23.x, e67.x, e23.y * sixteenth, e67.y * sixteenth};
+                    sum += ((float)e01.x + (float)e01.y) + ((float)e23.x + (float)e23.y) +
+                           ((float)e45.x + (float)e45.y) + ((float)e67.x + (float)e67.y);
+                }
+                qs[g] = xor32_sum(xor16_sum(sum));
+            }
+            // contraction index of the bias term: with up to two groups high and low parts side by side in slot 0, else the
+            // high parts in slot 0 and the low parts in slot 1
+            half_t part[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int g = GK <= 2 ? e % GK : e;
+                const float v = g < GK && (GK > 2 || e < 2 * GK) ? qs[g < GK ? g : 0] : 0.0f;
+                const half_t hi = (half_t)v;
+                const bool low = GK <= 2 ? e >= GK : qk == 1;
+                const half_t value = low ? (half_t)(v - (float)hi) : hi;
+                part[e] = qk < (GK <= 2 ? 1 : 2) ? value : (half_t)0.0f;
+            }
+            qsop[ct] = half4_t{part[0], part[1], part[2], part[3]};
+        }
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) {
+            n_min = min(n_min, __shfl_xor(n_min, off, 16));
+            n_max = max(n_max, __shfl_xor(n_max, off, 16));
+        }
+        n_min = uniform(n_min);
+        n_max = uniform(n_max);
+        float4_t acc[CT][4 * GV], pbacc[CT];
+        float pb[CT][GV], m_run[CT], l_run[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+            for (int c = 0; c < 4 * GV; ++c) acc[ct][c] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            pbacc[ct] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int g = 0; g < GV; ++g) pb[ct][g] = 0.0f;
+            m_run[ct] = kNegBig;
+            l_run[ct] = 0.0f;
+        }
+
+        // The query operand of two column tiles of wide heads lives in accumulator registers, which matrix instructions read directly.
+        if constexpr (CT * GK >= 6) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int g = 0; g < GK; ++g) asm volatile("" : "+a"(qop[ct][g][0]), "+a"(qop[ct][g][1]));
+        }
+
+        int buf = 0;
+        for (int i = 0; i < mine; ++i) {
+            const int t = u.tile + first + i * step, t0 = t * kWave;
+            const int ahead = min(mine - 1 - i, S::RING - 1);
+            const uint32_t base = (uint32_t)buf * S::TILE_BYTES;
+            const unsigned char *const params = region + base + S::K_BYTES + S::V_BYTES;
+            wait_scores(ahead);
+            const bool reachable = (reachable_bufs >> buf & 1u) != 0;
+            const bool edge = !(reachable && t0 + kWave <= n_min);
+            uint32_t s_top = 0;
+            {
+                // token `lane`'s parameters: converted from bfloat16, zero for tokens that no row sees (their slots may hold
+                // anything, and no NaN or infinity may reach a matrix operand)
+                const bool seen = reachable && t0 + lane < n_max;
+                auto row_of_params = [&](int at, int groups) __attribute__((always_inline)) {
+                    return reinterpret_cast<uint16_t *>(const_cast<unsigned char *>(params) + at) + lane * groups;
+                };
+                auto redo = [&](uint16_t *w, int groups) __attribute__((always_inline)) {
+                    for (int g = 0; g < groups; ++g) {
+                        const uint16_t v = BF ? float_to_half_bits(bf16_bits_to_float(w[g])) : w[g];
+                        w[g] = seen ? v : (uint16_t)0;
+                    }
+                };
+                if (BF || __builtin_expect(edge, 0)) {
+                    redo(row_of_params(S::KS_AT, GK), GK);
+                    redo(row_of_params(S::KB_AT, GK), GK);
+                    redo(row_of_params(S::VS_AT, GV), GV);
+                    redo(row_of_params(S::VB_AT, GV), GV);
+                }
+                const uint16_t *vs = row_of_params(S::VS_AT, GV);
+#pragma unroll
+                for (int g = 0; g < GV; ++g) s_top = max(s_top, (uint32_t)vs[g]);
+                wave_lds_sync();
+            }
+            const bool two_terms = __builtin_amdgcn_ballot_w64(s_top > kOneTermBits) != 0ull;
+            const bool wide = two_terms && __builtin_amdgcn_ballot_w64(s_top > kLiftScaleBits) != 0ull;
+
+            // ---- scores: z[ct][j][r] is token 16 j + 4 qk + r, row 16 ct + col, in units of 2^-24 / score_scale
+            float z[CT][4][4];
+            const float4_t zero = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            const uint32_t ka = k_at + base;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t b[2], s[2 * GK]; // bias row of token 16 j + col; scales of tokens 16 j + 4 qk .. + 3
+                const unsigned char *brow = params + S::KB_AT + (16 * j + col) * (2 * GK), *srow = params + S::KS_AT + (16 * j + 4 * qk) * (2 * GK);
+                if constexpr (GK == 4) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(brow);
+                    b[0] = w.x;
+                    b[1] = w.y;
+                } else if constexpr (GK == 3) {
+                    const uint16_t *w = reinterpret_cast<const uint16_t *>(brow);
+                    b[0] = (uint32_t)w[0] | (uint32_t)w[1] << 16;
+                    b[1] = w[2];
+                } else if constexpr (GK == 2) {
+                    b[0] = b[1] = *reinterpret_cast<const uint32_t *>(brow);
+                } else {
+                    const uint32_t w = *reinterpret_cast<const uint16_t *>(brow);
+                    b[0] = w | w << 16;
+                    b[1] = 0;
+                }
+                __builtin_memcpy(s, __builtin_assume_aligned(srow, GK % 2 == 0 ? 16 : 8), 8 * GK);
+                const half4_t bop = __builtin_bit_cast(half4_t, make_uint2(b[0], b[1]));
+                float4_t sum[CT];
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    sum[ct] = __builtin_amdgcn_mfma_f32_16x16x16f16(bop, qsop[ct], zero, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[ct][r] *= 0x1p-24f; // the products' unit
+                }
+#pragma unroll
+                for (int g = 0; g < GK; ++g) {
+                    const uint2_t w = *(lds_uint2_ptr)(uintptr_t)((ka ^ (uint32_t)(Rows<DK>::set_xor(j, g) << 4)) +
+                                                              (uint32_t)(16 * j * Rows<DK>::BYTES + Rows<DK>::group_offset(g)));
+                    const half8_t a0 = code_operand(w.x), a1 = code_operand(w.y);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        float4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, qop[ct][g][0], zero, 0, 0, 0);
+                        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, qop[ct][g][1], d, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int at = r * GK + g;
+                            sum[ct][r] = fmaf(half_of(s[at / 2], at & 1), d[r], sum[ct][r]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[ct][j][r] = sum[ct][r];
+                if (kTight) __builtin_amdgcn_sched_barrier(0);
+            }
+            // K of this buffer has been read: the next tile for it
+            const bool more = i + S::RING < mine;
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                issue_k(t + S::RING * step, buf);
+            }
+
+            // ---- online softmax.  m_run is the reference the exponentials are taken against: it moves only when a tile's maximum
+            // exceeds it by more than 7 (in log2 units), and then to 4 below that maximum.  p <= 2^7 then, and p s stays inside
+            // binary16 for scales up to 252; in a tile with a larger one p <= 2^2.5.
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float zs = p.score_scale * kCodeScaleA;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) z[ct][k / 4][k % 4] *= zs;
+                if (__builtin_expect(edge, 0)) {
+                    asm volatile("");
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (!(reachable && t0 + 16 * j + 4 * qk + r < n_row[ct])) z[ct][j][r] = -INFINITY;
+                }
+                float mt = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) mt = fmaxf(mt, z[ct][k / 4][k % 4]);
+                mt = xor32_max(xor16_max(mt));
+                const bool above = mt > m_run[ct] + (wide ? 2.5f : 7.0f);
+                const float m_new = above ? mt - (wide ? 0.0f : 4.0f) : m_run[ct];
+                float psum = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float pr = __builtin_amdgcn_exp2f(z[ct][k / 4][k % 4] - m_new);
+                    z[ct][k / 4][k % 4] = pr;
+                    psum += pr;
+                }
+                if (i > 0 && __builtin_amdgcn_ballot_w64(above) != 0ull) {
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[ct] - m_new);
+                    l_run[ct] *= alpha;
+                    pbacc[ct] *= alpha;
+#pragma unroll
+                    for (int g = 0; g < GV; ++g) pb[ct][g] *= alpha;
+#pragma unroll
+                    for (int c = 0; c < 4 * GV; ++c) acc[ct][c] *= alpha;
+                }
+                l_run[ct] += psum;
+                m_run[ct] = m_new;
+            }
+
+            // ---- values
+            half2_t p16[CT][2][4]; // [half of the sets][r]: tokens 4 qk + r of sets 2 h and 2 h + 1
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p16[ct][h][r] = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
+            if constexpr (GV == 4) {
+                // rows of A = groups: the transposing read gives lane `col` group col % 4 of the four tokens that lanes 0, 4, 8, 12
+                // of its 16 point at
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int tok = 16 * (2 * h + ((col >> 2) & 1)) + 4 * qk + (col >> 3);
+                    const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + S::VB_AT + tok * 8;
+                    const short4_t b0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)at);
+                    const short4_t b1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + 16));
+                    const uint2 w0 = __builtin_bit_cast(uint2, b0), w1 = __builtin_bit_cast(uint2, b1);
+                    const half8_t bop = words_to_half8(w0.x, w0.y, w1.x, w1.y);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const half8_t pop = words_to_half8(half2_to_bits(p16[ct][h][0]), half2_to_bits(p16[ct][h][1]),
+                                                           half2_to_bits(p16[ct][h][2]), half2_to_bits(p16[ct][h][3]));
+                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, pop, pbacc[ct], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t b[2 * GV];
+                    __builtin_memcpy(b, __builtin_assume_aligned(params + S::VB_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int g = 0; g < GV; ++g)
+                                pb[ct][g] = fmaf(z[ct][j][r], half_of(b[(r * GV + g) / 2], (r * GV + g) & 1), pb[ct][g]);
+                }
+            }
+            // scales of tokens 16 j + 4 qk + r, paired over the two sets of a half
+            uint32_t s2[2][4][GV];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t even[2 * GV], odd[2 * GV];
+                const unsigned char *at = params + S::VS_AT + (32 * h + 4 * qk) * (2 * GV);
+                __builtin_memcpy(even, __builtin_assume_aligned(at, 8), 8 * GV);
+                __builtin_memcpy(odd, __builtin_assume_aligned(at + 16 * (2 * GV), 8), 8 * GV);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int g = 0; g < GV; ++g) {
+                        const int k = r * GV + g;
+                        s2[h][r][g] = __builtin_amdgcn_perm(odd[k / 2], even[k / 2], (k & 1) ? 0x07060302u : 0x05040100u);
+                    }
+            }
+            const half2_t sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f}; // codes of the odd rows r arrive 16 times larger
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    p16[ct][h][1] *= sixteenth;
+                    p16[ct][h][3] *= sixteenth;
+                }
+            wait_values(min(mine - 1 - i, S::RING));
+            const uint32_t va = v_at + base;
+            auto sum_values = [&](auto terms) __attribute__((always_inline)) {
+                constexpr bool TWO = decltype(terms)::value == 2;
+#pragma unroll
+                for (int g = 0; g < GV; ++g) {
+                    if (kTight) __builtin_amdgcn_sched_barrier(0);
+                    half8_t hi[CT][2], lo[CT][2];
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t a[4], b[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const half2_t s = bits_to_half2(s2[h][r][g]), ps = p16[ct][h][r] * s;
+                                a[r] = half2_to_bits(ps);
+                                if (TWO) b[r] = half2_to_bits(__builtin_elementwise_fma(p16[ct][h][r], s, -ps));
+                            }
+                            hi[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
+                            if (TWO) lo[ct][h] = words_to_half8(b[0], b[1], b[2], b[3]);
+                        }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = 4 * g + k;
+                        const int2_t w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_int2_ptr)(uintptr_t)((va ^ (uint32_t)((c >> 1) << 4)) + (c & 1) * 8));
+                        const half8_t a0 = code_operand((uint32_t)w.x), a1 = code_operand((uint32_t)w.y);
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) {
+                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, hi[ct][0], acc[ct][c], 0, 0, 0);
+                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, hi[ct][1], acc[ct][c], 0, 0, 0);
+                            if (TWO) {
+                                acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, lo[ct][0], acc[ct][c], 0, 0, 0);
+                                acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, lo[ct][1], acc[ct][c], 0, 0, 0);
+                            }
+                        }
+                    }
+                }
+            };
+            if (__builtin_expect(two_terms, 0)) sum_values(Int<2>());
+            else sum_values(Int<1>());
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                issue_rest(t + S::RING * step, buf);
+            }
+            buf = buf + 1 == S::RING ? 0 : buf + 1;
+        }
+
+        // ---- the rows' sums of this wave: lane (col, qk) holds elements 16 c + 4 qk .. + 3 of row 16 ct + col.  What is worked out
+        // from the lane here is worked out from an opaque copy of it, or it would be kept in registers through the tile loop.
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const int col = tid % 16, qk = tid % kWave / 16;
+        auto sums = [&](int ct, int c) __attribute__((always_inline)) {
+            float4_t o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(acc[ct][c][r], kCodeScaleA, GV == 4 ? pbacc[ct][c / 4] : pb[ct][c / 4]);
+            return o;
+        };
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
+            if (GV != 4) {
+#pragma unroll
+                for (int g = 0; g < GV; ++g) pb[ct][g] = xor32_sum(xor16_sum(pb[ct][g]));
+            }
+        }
+        auto finish_quad = [&](int64_t row, int e, float m, float l, float4_t o) __attribute__((always_inline)) {
+            if (u.whole_row) {
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                const half2_t a = half2_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv)}, b = half2_t{(half_t)(o[2] * inv), (half_t)(o[3] * inv)};
+                *reinterpret_cast<uint2 *>(p.out + row * DV + e) = make_uint2(half2_to_bits(a), half2_to_bits(b));
+            } else {
+                const int64_t rec = row * (2 * p.slots) + u.which * p.slots + u.slot;
+                *reinterpret_cast<float4_t *>(p.part_acc + rec * DV + e) = o;
+                if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + rec * 2) = make_float2(m, l);
+            }
+        };
+        if (solo) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if (16 * ct + col >= u.rows) continue;
+                int agent;
+                const int64_t row = row_index(p, u, 16 * ct + col, agent);
+#pragma unroll
+                for (int c = 0; c < 4 * GV; ++c) finish_quad(row, 16 * c + 4 * qk, m_run[ct], l_run[ct], sums(ct, c));
+            }
+            return;
+        }
+        // the four waves of the workgroup join theirs, in wave order, by way of the tile buffers (nothing is on its way to them)
+        float *const mine_lds = reinterpret_cast<float *>(region);
+        wave_lds_sync();
+        if (mine > 0) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if (16 * ct + col >= u.rows) continue;
+#pragma unroll
+                for (int c = 0; c < 4 * GV; ++c)
+                    *reinterpret_cast<float4_t *>(mine_lds + (16 * ct + col) * S::ROW_PITCH + 16 * c + 4 * qk) = sums(ct, c);
+            }
+        }
+        if (qk == 0) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                ml_lds[wave][16 * ct + col][0] = m_run[ct];
+                ml_lds[wave][16 * ct + col][1] = mine > 0 ? l_run[ct] : 0.0f;
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < u.rows * (DV / 4); i += kThreads) {
+            const int r = i / (DV / 4), e = 4 * (i % (DV / 4));
+            float m = kNegBig, l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+                if (ml_lds[w][r][1] > 0.0f) m = fmaxf(m, ml_lds[w][r][0]);
+            float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float lw = ml_lds[w][r][1];
+                if (lw > 0.0f) {
+                    const float weight = __builtin_amdgcn_exp2f(ml_lds[w][r][0] - m);
+                    o += weight * *reinterpret_cast<const float4_t *>(tiles_lds + w * S::WAVE_BYTES + 4 * (r * S::ROW_PITCH + e));
+                    l = fmaf(weight, lw, l);
+                }
+            }
+            int agent;
+            finish_quad(row_index(p, u, r, agent), e, m, l, o);
+        }
+        __syncthreads(); // the tile buffers are free again
+    };
+
+    for (int x = (int)begin; x < x1;) {
+        const Part u = locate(p, plan, x, x1, per, worker);
+        if (CTP > 1 && u.which == 0) run_part(Int<CTP>(), u);
+        else run_part(Int<1>(), u);
+        x += u.count;
+    }
+}
+
+// Joins the records of every (layer, agent, query head): first the prefix's, then those of the agent's own tokens, in the order
+// of their workers.  A thread owns four elements.  Rows that the attention launch finished itself are left alone; rows that see
+// no token become zeros.
+constexpr int kBatch = 8; // records asked for together
+
+__global__ __launch_bounds__(kThreads) void prefix_merge_kernel(const float *__restrict__ part_acc, const float *__restrict__ part_ml,
+                                                                const int32_t *__restrict__ plan, uint16_t *__restrict__ out,
+                                                                int num_agents, int q_heads, int kv_heads, int v_dim, int slots,
+                                                                int row_tile, long long rows)
+{
+    const int quads = v_dim / 4;
+    const long long idx = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const long long row = idx / quads;
+    if (row >= rows) return;
+    const int e = 4 * (int)(idx % quads);
+    const int qh = (int)(row % q_heads), agent = (int)((row / q_heads) % num_agents), li = (int)(row / ((long long)q_heads * num_agents));
+    const int n_rep = q_heads / kv_heads, kvh = qh / n_rep;
+    const int per = plan[0], head_tiles = plan[1], group_tiles = plan[2];
+    const int own0 = plan[kHeader + agent], own_tiles = plan[kHeader + agent + 1] - own0;
+    const int shared = plan[kHeader + num_agents + 1 + agent];
+    const int group0 = plan[kHeader + 2 * num_agents + 1 + agent], first_agent = plan[kHeader + 3 * num_agents + 1 + agent];
+    const int base = (li * kv_heads + kvh) * head_tiles;
+    int n_prefix = 0, n_own = 0;
+    if (shared > 0) {
+        const int u0 = base + group0 + ((agent - first_agent) * n_rep + qh - kvh * n_rep) / row_tile * shared;
+        n_prefix = (u0 + shared - 1) / per - u0 / per + 1;
+    }
+    if (own_tiles > 0) {
+        const int u0 = base + group_tiles + own0;
+        n_own = (u0 + own_tiles - 1) / per - u0 / per + 1;
+    }
+    if (shared == 0 && n_own == 1) return;
+    const int records = n_prefix + n_own;
+    const long long rec0 = row * (2 * slots);
+    float m = kNegBig, l = 0.0f;
+    float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < records; s0 += kBatch) {
+        float mm[kBatch], ll[kBatch];
+        float4_t a[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int s = min(s0 + k, records - 1);
+            const long long rec = rec0 + (s < n_prefix ? s : slots + s - n_prefix);
+            const float2 t = *reinterpret_cast<const float2 *>(part_ml + rec * 2);
+            mm[k] = t.x;
+            ll[k] = s0 + k < records ? t.y : 0.0f;
+            a[k] = *reinterpret_cast<const float4_t *>(part_acc + rec * v_dim + e);
+        }
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (ll[k] > 0.0f) m_new = fmaxf(m_new, mm[k]);
+        const float keep = __builtin_amdgcn_exp2f(m - m_new);
+        l *= keep;
+        o *= keep;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (!(ll[k] > 0.0f)) continue;
+            const float weight = __builtin_amdgcn_exp2f(mm[k] - m_new);
+            l = fmaf(weight, ll[k], l);
+            o += weight * a[k];
+        }
+        m = m_new;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const half2_t lo = half2_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv)}, hi = half2_t{(half_t)(o[2] * inv), (half_t)(o[3] * inv)};
+    *reinterpret_cast<uint2 *>(out + row * v_dim + e) = make_uint2(half2_to_bits(lo), half2_to_bits(hi));
+}
+
+template <int DK, int DV, int CTP>
+hipError_t launch_t(const PrefixParams &p, bool bf, int compute_units, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(compute_units * Shape<DK, DV>::WAVES_PER_SIMD));
+    if (bf) hipLaunchKernelGGL((prefix_attention_kernel<DK, DV, CTP, true>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((prefix_attention_kernel<DK, DV, CTP, false>), grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+// Column tiles of a prefix unit: as many as the rows of an average group fill, up to two.
+int column_tiles(const q4kv_spec &s, int num_agents, int num_groups)
+{
+    if (num_groups == 0) return 1;
+    const int rows = s.num_q_heads / s.num_kv_heads * ((num_agents + num_groups - 1) / num_groups);
+    return rows > kCols ? 2 : 1;
+}
+
+// Records per row and part (see q4kv_shared_prefix_attention in api.hip for the workspace): a worker's range is at least
+// kLeastTiles (a workgroup's) or kSoloTiles (a wave's) long, and no shorter than an even share of all tiles, to which a unit of T
+// tiles contributes T for every layer and KV head.
+int record_slots(const q4kv_spec &s, int max_seq_len, int layers, int workgroups)
+{
+    const int64_t tiles = (max_seq_len + kWave - 1) / kWave, units = (int64_t)layers * s.num_kv_heads;
+    const int64_t shared = std::min<int64_t>(tiles / kLeastTiles, workgroups / units);
+    const int64_t solo = std::min<int64_t>(tiles / kSoloTiles, (int64_t)workgroups * kWaves / units);
+    return (int)std::max(shared, solo) + 2;
+}
+
+int prefix_workgroups(int compute_units) { return compute_units; }
+
+} // namespace
+
+int prefix_max_agents() { return kMaxAgents; }
+
+bool prefix_supported(const q4kv_spec &s)
+{
+    if (s.v_aliases_k || s.num_q_heads / s.num_kv_heads > kCols) return false;
+    return (s.k_dim == s.v_dim && (s.k_dim == 64 || s.k_dim == 128 || s.k_dim == 256)) || (s.k_dim == 192 && s.v_dim == 128);
+}
+
+int64_t prefix_tiles(const q4kv_spec &s, int num_agents, int num_groups, int max_seq_len, int layers)
+{
+    const int row_tile = kCols * column_tiles(s, num_agents, num_groups), n_rep = s.num_q_heads / s.num_kv_heads;
+    const int64_t row_tiles = ((int64_t)num_agents * n_rep + row_tile - 1) / row_tile + num_groups;
+    return (int64_t)layers * s.num_kv_heads * (num_agents + row_tiles) * ((max_seq_len + kWave - 1) / kWave);
+}
+
+size_t prefix_workspace_bytes(const q4kv_spec &s, int num_agents, int max_seq_len, int layers, int compute_units, size_t &acc_at, size_t &ml_at)
+{
+    const int slots = record_slots(s, max_seq_len, layers, prefix_workgroups(compute_units));
+    const size_t records = (size_t)layers * num_agents * s.num_q_heads * 2 * slots;
+    acc_at = ((size_t)plan_ints(num_agents) * sizeof(int32_t) + 255) / 256 * 256;
+    ml_at = acc_at + records * s.v_dim * sizeof(float);
+    return ml_at + records * 2 * sizeof(float);
+}
+
+hipError_t launch_prefix_attention(const PrefixArgs &a, hipStream_t stream)
+{
+    const q4kv_spec &s = *a.spec;
+    PrefixParams p;
+    p.k_codes = a.k->codes; p.k_scale = a.k->scale; p.k_bias = a.k->bias;
+    p.v_codes = a.v->codes; p.v_scale = a.v->scale; p.v_bias = a.v->bias;
+    p.q = a.q; p.out = a.out;
+    p.block_table = a.block_table; p.seq_len = a.seq_len; p.group_begin = a.group_begin; p.prefix_len = a.prefix_len;
+    size_t acc_at, ml_at;
+    prefix_workspace_bytes(s, a.num_agents, a.max_seq_len, a.layers, a.compute_units, acc_at, ml_at);
+    p.plan = static_cast<int32_t *>(a.workspace);
+    p.part_acc = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + acc_at);
+    p.part_ml = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ml_at);
+    p.num_agents = a.num_agents; p.num_groups = a.num_groups; p.max_blocks = a.max_blocks; p.num_blocks = a.k->num_blocks;
+    p.kv_heads = s.num_kv_heads; p.q_heads = s.num_q_heads; p.n_rep = s.num_q_heads / s.num_kv_heads;
+    p.layer_begin = a.layer_begin; p.layers = a.layers; p.max_seq_len = a.max_seq_len;
+    p.slots = record_slots(s, a.max_seq_len, a.layers, prefix_workgroups(a.compute_units));
+    const int ct = column_tiles(s, a.num_agents, a.num_groups);
+    p.row_tile = kCols * ct;
+    p.score_scale = a.sm_scale * kLog2e;
+    const bool bf = s.param_format == Q4KV_PARAMS_BF16;
+    hipError_t e = hipErrorInvalidValue;
+#define Q4KV_PREFIX(DK, DV) e = ct == 2 ? launch_t<DK, DV, 2>(p, bf, a.compute_units, stream) : launch_t<DK, DV, 1>(p, bf, a.compute_units, stream)
+    if (s.k_dim == 256) Q4KV_PREFIX(256, 256);
+    else if (s.k_dim == 192) Q4KV_PREFIX(192, 128);
+    else if (s.k_dim == 128) Q4KV_PREFIX(128, 128);
+    else if (s.k_dim == 64) Q4KV_PREFIX(64, 64);
+#undef Q4KV_PREFIX
+    if (e != hipSuccess) return e;
+    const int64_t rows = (int64_t)a.layers * a.num_agents * s.num_q_heads, threads = rows * (s.v_dim / 4);
+    hipLaunchKernelGGL(prefix_merge_kernel, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p.part_acc,
+                       p.part_ml, p.plan, p.out, a.num_agents, s.num_q_heads, s.num_kv_heads, s.v_dim, p.slots, p.row_tile, (long long)rows);
+    return hipGetLastError();
+}
+
+} // namespace q4kv

@@ -91,6 +91,26 @@ size_t chunk_workspace_bytes(const q4kv_spec &spec, int num_agents, int q_len, i
                              size_t &acc_bytes);
 hipError_t launch_chunk_attention(const AttentionArgs &a, hipStream_t stream);
 
+// prefix_attention.hip: decode attention of agents that share prefixes
+struct PrefixArgs {
+    const q4kv_spec *spec;
+    const q4kv_pool *k, *v;
+    const uint16_t *q;
+    uint16_t *out;
+    const int32_t *block_table, *seq_len, *group_begin, *prefix_len;
+    int max_blocks, num_agents, num_groups, max_seq_len, layer_begin, layers, compute_units;
+    float sm_scale;
+    void *workspace;
+};
+int prefix_max_agents();
+bool prefix_supported(const q4kv_spec &s);
+// an upper bound of the 64-token tiles of a call
+int64_t prefix_tiles(const q4kv_spec &s, int num_agents, int num_groups, int max_seq_len, int layers);
+// bytes of workspace, and where in it the sums and the maxima and denominators of the records begin
+size_t prefix_workspace_bytes(const q4kv_spec &s, int num_agents, int max_seq_len, int layers, int compute_units, size_t &acc_at,
+                              size_t &ml_at);
+hipError_t launch_prefix_attention(const PrefixArgs &a, hipStream_t stream);
+
 // persist.hip: bytes of one (layer, block) record of a block image; gather (to_image) or scatter of `num_blocks`
 // listed blocks of every layer between the pools and the image (v: null when V aliases K)
 size_t image_record_bytes(const q4kv_spec &s);

@@ -120,3 +120,39 @@ def test_pool_around_arrays_and_head_forms_check_their_shapes():
         b.HeadForm(rot_dim=64, cos=torch.ones(10, 32)).c(1)
     c = b.HeadForm().c(1)
     assert c.q_weight is None and c.rot_dim == 0 and c.table_len == 0
+
+
+def test_shared_prefix_argument_errors():
+    l, spec = b.lib(), b.make_spec(2, 4, 2, 128)
+
+    def call(spec=spec, kp=_pool(), vp=_pool(), q=0x4000, out=0x5000, bt=0x6000, mb=4, sl=0x7000, A=3, gb=0x8000, pl=0x9000, G=2, msl=1024, lb=0, le=2,
+             ws=0xA000, wsb=1 << 40):
+        return l.q4kv_shared_prefix_attention(C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), q, out, bt, mb, sl, A, gb, pl, G, msl, 0.1,
+                                              lb, le, ws, wsb, None)
+
+    assert call(A=0, G=0) == 0 and call(lb=1, le=1) == 0                        # nothing to do
+    assert call(msl=1025) == -3 and "max_blocks" in _err()
+    assert call(A=513) == -3 and "512" in _err() and call(G=4) == -3            # more groups than agents
+    for bad in (dict(le=3), dict(lb=-1), dict(A=-1), dict(G=-1), dict(mb=0), dict(msl=-1), dict(q=None), dict(out=None), dict(bt=None), dict(sl=None),
+                dict(gb=None), dict(pl=None), dict(q=0x4008), dict(out=0x5002), dict(kp=b._CPool(0x1004, 0x2000, 0x3000, 4)), dict(vp=_pool(5)),
+                dict(vp=None)):
+        assert call(**bad) == -1, bad
+    need = b.q4kv_shared_prefix_workspace_bytes(spec, 3, 1024, 2)
+    assert need > 0 and call(wsb=need - 1) == -4 and "workspace" in _err() and call(ws=None) == -4 and call(ws=0xA008) == -4
+    assert call(G=0, gb=None, pl=None, wsb=need - 1) == -4                      # no groups: the arrays are not looked at
+    for bad in (b.make_spec(2, 16, 1, 576, 512, True), b.make_spec(2, 34, 2, 128), b.make_spec(2, 4, 2, 192, 192), b.make_spec(2, 4, 2, 512),
+                b.make_spec(2, 4, 2, 128, 64)):
+        assert call(spec=bad) == -2 and "no shared-prefix kernel" in _err()
+    assert call(spec=b.make_spec(2, 5, 2, 128)) == -2
+    huge = b.make_spec(4000, 64, 64, 128)
+    assert call(spec=huge, A=512, G=1, mb=1 << 16, msl=1 << 24, le=4000) == -3 and "tiles" in _err()
+    assert b.q4kv_shared_prefix_workspace_bytes(spec, 0, 1024, 2) == 0 and b.q4kv_shared_prefix_workspace_bytes(spec, 3, -1, 2) == 0
+    assert b.q4kv_shared_prefix_workspace_bytes(spec, 3, 1024, 0) == 0
+
+
+def test_shared_prefix_workspace_does_not_fall_with_agents():
+    spec = b.make_spec(48, 16, 8, 256)
+    for layers in (1, 3, 48):
+        for top in (64, 1000, 32768):
+            sizes = [b.q4kv_shared_prefix_workspace_bytes(spec, a, top, layers) for a in (1, 2, 10, 100, 512)]
+            assert sizes == sorted(sizes) and all(n % 8 == 0 for n in sizes)
