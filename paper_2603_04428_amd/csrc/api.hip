@@ -535,7 +535,7 @@ int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, cons
     const int layers = layer_end - layer_begin;
     if (q4kv::prefix_tiles(*spec, num_agents, num_groups, max_seq_len, layers) > 0x7fffffffLL)
         return fail(Q4KV_ERANGE, "more than 2^31 tiles in one call: split the layer range");
-    if ((int64_t)layers * num_agents * spec->num_q_heads * (spec->v_dim / 4) > 0x7fffffffLL * 256)
+    if ((int64_t)layers * num_agents * spec->num_q_heads > 0x7fffffffLL)
         return fail(Q4KV_ERANGE, "more rows than a launch can have: split the layer range");
     size_t acc_at, ml_at;
     const size_t need = q4kv::prefix_workspace_bytes(*spec, num_agents, max_seq_len, layers, compute_units(), acc_at, ml_at);

@@ -38,7 +38,7 @@ constexpr int kSoloTiles = 16;     // tiles per wave from which the waves of a w
 constexpr int kLeastTiles = 4;     // smallest range of a workgroup: a tile per wave
 constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint32_t kOneTermBits = 0x37D7;   // binary16 0.49: largest value scale for which one binary16 term of p s keeps the tolerance
+constexpr uint32_t kOneTermBits = 0x3B5C;   // binary16 0.92: largest value scale for which one binary16 term of p s keeps the tolerance
 constexpr uint32_t kLiftScaleBits = 0x5BE0; // binary16 252: 2^8 times that is still below 65504
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
@@ -66,23 +66,24 @@ struct PrefixParams {
     float score_scale;
 };
 
-// What the merge needs to know of the plan, written by workgroup 0: header, then per agent the tiles in front of its own part,
-// where that part begins (in tiles; the tiles of the prefix it shares), the tiles in front of its group's units, and the
-// group's first agent.
-constexpr int kHeader = 4; // [0] tiles per worker  [1] tiles of a (layer, KV head)  [2] tiles of its prefix units
-__host__ __device__ constexpr int plan_ints(int agents) { return kHeader + 4 * agents + 1; }
+// What the merge needs to know of the plan, written by workgroup 0: header, then per agent what is counted in front of its own
+// part, that part's tiles, where it begins (the tiles of the prefix it shares), what is counted in front of its group's units,
+// and the group's first agent.
+constexpr int kHeader = 4; // [0] tiles per worker  [1] tiles counted for a (layer, KV head)  [2] for its prefix units  [3] Plan::round
+__host__ __device__ constexpr int plan_ints(int agents) { return kHeader + 5 * agents; }
 
 // ---------------------------------------------------------------------------------------------- the plan
 
 // The tiles of a (layer, KV head): all prefix units (group by group, row tile by row tile), then the agents' own parts.  Every
-// workgroup works it out for itself, in LDS.
+// workgroup works it out for itself, in LDS.  A unit may count for more tiles than it has: see spread().
 struct Plan {
-    int own[kMaxAgents + 1];   // tiles of the agents in front of an agent
-    int group[kMaxAgents + 1]; // tiles of the prefix units of the groups in front of a group
+    int own[kMaxAgents + 1];   // tiles that the agents in front of an agent count for
+    int group[kMaxAgents + 1]; // tiles that the prefix units of the groups in front of a group count for
     int len[kMaxAgents];       // visible tokens of an agent
     int start[kMaxAgents];     // tile its own part begins with
     int begin[kMaxAgents + 1]; // first agent of a group
-    int wave_sum[2][kWaves];
+    int wave_sum[4][kWaves];
+    int per, round, solo; // tiles of a worker; a unit's tiles are counted as the next multiple of `round`; 1: waves are the workers
 };
 
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + kWave - 1) / kWave; }
@@ -98,6 +99,7 @@ __device__ __forceinline__ int wave_scan(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false); // row_bcast31 into rows 2 and 3
     return v;
 }
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), kWave - 1); }
 
 // inclusive maximum over the lanes of values that are not negative
 __device__ __forceinline__ int wave_scan_max(int v)
@@ -111,8 +113,20 @@ __device__ __forceinline__ int wave_scan_max(int v)
     return v;
 }
 
-// the last index of 0 .. count - 1 whose entry is at most x (entries do not fall; entry 0 is at most x)
+// the last index of 0 .. count - 1 whose entry is at most x (entries do not fall; entry 0 is at most x), by all lanes of a wave
 __device__ __forceinline__ int last_at_most(const int *pre, int count, int x)
+{
+    int found = 0;
+    for (int i0 = 0; i0 < count; i0 += kWave) {
+        const int i = i0 + (int)(threadIdx.x % kWave);
+        const uint64_t below = __builtin_amdgcn_ballot_w64(i < count && pre[i < count ? i : 0] <= x);
+        if (below == 0) break;
+        found = i0 + 63 - __builtin_clzll(below);
+    }
+    return found;
+}
+// the same by one lane, each its own x
+__device__ __forceinline__ int lane_last_at_most(const int *pre, int count, int x)
 {
     int lo = 0, hi = count - 1;
     while (lo < hi) {
@@ -122,17 +136,96 @@ __device__ __forceinline__ int last_at_most(const int *pre, int count, int x)
     return lo;
 }
 
-__device__ __forceinline__ void make_plan(const PrefixParams &p, Plan &pl)
+__device__ __forceinline__ int rounded_up(int v, int round) { return (v + round - 1) / round * round; }
+
+// Tiles of a worker, and what units' tiles are rounded up to.  `total`: all tiles of the call, `padded(r)`: the same with every
+// unit's tiles rounded up to r.
+//   Many tiles: every wave takes an equal range of its own, wherever it begins.
+//   Few: every workgroup takes an equal range, its waves tile by tile in turn.  Where a range begins inside a unit and ends in
+//   another the workgroup pays for a second beginning and end (5 us: block ids, first tiles, queries, the join of the waves, against
+//   2 to 3 us a round of tiles), so units are cut into ranges of their own, each a multiple of a tile per wave, if that gives
+//   no more ranges than workgroups and none much longer than the even share.
+template <typename F>
+__device__ __forceinline__ bool spread(long long total, int workgroups, int &per, int &round, F padded)
+{
+    round = 1;
+    per = (int)((total + workgroups * kWaves - 1) / (workgroups * kWaves));
+    if (per >= kSoloTiles) return true;
+    per = max(kLeastTiles, (int)((total + workgroups - 1) / workgroups));
+    const int least = rounded_up(per, kWaves);
+    for (int r = least; r <= least + least / 2 + kWaves; r += kWaves)
+        if (padded(r) <= (long long)r * workgroups) {
+            per = round = r;
+            break;
+        }
+    return false;
+}
+
+// For up to 64 agents a wave does it in its lanes: lane a holds agent a, lane g group g.
+__device__ __forceinline__ void make_plan_few(const PrefixParams &p, Plan &pl)
+{
+    if (threadIdx.x < kWave) {
+        const int lane = threadIdx.x, A = p.num_agents, G = p.num_groups;
+        int n = lane < A ? p.seq_len[lane] : 0, prefix = lane < G ? p.prefix_len[lane] : 0;
+        const int bound = lane < G ? p.group_begin[lane] : 0, last = G > 0 ? p.group_begin[G] : 0;
+        n = min(max(n, 0), p.max_seq_len);
+        const int begin = wave_scan_max(min(max(bound, 0), A)); // bounds that fall are raised: groups never overlap
+        const int end = max(__builtin_amdgcn_readlane(begin, kWave - 1), min(max(last, 0), A));
+        int next = __shfl_down(begin, 1, kWave);
+        if (lane >= G - 1) next = end;
+        const int agents = lane < G ? next - begin : 0;
+        const int shared = agents > 1 ? min(max(prefix, 0), p.max_seq_len) / kWave : 0; // a group of one shares nothing
+        const int row_tiles = (agents * p.n_rep + p.row_tile - 1) / p.row_tile;
+        // lane a: the group its agent is in, from the first agents of the groups that have any
+        pl.start[lane] = 0;
+        wave_lds_sync();
+        if (agents > 0) pl.start[begin] = lane + 1;
+        wave_lds_sync();
+        const int mark = pl.start[lane];
+        const uint64_t upto = __builtin_amdgcn_ballot_w64(mark > 0) & (~0ull >> (63 - lane));
+        const int of = __shfl(mark, upto ? 63 - __builtin_clzll(upto) : lane, kWave); // group number + 1
+        wave_lds_sync();
+        const int of_end = __shfl(next, of - 1 < 0 ? 0 : of - 1, kWave), of_shared = __shfl(shared, of - 1 < 0 ? 0 : of - 1, kWave);
+        const int start = of > 0 && lane < of_end ? of_shared : 0;
+        const int own = lane < A ? max(0, tiles_of(n) - start) : 0;
+        const int units = p.layers * p.kv_heads; // (layer, KV head) pairs
+        int per, round;
+        const bool solo = spread((long long)wave_total(own + row_tiles * shared) * units, gridDim.x, per, round,
+                                 [&](int r) { return (long long)wave_total(rounded_up(own, r) + row_tiles * rounded_up(shared, r)) * units; });
+        const int group_counts = row_tiles * rounded_up(shared, round), own_counts = rounded_up(own, round);
+        const int group_incl = wave_scan(group_counts), own_incl = wave_scan(own_counts);
+        if (lane < A) {
+            pl.len[lane] = n;
+            pl.start[lane] = start;
+            pl.own[lane] = own_incl - own_counts;
+        }
+        if (lane < G) {
+            pl.begin[lane] = begin;
+            pl.group[lane] = group_incl - group_counts;
+        }
+        if (lane == kWave - 1) {
+            pl.own[A] = own_incl;
+            pl.group[G] = group_incl;
+            pl.begin[G] = end;
+            pl.per = per;
+            pl.round = round;
+            pl.solo = solo ? 1 : 0;
+        }
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
 {
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     constexpr int EACH = kMaxAgents / kThreads; // agents (and groups) of a thread
     const int A = p.num_agents, G = p.num_groups;
-    int n[EACH], shared_tiles[EACH], first[EACH];
+    int n[EACH], shared[EACH], first[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int a = tid * EACH + i;
         n[i] = a < A ? min(max(p.seq_len[a], 0), p.max_seq_len) : 0;
-        shared_tiles[i] = a < G ? min(max(p.prefix_len[a], 0), p.max_seq_len) / kWave : 0;
+        shared[i] = a < G ? min(max(p.prefix_len[a], 0), p.max_seq_len) / kWave : 0;
         if (a < A) pl.len[a] = n[i];
         first[i] = a < G ? min(max(p.group_begin[a], 0), A) : 0;
     }
@@ -152,77 +245,106 @@ __device__ __forceinline__ void make_plan(const PrefixParams &p, Plan &pl)
     if (tid == kThreads - 1) pl.begin[G] = G > 0 ? max(max(top, first[EACH - 1]), min(max(p.group_begin[G], 0), A)) : 0;
     __syncthreads();
     // a group of one agent shares nothing
-    int group_tiles[EACH], own_tiles[EACH], group_sum = 0, own_sum = 0;
+    int row_tiles[EACH], own[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int g = tid * EACH + i;
-        group_tiles[i] = 0;
+        row_tiles[i] = 0;
         if (g < G) {
             const int agents = pl.begin[g + 1] - pl.begin[g];
-            if (agents < 2) shared_tiles[i] = 0;
-            group_tiles[i] = shared_tiles[i] * (agents < 2 ? 0 : (agents * p.n_rep + p.row_tile - 1) / p.row_tile);
-            pl.group[g] = shared_tiles[i]; // for the agents, until the sums are taken
+            if (agents < 2) shared[i] = 0;
+            row_tiles[i] = (agents * p.n_rep + p.row_tile - 1) / p.row_tile;
+            pl.group[g] = shared[i]; // for the agents, until the sums are taken
         }
-        group_sum += group_tiles[i];
     }
     __syncthreads();
+    int sum = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int a = tid * EACH + i;
-        own_tiles[i] = 0;
+        own[i] = 0;
         if (a < A) {
             int start = 0;
             if (G > 0 && a >= pl.begin[0]) {
-                const int g = last_at_most(pl.begin, G, a);
+                const int g = lane_last_at_most(pl.begin, G, a);
                 if (a < pl.begin[g + 1]) start = pl.group[g];
             }
             pl.start[a] = start;
-            own_tiles[i] = max(0, tiles_of(n[i]) - start);
+            own[i] = max(0, tiles_of(n[i]) - start);
         }
-        own_sum += own_tiles[i];
+        sum += own[i] + row_tiles[i] * shared[i];
+    }
+    auto total = [&](int v, int slot) { // over the workgroup; every thread
+        const int of_wave = wave_total(v);
+        if (lane == 0) pl.wave_sum[slot][wave] = of_wave;
+        __syncthreads();
+        long long t = 0;
+        for (int w = 0; w < kWaves; ++w) t += pl.wave_sum[slot][w];
+        __syncthreads();
+        return t;
+    };
+    const int units = p.layers * p.kv_heads;
+    int per, round;
+    const bool solo = spread(total(sum, 1) * units, gridDim.x, per, round, [&](int r) {
+        int v = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) v += rounded_up(own[i], r) + row_tiles[i] * rounded_up(shared[i], r);
+        return total(v, 1) * units;
+    });
+    int group_sum = 0, own_sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        own[i] = rounded_up(own[i], round);
+        row_tiles[i] *= rounded_up(shared[i], round);
+        group_sum += row_tiles[i];
+        own_sum += own[i];
     }
     const int group_incl = wave_scan(group_sum), own_incl = wave_scan(own_sum);
     if (lane == kWave - 1) {
-        pl.wave_sum[0][wave] = group_incl;
-        pl.wave_sum[1][wave] = own_incl;
+        pl.wave_sum[2][wave] = group_incl;
+        pl.wave_sum[3][wave] = own_incl;
     }
     __syncthreads();
     int group_at = group_incl - group_sum, own_at = own_incl - own_sum;
     for (int w = 0; w < wave; ++w) {
-        group_at += pl.wave_sum[0][w];
-        own_at += pl.wave_sum[1][w];
+        group_at += pl.wave_sum[2][w];
+        own_at += pl.wave_sum[3][w];
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int a = tid * EACH + i;
         if (a <= G) pl.group[a] = group_at;
         if (a <= A) pl.own[a] = own_at;
-        group_at += group_tiles[i];
-        own_at += own_tiles[i];
+        group_at += row_tiles[i];
+        own_at += own[i];
     }
     if (tid == kThreads - 1) { // counts of exactly kMaxAgents
         if (G == kMaxAgents) pl.group[G] = group_at;
         if (A == kMaxAgents) pl.own[A] = own_at;
+        pl.per = per;
+        pl.round = round;
+        pl.solo = solo ? 1 : 0;
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ void write_plan(const PrefixParams &p, const Plan &pl, int per)
+__device__ __forceinline__ void write_plan(const PrefixParams &p, const Plan &pl)
 {
     const int A = p.num_agents, G = p.num_groups;
     if (threadIdx.x == 0) {
-        p.plan[0] = per;
+        p.plan[0] = pl.per;
         p.plan[1] = pl.group[G] + pl.own[A];
         p.plan[2] = pl.group[G];
+        p.plan[3] = pl.round;
     }
     for (int a = threadIdx.x; a < A; a += kThreads) {
-        const int g = G > 0 && a >= pl.begin[0] ? last_at_most(pl.begin, G, a) : 0;
+        const int g = G > 0 && a >= pl.begin[0] ? lane_last_at_most(pl.begin, G, a) : 0;
         p.plan[kHeader + a] = pl.own[a];
-        p.plan[kHeader + A + 1 + a] = pl.start[a];
-        p.plan[kHeader + 2 * A + 1 + a] = pl.group[g];
-        p.plan[kHeader + 3 * A + 1 + a] = pl.begin[g];
+        p.plan[kHeader + A + a] = max(0, tiles_of(pl.len[a]) - pl.start[a]);
+        p.plan[kHeader + 2 * A + a] = pl.start[a];
+        p.plan[kHeader + 3 * A + a] = pl.group[g];
+        p.plan[kHeader + 4 * A + a] = pl.begin[g];
     }
-    if (threadIdx.x == 0) p.plan[kHeader + A] = pl.own[A];
 }
 
 // ---------------------------------------------------------------------------------------------- tiles in LDS
@@ -238,9 +360,33 @@ __device__ __forceinline__ half8_t code_operand(uint32_t w)
     return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
 }
 
+// b + 8 s of two binary16 pairs: the middle of a group's range (s >= 0)
+__device__ __forceinline__ half2_t middle(uint32_t s, uint32_t b)
+{
+    return __builtin_elementwise_fma(bits_to_half2(s), half2_t{(half_t)8.0f, (half_t)8.0f}, bits_to_half2(b));
+}
+
 __device__ __forceinline__ float half_of(uint32_t pair, int hi)
 {
     return half_bits_to_float((uint16_t)(hi ? pair >> 16 : pair & 0xffffu));
+}
+
+// binary16 of p * s, rounded once, into the lower or the upper half of a register; s is the lower or the upper half of a word.
+// Written out: the compiler converts s, multiplies and converts back.
+template <bool UPPER>
+__device__ __forceinline__ uint32_t product_lower(float p, uint32_t s)
+{
+    uint32_t d;
+    if constexpr (UPPER) asm("v_fma_mixlo_f16 %0, %1, %2, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "=v"(d) : "v"(p), "v"(s));
+    else asm("v_fma_mixlo_f16 %0, %1, %2, 0 op_sel_hi:[0,1,0]" : "=v"(d) : "v"(p), "v"(s));
+    return d;
+}
+template <bool UPPER>
+__device__ __forceinline__ uint32_t product_upper(uint32_t d, float p, uint32_t s)
+{
+    if constexpr (UPPER) asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
+    else asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
+    return d;
 }
 
 __device__ __forceinline__ float xor16_max(float x)
@@ -372,27 +518,28 @@ struct Part {
     int agent, agents; // the agents whose rows read it: first, number
     int row0, rows;    // rows of this unit: row0 .. row0 + rows - 1 of those agents' rows
     int tile, count;   // the part: first tile (of the agent's tokens), number of tiles
-    int slot, slots;   // the part's record among the unit's
+    int counted;       // what it counts for in the plan
+    int slot;          // the part's record among the unit's
     int which;         // 0: prefix, 1: own tokens
     int whole_row;     // 1: there is nothing else to join, the rows' outputs are final
 };
 
-__device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, int x, int x1, int per, int worker)
+__device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, int x, int x1, int per, int round, int worker)
 {
     Part u;
-    const int group_tiles = pl.group[p.num_groups], head_tiles = group_tiles + pl.own[p.num_agents];
+    const int group_tiles = uniform(pl.group[p.num_groups]), head_tiles = group_tiles + uniform(pl.own[p.num_agents]);
     const int lk = x / head_tiles;
-    int r = x - lk * head_tiles, tiles, unit0;
+    int r = x - lk * head_tiles, tiles;
     u.li = lk / p.kv_heads;
     u.kvh = lk - u.li * p.kv_heads;
     if (r < group_tiles) {
         const int g = last_at_most(pl.group, p.num_groups, r);
-        u.agent = pl.begin[g];
-        u.agents = pl.begin[g + 1] - u.agent;
-        tiles = pl.start[u.agent];
-        r -= pl.group[g];
-        const int rt = r / tiles;
-        r -= rt * tiles;
+        u.agent = uniform(pl.begin[g]);
+        u.agents = uniform(pl.begin[g + 1]) - u.agent;
+        tiles = uniform(pl.start[u.agent]);
+        r -= uniform(pl.group[g]);
+        const int counted = rounded_up(tiles, round), rt = r / counted;
+        r -= rt * counted;
         u.row0 = rt * p.row_tile;
         u.rows = min(p.row_tile, u.agents * p.n_rep - u.row0);
         u.tile = r;
@@ -401,22 +548,23 @@ __device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, in
         r -= group_tiles;
         u.agent = last_at_most(pl.own, p.num_agents, r);
         u.agents = 1;
-        tiles = pl.own[u.agent + 1] - pl.own[u.agent];
-        r -= pl.own[u.agent];
+        const int start = uniform(pl.start[u.agent]);
+        tiles = max(0, tiles_of(uniform(pl.len[u.agent])) - start);
+        r -= uniform(pl.own[u.agent]);
         u.row0 = 0;
         u.rows = p.n_rep;
-        u.tile = r + pl.start[u.agent];
+        u.tile = r + start;
         u.which = 1;
     }
-    u.count = min(tiles - r, x1 - x);
-    unit0 = x - r;
-    const int first = unit0 / per;
-    u.slot = worker - first;
-    u.slots = (unit0 + tiles - 1) / per - first + 1;
-    u.whole_row = u.which == 1 && u.slots == 1 && pl.start[u.agent] == 0;
+    const int unit0 = x - r, counted = rounded_up(tiles, round);
+    u.counted = min(counted - r, x1 - x);
+    u.count = min(tiles - r, x1 - x); // at least one: what a unit counts for beyond its tiles is less than a worker's range
+    // a unit that begins in front of this worker's range may have begun several ranges before
+    u.slot = r == 0 ? 0 : worker - unit0 / per;
+    u.whole_row = u.which == 1 && u.tile == r && u.slot == 0 && u.count == tiles;
     u.li = uniform(u.li); u.kvh = uniform(u.kvh); u.agent = uniform(u.agent); u.agents = uniform(u.agents);
     u.row0 = uniform(u.row0); u.rows = uniform(u.rows); u.tile = uniform(u.tile); u.count = uniform(u.count);
-    u.slot = uniform(u.slot); u.slots = uniform(u.slots); u.which = uniform(u.which); u.whole_row = uniform(u.whole_row);
+    u.counted = uniform(u.counted); u.slot = uniform(u.slot); u.whole_row = uniform(u.whole_row); u.which = uniform(u.which);
     return u;
 }
 
@@ -439,14 +587,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
     __shared__ float ml_lds[kWaves][CTP * kCols][2];
 
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
-    make_plan(p, plan);
-    const int head_tiles = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]);
-    const int total = head_tiles * p.kv_heads * p.layers; // the host keeps this below 2^31
-    const int workgroups = gridDim.x;
-    int per = (total + workgroups * kWaves - 1) / (workgroups * kWaves);
-    const bool solo = per >= kSoloTiles;
-    if (!solo) per = max(kLeastTiles, (total + workgroups - 1) / workgroups);
-    if (blockIdx.x == 0) write_plan(p, plan, per);
+    if (p.num_agents <= kWave) make_plan_few(p, plan);
+    else make_plan_many(p, plan);
+    const int per = uniform(plan.per), round = uniform(plan.round);
+    const int total = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]) * p.kv_heads * p.layers; // the host keeps it below 2^31
+    const bool solo = uniform(plan.solo) != 0;
+    if (blockIdx.x == 0) write_plan(p, plan);
     const int worker = solo ? (int)blockIdx.x * kWaves + wave : (int)blockIdx.x;
     const long long begin = (long long)worker * per;
     if (begin >= total) return; // a whole workgroup, or a wave on its own
@@ -598,14 +744,14 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         n_min = uniform(n_min);
         n_max = uniform(n_max);
         float4_t acc[CT][4 * GV], pbacc[CT];
-        float pb[CT][GV], m_run[CT], l_run[CT];
+        float pb[CT][2 * GV], m_run[CT], l_run[CT]; // pb (up to two groups): even and odd rows r of the bias sums
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
             for (int c = 0; c < 4 * GV; ++c) acc[ct][c] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
             pbacc[ct] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int g = 0; g < GV; ++g) pb[ct][g] = 0.0f;
+            for (int g = 0; g < 2 * GV; ++g) pb[ct][g] = 0.0f;
             m_run[ct] = kNegBig;
             l_run[ct] = 0.0f;
         }
@@ -718,12 +864,17 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
 
             // ---- online softmax.  m_run is the reference the exponentials are taken against: it moves only when a tile's maximum
             // exceeds it by more than 7 (in log2 units), and then to 4 below that maximum.  p <= 2^7 then, and p s stays inside
-            // binary16 for scales up to 252; in a tile with a larger one p <= 2^2.5.
+            // binary16 for scales up to 252; in a tile with a larger one p <= 2^2.5.  The codes of the odd rows r arrive 16 times
+            // larger in operand A (code_operand): z of an odd r becomes p / 16.
+            float zs = p.score_scale * kCodeScaleA;
+            if (__builtin_expect(!(p.score_scale > 0.0f), 0)) { // the maximum may not be taken before the scale is applied
+                asm volatile("");
+#pragma unroll
+                for (int k = 0; k < 16 * CT; ++k) z[k / 16][k / 4 % 4][k % 4] *= zs;
+                zs = 1.0f;
+            }
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                const float zs = p.score_scale * kCodeScaleA;
-#pragma unroll
-                for (int k = 0; k < 16; ++k) z[ct][k / 4][k % 4] *= zs;
                 if (__builtin_expect(edge, 0)) {
                     asm volatile("");
 #pragma unroll
@@ -735,93 +886,85 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 float mt = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) mt = fmaxf(mt, z[ct][k / 4][k % 4]);
-                mt = xor32_max(xor16_max(mt));
+                mt = xor32_max(xor16_max(mt)) * zs;
                 const bool above = mt > m_run[ct] + (wide ? 2.5f : 7.0f);
                 const float m_new = above ? mt - (wide ? 0.0f : 4.0f) : m_run[ct];
-                float psum = 0.0f;
+                const float minus_even = -m_new, minus_odd = -(m_new + 4.0f);
+                float even_sum = 0.0f, odd_sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float pr = __builtin_amdgcn_exp2f(z[ct][k / 4][k % 4] - m_new);
+                    const float pr = __builtin_amdgcn_exp2f(fmaf(z[ct][k / 4][k % 4], zs, (k & 1) ? minus_odd : minus_even));
                     z[ct][k / 4][k % 4] = pr;
-                    psum += pr;
+                    if (k & 1) odd_sum += pr; else even_sum += pr;
                 }
                 if (i > 0 && __builtin_amdgcn_ballot_w64(above) != 0ull) {
                     const float alpha = __builtin_amdgcn_exp2f(m_run[ct] - m_new);
                     l_run[ct] *= alpha;
                     pbacc[ct] *= alpha;
+                    if constexpr (GV != 4) {
 #pragma unroll
-                    for (int g = 0; g < GV; ++g) pb[ct][g] *= alpha;
+                        for (int g = 0; g < 2 * GV; ++g) pb[ct][g] *= alpha;
+                    }
 #pragma unroll
                     for (int c = 0; c < 4 * GV; ++c) acc[ct][c] *= alpha;
                 }
-                l_run[ct] += psum;
+                l_run[ct] += fmaf(16.0f, odd_sum, even_sum);
                 m_run[ct] = m_new;
             }
 
-            // ---- values
-            half2_t p16[CT][2][4]; // [half of the sets][r]: tokens 4 qk + r of sets 2 h and 2 h + 1
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) p16[ct][h][r] = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
+            // ---- values: V_hat = (c - 8) s + (b + 8 s).  The one rounding of p s is then relative to |c - 8| s, the size of the value
+            // around the middle of its group, and not to a code counted from the group's end.  The eight comes off behind the
+            // products: sum (c - 8) ps = sum c ps - 8 sum ps with the ps that were rounded, one more instruction per group and
+            // half, into the accumulator of the bias sums (its rows = groups).
             if constexpr (GV == 4) {
                 // rows of A = groups: the transposing read gives lane `col` group col % 4 of the four tokens that lanes 0, 4, 8, 12
                 // of its 16 point at
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int tok = 16 * (2 * h + ((col >> 2) & 1)) + 4 * qk + (col >> 3);
-                    const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + S::VB_AT + tok * 8;
-                    const short4_t b0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)at);
-                    const short4_t b1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + 16));
-                    const uint2 w0 = __builtin_bit_cast(uint2, b0), w1 = __builtin_bit_cast(uint2, b1);
-                    const half8_t bop = words_to_half8(w0.x, w0.y, w1.x, w1.y);
+                    const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + tok * 8;
+                    half2_t mid[4];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VB_AT + 16 * k)));
+                        const uint2 s = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VS_AT + 16 * k)));
+                        mid[2 * k] = middle(s.x, b.x);
+                        mid[2 * k + 1] = middle(s.y, b.y);
+                    }
+                    const half8_t bop = words_to_half8(half2_to_bits(mid[0]), half2_to_bits(mid[1]), half2_to_bits(mid[2]), half2_to_bits(mid[3]));
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
-                        const half8_t pop = words_to_half8(half2_to_bits(p16[ct][h][0]), half2_to_bits(p16[ct][h][1]),
-                                                           half2_to_bits(p16[ct][h][2]), half2_to_bits(p16[ct][h][3]));
-                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, pop, pbacc[ct], 0, 0, 0);
+                        uint32_t w[4]; // p of the tokens 4 qk + r of sets 2 h and 2 h + 1
+                        const half2_t sixteen = half2_t{(half_t)16.0f, (half_t)16.0f};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            half2_t v = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
+                            if (r & 1) v *= sixteen;
+                            w[r] = half2_to_bits(v);
+                        }
+                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(w[0], w[1], w[2], w[3]), pbacc[ct], 0, 0, 0);
                     }
                 }
-            } else {
+            }
+            // scales of tokens 16 j + 4 qk + r, four tokens a read
+            uint32_t s4[4][2 * GV];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 4; ++j) {
+                __builtin_memcpy(s4[j], __builtin_assume_aligned(params + S::VS_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
+                if constexpr (GV != 4) {
                     uint32_t b[2 * GV];
                     __builtin_memcpy(b, __builtin_assume_aligned(params + S::VB_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
+#pragma unroll
+                    for (int k = 0; k < 2 * GV; ++k) b[k] = half2_to_bits(middle(s4[j][k], b[k]));
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
 #pragma unroll
-                            for (int g = 0; g < GV; ++g)
-                                pb[ct][g] = fmaf(z[ct][j][r], half_of(b[(r * GV + g) / 2], (r * GV + g) & 1), pb[ct][g]);
+                            for (int g = 0; g < GV; ++g) // even and odd r apart: the odd ones are sixteenths
+                                pb[ct][(r & 1) * GV + g] = fmaf(z[ct][j][r], half_of(b[(r * GV + g) / 2], (r * GV + g) & 1), pb[ct][(r & 1) * GV + g]);
                 }
             }
-            // scales of tokens 16 j + 4 qk + r, paired over the two sets of a half
-            uint32_t s2[2][4][GV];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t even[2 * GV], odd[2 * GV];
-                const unsigned char *at = params + S::VS_AT + (32 * h + 4 * qk) * (2 * GV);
-                __builtin_memcpy(even, __builtin_assume_aligned(at, 8), 8 * GV);
-                __builtin_memcpy(odd, __builtin_assume_aligned(at + 16 * (2 * GV), 8), 8 * GV);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int g = 0; g < GV; ++g) {
-                        const int k = r * GV + g;
-                        s2[h][r][g] = __builtin_amdgcn_perm(odd[k / 2], even[k / 2], (k & 1) ? 0x07060302u : 0x05040100u);
-                    }
-            }
-            const half2_t sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f}; // codes of the odd rows r arrive 16 times larger
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    p16[ct][h][1] *= sixteenth;
-                    p16[ct][h][3] *= sixteenth;
-                }
             wait_values(min(mine - 1 - i, S::RING));
             const uint32_t va = v_at + base;
             auto sum_values = [&](auto terms) __attribute__((always_inline)) {
@@ -830,6 +973,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 for (int g = 0; g < GV; ++g) {
                     if (kTight) __builtin_amdgcn_sched_barrier(0);
                     half8_t hi[CT][2], lo[CT][2];
+                    const uint32_t minus_eight = col % 4 == g ? 0xC800C800u : 0u, sixteen_times = col % 4 == g ? 0xD800D800u : 0u;
+                    const half8_t eights = words_to_half8(minus_eight, sixteen_times, minus_eight, sixteen_times);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -837,12 +982,25 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                             uint32_t a[4], b[4];
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                const half2_t s = bits_to_half2(s2[h][r][g]), ps = p16[ct][h][r] * s;
-                                a[r] = half2_to_bits(ps);
-                                if (TWO) b[r] = half2_to_bits(__builtin_elementwise_fma(p16[ct][h][r], s, -ps));
+                                const int at = r * GV + g;
+                                if constexpr (!TWO) {
+                                    const uint32_t w0 = s4[2 * h][at / 2], w1 = s4[2 * h + 1][at / 2];
+                                    const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
+                                    a[r] = at & 1 ? product_upper<true>(product_lower<true>(p0, w0), p1, w1)
+                                                  : product_upper<false>(product_lower<false>(p0, w0), p1, w1);
+                                    continue;
+                                }
+                                const float s0 = half_of(s4[2 * h][at / 2], at & 1), s1 = half_of(s4[2 * h + 1][at / 2], at & 1);
+                                const half_t p0 = (half_t)(z[ct][2 * h][r] * s0), p1 = (half_t)(z[ct][2 * h + 1][r] * s1);
+                                a[r] = half2_to_bits(half2_t{p0, p1});
+                                b[r] = half2_to_bits(half2_t{(half_t)fmaf(z[ct][2 * h][r], s0, -(float)p0), (half_t)fmaf(z[ct][2 * h + 1][r], s1, -(float)p1)});
                             }
+                            // the compiler does not see vector instructions in asm statements: the distance a matrix instruction may want
+                            if (!TWO) asm("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
                             hi[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
                             if (TWO) lo[ct][h] = words_to_half8(b[0], b[1], b[2], b[3]);
+                            pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, hi[ct][h], pbacc[ct], 0, 0, 0);
+                            if (TWO) pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, lo[ct][h], pbacc[ct], 0, 0, 0);
                         }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -878,7 +1036,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         auto sums = [&](int ct, int c) __attribute__((always_inline)) {
             float4_t o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = fmaf(acc[ct][c][r], kCodeScaleA, GV == 4 ? pbacc[ct][c / 4] : pb[ct][c / 4]);
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(acc[ct][c][r], kCodeScaleA, GV == 4 ? pbacc[ct][c / 4] : pb[ct][c / 4] + pbacc[ct][c / 4]);
             return o;
         };
 #pragma unroll
@@ -886,7 +1044,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
             if (GV != 4) {
 #pragma unroll
-                for (int g = 0; g < GV; ++g) pb[ct][g] = xor32_sum(xor16_sum(pb[ct][g]));
+                for (int g = 0; g < GV; ++g) pb[ct][g] = xor32_sum(xor16_sum(fmaf(16.0f, pb[ct][GV + g], pb[ct][g])));
             }
         }
         auto finish_quad = [&](int64_t row, int e, float m, float l, float4_t o) __attribute__((always_inline)) {
@@ -954,60 +1112,53 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
     };
 
     for (int x = (int)begin; x < x1;) {
-        const Part u = locate(p, plan, x, x1, per, worker);
+        const Part u = locate(p, plan, x, x1, per, round, worker);
         if (CTP > 1 && u.which == 0) run_part(Int<CTP>(), u);
         else run_part(Int<1>(), u);
-        x += u.count;
+        x += u.counted;
     }
 }
 
-// Joins the records of every (layer, agent, query head): first the prefix's, then those of the agent's own tokens, in the order
-// of their workers.  A thread owns four elements.  Rows that the attention launch finished itself are left alone; rows that see
-// no token become zeros.
-constexpr int kBatch = 8; // records asked for together
+// Joins the records of every (layer, agent, query head): the prefix's, then those of the agent's own tokens.  A workgroup owns a row;
+// a thread four elements of every PARTS-th record, kBatch of them asked for together; the threads' sums are joined in order.  Rows
+// that the attention launch finished itself are left alone; rows that see no token become zeros.
+constexpr int kBatch = 4;
 
+template <int DV>
 __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(const float *__restrict__ part_acc, const float *__restrict__ part_ml,
                                                                 const int32_t *__restrict__ plan, uint16_t *__restrict__ out,
-                                                                int num_agents, int q_heads, int kv_heads, int v_dim, int slots,
-                                                                int row_tile, long long rows)
+                                                                int num_agents, int q_heads, int kv_heads, int slots, int row_tile)
 {
-    const int quads = v_dim / 4;
-    const long long idx = (long long)blockIdx.x * kThreads + threadIdx.x;
-    const long long row = idx / quads;
-    if (row >= rows) return;
-    const int e = 4 * (int)(idx % quads);
-    const int qh = (int)(row % q_heads), agent = (int)((row / q_heads) % num_agents), li = (int)(row / ((long long)q_heads * num_agents));
+    constexpr int QUADS = DV / 4, PARTS = kThreads / QUADS;
+    __shared__ float4_t s_acc[PARTS][QUADS];
+    __shared__ float s_ml[PARTS][2];
+    const int64_t row = blockIdx.x;
+    const int quad = threadIdx.x % QUADS, part = threadIdx.x / QUADS;
+    const int qh = (int)(row % q_heads), agent = (int)(row / q_heads % num_agents), li = (int)(row / q_heads / num_agents);
     const int n_rep = q_heads / kv_heads, kvh = qh / n_rep;
-    const int per = plan[0], head_tiles = plan[1], group_tiles = plan[2];
-    const int own0 = plan[kHeader + agent], own_tiles = plan[kHeader + agent + 1] - own0;
-    const int shared = plan[kHeader + num_agents + 1 + agent];
-    const int group0 = plan[kHeader + 2 * num_agents + 1 + agent], first_agent = plan[kHeader + 3 * num_agents + 1 + agent];
+    const int per = plan[0], head_tiles = plan[1], group_tiles = plan[2], round = plan[3];
+    const int own0 = plan[kHeader + agent], own_tiles = plan[kHeader + num_agents + agent], shared = plan[kHeader + 2 * num_agents + agent];
+    const int group0 = plan[kHeader + 3 * num_agents + agent], first_agent = plan[kHeader + 4 * num_agents + agent];
     const int base = (li * kv_heads + kvh) * head_tiles;
-    int n_prefix = 0, n_own = 0;
-    if (shared > 0) {
-        const int u0 = base + group0 + ((agent - first_agent) * n_rep + qh - kvh * n_rep) / row_tile * shared;
-        n_prefix = (u0 + shared - 1) / per - u0 / per + 1;
-    }
-    if (own_tiles > 0) {
-        const int u0 = base + group_tiles + own0;
-        n_own = (u0 + own_tiles - 1) / per - u0 / per + 1;
-    }
+    auto records_of = [&](int u0, int tiles) { return tiles > 0 ? (u0 + rounded_up(tiles, round) - 1) / per - u0 / per + 1 : 0; };
+    const int n_prefix = records_of(base + group0 + ((agent - first_agent) * n_rep + qh - kvh * n_rep) / row_tile * rounded_up(shared, round), shared);
+    const int n_own = records_of(base + group_tiles + own0, own_tiles);
     if (shared == 0 && n_own == 1) return;
     const int records = n_prefix + n_own;
-    const long long rec0 = row * (2 * slots);
+    const int64_t rec0 = row * (2 * slots);
     float m = kNegBig, l = 0.0f;
     float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s0 = 0; s0 < records; s0 += kBatch) {
+    for (int s0 = part; s0 < records; s0 += PARTS * kBatch) {
         float mm[kBatch], ll[kBatch];
         float4_t a[kBatch];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const int s = min(s0 + k, records - 1);
-            const long long rec = rec0 + (s < n_prefix ? s : slots + s - n_prefix);
+            const int at = s0 + k * PARTS, s = min(at, records - 1);
+            const int64_t rec = rec0 + (s < n_prefix ? s : slots + s - n_prefix);
             const float2 t = *reinterpret_cast<const float2 *>(part_ml + rec * 2);
             mm[k] = t.x;
-            ll[k] = s0 + k < records ? t.y : 0.0f;
-            a[k] = *reinterpret_cast<const float4_t *>(part_acc + rec * v_dim + e);
+            ll[k] = at < records ? t.y : 0.0f;
+            a[k] = *reinterpret_cast<const float4_t *>(part_acc + rec * DV + 4 * quad);
         }
         float m_new = m;
 #pragma unroll
@@ -1025,9 +1176,28 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(const float *__r
         }
         m = m_new;
     }
+    s_acc[part][quad] = o;
+    if (quad == 0) {
+        s_ml[part][0] = m;
+        s_ml[part][1] = l;
+    }
+    __syncthreads();
+    if (part > 0) return;
+    const int parts = min(PARTS, max(records, 1)); // that have any
+    m = kNegBig;
+    for (int k = 0; k < parts; ++k)
+        if (s_ml[k][1] > 0.0f) m = fmaxf(m, s_ml[k][0]);
+    l = 0.0f;
+    o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < parts; ++k) {
+        if (!(s_ml[k][1] > 0.0f)) continue;
+        const float weight = __builtin_amdgcn_exp2f(s_ml[k][0] - m);
+        l = fmaf(weight, s_ml[k][1], l);
+        o += weight * s_acc[k][quad];
+    }
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     const half2_t lo = half2_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv)}, hi = half2_t{(half_t)(o[2] * inv), (half_t)(o[3] * inv)};
-    *reinterpret_cast<uint2 *>(out + row * v_dim + e) = make_uint2(half2_to_bits(lo), half2_to_bits(hi));
+    *reinterpret_cast<uint2 *>(out + row * DV + 4 * quad) = make_uint2(half2_to_bits(lo), half2_to_bits(hi));
 }
 
 template <int DK, int DV, int CTP>
@@ -1115,9 +1285,9 @@ hipError_t launch_prefix_attention(const PrefixArgs &a, hipStream_t stream)
     else if (s.k_dim == 64) Q4KV_PREFIX(64, 64);
 #undef Q4KV_PREFIX
     if (e != hipSuccess) return e;
-    const int64_t rows = (int64_t)a.layers * a.num_agents * s.num_q_heads, threads = rows * (s.v_dim / 4);
-    hipLaunchKernelGGL(prefix_merge_kernel, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p.part_acc,
-                       p.part_ml, p.plan, p.out, a.num_agents, s.num_q_heads, s.num_kv_heads, s.v_dim, p.slots, p.row_tile, (long long)rows);
+    const auto merge = s.v_dim == 256 ? prefix_merge_kernel<256> : s.v_dim == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>;
+    hipLaunchKernelGGL(merge, dim3((unsigned)((int64_t)a.layers * a.num_agents * s.num_q_heads)), dim3(kThreads), 0, stream, p.part_acc, p.part_ml,
+                       p.plan, p.out, a.num_agents, s.num_q_heads, s.num_kv_heads, p.slots, p.row_tile);
     return hipGetLastError();
 }
 
