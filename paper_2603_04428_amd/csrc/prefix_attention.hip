@@ -62,8 +62,9 @@ struct PrefixParams {
     float *part_acc, *part_ml;
     int num_agents, num_groups, max_blocks, num_blocks, kv_heads, q_heads, n_rep, layer_begin, layers, max_seq_len;
     int slots;    // records reserved per row for the prefix, and as many for the agent's own tokens
-    int row_tile; // rows of a prefix unit: 16 * CT
+    int row_tile, row_tile_log2; // rows of a prefix unit: 16 * CT, a power of two
     float score_scale;
+    float inv_n_rep;
 };
 
 // What the merge needs to know of the plan, written by workgroup 0: header, then per agent what is counted in front of its own
@@ -83,6 +84,7 @@ struct Plan {
     int start[kMaxAgents];     // tile its own part begins with
     int begin[kMaxAgents + 1]; // first agent of a group
     int wave_sum[4][kWaves];
+    int mark[kWaves][kWave]; // of up to 64 agents
     int per, round, solo; // tiles of a worker; a unit's tiles are counted as the next multiple of `round`; 1: waves are the workers
 };
 
@@ -136,7 +138,18 @@ __device__ __forceinline__ int lane_last_at_most(const int *pre, int count, int 
     return lo;
 }
 
-__device__ __forceinline__ int rounded_up(int v, int round) { return (v + round - 1) / round * round; }
+
+// n / d for 0 <= n < 2^31, 0 < d and a quotient below 2^21: the product with the reciprocal errs by less than one
+__device__ __forceinline__ int quotient(int n, int d)
+{
+    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
+    const int r = n - q * d;
+    q += r < 0 ? -1 : (r >= d ? 1 : 0);
+    return q;
+}
+
+// (v below 2^21 * round)
+__device__ __forceinline__ int rounded_up(int v, int round) { return round == 1 ? v : quotient(v + round - 1, round) * round; }
 
 // Tiles of a worker, and what units' tiles are rounded up to.  `total`: all tiles of the call, `padded(r)`: the same with every
 // unit's tiles rounded up to r.
@@ -161,30 +174,41 @@ __device__ __forceinline__ bool spread(long long total, int workgroups, int &per
     return false;
 }
 
-// For up to 64 agents a wave does it in its lanes: lane a holds agent a, lane g group g.
-__device__ __forceinline__ void make_plan_few(const PrefixParams &p, Plan &pl)
+// What a lane reads for the plan of up to 64 agents: lane a of agent a, lane g of group g.
+struct PlanInputs {
+    int len, prefix, bound, last;
+};
+__device__ __forceinline__ PlanInputs plan_inputs(const PrefixParams &p, int lane)
 {
-    if (threadIdx.x < kWave) {
-        const int lane = threadIdx.x, A = p.num_agents, G = p.num_groups;
-        int n = lane < A ? p.seq_len[lane] : 0, prefix = lane < G ? p.prefix_len[lane] : 0;
-        const int bound = lane < G ? p.group_begin[lane] : 0, last = G > 0 ? p.group_begin[G] : 0;
-        n = min(max(n, 0), p.max_seq_len);
+    PlanInputs in;
+    in.len = lane < p.num_agents ? p.seq_len[lane] : 0;
+    in.prefix = lane < p.num_groups ? p.prefix_len[lane] : 0;
+    in.bound = lane < p.num_groups ? p.group_begin[lane] : 0;
+    in.last = p.num_groups > 0 ? p.group_begin[p.num_groups] : 0;
+    return in;
+}
+
+// For up to 64 agents every wave makes the plan for itself, in its lanes (all write the same).
+__device__ __forceinline__ void make_plan_few(const PrefixParams &p, const PlanInputs &in, int lane, int wave, Plan &pl)
+{
+    {
+        const int A = p.num_agents, G = p.num_groups;
+        const int n = min(max(in.len, 0), p.max_seq_len), prefix = in.prefix, bound = in.bound, last = in.last;
         const int begin = wave_scan_max(min(max(bound, 0), A)); // bounds that fall are raised: groups never overlap
         const int end = max(__builtin_amdgcn_readlane(begin, kWave - 1), min(max(last, 0), A));
         int next = __shfl_down(begin, 1, kWave);
         if (lane >= G - 1) next = end;
         const int agents = lane < G ? next - begin : 0;
         const int shared = agents > 1 ? min(max(prefix, 0), p.max_seq_len) / kWave : 0; // a group of one shares nothing
-        const int row_tiles = (agents * p.n_rep + p.row_tile - 1) / p.row_tile;
+        const int row_tiles = (agents * p.n_rep + p.row_tile - 1) >> p.row_tile_log2;
         // lane a: the group its agent is in, from the first agents of the groups that have any
-        pl.start[lane] = 0;
+        pl.mark[wave][lane] = 0;
         wave_lds_sync();
-        if (agents > 0) pl.start[begin] = lane + 1;
+        if (agents > 0) pl.mark[wave][begin] = lane + 1;
         wave_lds_sync();
-        const int mark = pl.start[lane];
+        const int mark = pl.mark[wave][lane];
         const uint64_t upto = __builtin_amdgcn_ballot_w64(mark > 0) & (~0ull >> (63 - lane));
         const int of = __shfl(mark, upto ? 63 - __builtin_clzll(upto) : lane, kWave); // group number + 1
-        wave_lds_sync();
         const int of_end = __shfl(next, of - 1 < 0 ? 0 : of - 1, kWave), of_shared = __shfl(shared, of - 1 < 0 ? 0 : of - 1, kWave);
         const int start = of > 0 && lane < of_end ? of_shared : 0;
         const int own = lane < A ? max(0, tiles_of(n) - start) : 0;
@@ -212,7 +236,7 @@ __device__ __forceinline__ void make_plan_few(const PrefixParams &p, Plan &pl)
             pl.solo = solo ? 1 : 0;
         }
     }
-    __syncthreads();
+    wave_lds_sync();
 }
 
 __device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
@@ -253,7 +277,7 @@ __device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
         if (g < G) {
             const int agents = pl.begin[g + 1] - pl.begin[g];
             if (agents < 2) shared[i] = 0;
-            row_tiles[i] = (agents * p.n_rep + p.row_tile - 1) / p.row_tile;
+            row_tiles[i] = (agents * p.n_rep + p.row_tile - 1) >> p.row_tile_log2;
             pl.group[g] = shared[i]; // for the agents, until the sums are taken
         }
     }
@@ -528,9 +552,9 @@ __device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, in
 {
     Part u;
     const int group_tiles = uniform(pl.group[p.num_groups]), head_tiles = group_tiles + uniform(pl.own[p.num_agents]);
-    const int lk = x / head_tiles;
+    const int lk = quotient(x, head_tiles);
     int r = x - lk * head_tiles, tiles;
-    u.li = lk / p.kv_heads;
+    u.li = quotient(lk, p.kv_heads);
     u.kvh = lk - u.li * p.kv_heads;
     if (r < group_tiles) {
         const int g = last_at_most(pl.group, p.num_groups, r);
@@ -538,7 +562,7 @@ __device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, in
         u.agents = uniform(pl.begin[g + 1]) - u.agent;
         tiles = uniform(pl.start[u.agent]);
         r -= uniform(pl.group[g]);
-        const int counted = rounded_up(tiles, round), rt = r / counted;
+        const int counted = rounded_up(tiles, round), rt = quotient(r, counted);
         r -= rt * counted;
         u.row0 = rt * p.row_tile;
         u.rows = min(p.row_tile, u.agents * p.n_rep - u.row0);
@@ -560,7 +584,7 @@ __device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, in
     u.counted = min(counted - r, x1 - x);
     u.count = min(tiles - r, x1 - x); // at least one: what a unit counts for beyond its tiles is less than a worker's range
     // a unit that begins in front of this worker's range may have begun several ranges before
-    u.slot = r == 0 ? 0 : worker - unit0 / per;
+    u.slot = r == 0 ? 0 : worker - quotient(unit0, per);
     u.whole_row = u.which == 1 && u.tile == r && u.slot == 0 && u.count == tiles;
     u.li = uniform(u.li); u.kvh = uniform(u.kvh); u.agent = uniform(u.agent); u.agents = uniform(u.agents);
     u.row0 = uniform(u.row0); u.rows = uniform(u.rows); u.tile = uniform(u.tile); u.count = uniform(u.count);
@@ -571,7 +595,7 @@ __device__ __forceinline__ Part locate(const PrefixParams &p, const Plan &pl, in
 // the place of row `row` of a part: (layer, agent, query head)
 __device__ __forceinline__ int64_t row_index(const PrefixParams &p, const Part &u, int row, int &agent)
 {
-    const int idx = u.row0 + row, in_group = idx / p.n_rep;
+    const int idx = u.row0 + row, in_group = (int)(((float)idx + 0.5f) * p.inv_n_rep); // idx / n_rep: below 2^21 this is exact
     agent = u.agent + in_group;
     return ((int64_t)u.li * p.num_agents + agent) * p.q_heads + u.kvh * p.n_rep + (idx - in_group * p.n_rep);
 }
@@ -587,16 +611,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
     __shared__ float ml_lds[kWaves][CTP * kCols][2];
 
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
-    if (p.num_agents <= kWave) make_plan_few(p, plan);
-    else make_plan_many(p, plan);
-    const int per = uniform(plan.per), round = uniform(plan.round);
-    const int total = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]) * p.kv_heads * p.layers; // the host keeps it below 2^31
-    const bool solo = uniform(plan.solo) != 0;
-    if (blockIdx.x == 0) write_plan(p, plan);
-    const int worker = solo ? (int)blockIdx.x * kWaves + wave : (int)blockIdx.x;
-    const long long begin = (long long)worker * per;
-    if (begin >= total) return; // a whole workgroup, or a wave on its own
-    const int x1 = (int)min((long long)total, begin + per);
+    PlanInputs plan_in;
+    if (p.num_agents <= kWave) plan_in = plan_inputs(p, lane); // on their way while the lane's places are worked out
 
     unsigned char *const region = tiles_lds + wave * S::WAVE_BYTES;
     const uint32_t region_at = (uint32_t)(uintptr_t)(lds_ptr_t)region;
@@ -624,6 +640,17 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
     const int v_row = 16 * (col / 4) + 4 * qk + col % 4;
     const uint32_t v_at = region_at + S::K_BYTES + v_row * Rows<DV>::BYTES + (Rows<DV>::swizzle(v_row) << 4);
 
+    if (p.num_agents <= kWave) make_plan_few(p, plan_in, lane, wave, plan);
+    else make_plan_many(p, plan);
+    const int per = uniform(plan.per), round = uniform(plan.round);
+    const int total = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]) * p.kv_heads * p.layers; // the host keeps it below 2^31
+    const bool solo = uniform(plan.solo) != 0;
+    if (blockIdx.x == 0) write_plan(p, plan);
+    const int worker = solo ? (int)blockIdx.x * kWaves + wave : (int)blockIdx.x;
+    const long long begin = (long long)worker * per;
+    if (begin >= total) return; // a whole workgroup, or a wave on its own
+    const int x1 = (int)min((long long)total, begin + per);
+
     auto run_part = [&](auto column_tiles, const Part &u) __attribute__((always_inline)) {
         constexpr int CT = decltype(column_tiles)::value;
         constexpr bool kTight = CT * (GK + GV) >= 16; // registers for everything only if loads from LDS do not move far ahead
@@ -635,7 +662,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         // block ids of 64 blocks from table_base on, one per lane
         int table_base = (u.tile + first) / 4;
         auto fetch_table = [&]() { return table_base + lane < p.max_blocks ? table[table_base + lane] : -1; };
-        int table_ids = fetch_table();
+        int table_ids = -1;
         auto block_of = [&](int t) __attribute__((always_inline)) { // wave-uniform
             const int b = t / 4;
             if (__builtin_expect(b >= table_base + kWave, 0)) {
@@ -685,40 +712,55 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             else wait_for_all_but<0>();
         };
 
-        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0): the counts below start from nothing, and all reads of LDS are done
+        // ---- the rows' queries are asked for first, with the block ids: loads complete in order
+        uint4 raw[CT][GK][2];
+        int n_row[CT], n_min = 0x7fffffff, n_max = 0;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            int agent;
+            const int64_t row = row_index(p, u, min(16 * ct + col, u.rows - 1), agent);
+            n_row[ct] = agent;
+            const uint16_t *qrow = p.q + row * DK + 16 * qk;
+#pragma unroll
+            for (int g = 0; g < GK; ++g) {
+                raw[ct][g][0] = *reinterpret_cast<const uint4 *>(qrow + g * kGroup);
+                raw[ct][g][1] = *reinterpret_cast<const uint4 *>(qrow + g * kGroup + 8);
+            }
+        }
+        table_ids = fetch_table();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // all reads of the tile buffers are done
+#pragma unroll 1
         for (int i = 0; i < S::RING; ++i)
             if (i < mine) {
                 issue_k(u.tile + first + i * step, i);
                 issue_rest(u.tile + first + i * step, i);
             }
 
-        // ---- the rows: query operand (element order of code_operand, odd elements / 16 because their codes arrive 16 times
-        // larger), group sums of q, visible tokens
+        // ---- the query operand: the element order of code_operand, odd elements / 16 because their codes arrive 16 times larger;
+        // group sums of q
         half8_t qop[CT][GK][2];
         half4_t qsop[CT];
-        int n_row[CT], n_min = 0x7fffffff, n_max = 0;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            int agent;
-            const int64_t row = row_index(p, u, min(16 * ct + col, u.rows - 1), agent);
-            n_row[ct] = plan.len[agent];
+            n_row[ct] = plan.len[n_row[ct]];
             n_min = min(n_min, n_row[ct]);
             n_max = max(n_max, n_row[ct]);
-            const uint16_t *qrow = p.q + row * DK + 16 * qk;
             float qs[GK];
 #pragma unroll
             for (int g = 0; g < GK; ++g) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const uint4 raw = *reinterpret_cast<const uint4 *>(qrow + g * kGroup + 8 * r);
-                    const half2_t e01 = bits_to_half2(raw.x), e23 = bits_to_half2(raw.y);
-                    const half2_t e45 = bits_to_half2(raw.z), e67 = bits_to_half2(raw.w);
-                    const half_t sixteenth = (half_t)0.0625f;
-                    qop[ct][g][r] = half8_t{e01.x, e45.x, e01.y * sixteenth, e45.y * sixteenth,
-                                            e23.x, e67.x, e23.y * sixteenth, e67.y * sixteenth};
-                    sum += ((float)e01.x + (float)e01.y) + ((float)e23.x + (float)e23.y) +
-                           ((float)e45.x + (float)e45.y) + ((float)e67.x + (float)e67.y);
+                    const uint4 w = raw[ct][g][r];
+                    const half2_t ones = half2_t{(half_t)1.0f, (half_t)1.0f}, sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f};
+                    const half2_t e15 = bits_to_half2(__builtin_amdgcn_perm(w.z, w.x, 0x07060302u)) * sixteenth;
+                    const half2_t e37 = bits_to_half2(__builtin_amdgcn_perm(w.w, w.y, 0x07060302u)) * sixteenth;
+                    qop[ct][g][r] = words_to_half8(__builtin_amdgcn_perm(w.z, w.x, 0x05040100u), half2_to_bits(e15),
+                                                   __builtin_amdgcn_perm(w.w, w.y, 0x05040100u), half2_to_bits(e37));
+                    sum = __builtin_amdgcn_fdot2(bits_to_half2(w.x), ones, sum, false);
+                    sum = __builtin_amdgcn_fdot2(bits_to_half2(w.y), ones, sum, false);
+                    sum = __builtin_amdgcn_fdot2(bits_to_half2(w.z), ones, sum, false);
+                    sum = __builtin_amdgcn_fdot2(bits_to_half2(w.w), ones, sum, false);
                 }
                 qs[g] = xor32_sum(xor16_sum(sum));
             }
@@ -1089,24 +1131,42 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             }
         }
         __syncthreads();
-        for (int i = tid; i < u.rows * (DV / 4); i += kThreads) {
-            const int r = i / (DV / 4), e = 4 * (i % (DV / 4));
-            float m = kNegBig, l = 0.0f;
+        // a thread takes the same four elements of every STRIDE-th row, two rows at a time
+        constexpr int QUADS = DV / 4, STRIDE = kThreads / QUADS;
+        const int e = 4 * (tid % QUADS);
+        for (int r0 = tid / QUADS; r0 < u.rows; r0 += 2 * STRIDE) {
+            float4_t part[2][kWaves];
+            float ml[2][kWaves][2];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                if (ml_lds[w][r][1] > 0.0f) m = fmaxf(m, ml_lds[w][r][0]);
-            float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < 2; ++k) {
+                const int r = min(r0 + k * STRIDE, u.rows - 1);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float lw = ml_lds[w][r][1];
-                if (lw > 0.0f) {
-                    const float weight = __builtin_amdgcn_exp2f(ml_lds[w][r][0] - m);
-                    o += weight * *reinterpret_cast<const float4_t *>(tiles_lds + w * S::WAVE_BYTES + 4 * (r * S::ROW_PITCH + e));
-                    l = fmaf(weight, lw, l);
+                for (int w = 0; w < kWaves; ++w) {
+                    part[k][w] = *reinterpret_cast<const float4_t *>(tiles_lds + w * S::WAVE_BYTES + 4 * (r * S::ROW_PITCH + e));
+                    ml[k][w][0] = ml_lds[w][r][0];
+                    ml[k][w][1] = ml_lds[w][r][1];
                 }
             }
-            int agent;
-            finish_quad(row_index(p, u, r, agent), e, m, l, o);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int r = r0 + k * STRIDE;
+                if (r >= u.rows) break;
+                float m = kNegBig, l = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    if (ml[k][w][1] > 0.0f) m = fmaxf(m, ml[k][w][0]);
+                float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    // what a wave without tiles left in its buffer is no number to multiply
+                    const float weight = ml[k][w][1] > 0.0f ? __builtin_amdgcn_exp2f(ml[k][w][0] - m) : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] += weight > 0.0f ? weight * part[k][w][i] : 0.0f;
+                    l = fmaf(weight, ml[k][w][1], l);
+                }
+                int agent;
+                finish_quad(row_index(p, u, r, agent), e, m, l, o);
+            }
         }
         __syncthreads(); // the tile buffers are free again
     };
@@ -1275,7 +1335,9 @@ hipError_t launch_prefix_attention(const PrefixArgs &a, hipStream_t stream)
     p.slots = record_slots(s, a.max_seq_len, a.layers, prefix_workgroups(a.compute_units));
     const int ct = column_tiles(s, a.num_agents, a.num_groups);
     p.row_tile = kCols * ct;
+    p.row_tile_log2 = ct == 2 ? 5 : 4;
     p.score_scale = a.sm_scale * kLog2e;
+    p.inv_n_rep = 1.0f / (float)p.n_rep;
     const bool bf = s.param_format == Q4KV_PARAMS_BF16;
     hipError_t e = hipErrorInvalidValue;
 #define Q4KV_PREFIX(DK, DV) e = ct == 2 ? launch_t<DK, DV, 2>(p, bf, a.compute_units, stream) : launch_t<DK, DV, 1>(p, bf, a.compute_units, stream)
