@@ -135,7 +135,7 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
  *             2n and 2n + 1.  rot_dim == 0: none, the tables are not read.
  * norm_dim and rot_begin are multiples of 8, rot_dim of 16, both spans lie inside k_dim and may overlap; weights and tables
  * are 16-byte aligned.  Results are those of binary64 arithmetic rounded once to binary16 (but for a result within about
- * 2^-50 of itself of a rounding border). */
+ * 2^-48 of itself of a rounding border); a row of zeros stays zeros whatever eps is. */
 typedef struct {
     const float *q_weight, *k_weight;
     const float *cos_table, *sin_table;

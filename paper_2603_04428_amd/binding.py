@@ -143,7 +143,7 @@ def _stream():
 def _dev(t, dtype, name):
     if t is None:
         return None
-    if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{name}: need a contiguous {dtype} tensor on the GPU, got {t.dtype} on {t.device}")
     return t.data_ptr()
 
@@ -196,19 +196,32 @@ class HeadForm:
         self.norm_dim, self.q_weight, self.k_weight, self.eps = norm_dim, q_weight, k_weight, eps
         self.rot_begin, self.rot_dim, self.neighbours, self.cos, self.sin = rot_begin, rot_dim, neighbours, cos, sin
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_checked", None)          # (layers, struct) of the last call with these attributes
+
     def c(self, layers):
-        for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
-            if t is not None and tuple(t.shape) != (layers, self.norm_dim):
-                raise ValueError(f"{name}: {tuple(t.shape)} instead of {(layers, self.norm_dim)}")
-        table_len = 0
-        if self.rot_dim:
-            if self.cos is None or self.sin is None or self.cos.shape != self.sin.shape or self.cos.dim() != 2 or \
-                    self.cos.shape[1] * 2 != self.rot_dim:
-                raise ValueError(f"cos and sin: one shape, [positions][{self.rot_dim // 2}]")
-            table_len = self.cos.shape[0]
-        return _CHeadForm(_dev(self.q_weight, torch.float32, "q_weight"), _dev(self.k_weight, torch.float32, "k_weight"),
-                          _dev(self.cos, torch.float32, "cos"), _dev(self.sin, torch.float32, "sin"), self.norm_dim, self.eps,
-                          self.rot_begin, self.rot_dim, 1 if self.neighbours else 0, table_len)
+        if self._checked is None or self._checked[0] != layers:
+            for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+                if t is not None and tuple(t.shape) != (layers, self.norm_dim):
+                    raise ValueError(f"{name}: {tuple(t.shape)} instead of {(layers, self.norm_dim)}")
+            table_len = 0
+            if self.rot_dim:
+                if self.cos is None or self.sin is None or self.cos.shape != self.sin.shape or self.cos.dim() != 2 or \
+                        self.cos.shape[1] * 2 != self.rot_dim:
+                    raise ValueError(f"cos and sin: one shape, [positions][{self.rot_dim // 2}]")
+                table_len = self.cos.shape[0]
+            for name in ("q_weight", "k_weight", "cos", "sin"):
+                _dev(getattr(self, name), torch.float32, name)
+            object.__setattr__(self, "_checked", (layers, _CHeadForm(
+                norm_dim=self.norm_dim, eps=self.eps, rot_begin=self.rot_begin, rot_dim=self.rot_dim,
+                neighbours=1 if self.neighbours else 0, table_len=table_len)))
+        f = self._checked[1]                                # shapes are checked once; where the tensors lie is asked every time
+        f.q_weight = None if self.q_weight is None else self.q_weight.data_ptr()
+        f.k_weight = None if self.k_weight is None else self.k_weight.data_ptr()
+        f.cos_table = None if self.cos is None else self.cos.data_ptr()
+        f.sin_table = None if self.sin is None else self.sin.data_ptr()
+        return f
 
 
 class BlockPool:
@@ -387,19 +400,20 @@ def q4kv_append(spec, kpool, vpool, k_new, v_new, block_table, seq_len_before, l
 
 def _token_rows(t, heads, dim, name):
     """[layers][agents][chunk][heads][dim] with contiguous tokens a fixed stride apart -> that stride in elements."""
-    if t.dim() != 5 or t.shape[3] != heads or t.shape[4] != dim or not t.is_cuda:
-        raise TypeError(f"{name}: need [layers][agents][chunk][{heads}][{dim}] on the GPU, got {tuple(t.shape)} on {t.device}")
-    Lr, A, Cn = t.shape[:3]
-    # the stride of an axis of one element means nothing: the first axis that has more gives the distance of two tokens
+    shape = t.shape
+    if len(shape) != 5 or shape[3] != heads or shape[4] != dim or not t.is_cuda:
+        raise TypeError(f"{name}: need [layers][agents][chunk][{heads}][{dim}] on the GPU, got {tuple(shape)} on {t.device}")
+    s0, s1, s2, s3, s4 = t.stride()
+    # the stride of an axis of one element means nothing: the last axis that has more gives the distance of two tokens
     stride, rows = None, 1
-    for size, step in ((Cn, t.stride(2)), (A, t.stride(1)), (Lr, t.stride(0))):
+    for size, step in ((shape[2], s2), (shape[1], s1), (shape[0], s0)):
         if size > 1:
             if stride is None and step % rows == 0:
                 stride = step // rows
             if stride is None or step != stride * rows:
                 raise TypeError(f"{name}: tokens are not a fixed stride apart (strides {t.stride()})")
         rows *= size
-    if (dim > 1 and t.stride(4) != 1) or (heads > 1 and t.stride(3) != dim):
+    if (dim > 1 and s4 != 1) or (heads > 1 and s3 != dim):
         raise TypeError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
     return heads * dim if stride is None else stride
 
@@ -409,24 +423,30 @@ def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table
     """q / k_new / v_new: fp16 or bf16 [layers_in_call][A][C][heads][dim], possibly parts of one fused projection (tokens a fixed
     stride apart); form: HeadForm.  Returns the prepared queries, fp16 [layers_in_call][A][C][q_heads][k_dim]."""
     layer_end = spec.num_layers if layer_end is None else layer_end
-    Lr, A, Cn = q.shape[:3]
-    strides = [_token_rows(q, spec.num_q_heads, spec.k_dim, "q"), _token_rows(k_new, spec.num_kv_heads, spec.k_dim, "k_new"),
-               0 if v_new is None else _token_rows(v_new, spec.num_kv_heads, spec.v_dim, "v_new")]
-    for t, name in ((q, "q"), (k_new, "k_new"), (v_new, "v_new")):
-        if t is not None and (t.dtype != q.dtype or t.shape[:3] != q.shape[:3] or t.dtype not in (torch.float16, torch.bfloat16)):
-            raise TypeError(f"{name}: fp16 or bf16, of one type and leading shape with q, got {t.dtype} {tuple(t.shape)}")
+    alias, hq, hkv, dk = spec.v_aliases_k, spec.num_q_heads, spec.num_kv_heads, spec.k_dim
+    q_stride, k_stride, v_stride = _token_rows(q, hq, dk, "q"), _token_rows(k_new, hkv, dk, "k_new"), 0
+    if v_new is not None:
+        v_stride = _token_rows(v_new, hkv, spec.v_dim, "v_new")
+    kind, lead = q.dtype, q.shape[:3]
+    if kind not in (torch.float16, torch.bfloat16) or k_new.dtype != kind or (v_new is not None and v_new.dtype != kind):
+        raise TypeError(f"q, k_new and v_new: fp16 or bf16, all of one type, got {kind}, {k_new.dtype}")
+    if k_new.shape[:3] != lead or (v_new is not None and v_new.shape[:3] != lead):
+        raise TypeError(f"q, k_new and v_new differ in layers, agents or tokens: {tuple(lead)}, {tuple(k_new.shape[:3])}")
+    Lr, A, Cn = lead
     if Lr != layer_end - layer_begin:
         raise ValueError(f"{Lr} layers of projections for {layer_end - layer_begin} layers")
     if q_out is None:
-        q_out = torch.empty((Lr, A, Cn, spec.num_q_heads, spec.k_dim), dtype=torch.float16, device=q.device)
+        q_out = torch.empty((Lr, A, Cn, hq, dk), dtype=torch.float16, device=q.device)
+    elif q_out.shape != (Lr, A, Cn, hq, dk):
+        raise ValueError(f"q_out: {tuple(q_out.shape)} instead of {(Lr, A, Cn, hq, dk)}")
+    if block_table.shape[0] != A or seq_len_before.numel() != A:
+        raise ValueError(f"{A} agents, {block_table.shape[0]} rows of blocks, {seq_len_before.numel()} lengths")
     if positions is not None and tuple(positions.shape) != (A, Cn):
         raise ValueError(f"positions: {tuple(positions.shape)} instead of {(A, Cn)}")
-    kp, cform = kpool.c(), form.c(Lr)
-    vp = None if spec.v_aliases_k else vpool.c()
     _check(lib().q4kv_norm_rope_append(
-        C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), C.byref(cform), q.data_ptr(), k_new.data_ptr(),
-        None if v_new is None else v_new.data_ptr(), 1 if q.dtype == torch.bfloat16 else 0, *strides,
-        _dev(q_out, torch.float16, "q_out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
+        C.byref(spec), C.byref(kpool.c()), None if alias else C.byref(vpool.c()), C.byref(form.c(Lr)), q.data_ptr(),
+        k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), 1 if kind == torch.bfloat16 else 0, q_stride, k_stride,
+        v_stride, _dev(q_out, torch.float16, "q_out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
         _dev(seq_len_before, torch.int32, "seq_len_before"), _dev(positions, torch.int32, "positions"), A, Cn, layer_begin,
         layer_end, _stream()))
     return q_out
@@ -499,8 +519,14 @@ def q4kv_shared_prefix_attention(spec, kpool, vpool, q, block_table, seq_len, gr
     groups = 0 if prefix_len is None else prefix_len.numel()
     if groups and (group_begin is None or group_begin.numel() != groups + 1):
         raise ValueError(f"{groups} groups need {groups + 1} bounds")
+    if q.shape[3] != spec.num_q_heads or q.shape[4] != spec.k_dim or Lr != layer_end - layer_begin:
+        raise ValueError(f"q: {tuple(q.shape)} for {layer_end - layer_begin} layers of {spec.num_q_heads} heads, {spec.k_dim} wide")
+    if block_table.shape[0] != A or seq_len.numel() != A:
+        raise ValueError(f"{A} agents, {block_table.shape[0]} rows of blocks, {seq_len.numel()} lengths")
     if out is None:
         out = torch.empty((Lr, A, 1, spec.num_q_heads, spec.v_dim), dtype=torch.float16, device=q.device)
+    elif out.shape != (Lr, A, 1, spec.num_q_heads, spec.v_dim):
+        raise ValueError(f"out: {tuple(out.shape)} instead of {(Lr, A, 1, spec.num_q_heads, spec.v_dim)}")
     if workspace is None:
         need = q4kv_shared_prefix_workspace_bytes(spec, max(A, 1), max_seq_len, max(Lr, 1))
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)

@@ -37,7 +37,7 @@ struct HeadAppendParams {
     uint16_t *scale[2], *bias[2];
     const float *cos, *sin;
     const int32_t *block_table, *seq_len_before, *positions;
-    double eps;
+    double eps, inv_norm_dim;
     int norm_dim, rot_begin, rot_dim, neighbours, table_len;
     int agents, chunk, max_blocks, num_blocks, layer_begin;
     int tokens_log2; // tokens of a workgroup's rows
@@ -49,7 +49,7 @@ struct HeadAppendParams {
 __device__ __forceinline__ half_t half_once(double d)
 {
     const uint64_t u = __builtin_bit_cast(uint64_t, d);
-    const uint32_t hi = (uint32_t)(u >> 32) | ((uint32_t)u != 0u ? 1u : 0u);
+    const uint32_t hi = (uint32_t)(u >> 32) | min((uint32_t)u, 1u);
     return (half_t)(float)__builtin_bit_cast(double, (uint64_t)hi << 32);
 }
 
@@ -64,8 +64,50 @@ __device__ __forceinline__ void widen(const uint4 &raw, float (&x)[8])
     }
 }
 
+// Sum over the LPR lanes of a row, in all of them: exchanges inside 16 lanes as data-parallel-primitive moves, the rest as swaps
+// of half rows.
+template <int CTRL>
+__device__ __forceinline__ double dpp_add(double v)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
+    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int LPR>
+__device__ __forceinline__ double row_sum(double v)
+{
+    v = dpp_add<0xB1>(v);  // quad_perm [1,0,3,2]
+    v = dpp_add<0x4E>(v);  // quad_perm [2,3,0,1]
+    v = dpp_add<0x141>(v); // row_half_mirror
+    if constexpr (LPR >= 16) v = dpp_add<0x140>(v); // row_mirror
+    if constexpr (LPR >= 32) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+        v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+    }
+    if constexpr (LPR >= 64) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+        v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+    }
+    return v;
+}
+
+// 1 / sqrt(v): the instruction is good to 2^-23 or better, two Newton steps to a few 2^-53.  A row of zeros without an eps stays zeros.
+__device__ __forceinline__ double inverse_root(double v)
+{
+    if (!(v > 0.0)) return 0.0;
+    double r = __builtin_amdgcn_rsq(v);
+    r = __builtin_fma(r * 0.5, __builtin_fma(-v * r, r, 1.0), r);
+    return __builtin_fma(r * 0.5, __builtin_fma(-v * r, r, 1.0), r);
+}
+
 // LPR: lanes of a row (a power of two); CPL: passes over a row.  BF: type of the stored parameters, IN_BF: of the projections.
-template <int LPR, int CPL, bool BF, bool IN_BF>
+// SPLIT: the norm ends inside the rotated span, so that of some pairs only one half is normed.
+template <int LPR, int CPL, bool BF, bool IN_BF, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void head_append_kernel(HeadAppendParams p)
 {
     constexpr int ROWS = kThreads / LPR; // rows of a workgroup: 2^tokens_log2 tokens of as many heads as that leaves
@@ -92,141 +134,171 @@ __global__ __launch_bounds__(kThreads) void head_append_kernel(HeadAppendParams 
     }
     const int64_t token = ((int64_t)li * p.agents + a) * p.chunk + c;
     const uint16_t *src = s.x + token * s.token_stride;
-    const bool prepared = which < 2;
-    const bool normed = prepared && s.weight != nullptr;
+    const bool normed = which < 2 && s.weight != nullptr;
+    const bool prepared = which < 2 && (normed || p.rot_dim > 0); // else rows go as they are
 
-    // what a chunk of eight elements is multiplied with: y = (x ca + x' cb) / rms, x' its partners in the rotation
+    // what a chunk of eight elements is multiplied with: y = (x ca + x' cb) f, x' its partners in the rotation (itself and zero
+    // where it is not rotated), f = 1 / rms under the norm
     double ca[CPL][8], cb[CPL][8];
-    int partner[CPL]; // element the partners begin at; < 0: the chunk is not rotated
-    bool front[CPL];  // under the norm
+    int partner[CPL];       // element the partners begin at
+    bool front[CPL], partner_front[CPL]; // under the norm
+    const bool pairs_inside = p.neighbours != 0;
+    if (prepared) {
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-        const int d = 8 * (in_row + LPR * i), r = d - p.rot_begin;
-        front[i] = normed && d < p.norm_dim;
-        partner[i] = -1;
+        for (int i = 0; i < CPL; ++i) {
+            const int d = 8 * (in_row + LPR * i), r = d - p.rot_begin;
+            front[i] = partner_front[i] = normed && d < p.norm_dim;
+            partner[i] = d < s.dim ? d : 0;
+            float w[8], wp[8], cs[8], sn[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ca[i][e] = 1.0;
-            cb[i][e] = 0.0;
-        }
-        if (!prepared || d >= s.dim) continue;
-        float w[8], wp[8];
+            for (int e = 0; e < 8; ++e) {
+                w[e] = wp[e] = cs[e] = 1.0f;
+                sn[e] = 0.0f;
+            }
+            const float *weight = s.weight + (int64_t)li * p.norm_dim;
+            if (front[i]) __builtin_memcpy(w, __builtin_assume_aligned(weight + d, 16), 32);
+            if (d < s.dim && r >= 0 && r < p.rot_dim) {
+                const int half_span = p.rot_dim / 2;
+                const float *cos = p.cos + (int64_t)pos * half_span, *sin = p.sin + (int64_t)pos * half_span;
+                if (pairs_inside) {
+                    float c4[4], s4[4];
+                    __builtin_memcpy(c4, __builtin_assume_aligned(cos + r / 2, 16), 16);
+                    __builtin_memcpy(s4, __builtin_assume_aligned(sin + r / 2, 16), 16);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = wp[e] = 1.0f;
-        const float *weight = s.weight + (int64_t)li * p.norm_dim;
-        if (front[i]) __builtin_memcpy(w, __builtin_assume_aligned(weight + d, 16), 32);
-        const bool rotated = r >= 0 && r < p.rot_dim;
-        if (rotated) {
-            const int half_span = p.rot_dim / 2;
-            float cs[8], sn[8];
-            const float *cos = p.cos + (int64_t)pos * half_span, *sin = p.sin + (int64_t)pos * half_span;
-            if (p.neighbours) {
-                partner[i] = d;
-                float c4[4], s4[4];
-                __builtin_memcpy(c4, __builtin_assume_aligned(cos + r / 2, 16), 16);
-                __builtin_memcpy(s4, __builtin_assume_aligned(sin + r / 2, 16), 16);
+                    for (int e = 0; e < 8; ++e) {
+                        cs[e] = c4[e / 2];
+                        sn[e] = (e & 1) ? s4[e / 2] : -s4[e / 2];
+                        wp[e] = w[e ^ 1];
+                    }
+                } else {
+                    const bool upper = r >= half_span;
+                    const int at = upper ? r - half_span : r;
+                    partner[i] = upper ? d - half_span : d + half_span;
+                    partner_front[i] = normed && partner[i] < p.norm_dim;
+                    __builtin_memcpy(cs, __builtin_assume_aligned(cos + at, 16), 32);
+                    __builtin_memcpy(sn, __builtin_assume_aligned(sin + at, 16), 32);
+                    if (partner_front[i]) __builtin_memcpy(wp, __builtin_assume_aligned(weight + partner[i], 16), 32);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    cs[e] = c4[e / 2];
-                    sn[e] = (e & 1) ? s4[e / 2] : -s4[e / 2];
-                    wp[e] = w[e ^ 1];
+                    for (int e = 0; e < 8; ++e) sn[e] = upper ? sn[e] : -sn[e];
                 }
-            } else {
-                const bool upper = r >= half_span;
-                const int at = upper ? r - half_span : r;
-                partner[i] = upper ? d - half_span : d + half_span;
-                __builtin_memcpy(cs, __builtin_assume_aligned(cos + at, 16), 32);
-                __builtin_memcpy(sn, __builtin_assume_aligned(sin + at, 16), 32);
-                if (normed && partner[i] < p.norm_dim) __builtin_memcpy(wp, __builtin_assume_aligned(weight + partner[i], 16), 32);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sn[e] = upper ? sn[e] : -sn[e];
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 ca[i][e] = (double)w[e] * (double)cs[e];
                 cb[i][e] = (double)wp[e] * (double)sn[e];
             }
-        } else if (front[i]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ca[i][e] = (double)w[e];
         }
     }
 
     const int G = s.dim / kGroup;
-    for (int h = split * heads_step + (row >> p.tokens_log2); h < s.heads; h += s.splits * heads_step) {
+    const int h0 = split * heads_step + (row >> p.tokens_log2), step = s.splits * heads_step;
+    uint4 raw[CPL], other[CPL]; // of the head in hand; the next one's are asked for as soon as these have been taken apart
+    auto load = [&](int h) {
         const uint16_t *x_row = src + (int64_t)h * s.dim;
-        uint4 raw[CPL], other[CPL];
 #pragma unroll
         for (int i = 0; i < CPL; ++i) {
             const int d = 8 * (in_row + LPR * i);
-            raw[i] = other[i] = make_uint4(0, 0, 0, 0);
+            raw[i] = make_uint4(0, 0, 0, 0);
             if (d < s.dim) raw[i] = *reinterpret_cast<const uint4 *>(x_row + d);
-            if (partner[i] >= 0) other[i] = *reinterpret_cast<const uint4 *>(x_row + partner[i]);
+            if (prepared && !pairs_inside) other[i] = *reinterpret_cast<const uint4 *>(x_row + partner[i]);
         }
+    };
+    auto finish = [&](int h, int i, const uint4 &y8) { // eight prepared elements: out, or into the cache
+        const int chunk = in_row + LPR * i;
+        if (8 * chunk >= s.dim) return; // whole octets: dim is a multiple of 64
+        if (which == 0) {
+            *reinterpret_cast<uint4 *>(p.q_out + (token * s.heads + h) * s.dim + 8 * chunk) = y8;
+        } else {
+            const int sub = threadIdx.x & 7, pool = which - 1;
+            uint16_t sb, bb;
+            const uint32_t word = quantize_octet<BF>(y8, sub, &sb, &bb);
+            const int64_t dst = dst0 + (int64_t)h * kBlockTokens;
+            p.codes[pool][dst * (s.dim / 8) + chunk] = word;
+            if (sub < 2) (sub == 0 ? p.scale[pool] : p.bias[pool])[dst * G + chunk / 8] = sub == 0 ? sb : bb;
+        }
+    };
+    if (h0 < s.heads) load(h0);
+    if (!prepared) {
+        for (int h = h0; h < s.heads; h += step) {
+            uint4 now[CPL];
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) now[i] = raw[i];
+            if (h + step < s.heads) load(h + step);
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                if constexpr (IN_BF) {
+                    float x[8];
+                    widen<true>(now[i], x);
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = half2_to_bits(half2_t{(half_t)x[2 * e], (half_t)x[2 * e + 1]});
+                    now[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+                finish(h, i, now[i]);
+            }
+        }
+        return;
+    }
+    for (int h = h0; h < s.heads; h += step) {
+        float x[CPL][8], xp[CPL][8];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            widen<IN_BF>(raw[i], x[i]);
+            if (pairs_inside) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xp[i][e] = x[i][e ^ 1];
+            } else {
+                widen<IN_BF>(other[i], xp[i]);
+            }
+        }
+        if (h + step < s.heads) load(h + step);
+        double x64[CPL][8];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x64[i][e] = (double)x[i][e];
         double inv = 1.0;
         if (normed) {
             double sum = 0.0;
 #pragma unroll
             for (int i = 0; i < CPL; ++i) {
-                if (!front[i]) continue;
-                float x[8];
-                widen<IN_BF>(raw[i], x);
+                double part = 0.0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)x[e], (double)x[e], sum);
+                for (int e = 0; e < 8; ++e) part = __builtin_fma(x64[i][e], x64[i][e], part);
+                sum += front[i] ? part : 0.0;
             }
-#pragma unroll
-            for (int off = LPR / 2; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, LPR);
-            inv = 1.0 / sqrt(sum / (double)p.norm_dim + p.eps);
+            inv = inverse_root(__builtin_fma(row_sum<LPR>(sum), p.inv_norm_dim, p.eps));
         }
 #pragma unroll
         for (int i = 0; i < CPL; ++i) {
-            const int chunk = in_row + LPR * i;
-            if (8 * chunk >= s.dim) continue; // whole octets: dim is a multiple of 64
+            const double f = front[i] ? inv : 1.0;
+            double g = 1.0; // a partner's factor over this one's
+            if constexpr (SPLIT) g = (partner_front[i] ? inv : 1.0) / f;
+            half_t o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                double v = (double)xp[i][e];
+                if constexpr (SPLIT) v *= g;
+                o[e] = half_once(__builtin_fma(v, cb[i][e], x64[i][e] * ca[i][e]) * f);
+            }
             uint32_t out[4];
-            if (front[i] || partner[i] >= 0) {
-                float x[8], y[8];
-                widen<IN_BF>(raw[i], x);
-                widen<IN_BF>(other[i], y);
-                // of a pair under the norm one half may lie behind it (norm_dim inside the rotated span)
-                const double own = front[i] ? inv : 1.0;
-                const double theirs = partner[i] >= 0 && normed && (p.neighbours ? 8 * chunk : partner[i]) < p.norm_dim ? inv : 1.0;
-                half_t o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const double mine = (double)x[e] * ca[i][e] * own;
-                    const float xp = p.neighbours ? y[e ^ 1] : y[e];
-                    o[e] = half_once(partner[i] >= 0 ? __builtin_fma((double)xp * theirs, cb[i][e], mine) : mine);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = half2_to_bits(half2_t{o[2 * e], o[2 * e + 1]});
-            } else if (IN_BF) {
-                float x[8];
-                widen<IN_BF>(raw[i], x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = half2_to_bits(half2_t{(half_t)x[2 * e], (half_t)x[2 * e + 1]});
-            } else {
-                out[0] = raw[i].x; out[1] = raw[i].y; out[2] = raw[i].z; out[3] = raw[i].w;
-            }
-            const uint4 y8 = make_uint4(out[0], out[1], out[2], out[3]);
-            if (which == 0) {
-                *reinterpret_cast<uint4 *>(p.q_out + (token * s.heads + h) * s.dim + 8 * chunk) = y8;
-            } else {
-                const int sub = threadIdx.x & 7, pool = which - 1;
-                uint16_t sb, bb;
-                const uint32_t word = quantize_octet<BF>(y8, sub, &sb, &bb);
-                const int64_t dst = dst0 + (int64_t)h * kBlockTokens;
-                p.codes[pool][dst * (s.dim / 8) + chunk] = word;
-                if (sub < 2) (sub == 0 ? p.scale[pool] : p.bias[pool])[dst * G + chunk / 8] = sub == 0 ? sb : bb;
-            }
+            for (int e = 0; e < 4; ++e) out[e] = half2_to_bits(half2_t{o[2 * e], o[2 * e + 1]});
+            finish(h, i, make_uint4(out[0], out[1], out[2], out[3]));
         }
     }
 }
 
-template <int LPR, int CPL>
-hipError_t launch_rows(const HeadAppendParams &p, bool bf, bool in_bf, dim3 grid, hipStream_t stream)
+template <int LPR, int CPL, bool BF, bool IN_BF>
+auto kernel_of(bool split)
 {
-    const auto kernel = bf ? (in_bf ? head_append_kernel<LPR, CPL, true, true> : head_append_kernel<LPR, CPL, true, false>)
-                           : (in_bf ? head_append_kernel<LPR, CPL, false, true> : head_append_kernel<LPR, CPL, false, false>);
+    return split ? head_append_kernel<LPR, CPL, BF, IN_BF, true> : head_append_kernel<LPR, CPL, BF, IN_BF, false>;
+}
+template <int LPR, int CPL>
+hipError_t launch_rows(const HeadAppendParams &p, bool bf, bool in_bf, bool split, dim3 grid, hipStream_t stream)
+{
+    const auto kernel = bf ? (in_bf ? kernel_of<LPR, CPL, true, true>(split) : kernel_of<LPR, CPL, true, false>(split))
+                           : (in_bf ? kernel_of<LPR, CPL, false, true>(split) : kernel_of<LPR, CPL, false, false>(split));
     hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
@@ -255,6 +327,7 @@ hipError_t launch_head_append(const HeadAppendArgs &a, hipStream_t stream)
     p.seq_len_before = a.seq_len_before;
     p.positions = a.positions;
     p.eps = a.form->eps;
+    p.inv_norm_dim = a.form->norm_dim > 0 ? 1.0 / a.form->norm_dim : 0.0;
     p.norm_dim = a.form->norm_dim;
     p.rot_begin = a.form->rot_begin;
     p.rot_dim = a.form->rot_dim;
@@ -273,25 +346,30 @@ hipError_t launch_head_append(const HeadAppendArgs &a, hipStream_t stream)
     while ((1 << p.tokens_log2) < rows && (1 << p.tokens_log2) < a.chunk_len) ++p.tokens_log2;
     const int tokens = 1 << p.tokens_log2, heads_step = rows / tokens;
     p.token_chunks = (uint32_t)((a.chunk_len + tokens - 1) / tokens);
-    // A lane visits several heads of its token, with the same weights and table entries in its registers, as soon as the launch
-    // keeps eight workgroups per compute unit without it.
+    // A lane visits up to eight heads of its token, with the same weights and table entries in its registers (a wave spends about 500
+    // instructions on them, and 120 to 280 on a head), as long as Q, K and V each keep three workgroups per compute unit.  Measured
+    // (us a call, 16 / 8 / 4 / 3 / 2 workgroups): 512 tokens of ten agents, 256-wide 56.3 / 42.3 / 38.3 / 38.2 / 39.1; 301 of five, latent rows
+    // 33.6 / 24.9 / 21.2 / 21.3 / 23.5; 700 of eight, 64-wide, three layers 20.2 / 15.9 / 15.5 / 15.5 / 18.3; 300 of three, 192 + 128 17.3 / 16.8 /
+    // 16.8 / 13.8 / 13.8; 2,000 of one, 128-wide, two layers 35.5 / 28.5 / 25.6 / 22.5 / 22.6.
     const int64_t columns = (int64_t)p.token_chunks * a.num_agents * layers;
     int total = 0;
     for (HeadSection &sec : p.sec) {
         if (sec.heads == 0) continue;
         const int steps = (sec.heads + heads_step - 1) / heads_step;
         int per = 1;
-        while (per < 8 && per * 2 <= steps && columns * (steps / (per * 2)) >= 8 * (int64_t)a.compute_units) per *= 2;
+        while (per < 8 && per * 2 <= steps && columns * (steps / (per * 2)) >= 3 * (int64_t)a.compute_units) per *= 2;
         sec.splits = (steps + per - 1) / per;
         total += sec.splits;
     }
     const dim3 grid(p.token_chunks * (unsigned)total, (unsigned)a.num_agents, (unsigned)layers);
     const bool bf = s.param_format == Q4KV_PARAMS_BF16, in_bf = a.in_format == Q4KV_PARAMS_BF16;
-    if (dim <= 64) return launch_rows<8, 1>(p, bf, in_bf, grid, stream);
-    if (dim <= 128) return launch_rows<16, 1>(p, bf, in_bf, grid, stream);
-    if (dim <= 256) return launch_rows<32, 1>(p, bf, in_bf, grid, stream);
-    if (dim <= 512) return launch_rows<64, 1>(p, bf, in_bf, grid, stream);
-    return launch_rows<64, 2>(p, bf, in_bf, grid, stream);
+    const q4kv_head_form &f = *a.form;
+    const bool split = (f.q_weight || f.k_weight) && !f.neighbours && f.norm_dim > f.rot_begin && f.norm_dim < f.rot_begin + f.rot_dim;
+    if (dim <= 64) return launch_rows<8, 1>(p, bf, in_bf, split, grid, stream);
+    if (dim <= 128) return launch_rows<16, 1>(p, bf, in_bf, split, grid, stream);
+    if (dim <= 256) return launch_rows<32, 1>(p, bf, in_bf, split, grid, stream);
+    if (dim <= 512) return launch_rows<64, 1>(p, bf, in_bf, split, grid, stream);
+    return launch_rows<64, 2>(p, bf, in_bf, split, grid, stream);
 }
 
 } // namespace q4kv

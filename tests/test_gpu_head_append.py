@@ -159,6 +159,25 @@ def test_rows_of_zeros_and_equal_values():
     p.check()
 
 
+def test_a_row_of_zeros_without_eps_stays_zeros():
+    p = Problem(1, 2, 1, 64, 64, False, (0,), 3, norm=64, rot=(0, 64), seed=8)
+    p.form.eps = p.f["eps"] = 0.0
+    for g, h in zip(p.g, p.h):
+        g[:, :, 1], h[:, :, 1] = 0, 0
+    q_out = p.call()
+    h = [x.copy() for x in p.h]
+    for x in p.h:
+        x[:, :, 1] = 1                               # any row: its place is filled with zeros below
+    q, k, v = p.want_rows()
+    q[:, :, 1], k[:, :, 1], v[:, :, 1] = 0, 0, 0
+    assert not h[0][:, :, 1].any()
+    oracle.append(p.ospec, p.okp, p.ovp, k, v, p.table, p.before)
+    torch.cuda.synchronize()
+    assert torch.equal(q_out, torch.from_numpy(q).to(DEV))
+    zero = (bits(p.kp.codes) == p.okp.codes).all() and np.array_equal(bits(p.kp.scale), p.okp.scale)
+    assert zero and np.array_equal(bits(p.kp.bias) & 0x7FFF, p.okp.bias & 0x7FFF)
+
+
 def test_skipped_tokens_leave_everything_as_it_was():
     """Positions outside the tables: nothing is written.  No slot (table too short, bad block id, negative length): the query is."""
     L, A, C = 1, 4, 3
@@ -213,16 +232,24 @@ def test_on_a_side_stream_and_captured():
 
 
 def test_types_and_shapes_that_do_not_fit_are_refused():
-    p = Problem(1, 4, 2, 128, 128, False, (0,), 2, seed=7)
+    p = Problem(1, 4, 2, 128, 128, False, (0,), 2, norm=128, seed=7)
     table, before = torch.from_numpy(p.table).to(DEV), torch.from_numpy(p.before).to(DEV)
 
     def call(q=p.g[0], k=p.g[1], v=p.g[2], **kw):
         return b.q4kv_norm_rope_append(p.spec, p.kp, p.vp, p.form, q, k, v, table, before, **kw)
     for bad in (dict(q=p.g[0].float()), dict(k=p.g[1].bfloat16()), dict(v=p.g[2][:, :, :1]), dict(q=p.g[0].cpu()),
-                dict(k=p.g[1].transpose(3, 4).contiguous().transpose(3, 4)), dict(q_out=torch.empty(1, dtype=torch.float32, device=DEV))):
+                dict(k=p.g[1].transpose(3, 4).contiguous().transpose(3, 4)), dict(q_out=torch.empty((1, 1, 2, 4, 128), dtype=torch.float32, device=DEV))):
         with pytest.raises(TypeError):
             call(**bad)
     with pytest.raises(ValueError):
         call(positions=torch.zeros((2, 2), dtype=torch.int32, device=DEV))
     with pytest.raises(ValueError):
         call(layer_begin=1)
+    with pytest.raises(ValueError):
+        call(q_out=torch.empty((1, 1, 1, 4, 128), dtype=torch.float16, device=DEV))
+    p.form.eps = -1.0                                # a form that is changed after a call
+    with pytest.raises(b.Q4KVError):
+        call()
+    p.form.rot_dim = 32
+    with pytest.raises(ValueError):
+        call()

@@ -257,6 +257,23 @@ def test_two_calls_at_once_with_a_workspace_each():
         assert all(torch.equal(x, y) for x, y in zip(got, want))
 
 
+def test_shapes_that_do_not_fit_are_refused():
+    f = Family(1, *LLAMA, [(256, (1, 2))], seed=19)
+    f.call()
+    for bad in (dict(out=torch.empty((1, 2, 1, 8, 64), dtype=torch.float16, device=DEV)), dict(lens=[3]), dict(table=f.table[:1]),
+                dict(begin=[0, 1, 2], prefix=[256])):
+        with pytest.raises(ValueError):
+            f.call(**bad)
+    with pytest.raises(TypeError):
+        f.call(out=torch.empty((1, 2, 1, 8, 128), dtype=torch.float32, device=DEV))
+    with pytest.raises(b.Q4KVError) as e:
+        f.call(workspace=torch.empty(100, dtype=torch.uint8, device=DEV))
+    assert e.value.code == -4
+    f.q = f.q[..., :64].copy()
+    with pytest.raises(ValueError):
+        f.call()
+
+
 def test_forked_agents_take_a_step():
     """Fork, prepare and append the step's token, attend: the three calls together, against the oracle's append and attention
     of the same prepared rows."""
