@@ -34,8 +34,9 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kCols = 16;          // query rows of a column tile
 constexpr int kMaxAgents = 512;    // agents of a call: their lengths and tile counts are kept in LDS
-constexpr int kSoloTiles = 16;     // tiles per wave from which the waves of a workgroup take ranges of their own
-constexpr int kLeastTiles = 4;     // smallest range of a workgroup: a tile per wave
+constexpr int kSoloTiles = 2;      // smallest range of a wave on its own
+constexpr int kPart = 3, kJoin = 1; // in tiles' time: see spread()
+constexpr int kJoinBelow = 16;     // tiles per wave from which workgroups are not considered
 constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kOneTermBits = 0x3B5C;   // binary16 0.92: largest value scale for which one binary16 term of p s keeps the tolerance
@@ -62,7 +63,7 @@ struct PrefixParams {
     float *part_acc, *part_ml;
     int num_agents, num_groups, max_blocks, num_blocks, kv_heads, q_heads, n_rep, layer_begin, layers, max_seq_len;
     int slots;    // records reserved per row for the prefix, and as many for the agent's own tokens
-    int row_tile, row_tile_log2; // rows of a prefix unit: 16 * CT, a power of two
+    int row_tile; // rows of a prefix unit: 16 * CT
     float score_scale;
     float inv_n_rep;
 };
@@ -151,27 +152,39 @@ __device__ __forceinline__ int quotient(int n, int d)
 // (v below 2^21 * round)
 __device__ __forceinline__ int rounded_up(int v, int round) { return round == 1 ? v : quotient(v + round - 1, round) * round; }
 
-// Tiles of a worker, and what units' tiles are rounded up to.  `total`: all tiles of the call, `padded(r)`: the same with every
-// unit's tiles rounded up to r.
-//   Many tiles: every wave takes an equal range of its own, wherever it begins.
-//   Few: every workgroup takes an equal range, its waves tile by tile in turn.  Where a range begins inside a unit and ends in
-//   another the workgroup pays for a second beginning and end (5 us: block ids, first tiles, queries, the join of the waves, against
-//   2 to 3 us a round of tiles), so units are cut into ranges of their own, each a multiple of a tile per wave, if that gives
-//   no more ranges than workgroups and none much longer than the even share.
+// How the tiles of a call are dealt out: `per` tiles a worker, units counted as the next multiple of `round`; true: the waves are
+// the workers, else the workgroups, whose waves take a range tile by tile in turn.  `total`: tiles of the call, `units`: units that
+// have any, padded(r): the tiles with every unit's rounded up to r.
+// A worker pays for every part of a unit it begins (block ids, first tiles, queries: kPart tiles' time), so units are
+// cut into ranges of their own that are equally long but for each unit's last, if there are workers enough for them all and the
+// ranges are not much longer for it.  A workgroup as a worker joins its waves' sums in LDS (kJoin tiles' time) and leaves one
+// record instead of four.  Else every wave takes an equal range wherever it begins.  Measured (us; only workgroups or, from 16 tiles a
+// wave on, waves with ranges anywhere / as here): 128-wide, ten agents behind 4,096, four layers 50.2 / 37.9; 64-wide, 14 behind 5,376,
+// eleven layers 47.0 / 29.7; 192 + 128, eight behind 2,048, three layers 38.8 / 27.9; 256-wide, 40 behind 1,024 46.4 / 35.3, ten behind
+// 8,192 27.9 / 27.8.  Ranges of their own whatever their length: 32 agents of 128-wide heads behind 16,384, two layers 82 -> 104.
 template <typename F>
-__device__ __forceinline__ bool spread(long long total, int workgroups, int &per, int &round, F padded)
+__device__ __forceinline__ bool spread(int total, int units, int workgroups, int &per, int &round, F padded)
 {
-    round = 1;
-    per = (int)((total + workgroups * kWaves - 1) / (workgroups * kWaves));
-    if (per >= kSoloTiles) return true;
-    per = max(kLeastTiles, (int)((total + workgroups - 1) / workgroups));
-    const int least = rounded_up(per, kWaves);
-    for (int r = least; r <= least + least / 2 + kWaves; r += kWaves)
-        if (padded(r) <= (long long)r * workgroups) {
-            per = round = r;
-            break;
-        }
-    return false;
+    auto fit = [&](int workers, int step) { // the shortest range, a multiple of `step`; 0: none
+        if (units > workers) return 0;
+        int r = rounded_up(quotient(total, workers - units / 2) + 1, step); // a unit's last range is half empty, about
+        for (int k = 0; k < 4; ++k, r += max(step, r / 8 / step * step))
+            if (padded(r) <= (long long)r * workers) return r;
+        return 0;
+    };
+    const int waves = workgroups * kWaves, even = max(kSoloTiles, quotient(total + waves - 1, waves));
+    // an equal range wherever it begins: some wave has a unit's beginning more than the average
+    const int anywhere = even + kPart + quotient(kPart * units, waves);
+    int alone = fit(waves, 1);
+    if (alone > anywhere) alone = 0;
+    const int best = alone > 0 ? alone : anywhere, together = even <= kJoinBelow ? fit(workgroups, kWaves) : 0;
+    if (together > 0 && together <= kWaves * (best + kJoin)) {
+        per = round = together;
+        return false;
+    }
+    per = alone > 0 ? max(alone, kSoloTiles) : even;
+    round = alone > 0 ? per : 1;
+    return true;
 }
 
 // What a lane reads for the plan of up to 64 agents: lane a of agent a, lane g of group g.
@@ -200,7 +213,7 @@ __device__ __forceinline__ void make_plan_few(const PrefixParams &p, const PlanI
         if (lane >= G - 1) next = end;
         const int agents = lane < G ? next - begin : 0;
         const int shared = agents > 1 ? min(max(prefix, 0), p.max_seq_len) / kWave : 0; // a group of one shares nothing
-        const int row_tiles = (agents * p.n_rep + p.row_tile - 1) >> p.row_tile_log2;
+        const int row_tiles = quotient(agents * p.n_rep + p.row_tile - 1, p.row_tile);
         // lane a: the group its agent is in, from the first agents of the groups that have any
         pl.mark[wave][lane] = 0;
         wave_lds_sync();
@@ -214,7 +227,8 @@ __device__ __forceinline__ void make_plan_few(const PrefixParams &p, const PlanI
         const int own = lane < A ? max(0, tiles_of(n) - start) : 0;
         const int units = p.layers * p.kv_heads; // (layer, KV head) pairs
         int per, round;
-        const bool solo = spread((long long)wave_total(own + row_tiles * shared) * units, gridDim.x, per, round,
+        const int busy = __builtin_popcountll(__builtin_amdgcn_ballot_w64(own > 0)) + wave_total(shared > 0 ? row_tiles : 0);
+        const bool solo = spread(wave_total(own + row_tiles * shared) * units, busy * units, gridDim.x, per, round,
                                  [&](int r) { return (long long)wave_total(rounded_up(own, r) + row_tiles * rounded_up(shared, r)) * units; });
         const int group_counts = row_tiles * rounded_up(shared, round), own_counts = rounded_up(own, round);
         const int group_incl = wave_scan(group_counts), own_incl = wave_scan(own_counts);
@@ -277,12 +291,12 @@ __device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
         if (g < G) {
             const int agents = pl.begin[g + 1] - pl.begin[g];
             if (agents < 2) shared[i] = 0;
-            row_tiles[i] = (agents * p.n_rep + p.row_tile - 1) >> p.row_tile_log2;
+            row_tiles[i] = quotient(agents * p.n_rep + p.row_tile - 1, p.row_tile);
             pl.group[g] = shared[i]; // for the agents, until the sums are taken
         }
     }
     __syncthreads();
-    int sum = 0;
+    int sum = 0, busy = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int a = tid * EACH + i;
@@ -297,6 +311,7 @@ __device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
             own[i] = max(0, tiles_of(n[i]) - start);
         }
         sum += own[i] + row_tiles[i] * shared[i];
+        busy += (own[i] > 0 ? 1 : 0) + (shared[i] > 0 ? row_tiles[i] : 0);
     }
     auto total = [&](int v, int slot) { // over the workgroup; every thread
         const int of_wave = wave_total(v);
@@ -309,7 +324,8 @@ __device__ __forceinline__ void make_plan_many(const PrefixParams &p, Plan &pl)
     };
     const int units = p.layers * p.kv_heads;
     int per, round;
-    const bool solo = spread(total(sum, 1) * units, gridDim.x, per, round, [&](int r) {
+    const int units_busy = (int)total(busy, 1) * units;
+    const bool solo = spread((int)total(sum, 1) * units, units_busy, gridDim.x, per, round, [&](int r) {
         int v = 0;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) v += rounded_up(own[i], r) + row_tiles[i] * rounded_up(shared[i], r);
@@ -786,14 +802,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         n_min = uniform(n_min);
         n_max = uniform(n_max);
         float4_t acc[CT][4 * GV], pbacc[CT];
-        float pb[CT][2 * GV], m_run[CT], l_run[CT]; // pb (up to two groups): even and odd rows r of the bias sums
+        float m_run[CT], l_run[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
             for (int c = 0; c < 4 * GV; ++c) acc[ct][c] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
             pbacc[ct] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int g = 0; g < 2 * GV; ++g) pb[ct][g] = 0.0f;
             m_run[ct] = kNegBig;
             l_run[ct] = 0.0f;
         }
@@ -943,10 +957,6 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                     const float alpha = __builtin_amdgcn_exp2f(m_run[ct] - m_new);
                     l_run[ct] *= alpha;
                     pbacc[ct] *= alpha;
-                    if constexpr (GV != 4) {
-#pragma unroll
-                        for (int g = 0; g < 2 * GV; ++g) pb[ct][g] *= alpha;
-                    }
 #pragma unroll
                     for (int c = 0; c < 4 * GV; ++c) acc[ct][c] *= alpha;
                 }
@@ -958,53 +968,55 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             // around the middle of its group, and not to a code counted from the group's end.  The eight comes off behind the
             // products: sum (c - 8) ps = sum c ps - 8 sum ps with the ps that were rounded, one more instruction per group and
             // half, into the accumulator of the bias sums (its rows = groups).
-            if constexpr (GV == 4) {
-                // rows of A = groups: the transposing read gives lane `col` group col % 4 of the four tokens that lanes 0, 4, 8, 12
-                // of its 16 point at
+            // scales of tokens 16 j + 4 qk + r, four tokens a read
+            uint32_t s4[4][2 * GV];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+            for (int j = 0; j < 4; ++j)
+                __builtin_memcpy(s4[j], __builtin_assume_aligned(params + S::VS_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // operand A: row `col` is group col % 4, its elements the middles of the tokens 4 qk + r of sets 2 h and 2 h + 1, side by
+                // side for each r
+                uint32_t mid[4];
+                if constexpr (GV == 4) {
+                    // the transposing read gives lane `col` group col % 4 of the four tokens that lanes 0, 4, 8, 12 of its 16 point at
                     const int tok = 16 * (2 * h + ((col >> 2) & 1)) + 4 * qk + (col >> 3);
                     const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + tok * 8;
-                    half2_t mid[4];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VB_AT + 16 * k)));
                         const uint2 s = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VS_AT + 16 * k)));
-                        mid[2 * k] = middle(s.x, b.x);
-                        mid[2 * k + 1] = middle(s.y, b.y);
+                        mid[2 * k] = half2_to_bits(middle(s.x, b.x));
+                        mid[2 * k + 1] = half2_to_bits(middle(s.y, b.y));
                     }
-                    const half8_t bop = words_to_half8(half2_to_bits(mid[0]), half2_to_bits(mid[1]), half2_to_bits(mid[2]), half2_to_bits(mid[3]));
+                } else {
+                    uint32_t m[2][2 * GV];
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        uint32_t w[4]; // p of the tokens 4 qk + r of sets 2 h and 2 h + 1
-                        const half2_t sixteen = half2_t{(half_t)16.0f, (half_t)16.0f};
+                    for (int k = 0; k < 2; ++k) {
+                        const int j = 2 * h + k;
+                        __builtin_memcpy(m[k], __builtin_assume_aligned(params + S::VB_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            half2_t v = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
-                            if (r & 1) v *= sixteen;
-                            w[r] = half2_to_bits(v);
-                        }
-                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(w[0], w[1], w[2], w[3]), pbacc[ct], 0, 0, 0);
+                        for (int w = 0; w < 2 * GV; ++w) m[k][w] = half2_to_bits(middle(s4[j][w], m[k][w]));
                     }
+                    // which half of a token's word: the group's (rows behind the last group repeat it and are not used)
+                    const uint32_t pick = GV == 2 && (col & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        mid[r] = GV == 2 ? __builtin_amdgcn_perm(m[1][r], m[0][r], pick)
+                                         : __builtin_amdgcn_perm(m[1][r / 2], m[0][r / 2], (r & 1) ? 0x07060302u : 0x05040100u);
                 }
-            }
-            // scales of tokens 16 j + 4 qk + r, four tokens a read
-            uint32_t s4[4][2 * GV];
+                const half8_t bop = words_to_half8(mid[0], mid[1], mid[2], mid[3]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                __builtin_memcpy(s4[j], __builtin_assume_aligned(params + S::VS_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
-                if constexpr (GV != 4) {
-                    uint32_t b[2 * GV];
-                    __builtin_memcpy(b, __builtin_assume_aligned(params + S::VB_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
+                for (int ct = 0; ct < CT; ++ct) {
+                    uint32_t w[4]; // p of the same tokens
+                    const half2_t sixteen = half2_t{(half_t)16.0f, (half_t)16.0f};
 #pragma unroll
-                    for (int k = 0; k < 2 * GV; ++k) b[k] = half2_to_bits(middle(s4[j][k], b[k]));
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-#pragma unroll
-                            for (int g = 0; g < GV; ++g) // even and odd r apart: the odd ones are sixteenths
-                                pb[ct][(r & 1) * GV + g] = fmaf(z[ct][j][r], half_of(b[(r * GV + g) / 2], (r * GV + g) & 1), pb[ct][(r & 1) * GV + g]);
+                    for (int r = 0; r < 4; ++r) {
+                        half2_t v = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
+                        if (r & 1) v *= sixteen;
+                        w[r] = half2_to_bits(v);
+                    }
+                    pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(w[0], w[1], w[2], w[3]), pbacc[ct], 0, 0, 0);
                 }
             }
             wait_values(min(mine - 1 - i, S::RING));
@@ -1078,17 +1090,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         auto sums = [&](int ct, int c) __attribute__((always_inline)) {
             float4_t o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = fmaf(acc[ct][c][r], kCodeScaleA, GV == 4 ? pbacc[ct][c / 4] : pb[ct][c / 4] + pbacc[ct][c / 4]);
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(acc[ct][c][r], kCodeScaleA, pbacc[ct][c / 4]);
             return o;
         };
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
-            if (GV != 4) {
-#pragma unroll
-                for (int g = 0; g < GV; ++g) pb[ct][g] = xor32_sum(xor16_sum(fmaf(16.0f, pb[ct][GV + g], pb[ct][g])));
-            }
-        }
+        for (int ct = 0; ct < CT; ++ct) l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
         auto finish_quad = [&](int64_t row, int e, float m, float l, float4_t o) __attribute__((always_inline)) {
             if (u.whole_row) {
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -1173,7 +1179,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
 
     for (int x = (int)begin; x < x1;) {
         const Part u = locate(p, plan, x, x1, per, round, worker);
-        if (CTP > 1 && u.which == 0) run_part(Int<CTP>(), u);
+        if (CTP > 1 && u.rows > kCols) run_part(Int<CTP>(), u);
         else run_part(Int<1>(), u);
         x += u.counted;
     }
@@ -1269,21 +1275,31 @@ hipError_t launch_t(const PrefixParams &p, bool bf, int compute_units, hipStream
     return hipGetLastError();
 }
 
-// Column tiles of a prefix unit: as many as the rows of an average group fill, up to two.
+template <int DK, int DV, int CTP>
+hipError_t launch_columns(int ct, const PrefixParams &p, bool bf, int compute_units, hipStream_t stream)
+{
+    if constexpr (CTP > 1)
+        if (ct < CTP) return launch_columns<DK, DV, CTP - 1>(ct, p, bf, compute_units, stream);
+    return launch_t<DK, DV, CTP>(p, bf, compute_units, stream);
+}
+
+// Column tiles of a prefix unit: the rows of an average group in as few units as pay, all alike.  Three column tiles of 64-wide
+// heads, two of wider ones: a third of 128-wide heads (85.5 -> 95.2 us for two layers of 128 rows behind 16,384 tokens) lives in
+// copies to and from accumulator registers, a fourth spills.
 int column_tiles(const q4kv_spec &s, int num_agents, int num_groups)
 {
     if (num_groups == 0) return 1;
     const int rows = s.num_q_heads / s.num_kv_heads * ((num_agents + num_groups - 1) / num_groups);
-    return rows > kCols ? 2 : 1;
+    const int tiles = (rows + kCols - 1) / kCols, most = s.v_dim == 64 ? 3 : 2, units = (tiles + most - 1) / most;
+    return (tiles + units - 1) / units;
 }
 
-// Records per row and part (see q4kv_shared_prefix_attention in api.hip for the workspace): a worker's range is at least
-// kLeastTiles (a workgroup's) or kSoloTiles (a wave's) long, and no shorter than an even share of all tiles, to which a unit of T
-// tiles contributes T for every layer and KV head.
+// Records per row and part: a worker's range is at least kSoloTiles (a wave's) or kWaves tiles (a workgroup's) long, and no shorter
+// than an even share of all tiles, to which a unit of T tiles contributes T for every layer and KV head.
 int record_slots(const q4kv_spec &s, int max_seq_len, int layers, int workgroups)
 {
     const int64_t tiles = (max_seq_len + kWave - 1) / kWave, units = (int64_t)layers * s.num_kv_heads;
-    const int64_t shared = std::min<int64_t>(tiles / kLeastTiles, workgroups / units);
+    const int64_t shared = std::min<int64_t>(tiles / kWaves, workgroups / units);
     const int64_t solo = std::min<int64_t>(tiles / kSoloTiles, (int64_t)workgroups * kWaves / units);
     return (int)std::max(shared, solo) + 2;
 }
@@ -1335,17 +1351,14 @@ hipError_t launch_prefix_attention(const PrefixArgs &a, hipStream_t stream)
     p.slots = record_slots(s, a.max_seq_len, a.layers, prefix_workgroups(a.compute_units));
     const int ct = column_tiles(s, a.num_agents, a.num_groups);
     p.row_tile = kCols * ct;
-    p.row_tile_log2 = ct == 2 ? 5 : 4;
     p.score_scale = a.sm_scale * kLog2e;
     p.inv_n_rep = 1.0f / (float)p.n_rep;
     const bool bf = s.param_format == Q4KV_PARAMS_BF16;
     hipError_t e = hipErrorInvalidValue;
-#define Q4KV_PREFIX(DK, DV) e = ct == 2 ? launch_t<DK, DV, 2>(p, bf, a.compute_units, stream) : launch_t<DK, DV, 1>(p, bf, a.compute_units, stream)
-    if (s.k_dim == 256) Q4KV_PREFIX(256, 256);
-    else if (s.k_dim == 192) Q4KV_PREFIX(192, 128);
-    else if (s.k_dim == 128) Q4KV_PREFIX(128, 128);
-    else if (s.k_dim == 64) Q4KV_PREFIX(64, 64);
-#undef Q4KV_PREFIX
+    if (s.k_dim == 256) e = launch_columns<256, 256, 2>(ct, p, bf, a.compute_units, stream);
+    else if (s.k_dim == 192) e = launch_columns<192, 128, 2>(ct, p, bf, a.compute_units, stream);
+    else if (s.k_dim == 128) e = launch_columns<128, 128, 2>(ct, p, bf, a.compute_units, stream);
+    else if (s.k_dim == 64) e = launch_columns<64, 64, 3>(ct, p, bf, a.compute_units, stream);
     if (e != hipSuccess) return e;
     const auto merge = s.v_dim == 256 ? prefix_merge_kernel<256> : s.v_dim == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>;
     hipLaunchKernelGGL(merge, dim3((unsigned)((int64_t)a.layers * a.num_agents * s.num_q_heads)), dim3(kThreads), 0, stream, p.part_acc, p.part_ml,

@@ -201,7 +201,7 @@ def test_many_agents():
     f.check(f.call())
     with pytest.raises(b.Q4KVError) as e:
         f.q = np.concatenate([f.q, f.q[:, :1]], 1)
-        f.call(lens=f.lens + [1])
+        f.call(lens=f.lens + [1], table=np.concatenate([f.table, f.table[:1]]))
     assert e.value.code == -3
 
 
