@@ -168,6 +168,7 @@ __device__ __forceinline__ bool spread(int total, int units, int workgroups, int
     auto fit = [&](int workers, int step) { // the shortest range, a multiple of `step`; 0: none
         if (units > workers) return 0;
         int r = rounded_up(quotient(total, workers - units / 2) + 1, step); // a unit's last range is half empty, about
+#pragma unroll 1
         for (int k = 0; k < 4; ++k, r += max(step, r / 8 / step * step))
             if (padded(r) <= (long long)r * workers) return r;
         return 0;
@@ -193,11 +194,14 @@ struct PlanInputs {
 };
 __device__ __forceinline__ PlanInputs plan_inputs(const PrefixParams &p, int lane)
 {
-    PlanInputs in;
-    in.len = lane < p.num_agents ? p.seq_len[lane] : 0;
-    in.prefix = lane < p.num_groups ? p.prefix_len[lane] : 0;
-    in.bound = lane < p.num_groups ? p.group_begin[lane] : 0;
-    in.last = p.num_groups > 0 ? p.group_begin[p.num_groups] : 0;
+    // lanes behind the last agent or group read that one again: a load behind a branch of its own would be waited for at its end
+    PlanInputs in = {p.seq_len[min(lane, p.num_agents - 1)], 0, 0, 0};
+    if (p.num_groups > 0) {
+        const int g = min(lane, p.num_groups - 1);
+        in.prefix = p.prefix_len[g];
+        in.bound = p.group_begin[g];
+        in.last = p.group_begin[p.num_groups];
+    }
     return in;
 }
 
@@ -206,7 +210,8 @@ __device__ __forceinline__ void make_plan_few(const PrefixParams &p, const PlanI
 {
     {
         const int A = p.num_agents, G = p.num_groups;
-        const int n = min(max(in.len, 0), p.max_seq_len), prefix = in.prefix, bound = in.bound, last = in.last;
+        const int n = lane < A ? min(max(in.len, 0), p.max_seq_len) : 0, prefix = in.prefix, last = in.last;
+        const int bound = lane < G ? in.bound : 0;
         const int begin = wave_scan_max(min(max(bound, 0), A)); // bounds that fall are raised: groups never overlap
         const int end = max(__builtin_amdgcn_readlane(begin, kWave - 1), min(max(last, 0), A));
         int next = __shfl_down(begin, 1, kWave);
@@ -728,7 +733,9 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             else wait_for_all_but<0>();
         };
 
-        // ---- the rows' queries are asked for first, with the block ids: loads complete in order
+        // ---- loads complete in order: the block ids, the rows' queries, the tiles
+        table_ids = fetch_table();
+        __builtin_amdgcn_sched_barrier(0);
         uint4 raw[CT][GK][2];
         int n_row[CT], n_min = 0x7fffffff, n_max = 0;
 #pragma unroll
@@ -743,7 +750,6 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 raw[ct][g][1] = *reinterpret_cast<const uint4 *>(qrow + g * kGroup + 8);
             }
         }
-        table_ids = fetch_table();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // all reads of the tile buffers are done
 #pragma unroll 1
         for (int i = 0; i < S::RING; ++i)
