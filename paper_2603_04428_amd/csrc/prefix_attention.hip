@@ -525,8 +525,8 @@ __device__ __forceinline__ void transfer(uint32_t lds, const void *src, uint32_t
                      : "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072" ::"s"(lds),
-                     "s"(src), "v"(o0), "v"(o1), "v"(o2), "v"(o3)
+                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:%6" ::"s"(lds),
+                     "s"(src), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "n"(3 * 1024)
                      : "memory");
 }
 // the code rows of a tile
@@ -925,9 +925,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             }
 
             // ---- online softmax.  m_run is the reference the exponentials are taken against: it moves only when a tile's maximum
-            // exceeds it by more than 7 (in log2 units), and then to 4 below that maximum.  p <= 2^7 then, and p s stays inside
-            // binary16 for scales up to 252; in a tile with a larger one p <= 2^2.5.  The codes of the odd rows r arrive 16 times
-            // larger in operand A (code_operand): z of an odd r becomes p / 16.
+            // exceeds it by more than `above_by` (in log2 units), and then to three below what it may be exceeded by.  p as well as p s
+            // stay inside binary16 (65504) then: p <= 2^15 with scales up to 0.92, 2^7 with scales up to 252, 2^2.5 with larger ones
+            // (no binary16 row has one above 8734); and what is far below a row's maximum keeps its bits: tokens of which there are many
+            // may weigh as much together as the few at the top.  The codes of the odd rows r arrive 16 times larger in operand A
+            // (code_operand): z of an odd r becomes p / 16.
+            const float above_by = wide ? 2.5f : two_terms ? 7.0f : 15.0f, lift = wide ? 0.0f : two_terms ? 4.0f : 12.0f;
             float zs = p.score_scale * kCodeScaleA;
             if (__builtin_expect(!(p.score_scale > 0.0f), 0)) { // the maximum may not be taken before the scale is applied
                 asm volatile("");
@@ -949,8 +952,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
 #pragma unroll
                 for (int k = 0; k < 16; ++k) mt = fmaxf(mt, z[ct][k / 4][k % 4]);
                 mt = xor32_max(xor16_max(mt)) * zs;
-                const bool above = mt > m_run[ct] + (wide ? 2.5f : 7.0f);
-                const float m_new = above ? mt - (wide ? 0.0f : 4.0f) : m_run[ct];
+                const bool above = mt > m_run[ct] + above_by;
+                const float m_new = above ? mt - lift : m_run[ct];
                 const float minus_even = -m_new, minus_odd = -(m_new + 4.0f);
                 float even_sum = 0.0f, odd_sum = 0.0f;
 #pragma unroll
@@ -973,7 +976,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             // ---- values: V_hat = (c - 8) s + (b + 8 s).  The one rounding of p s is then relative to |c - 8| s, the size of the value
             // around the middle of its group, and not to a code counted from the group's end.  The eight comes off behind the
             // products: sum (c - 8) ps = sum c ps - 8 sum ps with the ps that were rounded, one more instruction per group and
-            // half, into the accumulator of the bias sums (its rows = groups).
+            // half.  Of the accumulator for it, rows 4 k + g are group g's: k = 0, 1 take sum 8 ps and k = 2, 3 sum p (b + 8 s).
+            // Matrix instructions cut off what lies too far below the exponent of their largest summand, and a subnormal operand
+            // counts with the exponent of the smallest normal number: sum c ps falls short by 2^-19 of itself, about, while outputs
+            // over many tokens are only some hundredths of it.  So the eight is a code as well, cut off alike (8,192 tokens, 256-wide
+            // heads: the error of the outputs goes from 3.0e-4 to 2.7e-4 of their size, of which 2.1e-4 is their own rounding).
             // scales of tokens 16 j + 4 qk + r, four tokens a read
             uint32_t s4[4][2 * GV];
 #pragma unroll
@@ -1011,7 +1018,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                         mid[r] = GV == 2 ? __builtin_amdgcn_perm(m[1][r], m[0][r], pick)
                                          : __builtin_amdgcn_perm(m[1][r / 2], m[0][r / 2], (r & 1) ? 0x07060302u : 0x05040100u);
                 }
-                const half8_t bop = words_to_half8(mid[0], mid[1], mid[2], mid[3]);
+                const uint32_t is_mid = col >= 8 ? 0xFFFFFFFFu : 0u;
+                const half8_t bop = words_to_half8(mid[0] & is_mid, mid[1] & is_mid, mid[2] & is_mid, mid[3] & is_mid);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     uint32_t w[4]; // p of the same tokens
@@ -1033,8 +1041,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 for (int g = 0; g < GV; ++g) {
                     if (kTight) __builtin_amdgcn_sched_barrier(0);
                     half8_t hi[CT][2], lo[CT][2];
-                    const uint32_t minus_eight = col % 4 == g ? 0xC800C800u : 0u, sixteen_times = col % 4 == g ? 0xD800D800u : 0u;
-                    const half8_t eights = words_to_half8(minus_eight, sixteen_times, minus_eight, sixteen_times);
+                    const uint32_t eight = (col & 11) == g ? 0x00080008u : 0u, sixteen_times = (col & 11) == g ? 0x00800080u : 0u;
+                    const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -1100,7 +1108,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             return o;
         };
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
+        for (int ct = 0; ct < CT; ++ct) {
+            l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
+#pragma unroll
+            for (int g = 0; g < GV; ++g) pbacc[ct][g] = xor32_sum(qk < 2 ? -kCodeScaleA * pbacc[ct][g] : pbacc[ct][g]);
+        }
         auto finish_quad = [&](int64_t row, int e, float m, float l, float4_t o) __attribute__((always_inline)) {
             if (u.whole_row) {
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
