@@ -868,6 +868,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             float z[CT][4][4];
             const float4_t zero = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
             const uint32_t ka = k_at + base;
+            auto read_keys = [&](int j, int g) __attribute__((always_inline)) {
+                return *(lds_uint2_ptr)(uintptr_t)((ka ^ (uint32_t)(Rows<DK>::set_xor(j, g) << 4)) + (uint32_t)(16 * j * Rows<DK>::BYTES + Rows<DK>::group_offset(g)));
+            };
+            uint2_t keys[2][GK];
+#pragma unroll
+            for (int g = 0; g < GK; ++g) keys[0][g] = read_keys(0, g);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t b[2], s[2 * GK]; // bias row of token 16 j + col; scales of tokens 16 j + 4 qk .. + 3
@@ -898,8 +904,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 }
 #pragma unroll
                 for (int g = 0; g < GK; ++g) {
-                    const uint2_t w = *(lds_uint2_ptr)(uintptr_t)((ka ^ (uint32_t)(Rows<DK>::set_xor(j, g) << 4)) +
-                                                              (uint32_t)(16 * j * Rows<DK>::BYTES + Rows<DK>::group_offset(g)));
+                    const uint2_t w = keys[j % 2][g];
+                    if (j < 3) keys[(j + 1) % 2][g] = read_keys(j + 1, g); // ahead of their use
                     const half8_t a0 = code_operand(w.x), a1 = code_operand(w.y);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
@@ -986,6 +992,14 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             // (sixteen registers fewer: the sums need not be moved out of the way, 108.0 -> 103.8 us for 12 layers of 20 rows)
             constexpr bool kPairs = GV == 4;
             uint32_t s4[4][2 * GV];
+            auto read_pair = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        s4[j][(r * GV + g) / 2] = *reinterpret_cast<const uint32_t *>(params + S::VS_AT + (16 * j + 4 * qk + r) * (2 * GV) + 2 * g);
+            };
+            if (kPairs) read_pair(0);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (!kPairs) __builtin_memcpy(s4[j], __builtin_assume_aligned(params + S::VS_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
@@ -1038,18 +1052,15 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             }
             wait_values(min(mine - 1 - i, S::RING));
             const uint32_t va = v_at + base;
+            auto read_codes = [&](int c) __attribute__((always_inline)) {
+                return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_int2_ptr)(uintptr_t)((va ^ (uint32_t)((c >> 1) << 4)) + (c & 1) * 8));
+            };
             auto sum_values = [&](auto terms) __attribute__((always_inline)) {
                 constexpr bool TWO = decltype(terms)::value == 2;
+                int2_t words[2] = {read_codes(0), read_codes(1)}; // read two ahead of their use: left to itself, the compiler waits for each
 #pragma unroll
                 for (int g = 0; g < GV; ++g) {
                     if (kTight) __builtin_amdgcn_sched_barrier(0);
-                    if (kPairs && g % 2 == 0) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                s4[j][(r * GV + g) / 2] = *reinterpret_cast<const uint32_t *>(params + S::VS_AT + (16 * j + 4 * qk + r) * (2 * GV) + 2 * g);
-                    }
                     half8_t hi[CT][2], lo[CT][2];
                     const uint32_t eight = (col & 11) == g ? 0x00080008u : 0u, sixteen_times = (col & 11) == g ? 0x00800080u : 0u;
                     const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
@@ -1080,10 +1091,13 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                             pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, hi[ct][h], pbacc[ct], 0, 0, 0);
                             if (TWO) pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, lo[ct][h], pbacc[ct], 0, 0, 0);
                         }
+                    if (kPairs && g % 2 == 1 && g + 1 < GV) read_pair(g + 1);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int c = 4 * g + k;
-                        const int2_t w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_int2_ptr)(uintptr_t)((va ^ (uint32_t)((c >> 1) << 4)) + (c & 1) * 8));
+                        const int2_t w = words[c % 2];
+                        if (c + 2 < 4 * GV) words[c % 2] = read_codes(c + 2);
+                        __builtin_amdgcn_sched_barrier(0);
                         const half8_t a0 = code_operand((uint32_t)w.x), a1 = code_operand((uint32_t)w.y);
 #pragma unroll
                         for (int ct = 0; ct < CT; ++ct) {
