@@ -16,7 +16,7 @@
 //    tokens, group and 16 rows, operand A a code word masked in place (nibbles are binary16 subnormals), the scale applied to
 //    the binary32 results; the bias term is one 16x16x16 instruction over the groups, group sums of q split in two binary16
 //    parts.
-//  * output, transposed: O^T[e][row] = sum_t c[t,e] (p[row,t] s[t,g(e)]) + sum_t b[t,g(e)] p[row,t]: the transposing 4-bit LDS read
+//  * output, transposed: O^T[e][row] = sum_t (c[t,e] - 8) (p[row,t] s[t,g(e)]) + sum_t (b + 8 s)[t,g(e)] p[row,t]: the transposing 4-bit LDS read
 //    gives a lane 16 tokens of one element, masks unpack 8 of them into operand A; the lane that received S^T of (row, four
 //    tokens of each 16) supplies their p s as operand B, so probabilities never leave their registers.
 // Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
@@ -405,12 +405,6 @@ __device__ __forceinline__ half8_t code_operand(uint32_t w)
     return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
 }
 
-// b + 8 s of two binary16 pairs: the middle of a group's range (s >= 0)
-__device__ __forceinline__ half2_t middle(uint32_t s, uint32_t b)
-{
-    return __builtin_elementwise_fma(bits_to_half2(s), half2_t{(half_t)8.0f, (half_t)8.0f}, bits_to_half2(b));
-}
-
 __device__ __forceinline__ float half_of(uint32_t pair, int hi)
 {
     return half_bits_to_float((uint16_t)(hi ? pair >> 16 : pair & 0xffffu));
@@ -431,6 +425,15 @@ __device__ __forceinline__ uint32_t product_upper(uint32_t d, float p, uint32_t 
 {
     if constexpr (UPPER) asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
     else asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
+    return d;
+}
+
+// What the binary16 pair hi leaves of p0 f | p1 f.
+__device__ __forceinline__ uint32_t remainder_of(uint32_t hi, float p0, float p1, float f)
+{
+    uint32_t d;
+    asm("v_fma_mixlo_f16 %0, %1, %3, -%4 op_sel_hi:[0,0,1]\n\tv_fma_mixhi_f16 %0, %2, %3, -%4 op_sel:[0,0,1] op_sel_hi:[0,0,1]"
+        : "=&v"(d) : "v"(p0), "v"(p1), "s"(f), "v"(hi));
     return d;
 }
 
@@ -980,10 +983,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 m_run[ct] = m_new;
             }
 
-            // ---- values: V_hat = (c - 8) s + (b + 8 s).  The one rounding of p s is then relative to |c - 8| s, the size of the value
-            // around the middle of its group, and not to a code counted from the group's end.  The eight comes off behind the
-            // products: sum (c - 8) ps = sum c ps - 8 sum ps with the ps that were rounded, one more instruction per group and
-            // half.  Of the accumulator for it, rows 4 k + g are group g's: k = 0, 1 take sum 8 ps and k = 2, 3 sum p (b + 8 s).
+            // ---- values: V_hat = (c - 8) s + 8 s + b.  The one rounding of p s is then relative to |c - 8| s, the distance from the
+            // middle of the value's group, and not to a code counted from the group's end: sum (c - 8) ps = sum c ps - 8 sum ps with
+            // the ps that were rounded, one more instruction per group and half.  The middles may be any size, and cancel: sums of p b
+            // and p s take p in two binary16 terms.  All these sums share an accumulator, whose rows 4 k + g are group g's: k = 0 takes
+            // sum 8 ps, 2 sum p b and 3 sum p s.
             // Matrix instructions cut off what lies too far below the exponent of their largest summand, and a subnormal operand
             // counts with the exponent of the smallest normal number: sum c ps falls short by 2^-19 of itself, about, while outputs
             // over many tokens are only some hundredths of it.  So the eight is a code as well, cut off alike (8,192 tokens, 256-wide
@@ -1005,49 +1009,49 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 if (!kPairs) __builtin_memcpy(s4[j], __builtin_assume_aligned(params + S::VS_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                // operand A: row `col` is group col % 4, its elements the middles of the tokens 4 qk + r of sets 2 h and 2 h + 1, side by
-                // side for each r
-                uint32_t mid[4];
+                // operand A: row `col` is group col % 4, its elements zero (rows 0 to 7), b (to 11) or s of the tokens 4 qk + r of sets
+                // 2 h and 2 h + 1, side by side for each r
+                uint32_t word[4];
                 if constexpr (GV == 4) {
-                    // the transposing read gives lane `col` group col % 4 of the four tokens that lanes 0, 4, 8, 12 of its 16 point at
+                    // the transposing read gives lane `col` group col % 4 of four tokens, from the lanes col / 4, col / 4 + 4, .. of its 16:
+                    // those point at the tokens
                     const int tok = 16 * (2 * h + ((col >> 2) & 1)) + 4 * qk + (col >> 3);
-                    const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + tok * 8;
+                    const uint32_t at = region_at + base + S::K_BYTES + S::V_BYTES + tok * 8 + (col % 4 == 3 ? S::VS_AT : S::VB_AT);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VB_AT + 16 * k)));
-                        const uint2 s = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + S::VS_AT + 16 * k)));
-                        mid[2 * k] = half2_to_bits(middle(s.x, b.x));
-                        mid[2 * k + 1] = half2_to_bits(middle(s.y, b.y));
+                        const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(uintptr_t)(at + 16 * k)));
+                        word[2 * k] = w.x;
+                        word[2 * k + 1] = w.y;
                     }
                 } else {
                     uint32_t m[2][2 * GV];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int j = 2 * h + k;
-                        __builtin_memcpy(m[k], __builtin_assume_aligned(params + S::VB_AT + (16 * j + 4 * qk) * (2 * GV), 8), 8 * GV);
-#pragma unroll
-                        for (int w = 0; w < 2 * GV; ++w) m[k][w] = half2_to_bits(middle(s4[j][w], m[k][w]));
-                    }
+                    for (int k = 0; k < 2; ++k)
+                        __builtin_memcpy(m[k], __builtin_assume_aligned(params + (col < 12 ? S::VB_AT : S::VS_AT) + (16 * (2 * h + k) + 4 * qk) * (2 * GV), 8), 8 * GV);
                     // which half of a token's word: the group's (rows behind the last group repeat it and are not used)
                     const uint32_t pick = GV == 2 && (col & 1) ? 0x07060302u : 0x05040100u;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        mid[r] = GV == 2 ? __builtin_amdgcn_perm(m[1][r], m[0][r], pick)
-                                         : __builtin_amdgcn_perm(m[1][r / 2], m[0][r / 2], (r & 1) ? 0x07060302u : 0x05040100u);
+                        word[r] = GV == 2 ? __builtin_amdgcn_perm(m[1][r], m[0][r], pick)
+                                          : __builtin_amdgcn_perm(m[1][r / 2], m[0][r / 2], (r & 1) ? 0x07060302u : 0x05040100u);
                 }
-                const uint32_t is_mid = col >= 8 ? 0xFFFFFFFFu : 0u;
-                const half8_t bop = words_to_half8(mid[0] & is_mid, mid[1] & is_mid, mid[2] & is_mid, mid[3] & is_mid);
+                const uint32_t used = col >= 8 ? 0xFFFFFFFFu : 0u;
+                const half8_t bop = words_to_half8(word[0] & used, word[1] & used, word[2] & used, word[3] & used);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    uint32_t w[4]; // p of the same tokens
+                    uint32_t hi[4], lo[4]; // p of the same tokens
                     const half2_t sixteen = half2_t{(half_t)16.0f, (half_t)16.0f};
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        half2_t v = half2_t{(half_t)z[ct][2 * h][r], (half_t)z[ct][2 * h + 1][r]};
+                        const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
+                        half2_t v = half2_t{(half_t)p0, (half_t)p1};
                         if (r & 1) v *= sixteen;
-                        w[r] = half2_to_bits(v);
+                        hi[r] = half2_to_bits(v);
+                        lo[r] = remainder_of(hi[r], p0, p1, (r & 1) ? 16.0f : 1.0f);
                     }
-                    pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(w[0], w[1], w[2], w[3]), pbacc[ct], 0, 0, 0);
+                    asm("s_nop 1" : "+v"(lo[0]), "+v"(lo[1]), "+v"(lo[2]), "+v"(lo[3])); // as below
+                    pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(hi[0], hi[1], hi[2], hi[3]), pbacc[ct], 0, 0, 0);
+                    pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bop, words_to_half8(lo[0], lo[1], lo[2], lo[3]), pbacc[ct], 0, 0, 0);
                 }
             }
             wait_values(min(mine - 1 - i, S::RING));
@@ -1062,7 +1066,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 for (int g = 0; g < GV; ++g) {
                     if (kTight) __builtin_amdgcn_sched_barrier(0);
                     half8_t hi[CT][2], lo[CT][2];
-                    const uint32_t eight = (col & 11) == g ? 0x00080008u : 0u, sixteen_times = (col & 11) == g ? 0x00800080u : 0u;
+                    const uint32_t eight = col == g ? 0x00080008u : 0u, sixteen_times = col == g ? 0x00800080u : 0u;
                     const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
@@ -1135,7 +1139,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         for (int ct = 0; ct < CT; ++ct) {
             l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
 #pragma unroll
-            for (int g = 0; g < GV; ++g) pbacc[ct][g] = xor32_sum(qk < 2 ? -kCodeScaleA * pbacc[ct][g] : pbacc[ct][g]);
+            for (int g = 0; g < GV; ++g) pbacc[ct][g] = xor32_sum(xor16_sum(pbacc[ct][g] * (qk == 0 ? -kCodeScaleA : qk == 1 ? 0.0f : qk == 2 ? 1.0f : 8.0f)));
         }
         auto finish_quad = [&](int64_t row, int e, float m, float l, float4_t o) __attribute__((always_inline)) {
             if (u.whole_row) {

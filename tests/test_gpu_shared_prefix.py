@@ -16,7 +16,7 @@ class Family:
     """Pools on both sides, filled by the oracle: groups of (prefix tokens, own tokens of each agent).  The whole blocks of a
     prefix are listed by all agents of the group; what is left of it, each agent has in a block of its own."""
 
-    def __init__(self, L, Hq, Hkv, dk, dv, groups, fmt=0, seed=0, v_mult=1.0, extra=1, num_layers=None, layer_begin=0):
+    def __init__(self, L, Hq, Hkv, dk, dv, groups, fmt=0, seed=0, v_mult=1.0, v_away=0.0, extra=1, num_layers=None, layer_begin=0):
         rng = np.random.default_rng(seed)
         nl = num_layers or layer_begin + L
         self.L, self.lb, self.scale = L, layer_begin, 1.0 / np.sqrt(dk)
@@ -48,6 +48,8 @@ class Family:
             for h in range(Hkv):
                 k[..., h, loud[h]] *= 8
             v = rng.standard_normal((L, 1, tokens, Hkv, dv)) * v_mult
+            if v_away:  # a token's values lie around + or - v_away
+                v += v_away * rng.choice([-1.0, 1.0], (L, 1, tokens, Hkv, 1))
             new = [x.astype(np.float16) for x in (k, v)]
             for who, t0, t1 in [(a, first, first + tokens)] if isinstance(a, int) else a:
                 part = [x[:, :, t0 - first:t1 - first] for x in new]
@@ -164,6 +166,16 @@ def test_wide_and_tiny_values(heads, v_mult, fmt):
     size = 2 * 2 * 5.0 * v_mult                      # |x| < 5 v_mult: range below 10 v_mult
     assert np.all(np.abs(got - want) <= 2 * (2.0 ** -12 * size + 2.0 ** -11 * np.abs(want) + 2.0 ** -25))
     assert np.linalg.norm(got - want) <= 1.5e-3 * np.linalg.norm(want) + 2.0 ** -24 * np.sqrt(want.size)
+
+
+@pytest.mark.parametrize("heads", [LLAMA, GEMMA, PER_HEAD, NARROW], ids=["128", "256", "192", "64"])
+@pytest.mark.parametrize("away", [48.0, 1000.0])
+def test_values_far_from_zero_that_cancel(heads, away):
+    """Groups of small range around + and - `away`: a probability rounded to binary16 in front of the group's middle would be off by
+    up to 2^-12 of `away`, 0.01 and 0.25, where the outputs of a few tokens nearly cancel."""
+    for seed in range(4):
+        f = Family(1, *heads, [(64, (1, 2, 5, 9)), (0, (2, 3, 130)), (256, (1, 40))], seed=70 + seed, v_away=away, fmt=seed % 2)
+        f.check(f.call())
 
 
 def test_a_dominant_token_and_equal_scores():
