@@ -61,6 +61,8 @@ __global__ __launch_bounds__(kCopyThreads) void image_copy_kernel(ImageParams p)
 // pieces read from the source block and written to the destination block.  Only moves bytes: floor = 2 * bytes at the rate
 // of a copy.  A workgroup takes kCopyUnit bytes of one record, kCopyLoads independent 16-byte loads per lane before the
 // first store, and nothing is carried between workgroups, so that a single pair on a few layers already fills the chip.
+// Measured: nine 256-wide blocks of 48 layers 85 us (255 MB each way), 101 latent blocks of 27 layers 83 us (226 MB), one block of
+// 32 layers 5 us.
 constexpr int kCopyLoads = 4;
 constexpr int kCopyUnit = kCopyLoads * kChunkBytes;
 
