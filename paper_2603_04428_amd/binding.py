@@ -159,7 +159,7 @@ class Pool:
 
     def __init__(self, spec, dim, num_blocks, device="cuda", poison=False):
         shp = (spec.num_layers, num_blocks, spec.num_kv_heads, spec.block_tokens)
-        self.dim, self.num_blocks = dim, num_blocks
+        self.dim, self.num_blocks, self.extent = dim, num_blocks, (spec.num_layers, spec.num_kv_heads, dim)
         # torch has no uint32/uint16 arithmetic, and none is needed: int32 / int16 storage of the same bits
         self.codes = torch.zeros(shp + (dim // 8,), dtype=torch.int32, device=device)
         self.scale = torch.zeros(shp + (dim // 64,), dtype=torch.int16, device=device)
@@ -181,6 +181,7 @@ class Pool:
             _dev(t, kind, name)
         p = cls.__new__(cls)
         p.dim, p.num_blocks, p.codes, p.scale, p.bias = codes.shape[-1] * 8, codes.shape[1], codes, scale, bias
+        p.extent = (lead[0], lead[2], p.dim) if lead[3] == 256 else None
         return p
 
     def c(self):
@@ -398,6 +399,17 @@ def q4kv_append(spec, kpool, vpool, k_new, v_new, block_table, seq_len_before, l
                              _stream()))
 
 
+def _pools(spec, kpool, vpool):
+    """The pools of a call as the library takes them, refused where their arrays are not those of the spec."""
+    if kpool.extent != (spec.num_layers, spec.num_kv_heads, spec.k_dim):
+        raise ValueError(f"K pool of (layers, KV heads, width) {kpool.extent}, not {(spec.num_layers, spec.num_kv_heads, spec.k_dim)}")
+    if spec.v_aliases_k:
+        return C.byref(kpool.c()), None
+    if vpool is not None and vpool.extent != (spec.num_layers, spec.num_kv_heads, spec.v_dim):
+        raise ValueError(f"V pool of (layers, KV heads, width) {vpool.extent}, not {(spec.num_layers, spec.num_kv_heads, spec.v_dim)}")
+    return C.byref(kpool.c()), None if vpool is None else C.byref(vpool.c())
+
+
 def _token_rows(t, heads, dim, name):
     """[layers][agents][chunk][heads][dim] with contiguous tokens a fixed stride apart -> that stride in elements."""
     shape = t.shape
@@ -423,7 +435,7 @@ def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table
     """q / k_new / v_new: fp16 or bf16 [layers_in_call][A][C][heads][dim], possibly parts of one fused projection (tokens a fixed
     stride apart); form: HeadForm.  Returns the prepared queries, fp16 [layers_in_call][A][C][q_heads][k_dim]."""
     layer_end = spec.num_layers if layer_end is None else layer_end
-    alias, hq, hkv, dk = spec.v_aliases_k, spec.num_q_heads, spec.num_kv_heads, spec.k_dim
+    hq, hkv, dk = spec.num_q_heads, spec.num_kv_heads, spec.k_dim
     q_stride, k_stride, v_stride = _token_rows(q, hq, dk, "q"), _token_rows(k_new, hkv, dk, "k_new"), 0
     if v_new is not None:
         v_stride = _token_rows(v_new, hkv, spec.v_dim, "v_new")
@@ -443,8 +455,9 @@ def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table
         raise ValueError(f"{A} agents, {block_table.shape[0]} rows of blocks, {seq_len_before.numel()} lengths")
     if positions is not None and tuple(positions.shape) != (A, Cn):
         raise ValueError(f"positions: {tuple(positions.shape)} instead of {(A, Cn)}")
+    kp, vp = _pools(spec, kpool, vpool)
     _check(lib().q4kv_norm_rope_append(
-        C.byref(spec), C.byref(kpool.c()), None if alias else C.byref(vpool.c()), C.byref(form.c(Lr)), q.data_ptr(),
+        C.byref(spec), kp, vp, C.byref(form.c(Lr)), q.data_ptr(),
         k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), 1 if kind == torch.bfloat16 else 0, q_stride, k_stride,
         v_stride, _dev(q_out, torch.float16, "q_out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
         _dev(seq_len_before, torch.int32, "seq_len_before"), _dev(positions, torch.int32, "positions"), A, Cn, layer_begin,
@@ -456,10 +469,8 @@ def q4kv_copy_blocks(spec, kpool, vpool, src_ids, dst_ids):
     """Block dst_ids[i] becomes a copy of block src_ids[i], every layer, K and V; ids: int32 tensors on the GPU."""
     if src_ids.numel() != dst_ids.numel():
         raise ValueError(f"{src_ids.numel()} sources for {dst_ids.numel()} destinations")
-    kp = kpool.c()
-    vp = None if spec.v_aliases_k else vpool.c()
-    _check(lib().q4kv_copy_blocks(C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp),
-                                  _dev(src_ids, torch.int32, "src_ids"), _dev(dst_ids, torch.int32, "dst_ids"),
+    kp, vp = _pools(spec, kpool, vpool)
+    _check(lib().q4kv_copy_blocks(C.byref(spec), kp, vp, _dev(src_ids, torch.int32, "src_ids"), _dev(dst_ids, torch.int32, "dst_ids"),
                                   src_ids.numel(), _stream()))
 
 
@@ -530,13 +541,13 @@ def q4kv_shared_prefix_attention(spec, kpool, vpool, q, block_table, seq_len, gr
     if workspace is None:
         need = q4kv_shared_prefix_workspace_bytes(spec, max(A, 1), max_seq_len, max(Lr, 1))
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    kp, vp = kpool.c(), None if vpool is None else vpool.c()
+    kp, vp = _pools(spec, kpool, vpool)
     _check(lib().q4kv_shared_prefix_attention(
-        C.byref(spec), C.byref(kp), None if vp is None else C.byref(vp), _dev(q, torch.float16, "q"),
+        C.byref(spec), kp, vp, _dev(q, torch.float16, "q"),
         _dev(out, torch.float16, "out"), _dev(block_table, torch.int32, "block_table"), block_table.shape[1],
         _dev(seq_len, torch.int32, "seq_len"), A, _dev(group_begin, torch.int32, "group_begin"),
         _dev(prefix_len, torch.int32, "prefix_len"), groups, max_seq_len, float(sm_scale), layer_begin, layer_end,
-        workspace.data_ptr(), workspace.numel(), _stream()))
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
     return out
 
 

@@ -156,3 +156,17 @@ def test_shared_prefix_workspace_does_not_fall_with_agents():
         for top in (64, 1000, 32768):
             sizes = [b.q4kv_shared_prefix_workspace_bytes(spec, a, top, layers) for a in (1, 2, 10, 100, 512)]
             assert sizes == sorted(sizes) and all(n % 8 == 0 for n in sizes)
+
+
+def test_pools_of_another_spec_are_refused():
+    spec, other = b.make_spec(2, 4, 2, 192, 128), b.make_spec(3, 4, 2, 192, 128)
+    k, v = b.Pool(spec, 192, 2, "cpu"), b.Pool(spec, 128, 2, "cpu")
+    b._pools(spec, k, v)
+    b._pools(spec, k, None)
+    b._pools(b.make_spec(2, 4, 2, 192, 128, True), k, None)
+    for args in ((spec, v, v), (spec, k, k), (other, k, v), (b.make_spec(2, 4, 4, 192, 128), k, v), (spec, k, b.Pool(other, 128, 2, "cpu"))):
+        with pytest.raises(ValueError, match="pool"):
+            b._pools(*args)
+    ids = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="pool"):
+        b.q4kv_copy_blocks(other, k, v, ids, ids)

@@ -211,10 +211,9 @@ def test_many_tiles_per_wave(heads):
 def test_many_agents():
     f = Family(1, 2, 1, 64, 64, [(256, tuple(1 + i % 70 for i in range(300))), (64, (3,) * 100), (0, (9,) * 112)], seed=13)
     f.check(f.call())
-    with pytest.raises(b.Q4KVError) as e:
-        f.q = np.concatenate([f.q, f.q[:, :1]], 1)
+    f.q = np.concatenate([f.q, f.q[:, :1]], 1)
+    with pytest.raises(b.Q4KVError, match="at most 512 agents"):
         f.call(lens=f.lens + [1], table=np.concatenate([f.table, f.table[:1]]))
-    assert e.value.code == -3
 
 
 def test_same_bits_every_time_on_a_side_stream_and_captured():
@@ -278,9 +277,10 @@ def test_shapes_that_do_not_fit_are_refused():
             f.call(**bad)
     with pytest.raises(TypeError):
         f.call(out=torch.empty((1, 2, 1, 8, 128), dtype=torch.float32, device=DEV))
-    with pytest.raises(b.Q4KVError) as e:
+    with pytest.raises(b.Q4KVError, match="workspace needs"):  # (kept in a local, the error would keep this frame and its pools)
         f.call(workspace=torch.empty(100, dtype=torch.uint8, device=DEV))
-    assert e.value.code == -4
+    with pytest.raises(TypeError, match="workspace"):
+        f.call(workspace=torch.empty(1 << 20, dtype=torch.uint8))
     f.q = f.q[..., :64].copy()
     with pytest.raises(ValueError):
         f.call()
