@@ -1062,41 +1062,44 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             auto read_codes = [&](int c) __attribute__((always_inline)) {
                 return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_int2_ptr)(uintptr_t)((va ^ (uint32_t)((c >> 1) << 4)) + (c & 1) * 8));
             };
-            auto sum_values = [&](auto terms) __attribute__((always_inline)) {
-                constexpr bool TWO = decltype(terms)::value == 2;
+            // once with p s, and in a tile with wide groups again with what that rounding left
+            const int passes = two_terms ? 2 : 1;
+#pragma unroll 1
+            for (int pass = 0; pass < passes; ++pass) {
+                if (kPairs && __builtin_expect(pass > 0, 0)) read_pair(0);
                 int2_t words[2] = {read_codes(0), read_codes(1)}; // read two ahead of their use: left to itself, the compiler waits for each
 #pragma unroll
                 for (int g = 0; g < GV; ++g) {
                     if (kTight) __builtin_amdgcn_sched_barrier(0);
-                    half8_t hi[CT][2], lo[CT][2];
+                    half8_t ps[CT][2];
                     const uint32_t eight = col == g ? 0x00080008u : 0u, sixteen_times = col == g ? 0x00800080u : 0u;
                     const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            uint32_t a[4], b[4];
+                            uint32_t a[4];
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int at = r * GV + g;
-                                if constexpr (!TWO) {
-                                    const uint32_t w0 = s4[2 * h][at / 2], w1 = s4[2 * h + 1][at / 2];
-                                    const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
-                                    a[r] = at & 1 ? product_upper<true>(product_lower<true>(p0, w0), p1, w1)
-                                                  : product_upper<false>(product_lower<false>(p0, w0), p1, w1);
-                                    continue;
+                                const uint32_t w0 = s4[2 * h][at / 2], w1 = s4[2 * h + 1][at / 2];
+                                const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
+                                a[r] = at & 1 ? product_upper<true>(product_lower<true>(p0, w0), p1, w1)
+                                              : product_upper<false>(product_lower<false>(p0, w0), p1, w1);
+                            }
+                            if (__builtin_expect(pass > 0, 0)) {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const int at = r * GV + g;
+                                    const float s0 = half_of(s4[2 * h][at / 2], at & 1), s1 = half_of(s4[2 * h + 1][at / 2], at & 1);
+                                    const half2_t v = bits_to_half2(a[r]);
+                                    a[r] = half2_to_bits(half2_t{(half_t)fmaf(z[ct][2 * h][r], s0, -(float)v[0]), (half_t)fmaf(z[ct][2 * h + 1][r], s1, -(float)v[1])});
                                 }
-                                const float s0 = half_of(s4[2 * h][at / 2], at & 1), s1 = half_of(s4[2 * h + 1][at / 2], at & 1);
-                                const half_t p0 = (half_t)(z[ct][2 * h][r] * s0), p1 = (half_t)(z[ct][2 * h + 1][r] * s1);
-                                a[r] = half2_to_bits(half2_t{p0, p1});
-                                b[r] = half2_to_bits(half2_t{(half_t)fmaf(z[ct][2 * h][r], s0, -(float)p0), (half_t)fmaf(z[ct][2 * h + 1][r], s1, -(float)p1)});
                             }
                             // the compiler does not see vector instructions in asm statements: the distance a matrix instruction may want
-                            if (!TWO) asm("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
-                            hi[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
-                            if (TWO) lo[ct][h] = words_to_half8(b[0], b[1], b[2], b[3]);
-                            pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, hi[ct][h], pbacc[ct], 0, 0, 0);
-                            if (TWO) pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, lo[ct][h], pbacc[ct], 0, 0, 0);
+                            asm("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
+                            ps[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
+                            pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, ps[ct][h], pbacc[ct], 0, 0, 0);
                         }
                     if (kPairs && g % 2 == 1 && g + 1 < GV) read_pair(g + 1);
 #pragma unroll
@@ -1108,18 +1111,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                         const half8_t a0 = code_operand((uint32_t)w.x), a1 = code_operand((uint32_t)w.y);
 #pragma unroll
                         for (int ct = 0; ct < CT; ++ct) {
-                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, hi[ct][0], acc[ct][c], 0, 0, 0);
-                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, hi[ct][1], acc[ct][c], 0, 0, 0);
-                            if (TWO) {
-                                acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, lo[ct][0], acc[ct][c], 0, 0, 0);
-                                acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, lo[ct][1], acc[ct][c], 0, 0, 0);
-                            }
+                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, ps[ct][0], acc[ct][c], 0, 0, 0);
+                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, ps[ct][1], acc[ct][c], 0, 0, 0);
                         }
                     }
                 }
-            };
-            if (__builtin_expect(two_terms, 0)) sum_values(Int<2>());
-            else sum_values(Int<1>());
+            }
             if (more) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 issue_rest(buf);
