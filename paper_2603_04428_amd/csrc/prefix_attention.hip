@@ -21,7 +21,7 @@
 //    tokens of each 16) supplies their p s as operand B, so probabilities never leave their registers.
 // Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
 // What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (22 us for 10 agents x 8,192 tokens, 256-wide,
-// one layer), above that the issue of instructions (60 % of a wave's time; matrix pipe 19 %): 12 such layers 98 us, 301 MB of cache = 3.1
+// one layer), above that the issue of instructions (61 % of a wave's time; matrix pipe 19 %): 12 such layers 95 us, 301 MB of cache = 3.2
 // TB/s; 32 agents of four rows x 16,384, 128-wide, two layers 79 us.
 #include <algorithm>
 
@@ -42,7 +42,7 @@ constexpr int kPart = 3, kJoin = 1; // in tiles' time: see spread()
 constexpr int kJoinBelow = 16;     // tiles per wave from which workgroups are not considered
 constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint32_t kOneTermBits = 0x3B5C;   // binary16 0.92: largest value scale for which one binary16 term of p s keeps the tolerance
+constexpr uint32_t kOneTermBits = 0x3B5C;   // binary16 0.92: largest value scale for which one binary16 term of p s (2^-12 of 8 s p) keeps the tolerance of 2e-3
 constexpr uint32_t kLiftScaleBits = 0x5BE0; // binary16 252: 2^8 times that is still below 65504
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
