@@ -10,7 +10,7 @@
 // One pass over each unit's cache, 64 tokens at a time, per wave (no synchronisation inside the tile loop):
 //  * code words and parameters travel HBM -> LDS directly (global_load_lds, 16 bytes a lane) into a ring of tile buffers; the K
 //    part of a buffer is asked for again as soon as the scores of its tile are taken, the rest when its values are summed, so
-//    that kRing - 1/2 tiles are on their way while one is worked on.  Rows lie swizzled in LDS: 16-byte chunk c of token t at
+//    that RING - 1/2 tiles are on their way while one is worked on.  Rows lie swizzled in LDS: 16-byte chunk c of token t at
 //    chunk c ^ f(t), which spreads both kinds of reads below over all banks; the transfer fetches permuted chunks of one row.
 //  * scores, transposed: S^T[t][row] = sum_g s[t,g] (C_g Q_g^T)[t][row] + (b Qsum^T)[t][row]: two v_mfma_f32_16x16x32_f16 per 16
 //    tokens, group and 16 rows, operand A a code word masked in place (nibbles are binary16 subnormals), the scale applied to
@@ -20,8 +20,8 @@
 //    gives a lane 16 tokens of one element, masks unpack 8 of them into operand A; the lane that received S^T of (row, four
 //    tokens of each 16) supplies their p s as operand B, so probabilities never leave their registers.
 // Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
-// What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (22 us for 10 agents x 8,192 tokens, 256-wide,
-// one layer), above that the issue of instructions (61 % of a wave's time; matrix pipe 19 %): 12 such layers 95 us, 301 MB of cache = 3.2
+// What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (21 us for 10 agents x 8,192 tokens, 256-wide,
+// one layer), above that the issue of instructions (60 % of a wave's time; matrix pipe 21 %): 12 such layers 91 us, 301 MB of cache = 3.3
 // TB/s; 32 agents of four rows x 16,384, 128-wide, two layers 79 us.
 #include <algorithm>
 
@@ -930,6 +930,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                     for (int r = 0; r < 4; ++r) z[ct][j][r] = sum[ct][r];
                 if (kTight) __builtin_amdgcn_sched_barrier(0);
             }
+            // wide tiles' scores are final here: or the scaling sinks behind the branches below, and all products wait for it in registers
+            // (12 layers of 20 rows, 256-wide, 99.1 -> 93.3 us; 128-wide heads, which have room for that, are faster without: 82.4 for 84.6)
+            if constexpr (kTight) {
+#pragma unroll
+                for (int k = 0; k < 16 * CT; ++k) asm volatile("" : "+v"(z[k / 16][k / 4 % 4][k % 4]));
+            }
             // K of this buffer has been read: the next tile for it
             const bool more = i + S::RING < mine;
             if (more) {
@@ -1330,8 +1336,8 @@ hipError_t launch_columns(int ct, const PrefixParams &p, bool bf, int compute_un
 }
 
 // Column tiles of a prefix unit: the rows of an average group in as few units as pay, all alike.  Three column tiles of 64-wide
-// heads, two of wider ones: a third of 128-wide heads (85.5 -> 95.2 us for two layers of 128 rows behind 16,384 tokens) lives in
-// copies to and from accumulator registers, a fourth spills.
+// heads, two of wider ones.  Three or four of 128-wide heads take two layers of 128 rows behind 16,384 tokens from 82.0 to 96.6 and
+// 99.7 us (four layers of 40 rows behind 4,096 from 36.8 to 35.1 and 35.6): in the plan a tile counts for one however many rows it has.
 int column_tiles(const q4kv_spec &s, int num_agents, int num_groups)
 {
     if (num_groups == 0) return 1;
