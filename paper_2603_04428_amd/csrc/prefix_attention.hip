@@ -18,7 +18,7 @@
 //    parts.
 //  * output, transposed: O^T[e][row] = sum_t (c[t,e] - 8) (p[row,t] s[t,g(e)]) + sum_t (b + 8 s)[t,g(e)] p[row,t]: the transposing 4-bit LDS read
 //    gives a lane 16 tokens of one element, masks unpack 8 of them into operand A; the lane that received S^T of (row, four
-//    tokens of each 16) supplies their p s as operand B, so probabilities never leave their registers.
+//    tokens of each 16) supplies their p s as operand B, in two binary16 terms, so probabilities never leave their registers.
 // Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
 // What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (21 us for 10 agents x 8,192 tokens, 256-wide,
 // one layer), above that the issue of instructions (60 % of a wave's time; matrix pipe 21 %): 12 such layers 91 us, 301 MB of cache = 3.3
@@ -42,8 +42,9 @@ constexpr int kPart = 3, kJoin = 1; // in tiles' time: see spread()
 constexpr int kJoinBelow = 16;     // tiles per wave from which workgroups are not considered
 constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint32_t kOneTermBits = 0x3B5C;   // binary16 0.92: largest value scale for which one binary16 term of p s (2^-12 of 8 s p) keeps the tolerance of 2e-3
-constexpr uint32_t kLiftScaleBits = 0x5BE0; // binary16 252: 2^8 times that is still below 65504
+// Largest value scales (binary16 bits) with which probabilities may reach 2^15 and 2^7: their products stay below 65504.
+constexpr uint32_t kHighScaleBits = 0x3F9A; // 1.9
+constexpr uint32_t kMidScaleBits = 0x5BE0;  // 252
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 typedef int int2_t __attribute__((ext_vector_type(2)));
@@ -428,6 +429,23 @@ __device__ __forceinline__ uint32_t product_upper(uint32_t d, float p, uint32_t 
 {
     if constexpr (UPPER) asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
     else asm("v_fma_mixhi_f16 %0, %1, %2, 0 op_sel_hi:[0,1,0]" : "+v"(d) : "v"(p), "v"(s));
+    return d;
+}
+
+// What the product's rounding left: p s less a half of hi, exact but where it is subnormal.
+template <bool UPPER>
+__device__ __forceinline__ uint32_t rest_lower(float p, uint32_t s, uint32_t hi)
+{
+    uint32_t d;
+    if constexpr (UPPER) asm("v_fma_mixlo_f16 %0, %1, %2, -%3 op_sel:[0,1,0] op_sel_hi:[0,1,1]" : "=v"(d) : "v"(p), "v"(s), "v"(hi));
+    else asm("v_fma_mixlo_f16 %0, %1, %2, -%3 op_sel_hi:[0,1,1]" : "=v"(d) : "v"(p), "v"(s), "v"(hi));
+    return d;
+}
+template <bool UPPER>
+__device__ __forceinline__ uint32_t rest_upper(uint32_t d, float p, uint32_t s, uint32_t hi)
+{
+    if constexpr (UPPER) asm("v_fma_mixhi_f16 %0, %1, %2, -%3 op_sel:[0,1,1] op_sel_hi:[0,1,1]" : "+v"(d) : "v"(p), "v"(s), "v"(hi));
+    else asm("v_fma_mixhi_f16 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,1,1]" : "+v"(d) : "v"(p), "v"(s), "v"(hi));
     return d;
 }
 
@@ -867,8 +885,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 for (int g = 0; g < GV; ++g) s_top = max(s_top, (uint32_t)vs[g]);
                 wave_lds_sync();
             }
-            const bool two_terms = __builtin_amdgcn_ballot_w64(s_top > kOneTermBits) != 0ull;
-            const bool wide = two_terms && __builtin_amdgcn_ballot_w64(s_top > kLiftScaleBits) != 0ull;
+            const bool mid = __builtin_amdgcn_ballot_w64(s_top > kHighScaleBits) != 0ull;
+            const bool wide = mid && __builtin_amdgcn_ballot_w64(s_top > kMidScaleBits) != 0ull;
 
             // ---- scores: z[ct][j][r] is token 16 j + 4 qk + r, row 16 ct + col, in units of 2^-24 / score_scale
             float z[CT][4][4];
@@ -944,12 +962,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             }
 
             // ---- online softmax.  m_run is the reference the exponentials are taken against: it moves only when a tile's maximum
-            // exceeds it by more than `above_by` (in log2 units), and then to three below what it may be exceeded by.  p as well as p s
-            // stay inside binary16 (65504) then: p <= 2^15 with scales up to 0.92, 2^7 with scales up to 252, 2^2.5 with larger ones
+            // exceeds it by more than `above_by` (in log2 units), and then to `lift` below that maximum.  p as well as p s stay
+            // inside binary16 (65504) then: p <= 2^15 with scales up to 1.9, 2^7 with scales up to 252, 2^2.5 with larger ones
             // (no binary16 row has one above 8734); and what is far below a row's maximum keeps its bits: tokens of which there are many
             // may weigh as much together as the few at the top.  The codes of the odd rows r arrive 16 times larger in operand A
             // (code_operand): z of an odd r becomes p / 16.
-            const float above_by = wide ? 2.5f : two_terms ? 7.0f : 15.0f, lift = wide ? 0.0f : two_terms ? 4.0f : 12.0f;
+            const float above_by = wide ? 2.5f : mid ? 7.0f : 15.0f, lift = wide ? 0.0f : mid ? 4.0f : 12.0f;
             float zs = p.score_scale * kCodeScaleA;
             if (__builtin_expect(!(p.score_scale > 0.0f), 0)) { // the maximum may not be taken before the scale is applied
                 asm volatile("");
@@ -992,15 +1010,17 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 m_run[ct] = m_new;
             }
 
-            // ---- values: V_hat = (c - 8) s + 8 s + b.  The one rounding of p s is then relative to |c - 8| s, the distance from the
-            // middle of the value's group, and not to a code counted from the group's end: sum (c - 8) ps = sum c ps - 8 sum ps with
-            // the ps that were rounded, one more instruction per group and half.  The middles may be any size, and cancel: sums of p b
+            // ---- values: V_hat = (c - 8) s + 8 s + b.  p s goes in as two binary16 terms, what the first one's rounding left being the
+            // second, so that 2^-22 of it is lost, relative to |c - 8| s, the distance from the middle of the value's group: sum (c - 8) ps =
+            // sum c ps - 8 sum ps with the ps that were rounded, two more instructions per group and half.  One term alone would be 2^-12
+            // off, 2.6e-4 instead of 2.2e-4 of an output's size with the output's own rounding of 2.1e-4, and 82 us for 91 on two layers of
+            // 128 rows behind 16,384 tokens, 94 for 105 on twelve of 20, 256-wide, 26 for 28 on one.  The middles may be any size, and cancel: sums of p b
             // and p s take p in two binary16 terms.  All these sums share an accumulator, whose rows 4 k + g are group g's: k = 0 takes
             // sum 8 ps, 2 sum p b and 3 sum p s.
             // Matrix instructions cut off what lies too far below the exponent of their largest summand, and a subnormal operand
             // counts with the exponent of the smallest normal number: sum c ps falls short by 2^-19 of itself, about, while outputs
             // over many tokens are only some hundredths of it.  So the eight is a code as well, cut off alike (8,192 tokens, 256-wide
-            // heads: the error of the outputs goes from 3.0e-4 to 2.7e-4 of their size, of which 2.1e-4 is their own rounding).
+            // heads, p s in one term: the error of the outputs goes from 3.0e-4 to 2.7e-4 of their size).
             // scales of tokens 16 j + 4 qk + r, four tokens a read; of 256-wide heads two groups at a time, in front of their products
             // (sixteen registers fewer: the sums need not be moved out of the way, 108.0 -> 103.8 us for 12 layers of 20 rows)
             constexpr bool kPairs = GV == 4;
@@ -1068,58 +1088,52 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             auto read_codes = [&](int c) __attribute__((always_inline)) {
                 return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_int2_ptr)(uintptr_t)((va ^ (uint32_t)((c >> 1) << 4)) + (c & 1) * 8));
             };
-            // once with p s, and in a tile with wide groups again with what that rounding left
-            const int passes = two_terms ? 2 : 1;
-#pragma unroll 1
-            for (int pass = 0; pass < passes; ++pass) {
-                if (kPairs && __builtin_expect(pass > 0, 0)) read_pair(0);
-                int2_t words[2] = {read_codes(0), read_codes(1)}; // read two ahead of their use: left to itself, the compiler waits for each
+            int2_t words[2] = {read_codes(0), read_codes(1)}; // read two ahead of their use: left to itself, the compiler waits for each
 #pragma unroll
-                for (int g = 0; g < GV; ++g) {
-                    if (kTight) __builtin_amdgcn_sched_barrier(0);
-                    half8_t ps[CT][2];
-                    const uint32_t eight = col == g ? 0x00080008u : 0u, sixteen_times = col == g ? 0x00800080u : 0u;
-                    const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
+            for (int g = 0; g < GV; ++g) {
+                if (kTight) __builtin_amdgcn_sched_barrier(0);
+                half8_t ps[CT][2], rest[CT][2]; // p s in two binary16 terms
+                const uint32_t eight = col == g ? 0x00080008u : 0u, sixteen_times = col == g ? 0x00800080u : 0u;
+                const half8_t eights = words_to_half8(eight, sixteen_times, eight, sixteen_times);
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
+                for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t a[4];
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t a[4], b[4];
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const int at = r * GV + g;
-                                const uint32_t w0 = s4[2 * h][at / 2], w1 = s4[2 * h + 1][at / 2];
-                                const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
-                                a[r] = at & 1 ? product_upper<true>(product_lower<true>(p0, w0), p1, w1)
-                                              : product_upper<false>(product_lower<false>(p0, w0), p1, w1);
+                        for (int r = 0; r < 4; ++r) {
+                            const int at = r * GV + g;
+                            const uint32_t w0 = s4[2 * h][at / 2], w1 = s4[2 * h + 1][at / 2];
+                            const float p0 = z[ct][2 * h][r], p1 = z[ct][2 * h + 1][r];
+                            if (at & 1) {
+                                a[r] = product_upper<true>(product_lower<true>(p0, w0), p1, w1);
+                                b[r] = rest_upper<true>(rest_lower<true>(p0, w0, a[r]), p1, w1, a[r]);
+                            } else {
+                                a[r] = product_upper<false>(product_lower<false>(p0, w0), p1, w1);
+                                b[r] = rest_upper<false>(rest_lower<false>(p0, w0, a[r]), p1, w1, a[r]);
                             }
-                            if (__builtin_expect(pass > 0, 0)) {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) {
-                                    const int at = r * GV + g;
-                                    const float s0 = half_of(s4[2 * h][at / 2], at & 1), s1 = half_of(s4[2 * h + 1][at / 2], at & 1);
-                                    const half2_t v = bits_to_half2(a[r]);
-                                    a[r] = half2_to_bits(half2_t{(half_t)fmaf(z[ct][2 * h][r], s0, -(float)v[0]), (half_t)fmaf(z[ct][2 * h + 1][r], s1, -(float)v[1])});
-                                }
-                            }
-                            // the compiler does not see vector instructions in asm statements: the distance a matrix instruction may want
-                            asm("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
-                            ps[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
-                            pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, ps[ct][h], pbacc[ct], 0, 0, 0);
                         }
-                    if (kPairs && g % 2 == 1 && g + 1 < GV) read_pair(g + 1);
+                        // the compiler does not see vector instructions in asm statements: the distance a matrix instruction may want
+                        asm("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]), "+v"(b[2]), "+v"(b[3]));
+                        ps[ct][h] = words_to_half8(a[0], a[1], a[2], a[3]);
+                        rest[ct][h] = words_to_half8(b[0], b[1], b[2], b[3]);
+                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, ps[ct][h], pbacc[ct], 0, 0, 0);
+                        pbacc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eights, rest[ct][h], pbacc[ct], 0, 0, 0);
+                    }
+                if (kPairs && g % 2 == 1 && g + 1 < GV) read_pair(g + 1);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = 4 * g + k;
-                        const int2_t w = words[c % 2];
-                        if (c + 2 < 4 * GV) words[c % 2] = read_codes(c + 2);
-                        __builtin_amdgcn_sched_barrier(0);
-                        const half8_t a0 = code_operand((uint32_t)w.x), a1 = code_operand((uint32_t)w.y);
+                for (int k = 0; k < 4; ++k) {
+                    const int c = 4 * g + k;
+                    const int2_t w = words[c % 2];
+                    if (c + 2 < 4 * GV) words[c % 2] = read_codes(c + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                    const half8_t a0 = code_operand((uint32_t)w.x), a1 = code_operand((uint32_t)w.y);
 #pragma unroll
-                        for (int ct = 0; ct < CT; ++ct) {
-                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, ps[ct][0], acc[ct][c], 0, 0, 0);
-                            acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, ps[ct][1], acc[ct][c], 0, 0, 0);
-                        }
+                    for (int ct = 0; ct < CT; ++ct) {
+                        acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, ps[ct][0], acc[ct][c], 0, 0, 0);
+                        acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, ps[ct][1], acc[ct][c], 0, 0, 0);
+                        acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, rest[ct][0], acc[ct][c], 0, 0, 0);
+                        acc[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, rest[ct][1], acc[ct][c], 0, 0, 0);
                     }
                 }
             }
