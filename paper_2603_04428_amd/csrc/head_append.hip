@@ -274,14 +274,14 @@ __global__ __launch_bounds__(kThreads) void head_append_kernel(HeadAppendParams 
 #pragma unroll
         for (int i = 0; i < CPL; ++i) {
             const double f = front[i] ? inv : 1.0;
-            double g = 1.0; // a partner's factor over this one's
-            if constexpr (SPLIT) g = (partner_front[i] ? inv : 1.0) / f;
+            const double g = partner_front[i] ? inv : 1.0;
             half_t o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                double v = (double)xp[i][e];
-                if constexpr (SPLIT) v *= g;
-                o[e] = half_once(__builtin_fma(v, cb[i][e], x64[i][e] * ca[i][e]) * f);
+                const double v = (double)xp[i][e];
+                // where only one half of a pair is under the norm each factor goes to its own term: either may be zero
+                if constexpr (SPLIT) o[e] = half_once(__builtin_fma(v * g, cb[i][e], x64[i][e] * f * ca[i][e]));
+                else o[e] = half_once(__builtin_fma(v, cb[i][e], x64[i][e] * ca[i][e]) * f);
             }
             uint32_t out[4];
 #pragma unroll

@@ -253,3 +253,30 @@ def test_types_and_shapes_that_do_not_fit_are_refused():
     p.form.rot_dim = 32
     with pytest.raises(ValueError):
         call()
+
+
+@pytest.mark.parametrize("norm,rot", [(72, (16, 96)), (64, (32, 64)), (8, (0, 128))], ids=["inside", "half", "eight"])
+def test_zeros_under_a_norm_that_ends_inside_the_rotation_without_eps(norm, rot):
+    """Pairs with one half under the norm: a row of zeros stays zeros, and one that is zero under the norm alone keeps what the
+    rotation makes of the rest."""
+    p = Problem(1, 2, 2, 128, 128, False, (1, 2), 6, norm=norm, rot=rot, seed=9 + norm)
+    p.form.eps = p.f["eps"] = 0.0
+    for g, h in zip(p.g[:2], p.h[:2]):
+        g[:, :, 1], h[:, :, 1] = 0, 0
+        g[:, :, 3, :, :norm], h[:, :, 3, :, :norm] = 0, 0
+    p.f["eps"] = 1.0                                 # the zeros' rows: zero over any root
+    zeros = p.want_rows()
+    p.f["eps"] = 0.0
+    for x in p.h[:2]:
+        x[:, :, [1, 3]] = 1                          # any row: its place is taken below
+    q, k, v = p.want_rows()
+    for x, y in zip((q, k), zeros):
+        x[:, :, [1, 3]] = y[:, :, [1, 3]]
+    assert not q[:, :, 1].any() and q[:, :, 3].any()
+    q_out = p.call()
+    oracle.append(p.ospec, p.okp, p.ovp, k, v, p.table, p.before)
+    torch.cuda.synchronize()
+    assert np.array_equal(q_out.cpu().numpy(), q)    # (either zero)
+    assert np.array_equal(bits(p.kp.codes), p.okp.codes) and np.array_equal(bits(p.kp.scale), p.okp.scale)
+    got, want = bits(p.kp.bias), p.okp.bias
+    assert np.all((got == want) | ((got | want) == 0x8000))
