@@ -787,6 +787,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         // group sums of q
         half8_t qop[CT][GK][2];
         half4_t qsop[CT];
+        float sum_unit[CT]; // of the bias term: 2^-24, the unit of the products, times 2^6 for a row whose sums are taken down by that
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             n_row[ct] = plan.len[n_row[ct]];
@@ -811,13 +812,19 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 }
                 qs[g] = xor32_sum(xor16_sum(sum));
             }
+            // 64 finite values may sum up to 64 times the largest binary16 number; rows that stay below half of it keep their sums
+            float largest = 0.0f;
+#pragma unroll
+            for (int g = 0; g < GK; ++g) largest = fmaxf(largest, fabsf(qs[g]));
+            const float shrink = largest > 32768.0f ? 0x1p-6f : 1.0f;
+            sum_unit[ct] = largest > 32768.0f ? 0x1p-18f : 0x1p-24f;
             // contraction index of the bias term: with up to two groups high and low parts side by side in slot 0, else the
             // high parts in slot 0 and the low parts in slot 1
             half_t part[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int g = GK <= 2 ? e % GK : e;
-                const float v = g < GK && (GK > 2 || e < 2 * GK) ? qs[g < GK ? g : 0] : 0.0f;
+                const float v = g < GK && (GK > 2 || e < 2 * GK) ? qs[g < GK ? g : 0] * shrink : 0.0f;
                 const half_t hi = (half_t)v;
                 const bool low = GK <= 2 ? e >= GK : qk == 1;
                 const half_t value = low ? (half_t)(v - (float)hi) : hi;
@@ -924,7 +931,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 for (int ct = 0; ct < CT; ++ct) {
                     sum[ct] = __builtin_amdgcn_mfma_f32_16x16x16f16(bop, qsop[ct], zero, 0, 0, 0);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sum[ct][r] *= 0x1p-24f; // the products' unit
+                    for (int r = 0; r < 4; ++r) sum[ct][r] *= sum_unit[ct];
                 }
 #pragma unroll
                 for (int g = 0; g < GK; ++g) {

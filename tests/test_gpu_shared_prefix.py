@@ -333,3 +333,17 @@ def test_forked_agents_take_a_step():
         lens = [n + 1 for n in lens]
         want = oracle.attention(f.ospec, f.okp, f.ovp, qp.cpu().numpy(), table, lens, 0.09)
         f.check(out, want)
+
+
+@pytest.mark.parametrize("heads", [LLAMA, GEMMA, PER_HEAD, NARROW], ids=["128", "256", "192", "64"])
+@pytest.mark.parametrize("size", [800.0, 2000.0, 65504.0])
+def test_queries_whose_groups_sum_beyond_binary16(heads, size):
+    """Finite queries of any size: 64 of them sum up to 4.2 million.  Scores of ordinary size through the scale."""
+    f = Family(1, *heads, [(256, (5, 70)), (0, (9, 300, 1))], seed=20, fmt=sum(heads) % 2)
+    q = size * np.random.default_rng(21).uniform(0.6, 1.0, f.q.shape)
+    q[:, 1] = size                                   # the largest sum there is
+    q[:, 2] *= -1
+    q[:, 3, :, :, 64 % heads[2]:] *= 1e-4            # one large group beside small ones
+    f.q = q.astype(np.float16)
+    f.scale = 1.0 / (size * np.sqrt(heads[2]))
+    f.check(f.call())
