@@ -197,32 +197,22 @@ class HeadForm:
         self.norm_dim, self.q_weight, self.k_weight, self.eps = norm_dim, q_weight, k_weight, eps
         self.rot_begin, self.rot_dim, self.neighbours, self.cos, self.sin = rot_begin, rot_dim, neighbours, cos, sin
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        object.__setattr__(self, "_checked", None)          # (layers, struct) of the last call with these attributes
-
     def c(self, layers):
-        if self._checked is None or self._checked[0] != layers:
-            for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
-                if t is not None and tuple(t.shape) != (layers, self.norm_dim):
-                    raise ValueError(f"{name}: {tuple(t.shape)} instead of {(layers, self.norm_dim)}")
-            table_len = 0
-            if self.rot_dim:
-                if self.cos is None or self.sin is None or self.cos.shape != self.sin.shape or self.cos.dim() != 2 or \
-                        self.cos.shape[1] * 2 != self.rot_dim:
-                    raise ValueError(f"cos and sin: one shape, [positions][{self.rot_dim // 2}]")
-                table_len = self.cos.shape[0]
-            for name in ("q_weight", "k_weight", "cos", "sin"):
-                _dev(getattr(self, name), torch.float32, name)
-            object.__setattr__(self, "_checked", (layers, _CHeadForm(
-                norm_dim=self.norm_dim, eps=self.eps, rot_begin=self.rot_begin, rot_dim=self.rot_dim,
-                neighbours=1 if self.neighbours else 0, table_len=table_len)))
-        f = self._checked[1]                                # shapes are checked once; where the tensors lie is asked every time
-        f.q_weight = None if self.q_weight is None else self.q_weight.data_ptr()
-        f.k_weight = None if self.k_weight is None else self.k_weight.data_ptr()
-        f.cos_table = None if self.cos is None else self.cos.data_ptr()
-        f.sin_table = None if self.sin is None else self.sin.data_ptr()
-        return f
+        # everything is asked on every call: a tensor may change its shape, type or place (resize_, set_, .data) in between
+        q_weight, k_weight, cos, sin, table_len = self.q_weight, self.k_weight, self.cos, self.sin, 0
+        rows = layers, self.norm_dim
+        if q_weight is not None and q_weight.shape != rows:
+            raise ValueError(f"q_weight: {tuple(q_weight.shape)} instead of {rows}")
+        if k_weight is not None and k_weight.shape != rows:
+            raise ValueError(f"k_weight: {tuple(k_weight.shape)} instead of {rows}")
+        if self.rot_dim:
+            table = () if cos is None or sin is None else cos.shape
+            if len(table) != 2 or table[1] * 2 != self.rot_dim or sin.shape != table:
+                raise ValueError(f"cos and sin: one shape, [positions][{self.rot_dim // 2}]")
+            table_len = table[0]
+        f32 = torch.float32
+        return _CHeadForm(_dev(q_weight, f32, "q_weight"), _dev(k_weight, f32, "k_weight"), _dev(cos, f32, "cos"), _dev(sin, f32, "sin"),
+                          self.norm_dim, self.eps, self.rot_begin, self.rot_dim, 1 if self.neighbours else 0, table_len)
 
 
 class BlockPool:

@@ -170,3 +170,48 @@ def test_pools_of_another_spec_are_refused():
     ids = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError, match="pool"):
         b.q4kv_copy_blocks(other, k, v, ids, ids)
+
+
+class _SaysGpu(torch.Tensor):  # a CPU tensor that says it lies on the GPU; only its address is taken
+    @property
+    def is_cuda(self):
+        return True
+
+
+def _says_gpu(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(_SaysGpu)
+
+
+def test_a_head_form_looks_at_its_tensors_in_every_call():
+    """Weights and tables that change their shape, type or place behind a form's back: what the last call found is not kept."""
+    def form():
+        return b.HeadForm(norm_dim=64, q_weight=_says_gpu(2, 64), k_weight=_says_gpu(2, 64), rot_dim=64, cos=_says_gpu(100, 32), sin=_says_gpu(100, 32))
+
+    f = form()
+    c = f.c(2)
+    assert c.table_len == 100 and c.cos_table == f.cos.data_ptr() and c.q_weight == f.q_weight.data_ptr() and c.norm_dim == 64
+    f.cos.resize_(40, 32)
+    f.sin.resize_(40, 32)
+    assert f.c(2).table_len == 40                    # shorter tables: positions from 40 on are skipped, not read
+    f.sin.resize_(30, 32)
+    with pytest.raises(ValueError, match="cos and sin"):
+        f.c(2)
+    for name in ("q_weight", "k_weight"):
+        f = form()
+        f.c(2)
+        getattr(f, name).resize_(1, 64)
+        with pytest.raises(ValueError, match=name):
+            f.c(2)
+    for name in ("q_weight", "k_weight", "cos", "sin"):
+        f = form()
+        f.c(2)
+        was = getattr(f, name)
+        was.data = torch.zeros(was.shape, dtype=torch.float64).as_subclass(_SaysGpu)
+        with pytest.raises(TypeError, match=name):
+            f.c(2)
+        f = form()
+        f.c(2)
+        t = getattr(f, name)
+        t.set_(torch.zeros(t.shape[::-1]).t())       # the same shape, no longer contiguous
+        with pytest.raises(TypeError, match=name):
+            f.c(2)
