@@ -406,6 +406,8 @@ def _token_rows(t, heads, dim, name):
     if len(shape) != 5 or shape[3] != heads or shape[4] != dim or not t.is_cuda:
         raise TypeError(f"{name}: need [layers][agents][chunk][{heads}][{dim}] on the GPU, got {tuple(shape)} on {t.device}")
     s0, s1, s2, s3, s4 = t.stride()
+    if 0 in shape[:3]:                    # no tokens: nothing is a stride apart
+        return heads * dim
     # the stride of an axis of one element means nothing: the last axis that has more gives the distance of two tokens
     stride, rows = None, 1
     for size, step in ((shape[2], s2), (shape[1], s1), (shape[0], s0)):

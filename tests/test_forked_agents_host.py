@@ -215,3 +215,10 @@ def test_a_head_form_looks_at_its_tensors_in_every_call():
         t.set_(torch.zeros(t.shape[::-1]).t())       # the same shape, no longer contiguous
         with pytest.raises(TypeError, match=name):
             f.c(2)
+
+
+@pytest.mark.parametrize("lead", [(1, 2, 0), (2, 1, 0), (3, 0, 5), (3, 0, 0), (0, 2, 0), (0, 2, 5), (1, 1, 0), (2, 0, 1)])
+def test_projections_of_no_tokens_have_strides_too(lead):
+    assert b._token_rows(_says_gpu(*lead, 2, 64), 2, 64, "x") == 128
+    part = _says_gpu(*lead, 512)[..., 128:256].unflatten(-1, (2, 64))
+    assert b._token_rows(part, 2, 64, "x") == 128

@@ -280,3 +280,13 @@ def test_zeros_under_a_norm_that_ends_inside_the_rotation_without_eps(norm, rot)
     assert np.array_equal(bits(p.kp.codes), p.okp.codes) and np.array_equal(bits(p.kp.scale), p.okp.scale)
     got, want = bits(p.kp.bias), p.okp.bias
     assert np.all((got == want) | ((got | want) == 0x8000))
+
+
+@pytest.mark.parametrize("layers,agents,tokens", [(2, 2, 0), (2, 0, 4), (0, 2, 4), (0, 0, 0), (2, 1, 0)])
+def test_a_call_of_no_tokens_does_nothing(layers, agents, tokens):
+    p = Problem(2, 4, 2, 128, 128, False, (3, 300), 4, norm=128, rot=(0, 128), seed=10)
+    p.L, p.g = layers, [t[:layers, :agents, :tokens] for t in p.g]
+    p.form.q_weight = p.form.k_weight = p.form.q_weight[:layers]
+    assert p.call(table=p.table[:agents], before=p.before[:agents]).shape == (layers, agents, tokens, 4, 128)
+    torch.cuda.synchronize()
+    p.check_pools()
