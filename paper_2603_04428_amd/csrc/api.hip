@@ -533,8 +533,11 @@ int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, cons
         return fail(Q4KV_EINVAL, "NULL pointer");
     if (!aligned16(q) || !aligned16(out)) return fail(Q4KV_EINVAL, "q and out must be 16-byte aligned");
     const int layers = layer_end - layer_begin;
-    if (q4kv::prefix_tiles(*spec, num_agents, num_groups, max_seq_len, layers) > 0x7fffffffLL)
-        return fail(Q4KV_ERANGE, "more than 2^31 tiles in one call: split the layer range");
+    // the plan's quotients are exact up to 2^21 (layer, KV head) pairs; its places are int, and the last worker's range may end some
+    // thousand tiles behind the last
+    if ((int64_t)layers * spec->num_kv_heads > (1 << 21) - 1 ||
+        q4kv::prefix_tiles(*spec, num_agents, num_groups, max_seq_len, layers) > 0x7fff0000LL)
+        return fail(Q4KV_ERANGE, "close to 2^31 tiles or more, or 2^21 layers and KV heads, in one call: split the layer range");
     if ((int64_t)layers * num_agents * spec->num_q_heads > 0x7fffffffLL)
         return fail(Q4KV_ERANGE, "more rows than a launch can have: split the layer range");
     size_t acc_at, ml_at;

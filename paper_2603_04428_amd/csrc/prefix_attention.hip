@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "q4_device.h"
+#include "prefix_plan.h"
 #include "q4kv_internal.h"
 
 namespace q4kv {
@@ -34,12 +35,10 @@ namespace {
 template <int V> struct Int { static constexpr int value = V; };
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kWaves = kPlanWaves;
+static_assert(kWaves == kThreads / kWave, "the plan counts four waves a workgroup");
 constexpr int kCols = 16;          // query rows of a column tile
 constexpr int kMaxAgents = 512;    // agents of a call: their lengths and tile counts are kept in LDS
-constexpr int kSoloTiles = 2;      // smallest range of a wave on its own
-constexpr int kPart = 3, kJoin = 1; // in tiles' time: see spread()
-constexpr int kJoinBelow = 16;     // tiles per wave from which workgroups are not considered
 constexpr float kNegBig = -1.0e30f; // "minus infinity" that survives subtraction
 constexpr float kLog2e = 1.4426950408889634f;
 // Largest value scales (binary16 bits) with which probabilities may reach 2^15 and 2^7: their products stay below 65504.
@@ -143,54 +142,6 @@ __device__ __forceinline__ int lane_last_at_most(const int *pre, int count, int 
     return lo;
 }
 
-
-// n / d for 0 <= n < 2^31, 0 < d and a quotient below 2^21: the product with the reciprocal errs by less than one
-__device__ __forceinline__ int quotient(int n, int d)
-{
-    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
-    const int r = n - q * d;
-    q += r < 0 ? -1 : (r >= d ? 1 : 0);
-    return q;
-}
-
-// (v below 2^21 * round)
-__device__ __forceinline__ int rounded_up(int v, int round) { return round == 1 ? v : quotient(v + round - 1, round) * round; }
-
-// How the tiles of a call are dealt out: `per` tiles a worker, units counted as the next multiple of `round`; true: the waves are
-// the workers, else the workgroups, whose waves take a range tile by tile in turn.  `total`: tiles of the call, `units`: units that
-// have any, padded(r): the tiles with every unit's rounded up to r.
-// A worker pays for every part of a unit it begins (block ids, first tiles, queries: kPart tiles' time), so units are
-// cut into ranges of their own that are equally long but for each unit's last, if there are workers enough for them all and the
-// ranges are not much longer for it.  A workgroup as a worker joins its waves' sums in LDS (kJoin tiles' time) and leaves one
-// record instead of four.  Else every wave takes an equal range wherever it begins.  Measured (us; only workgroups or, from 16 tiles a
-// wave on, waves with ranges anywhere / as here): 128-wide, ten agents behind 4,096, four layers 50.2 / 37.9; 64-wide, 14 behind 5,376,
-// eleven layers 47.0 / 29.7; 192 + 128, eight behind 2,048, three layers 38.8 / 27.9; 256-wide, 40 behind 1,024 46.4 / 35.3, ten behind
-// 8,192 27.9 / 27.8.  Ranges of their own whatever their length: 32 agents of 128-wide heads behind 16,384, two layers 82 -> 104.
-template <typename F>
-__device__ __forceinline__ bool spread(int total, int units, int workgroups, int &per, int &round, F padded)
-{
-    auto fit = [&](int workers, int step) { // the shortest range, a multiple of `step`; 0: none
-        if (units > workers) return 0;
-        int r = rounded_up(quotient(total, workers - units / 2) + 1, step); // a unit's last range is half empty, about
-#pragma unroll 1
-        for (int k = 0; k < 4; ++k, r += max(step, r / 8 / step * step))
-            if (padded(r) <= (long long)r * workers) return r;
-        return 0;
-    };
-    const int waves = workgroups * kWaves, even = max(kSoloTiles, quotient(total + waves - 1, waves));
-    // an equal range wherever it begins: some wave has a unit's beginning more than the average
-    const int anywhere = even + kPart + quotient(kPart * units, waves);
-    int alone = fit(waves, 1);
-    if (alone > anywhere) alone = 0;
-    const int best = alone > 0 ? alone : anywhere, together = even <= kJoinBelow ? fit(workgroups, kWaves) : 0;
-    if (together > 0 && together <= kWaves * (best + kJoin)) {
-        per = round = together;
-        return false;
-    }
-    per = alone > 0 ? max(alone, kSoloTiles) : even;
-    round = alone > 0 ? per : 1;
-    return true;
-}
 
 // What a lane reads for the plan of up to 64 agents: lane a of agent a, lane g of group g.
 struct PlanInputs {
@@ -688,7 +639,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
     if (p.num_agents <= kWave) make_plan_few(p, plan_in, lane, wave, plan);
     else make_plan_many(p, plan);
     const int per = uniform(plan.per), round = uniform(plan.round);
-    const int total = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]) * p.kv_heads * p.layers; // the host keeps it below 2^31
+    const int total = uniform(plan.group[p.num_groups] + plan.own[p.num_agents]) * p.kv_heads * p.layers; // below 2^31: see spread()
     const bool solo = uniform(plan.solo) != 0;
     if (blockIdx.x == 0) write_plan(p, plan);
     const int worker = solo ? (int)blockIdx.x * kWaves + wave : (int)blockIdx.x;

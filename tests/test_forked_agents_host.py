@@ -222,3 +222,17 @@ def test_projections_of_no_tokens_have_strides_too(lead):
     assert b._token_rows(_says_gpu(*lead, 2, 64), 2, 64, "x") == 128
     part = _says_gpu(*lead, 512)[..., 128:256].unflatten(-1, (2, 64))
     assert b._token_rows(part, 2, 64, "x") == 128
+
+
+def test_shared_prefix_calls_that_outgrow_the_plan_are_refused():
+    """Fake pointers and a workspace of no bytes: what is not refused for its size ends at the workspace (-4), nothing is launched."""
+    def call(spec, A, mb, msl, layers):
+        return b.lib().q4kv_shared_prefix_attention(C.byref(spec), C.byref(_pool()), C.byref(_pool()), 0x4000, 0x5000, 0x6000, mb, 0x7000, A, None, None, 0,
+                                                    msl, 0.1, 0, layers, 0xA000, 0, None)
+
+    one = b.make_spec(1, 1, 1, 64)                                   # a tile per agent and row tile and 64 tokens: (A + ceil(A / 16))
+    assert call(one, 60, 1 << 23, 0x7fff0000 // 64 * 64, 1) == -4
+    assert call(one, 60, 1 << 23, 0x7fff0000, 1) == -4 and call(one, 61, 1 << 23, 0x7fff0000, 1) == -3 and "tiles" in _err()
+    pairs = b.make_spec(1 << 20, 2, 2, 64)
+    assert call(pairs, 1, 1, 64, (1 << 20) - 1) == -4 and call(pairs, 1, 1, 64, 1 << 20) == -3 and "2^21" in _err()
+    assert call(b.make_spec(1 << 30, 1 << 16, 1 << 16, 64), 512, 1 << 23, 0x7fffffff, 1 << 30) == -3
