@@ -538,8 +538,9 @@ int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, cons
     if ((int64_t)layers * spec->num_kv_heads > (1 << 21) - 1 ||
         q4kv::prefix_tiles(*spec, num_agents, num_groups, max_seq_len, layers) > 0x7fff0000LL)
         return fail(Q4KV_ERANGE, "close to 2^31 tiles or more, or 2^21 layers and KV heads, in one call: split the layer range");
-    if ((int64_t)layers * num_agents * spec->num_q_heads > 0x7fffffffLL)
-        return fail(Q4KV_ERANGE, "more rows than a launch can have: split the layer range");
+    // the join of the records is a launch of 256 threads a row, below 2^32 in all
+    if ((int64_t)layers * num_agents * spec->num_q_heads > (1 << 24) - 1)
+        return fail(Q4KV_ERANGE, "2^24 rows or more in one call: split the layer range");
     size_t acc_at, ml_at;
     const size_t need = q4kv::prefix_workspace_bytes(*spec, num_agents, max_seq_len, layers, compute_units(), acc_at, ml_at);
     if (!workspace || workspace_bytes < need || !aligned16(workspace))

@@ -236,3 +236,14 @@ def test_shared_prefix_calls_that_outgrow_the_plan_are_refused():
     pairs = b.make_spec(1 << 20, 2, 2, 64)
     assert call(pairs, 1, 1, 64, (1 << 20) - 1) == -4 and call(pairs, 1, 1, 64, 1 << 20) == -3 and "2^21" in _err()
     assert call(b.make_spec(1 << 30, 1 << 16, 1 << 16, 64), 512, 1 << 23, 0x7fffffff, 1 << 30) == -3
+
+
+def test_shared_prefix_calls_of_more_rows_than_a_launch_has_are_refused():
+    """2^24 workgroups of 256 threads are more than a launch takes: found in front of the first kernel."""
+    def call(A, layers):
+        spec = b.make_spec(4096, 8, 1, 64)
+        return b.lib().q4kv_shared_prefix_attention(C.byref(spec), C.byref(_pool()), C.byref(_pool()), 0x4000, 0x5000, 0x6000, 1, 0x7000, A, None, None, 0,
+                                                    64, 0.1, 0, layers, 0xA000, 0, None)
+
+    assert call(511, 4096) == -4 and call(512, 4095) == -4                      # the workspace of no bytes
+    assert call(512, 4096) == -3 and "2^24 rows" in _err()
