@@ -45,11 +45,14 @@ struct q4kv_block_pool {
         --free_count;
         return id;
     }
-    // One agent fewer lists the block (its list no longer holds it); 1 when that freed it.
+    // One agent fewer lists the block (its list no longer holds it); 1 when that freed it.  settle() follows the last one.
     int32_t drop(int32_t id, int64_t agent_id)
     {
         if (--refs[(size_t)id] > 0) {
-            if (owner[(size_t)id] == agent_id) owner[(size_t)id] = smallest_lister(id);
+            if (owner[(size_t)id] == agent_id) {
+                owner[(size_t)id] = INT64_MAX;
+                unsettled = true;
+            }
             return 0;
         }
         owner[(size_t)id] = -1;
@@ -58,18 +61,16 @@ struct q4kv_block_pool {
         ++free_count;
         return 1;
     }
-    int64_t smallest_lister(int32_t id) const
+    // The smallest lister of every block whose own has left it: one pass over all lists, however many blocks these are.
+    void settle()
     {
-        int64_t found = -1;
+        if (!unsettled) return;
+        unsettled = false;
         for (const auto &kv : agents)
-            if (found < 0 || kv.first < found)
-                for (int32_t b : kv.second.blocks)
-                    if (b == id) {
-                        found = kv.first;
-                        break;
-                    }
-        return found;
+            for (int32_t id : kv.second.blocks)
+                if (kv.first < owner[(size_t)id]) owner[(size_t)id] = kv.first;
     }
+    bool unsettled = false;
 };
 
 namespace {
@@ -130,6 +131,7 @@ int32_t q4kv_block_pool_release(q4kv_block_pool *pool, int64_t agent_id)
         pool->agents.erase(it);
         int32_t n = 0;
         for (int32_t id : blocks) n += pool->drop(id, agent_id);
+        pool->settle();
         return n;
     } catch (...) { // the free list had no room to grow: it never holds more than it did at the start
         return Q4KV_ENOSPACE;
@@ -271,6 +273,7 @@ int32_t q4kv_block_pool_truncate(q4kv_block_pool *pool, int64_t agent_id, int64_
             blocks.back() = *copy_to = pool->take(agent_id);
             pool->drop(*copy_from, agent_id);
         }
+        pool->settle();
         it->second.stamp = ++pool->clock;
         return (int32_t)blocks.size();
     } catch (...) {

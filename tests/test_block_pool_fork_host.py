@@ -1,6 +1,7 @@
 """Forking, truncating and compacting agents in the host-side block pool, against a plain Python model and against what
 sharing must keep: a block that several agents list is full of tokens that all of them have.  No GPU needed."""
 import random
+import time
 
 import pytest
 
@@ -182,3 +183,23 @@ def test_random_operations_against_a_model():
         for blk in range(N):
             users = [k for k, v in lists.items() if blk in v]
             assert p.shares(blk) == len(users) and p.owner(blk) == (min(users) if users else -1)
+
+
+def test_a_crowd_that_shares_a_long_prompt_leaves_one_by_one():
+    """512 agents behind 131,072 tokens: who owns the blocks is found in one pass over the lists per agent that leaves, not one
+    per block (9 s in all, 20 ms a release under the pool's lock)."""
+    A, N = 512, 512
+    p = b.BlockPool(N + 2)
+    p.reserve(0, N * 256)
+    for a in range(1, A):
+        p.fork(0, a, N * 256)
+    t = time.monotonic()
+    for a in range(A - 1):
+        if a % 100 == 50:
+            assert p.truncate(a, 256 * 200 + 1) == [(200, N)] and p.owner(200) == p.owner(N - 1) == a + 1 and p.owner(0) == a
+            assert p.release(a) == 1
+        else:
+            assert p.release(a) == 0
+        assert p.owner(0) == p.owner(N - 1) == a + 1 and p.shares(7) == A - 1 - a
+    assert time.monotonic() - t < 5
+    assert p.release(A - 1) == N and p.free_blocks() == N + 2
