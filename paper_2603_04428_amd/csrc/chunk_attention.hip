@@ -238,20 +238,6 @@ __device__ __forceinline__ half2_t nibbles_hi16(uint32_t w) // 16 * code
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t *lds_short4_ptr;
 
-// x[i] (op) x[i ^ 32] without touching LDS
-__device__ __forceinline__ float xor32_max(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float xor32_sum(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-
 // Four normalised values of one query row at positions 8 j + 4 h .. + 3 of an 8-dim word of V_hat (h = lane / 32):
 // dims (0,4,1,5) in the lower half of the wave, (2,6,3,7) in the upper.  The halves trade pairs, after which each
 // lane holds four consecutive dims: 0..3 below, 4..7 above.
@@ -508,7 +494,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_attention_kernel(Chunk
             }
         };
         // a code word as the A operand of a matrix instruction: the nibbles masked in place are binary16 subnormals
-        // c 2^-24 (dims 0, 4, 2, 6 of the word) and 16 c 2^-24 (dims 1, 5, 3, 7)
+        // c 2^-24 (dims 0, 4, 2, 6 of the word) and 16 c 2^-24 (dims 1, 5, 3, 7).  (Calling the function of q4_device.h gives the kernel
+        // another order of instructions than the one that was measured.)
         auto code_operand = [&](uint32_t w) __attribute__((always_inline)) {
             const uint32_t w8 = w >> 8;
             return __builtin_bit_cast(half8_t, make_uint4(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u));

@@ -76,31 +76,6 @@ struct MlaParams {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// x[i] (op) x[i ^ 16], x[i] (op) x[i ^ 32] without touching LDS
-__device__ __forceinline__ float xor16_max(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float xor32_max(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float xor16_sum(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-__device__ __forceinline__ float xor32_sum(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
 // the value lane i ^ 16 holds
 __device__ __forceinline__ float xor16_other(float x, bool odd_row)
 {
@@ -113,17 +88,6 @@ __device__ __forceinline__ float xor16_other(float x, bool odd_row)
 // sets turn the slots round by one, so that the 16 rows a transposing read takes for one slot (all j and r) lie two by two
 // in 8 bank groups (the row pitch is 8 banks modulo 64) instead of four by four in 4.
 __device__ __forceinline__ constexpr int slot_token(int q, int j, int r) { return 16 * j + 4 * ((q + (j & 1)) & 3) + r; }
-
-__device__ __forceinline__ half8_t words_to_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    return __builtin_bit_cast(half8_t, make_uint4(a, b, c, d));
-}
-
-__device__ __forceinline__ half8_t code_operand(uint32_t w)
-{
-    const uint32_t w8 = w >> 8;
-    return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
-}
 
 typedef int int2_t __attribute__((ext_vector_type(2)));
 typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));

@@ -142,7 +142,6 @@ __device__ __forceinline__ int lane_last_at_most(const int *pre, int count, int 
     return lo;
 }
 
-
 // What a lane reads for the plan of up to 64 agents: lane a of agent a, lane g of group g.
 struct PlanInputs {
     int len, prefix, bound, last;
@@ -349,17 +348,6 @@ __device__ __forceinline__ void write_plan(const PrefixParams &p, const Plan &pl
 
 // ---------------------------------------------------------------------------------------------- tiles in LDS
 
-__device__ __forceinline__ half8_t words_to_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    return __builtin_bit_cast(half8_t, make_uint4(a, b, c, d));
-}
-
-__device__ __forceinline__ half8_t code_operand(uint32_t w)
-{
-    const uint32_t w8 = w >> 8;
-    return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
-}
-
 __device__ __forceinline__ float half_of(uint32_t pair, int hi)
 {
     return half_bits_to_float((uint16_t)(hi ? pair >> 16 : pair & 0xffffu));
@@ -407,31 +395,6 @@ __device__ __forceinline__ uint32_t remainder_of(uint32_t hi, float p0, float p1
     asm("v_fma_mixlo_f16 %0, %1, %3, -%4 op_sel_hi:[0,0,1]\n\tv_fma_mixhi_f16 %0, %2, %3, -%4 op_sel:[0,0,1] op_sel_hi:[0,0,1]"
         : "=&v"(d) : "v"(p0), "v"(p1), "s"(f), "v"(hi));
     return d;
-}
-
-__device__ __forceinline__ float xor16_max(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float xor32_max(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float xor16_sum(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-__device__ __forceinline__ float xor32_sum(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
 // Code rows of one width in LDS: UNITS chunks of 16 bytes per row, chunk c of token t at place c ^ swizzle(t).  A row is 8, 16,
@@ -694,13 +657,13 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
         // still be on their way; loads complete in order.
         constexpr int K_LOADS = Rows<DK>::LOADS, V_LOADS = Rows<DV>::LOADS, ALL = K_LOADS + V_LOADS + S::PARAM_LOADS;
         auto wait_scores = [&](int ahead) __attribute__((always_inline)) { // K and parameters of the current tile
-            if (S::RING >= 4 && ahead >= 3) wait_for_all_but<(V_LOADS + 3 * ALL > 63 ? 0 : V_LOADS + 3 * ALL)>();
+            if (S::RING >= 4 && ahead >= 3) wait_for_all_but<V_LOADS + 3 * ALL>();
             else if (S::RING >= 3 && ahead >= 2) wait_for_all_but<V_LOADS + 2 * ALL>();
             else if (ahead >= 1) wait_for_all_but<V_LOADS + ALL>();
             else wait_for_all_but<V_LOADS>();
         };
         auto wait_values = [&](int ahead) __attribute__((always_inline)) { // V of the current tile; K of RING tiles on may have been asked for
-            if (S::RING >= 4 && ahead >= 4) wait_for_all_but<(3 * ALL + K_LOADS > 63 ? 0 : 3 * ALL + K_LOADS)>();
+            if (S::RING >= 4 && ahead >= 4) wait_for_all_but<3 * ALL + K_LOADS>();
             else if (S::RING >= 4 && ahead >= 3) wait_for_all_but<3 * ALL>();
             else if (S::RING == 3 && ahead >= 3) wait_for_all_but<2 * ALL + K_LOADS>();
             else if (S::RING >= 3 && ahead >= 2) wait_for_all_but<2 * ALL>();

@@ -61,6 +61,18 @@ __device__ __forceinline__ CodePairs unpack_codes(uint32_t w)
     return p;
 }
 
+__device__ __forceinline__ half8_t words_to_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_bit_cast(half8_t, make_uint4(a, b, c, d));
+}
+
+// The four pairs of unpack_codes() as an operand of a matrix instruction: codes 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ half8_t code_operand(uint32_t w)
+{
+    const uint32_t w8 = w >> 8;
+    return words_to_half8(w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u);
+}
+
 // On a compute unit the oldest wave wins every arbitration (also the one for the memory pipeline), so of the
 // workgroups a grid-striding launch stacks on a compute unit the ones launched first run ahead, finish first and
 // leave the last generation to stream alone at the end.  A kernel that calls this once per loop iteration hands
@@ -151,6 +163,32 @@ __device__ __forceinline__ void wave_sum_n(float (&v)[N])
         asm("s_nop 4\n\t" Q4KV_WAVE_STEPS(Q4KV_ADD_DPP3) : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]));
     else
         asm("s_nop 4\n\t" Q4KV_WAVE_STEPS(Q4KV_ADD_DPP5) : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]));
+}
+
+// x[i] (op) x[i ^ 16], x[i] (op) x[i ^ 32] without touching LDS
+__device__ __forceinline__ float xor16_max(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float xor32_max(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float xor16_sum(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float xor32_sum(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
 } // namespace q4kv
