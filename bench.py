@@ -33,27 +33,27 @@ HBM_PEAK_GBPS = 8000.0   # MI355X published HBM3E bandwidth
 # `--print-sources-hash` prints the current hash of every set of files named here).
 DECODE_FILES = ("decode_attention.hip", "stream_k.h", "q4_device.h", "q4kv_internal.h")
 LATENT_FILES = ("mla_decode.hip", "stream_k.h", "q4_device.h", "q4kv_internal.h")
-CODEC_FILES = ("codec.hip", "q4_device.h", "q4kv_internal.h")
+CODEC_FILES = ("codec.hip", "quantize_octet.h", "q4_device.h", "q4kv_internal.h")
 CHUNK_FILES = ("chunk_attention.hip", "chunk_rules.h", "q4_device.h", "q4kv_internal.h")
 MEASURED_TRAFFIC = {
     "gemma12b_10agents_48layers_ragged_1k_8k_decode": {
-        "read": 4786905372, "written": 20898816, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": DECODE_FILES, "sources": "d96d8a094186"},
+        "read": 4786221758, "written": 20898816, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": DECODE_FILES, "sources": "f7aec25374b9"},
     "llama8b_5agents_32layers_4k_decode": {
-        "read": 767897678, "written": 8134656, "file": "profiles/decode_attention_llama8b_5x4k.md",
-        "files": DECODE_FILES, "sources": "d96d8a094186"},
+        "read": 767855100, "written": 8134656, "file": "profiles/decode_attention_llama8b_5x4k.md",
+        "files": DECODE_FILES, "sources": "f7aec25374b9"},
     "dsv2lite_mla_per_head_5agents_27layers_8k_decode": {
-        "read": 3190045245, "written": 2958848, "file": "profiles/decode_attention_mla_per_head_5x8k.md",
-        "files": DECODE_FILES, "sources": "d96d8a094186"},
+        "read": 3190043027, "written": 2958848, "file": "profiles/decode_attention_mla_per_head_5x8k.md",
+        "files": DECODE_FILES, "sources": "f7aec25374b9"},
     "dsv2lite_mla_latent_5agents_27layers_32k_decode": {
-        "read": 1442820110, "written": 37895622, "file": "profiles/mla_decode_dsv2lite_5x32k.md",
-        "files": LATENT_FILES, "sources": "3aeca27a0fd8"},
+        "read": 1442821165, "written": 37889439, "file": "profiles/mla_decode_dsv2lite_5x32k.md",
+        "files": LATENT_FILES, "sources": "3998b41874f3"},
     "quantize_4k_cache": {
-        "read": 1610807914, "written": 452984832, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": CODEC_FILES, "sources": "ef1468fd419e"},
+        "read": 1610806109, "written": 452984832, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": CODEC_FILES, "sources": "3ae135dcacab"},
     "dequantize_4k_cache": {
-        "read": 453042913, "written": 1610616730, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": CODEC_FILES, "sources": "ef1468fd419e"},
+        "read": 453040946, "written": 1610613219, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": CODEC_FILES, "sources": "3ae135dcacab"},
 }
 
 
