@@ -134,8 +134,8 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
  *             [table_len][rot_dim / 2]) for the n-th pair: n and n + rot_dim / 2 inside the span, or with `neighbours` != 0
  *             2n and 2n + 1.  rot_dim == 0: none, the tables are not read.
  * norm_dim and rot_begin are multiples of 8, rot_dim of 16, both spans lie inside k_dim and may overlap; weights and tables
- * are 16-byte aligned.  Results are those of binary64 arithmetic rounded once to binary16 (but for a result within about
- * 2^-48 of itself of a rounding border); a row of zeros stays zeros whatever eps is. */
+ * are 16-byte aligned.  Results are those of binary64 arithmetic rounded once to binary16 (but for one within 2^-48 of
+ * |y_i c| + |y_j s| of a rounding border); where the elements under the norm are all zero they stay zeros whatever eps is. */
 typedef struct {
     const float *q_weight, *k_weight;
     const float *cos_table, *sin_table;
@@ -168,7 +168,8 @@ int q4kv_norm_rope_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_
 /* Sec. 3.4, second half of update_and_fetch, and Sec. 3.6 (GQA grouping, causal chunk masks):
  * out = softmax(sm_scale * q K_hat^T) V_hat per agent, layer and query head, directly on the Q4
  * pools (nothing is dequantized to memory).
- *   q            device, [layer_end-layer_begin][num_agents][q_len][num_q_heads][k_dim] binary16
+ *   q            device, [layer_end-layer_begin][num_agents][q_len][num_q_heads][k_dim] binary16.  With q_len > 1 and on a
+ *                shared latent no 64 elements of a group may sum up to more than 65504 (plain decode has no such bound)
  *   out          device out, same leading shape, v_dim wide, binary16
  *   seq_len      device int32 [num_agents]: keys visible to the LAST query row of each agent, the
  *                appended chunk included; row r sees the first seq_len[a] - (q_len-1-r) tokens
@@ -243,8 +244,11 @@ int q4kv_batched_attention_planned(const q4kv_spec *spec, const q4kv_pool *k, co
                                    void *hip_stream);
 
 /* Decode attention (q_len == 1) of agents that share prefixes: q4kv_batched_attention on global layers, with the tokens that
- * a group of agents has in common read once for all of them (Sec. 3.4, the decode loop of a batch; q4kv_block_pool_fork makes such
- * agents).  With ten agents behind a common prompt of 8,192 tokens the cache that a step reads is a seventh.
+ * a group of agents has in common read once for up to 32 of its query rows on a KV head, 48 with 64-wide heads (Sec. 3.4, the decode
+ * loop of a batch; q4kv_block_pool_fork makes such agents).  With ten agents of two query heads per KV head behind a common prompt of
+ * 8,192 tokens the cache that a step reads is a seventh.  The plain calls read shared blocks correctly too, once per agent: next to
+ * q4kv_batched_attention_planned, one layer a call, this one is the faster from four agents and about 4,096 shared tokens on, and
+ * the slower below 1,024.
  *   group_begin  device int32 [num_groups + 1]: group g is agents group_begin[g] .. group_begin[g + 1] - 1; ascending.  Agents
  *                outside all groups share nothing.  Bounds that fall are read as the largest one in front of them, and bounds
  *                outside [0, num_agents] as the nearest in it.
@@ -255,9 +259,10 @@ int q4kv_batched_attention_planned(const q4kv_spec *spec, const q4kv_pool *k, co
  *   num_groups   0: nobody shares anything, the two arrays may be NULL.  No more than num_agents
  *   workspace    device scratch of at least q4kv_shared_prefix_workspace_bytes(...) bytes, 16-byte aligned; contents before and
  *                after the call are unspecified.  Calls that overlap in time need one each.
- * All other arguments, block ids outside the pool, rows that see no token (zeros) and run-to-run identical bits as for
- * q4kv_batched_attention; the order of a row's sum is another one, so the bits are in general not that call's.  At most 512
- * agents (more -> Q4KV_ERANGE).  Head shapes: k_dim == v_dim of 64, 128 or 256, or 192 and 128; at most 16 query heads per KV
+ * All other arguments, block ids outside the pool (masked; the loads go to block 0 and are discarded), rows that see no token (zeros)
+ * and run-to-run identical bits as for q4kv_batched_attention; the order of a row's sum is another one, so the bits are in general
+ * not that call's.  Q4KV_ERANGE: more than 512 agents; 2^24 (layer, agent, query head) rows or 2^21 (layer, KV head) pairs and more;
+ * tiles of 64 tokens (layers * KV heads * (agents + row tiles) * max_seq_len / 64) close to 2^31 and more.  Head shapes: k_dim == v_dim of 64, 128 or 256, or 192 and 128; at most 16 query heads per KV
  * head; no shared latent (Q4KV_ESHAPE). */
 int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const uint16_t *q,
                                  uint16_t *out, const int32_t *block_table, int32_t max_blocks, const int32_t *seq_len,
@@ -265,7 +270,11 @@ int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, cons
                                  int32_t num_groups, int32_t max_seq_len, float sm_scale, int32_t layer_begin,
                                  int32_t layer_end, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Bytes of workspace q4kv_shared_prefix_attention needs for these arguments, whatever the groups.  0 on bad arguments. */
+/* Bytes of workspace q4kv_shared_prefix_attention needs for these arguments, whatever the groups.  0 on bad arguments.  A row (layer,
+ * agent, query head) may leave a record of v_dim + 2 binary32 values per range of 128 tokens and more, but no more than
+ * 1,024 / (layers * KV heads) + 2 of its prefix and as many of its own tokens (256 compute units): 24 MB for one layer of ten
+ * agents of 9,000 tokens with 32 query and 8 KV heads, 128-wide, 141 MB for two of 32 behind 16,384, 2.2 GB for one of 512
+ * agents and 131,072. */
 size_t q4kv_shared_prefix_workspace_bytes(const q4kv_spec *spec, int32_t num_agents, int32_t max_seq_len,
                                           int32_t num_layers_in_call);
 

@@ -9,8 +9,8 @@
 // What bounds it is memory: 2 bytes in per element of Q, K and V, 2 out for Q and 0.5625 for K and V.  A lane takes 8
 // consecutive elements (16 bytes), a row of up to 512 elements LPR lanes, a wider one two passes of a wave; a row of 192 leaves
 // a quarter of its 32 lanes idle, one of 576 44 % of its places (three passes of 32 lanes take 240 registers and longer: 23.2 us for
-// 21.7).  Measured: 512 tokens of ten agents, 16 + 8 + 8 256-wide heads, 38 to 42 us for 138 MB; 301 of five, latent rows, 22 us for 58 MB;
-// one token of ten 5 us.
+// 21.7 in replayed graphs).  Measured (kernel trace): 512 tokens of ten agents, 16 + 8 + 8 256-wide heads, 42 us for 138 MB; 301 of five,
+// latent rows, 23 us for 58 MB; one token of ten 5 us.
 //
 // All arithmetic in front of the rounding is binary64: codes come from roundings, so a result on the other side of a border
 // moves a cache value by a whole scale (a fifteenth of its group's range), and with binary32 about one element in 2,000 is

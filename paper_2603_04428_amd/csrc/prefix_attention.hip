@@ -1,17 +1,19 @@
 // Decode attention of agents that share a prefix (forked from one parent: their block-table rows begin with the same blocks):
 //   out[l][a][h] = softmax(sm * q K_hat^T) V_hat   over all of the agent's tokens, as in decode_attention.hip,
-// with the tokens that a group of agents shares read and unpacked once for the query rows of all of them.
+// with the tokens that a group of agents shares read and unpacked once for up to 32 of its query rows on a KV head (48 with 64-wide heads).
 //
-// A group's first prefix_len tokens are one unit per (layer, KV head) with (agents of the group) * n_rep query rows; what lies
-// behind them is one unit per (layer, KV head, agent) with n_rep rows.  A row's softmax over the two parts (and over the ranges
+// A group's first prefix_len tokens are one unit per (layer, KV head, row tile) of its (agents of the group) * n_rep query rows; what
+// lies behind them is one unit per (layer, KV head, agent) with n_rep rows.  A row's softmax over the two parts (and over the ranges
 // that several workers take of a unit) is joined from their un-normalised sums, maxima and denominators:
 //   m = max m_i,  out = sum_i 2^(m_i - m) acc_i / sum_i 2^(m_i - m) l_i.
 //
 // One pass over each unit's cache, 64 tokens at a time, per wave (no synchronisation inside the tile loop):
 //  * code words and parameters travel HBM -> LDS directly (global_load_lds, 16 bytes a lane) into a ring of tile buffers; the K
-//    part of a buffer is asked for again as soon as the scores of its tile are taken, the rest when its values are summed, so
-//    that RING - 1/2 tiles are on their way while one is worked on.  Rows lie swizzled in LDS: 16-byte chunk c of token t at
-//    chunk c ^ f(t), which spreads both kinds of reads below over all banks; the transfer fetches permuted chunks of one row.
+//    part of a buffer is asked for again as soon as the scores of its tile are taken, the rest when its values are summed.  The
+//    block ids of the tiles to come are in a register that a branch may load again, and behind that branch the compiler waits for all
+//    vector memory, the transfers among it: when a tile's K is asked for, everything asked for before has arrived, so that one tile,
+//    not RING - 1/2, is on its way while one is worked on.  Rows lie swizzled in LDS: 16-byte chunk c of token t at chunk
+//    c ^ f(t), which spreads both kinds of reads below over all banks; the transfer fetches permuted chunks of one row.
 //  * scores, transposed: S^T[t][row] = sum_g s[t,g] (C_g Q_g^T)[t][row] + (b Qsum^T)[t][row]: two v_mfma_f32_16x16x32_f16 per 16
 //    tokens, group and 16 rows, operand A a code word masked in place (nibbles are binary16 subnormals), the scale applied to
 //    the binary32 results; the bias term is one 16x16x16 instruction over the groups, group sums of q split in two binary16
@@ -20,9 +22,9 @@
 //    gives a lane 16 tokens of one element, masks unpack 8 of them into operand A; the lane that received S^T of (row, four
 //    tokens of each 16) supplies their p s as operand B, in two binary16 terms, so probabilities never leave their registers.
 // Unpacking (about 10 vector instructions per 64 codes of a lane) is shared by CT column tiles of 16 rows.
-// What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (21 us for 10 agents x 8,192 tokens, 256-wide,
-// one layer), above that the issue of instructions (60 % of a wave's time; matrix pipe 21 %): 12 such layers 91 us, 301 MB of cache = 3.3
-// TB/s; 32 agents of four rows x 16,384, 128-wide, two layers 79 us.
+// What bounds it: below about 2,000 tiles the chain plan - ids - tiles - meeting - records (23 us for 10 agents x 8,192 tokens, 256-wide,
+// one layer), above that the issue of instructions (60 % of a wave's time; matrix pipe 27 %) and the waits for the ring (26 %): 12 such
+// layers 105 us, 301 MB of cache = 2.9 TB/s; 32 agents of four rows x 16,384, 128-wide, two layers 89 us.
 #include <algorithm>
 
 #include "q4_device.h"
@@ -934,7 +936,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
             // ---- values: V_hat = (c - 8) s + 8 s + b.  p s goes in as two binary16 terms, what the first one's rounding left being the
             // second, so that 2^-22 of it is lost, relative to |c - 8| s, the distance from the middle of the value's group: sum (c - 8) ps =
             // sum c ps - 8 sum ps with the ps that were rounded, two more instructions per group and half.  One term alone would be 2^-12
-            // off, 2.6e-4 instead of 2.2e-4 of an output's size with the output's own rounding of 2.1e-4, and 82 us for 91 on two layers of
+            // off, 2.6e-4 instead of 2.2e-4 of an output's size with the output's own rounding of 2.1e-4, and 82 us for 90 on two layers of
             // 128 rows behind 16,384 tokens, 94 for 105 on twelve of 20, 256-wide, 26 for 28 on one.  The middles may be any size, and cancel: sums of p b
             // and p s take p in two binary16 terms.  All these sums share an accumulator, whose rows 4 k + g are group g's: k = 0 takes
             // sum 8 ps, 2 sum p b and 3 sum p s.
