@@ -912,13 +912,28 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
 #pragma unroll
                 for (int k = 0; k < 16; ++k) mt = fmaxf(mt, z[ct][k / 4][k % 4]);
                 mt = xor32_max(xor16_max(mt)) * zs;
-                const bool above = mt > m_run[ct] + above_by;
-                const float m_new = above ? mt - lift : m_run[ct];
-                const float minus_even = -m_new, minus_odd = -(m_new + 4.0f);
+                asm("" : "+v"(mt)); // rounded here, and not once more with each of the differences below
+                const bool above = mt - m_run[ct] > above_by;
+                float m_new = above ? mt - lift : m_run[ct], factor = zs, taken = m_new;
+                // The maximum is rounded once more than the exponents, by up to 2^-7 for scores of 2^18.  Beyond, where that would let
+                // weights out of binary16 (from 2^22 on) or vanish, all scores of the tile are rounded like it.
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(fabsf(mt) > 0x1p18f) != 0ull, 0)) {
+                    asm volatile("");
+                    if (above && fabsf(mt) > 0x1p22f) m_new = mt; // `lift` may be less than a step there
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float score = z[ct][k / 4][k % 4] * zs;
+                        asm("" : "+v"(score)); // a rounding of its own
+                        z[ct][k / 4][k % 4] = score - m_new;
+                    }
+                    factor = 1.0f;
+                    taken = 0.0f;
+                }
+                const float minus_even = -taken, minus_odd = -(taken + 4.0f);
                 float even_sum = 0.0f, odd_sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float pr = __builtin_amdgcn_exp2f(fmaf(z[ct][k / 4][k % 4], zs, (k & 1) ? minus_odd : minus_even));
+                    const float pr = __builtin_amdgcn_exp2f(fmaf(z[ct][k / 4][k % 4], factor, (k & 1) ? minus_odd : minus_even));
                     z[ct][k / 4][k % 4] = pr;
                     if (k & 1) odd_sum += pr; else even_sum += pr;
                 }

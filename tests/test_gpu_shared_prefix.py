@@ -347,3 +347,33 @@ def test_queries_whose_groups_sum_beyond_binary16(heads, size):
     f.q = q.astype(np.float16)
     f.scale = 1.0 / (size * np.sqrt(heads[2]))
     f.check(f.call())
+
+
+@pytest.mark.parametrize("heads", [LLAMA, GEMMA, PER_HEAD], ids=["128", "256", "192"])
+@pytest.mark.parametrize("v_scale", [0.95, 1.5, 1.9, 240.0])
+def test_scores_of_millions(heads, v_scale):
+    """Scores of 2^22 and more are binary32 numbers half a unit apart: a tile's maximum, rounded once more than the exponents, may
+    let a weight through that is larger than its bound.  Weights that far out are not checked; no product may leave binary16,
+    so an output lies between the values it is made of.  Every wave takes eight tiles and more."""
+    f = Family(1, *heads, [(2048, (0,))], seed=22, extra=0)
+    rng = np.random.default_rng(23)
+    tokens = f.nb * 256
+    k = rng.standard_normal((1, 1, tokens, heads[1], heads[2])) * 0.004
+    k[..., :64] = 300.0                              # one group makes the size, the others the differences
+    v = rng.uniform(-7.5, 7.5, (1, 1, tokens, heads[1], heads[3])) * v_scale
+    v[..., ::64], v[..., 1::64] = -7.5 * v_scale, 7.5 * v_scale
+    whole = np.arange(f.nb, dtype=np.int32)[None]
+    oracle.append(f.ospec, f.okp, f.ovp, k.astype(np.float16), v.astype(np.float16), whole, np.zeros(1, np.int32))
+    for g, o in ((f.kp, f.okp), (f.vp, f.ovp)):
+        for name, kind in (("codes", np.int32), ("scale", np.int16), ("bias", np.int16)):
+            getattr(g, name).copy_(torch.from_numpy(getattr(o, name).view(kind)))
+    A, blocks = 16, 64
+    f.table = rng.integers(0, f.nb, (A, blocks)).astype(np.int32)
+    f.lens = [256 * blocks - int(rng.integers(0, 100)) for _ in range(A)]
+    assert A * heads[1] * blocks * 4 >= 8 * 1024
+    for size in (2.0 ** 20, 2.0 ** 22.5, 2.0 ** 23.5, 2.0 ** 25.5, 2.0 ** 27.5, 2.0 ** 34):
+        f.q = rng.uniform(0.7, 1.0, (1, A, 1, heads[0], 1)).repeat(heads[2], -1).astype(np.float16)
+        f.scale = size / (19200.0 * 1.4427)          # in the units of exp2
+        got = f.call(begin=False).float().cpu().numpy()
+        largest = np.abs(got).max()
+        assert largest <= 7.5 * v_scale * (1 + 2.0 ** -10), size
