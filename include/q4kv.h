@@ -272,9 +272,8 @@ int q4kv_shared_prefix_attention(const q4kv_spec *spec, const q4kv_pool *k, cons
 
 /* Bytes of workspace q4kv_shared_prefix_attention needs for these arguments, whatever the groups.  0 on bad arguments.  A row (layer,
  * agent, query head) may leave a record of v_dim + 2 binary32 values per range of 128 tokens and more, but no more than
- * 1,024 / (layers * KV heads) + 2 of its prefix and as many of its own tokens (256 compute units): 24 MB for one layer of ten
- * agents of 9,000 tokens with 32 query and 8 KV heads, 128-wide, 141 MB for two of 32 behind 16,384, 2.2 GB for one of 512
- * agents and 131,072. */
+ * 1,024 / (layers * KV heads) + 4 (256 compute units): 12 MB for one layer of ten agents of 9,000 tokens with 32 query and 8 KV
+ * heads, 128-wide, 72 MB for two of 32 behind 16,384, 1.1 GB for one of 512 agents and 131,072. */
 size_t q4kv_shared_prefix_workspace_bytes(const q4kv_spec *spec, int32_t num_agents, int32_t max_seq_len,
                                           int32_t num_layers_in_call);
 

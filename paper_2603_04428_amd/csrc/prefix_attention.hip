@@ -67,7 +67,7 @@ struct PrefixParams {
     int32_t *plan;
     float *part_acc, *part_ml;
     int num_agents, num_groups, max_blocks, num_blocks, kv_heads, q_heads, n_rep, layer_begin, layers, max_seq_len;
-    int slots;    // records reserved per row for the prefix, and as many for the agent's own tokens
+    int slots;    // records reserved per row: those of the prefix from the front, of the agent's own tokens from the back
     int row_tile; // rows of a prefix unit: 16 * CT
     float score_scale;
     float inv_n_rep;
@@ -1105,7 +1105,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DK, DV>::WAVES_PER_SIMD)) void pre
                 const half2_t a = half2_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv)}, b = half2_t{(half_t)(o[2] * inv), (half_t)(o[3] * inv)};
                 *reinterpret_cast<uint2 *>(p.out + row * DV + e) = make_uint2(half2_to_bits(a), half2_to_bits(b));
             } else {
-                const int64_t rec = row * (2 * p.slots) + u.which * p.slots + u.slot;
+                const int64_t rec = row * p.slots + (u.which == 0 ? u.slot : p.slots - 1 - u.slot);
                 *reinterpret_cast<float4_t *>(p.part_acc + rec * DV + e) = o;
                 if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + rec * 2) = make_float2(m, l);
             }
@@ -1215,7 +1215,7 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(const float *__r
     const int n_own = records_of(base + group_tiles + own0, own_tiles);
     if (shared == 0 && n_own == 1) return;
     const int records = n_prefix + n_own;
-    const int64_t rec0 = row * (2 * slots);
+    const int64_t rec0 = row * slots;
     float m = kNegBig, l = 0.0f;
     float4_t o = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = part; s0 < records; s0 += PARTS * kBatch) {
@@ -1224,7 +1224,7 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(const float *__r
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int at = s0 + k * PARTS, s = min(at, records - 1);
-            const int64_t rec = rec0 + (s < n_prefix ? s : slots + s - n_prefix);
+            const int64_t rec = rec0 + (s < n_prefix ? s : slots - 1 - (s - n_prefix));
             const float2 t = *reinterpret_cast<const float2 *>(part_ml + rec * 2);
             mm[k] = t.x;
             ll[k] = at < records ? t.y : 0.0f;
@@ -1298,14 +1298,15 @@ int column_tiles(const q4kv_spec &s, int num_agents, int num_groups)
     return (tiles + units - 1) / units;
 }
 
-// Records per row and part: a worker's range is at least kSoloTiles (a wave's) or kWaves tiles (a workgroup's) long, and no shorter
-// than an even share of all tiles, to which a unit of T tiles contributes T for every layer and KV head.
+// Records per row: a worker's range is at least kSoloTiles (a wave's) or kWaves tiles (a workgroup's) long, and no shorter than an
+// even share of all tiles, to which a row's prefix and own tiles, T together and no more than max_seq_len has, contribute T for every
+// layer and KV head.  Each of the two may begin and end inside a range: two records more.
 int record_slots(const q4kv_spec &s, int max_seq_len, int layers, int workgroups)
 {
     const int64_t tiles = (max_seq_len + kWave - 1) / kWave, units = (int64_t)layers * s.num_kv_heads;
     const int64_t shared = std::min<int64_t>(tiles / kWaves, workgroups / units);
     const int64_t solo = std::min<int64_t>(tiles / kSoloTiles, (int64_t)workgroups * kWaves / units);
-    return (int)std::max(shared, solo) + 2;
+    return (int)std::max(shared, solo) + 4;
 }
 
 int prefix_workgroups(int compute_units) { return compute_units; }
@@ -1330,7 +1331,7 @@ int64_t prefix_tiles(const q4kv_spec &s, int num_agents, int num_groups, int max
 size_t prefix_workspace_bytes(const q4kv_spec &s, int num_agents, int max_seq_len, int layers, int compute_units, size_t &acc_at, size_t &ml_at)
 {
     const int slots = record_slots(s, max_seq_len, layers, prefix_workgroups(compute_units));
-    const size_t records = (size_t)layers * num_agents * s.num_q_heads * 2 * slots;
+    const size_t records = (size_t)layers * num_agents * s.num_q_heads * slots;
     acc_at = ((size_t)plan_ints(num_agents) * sizeof(int32_t) + 255) / 256 * 256;
     ml_at = acc_at + records * s.v_dim * sizeof(float);
     return ml_at + records * 2 * sizeof(float);

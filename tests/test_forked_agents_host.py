@@ -247,3 +247,11 @@ def test_shared_prefix_calls_of_more_rows_than_a_launch_has_are_refused():
 
     assert call(511, 4096) == -4 and call(512, 4095) == -4                      # the workspace of no bytes
     assert call(512, 4096) == -3 and "2^24 rows" in _err()
+
+
+def test_shared_prefix_workspace_holds_a_rows_records_once():
+    """A row's prefix and own tokens share one range of records: 1,024 waves / (layers * KV heads) and four, each v_dim + 2 words."""
+    spec = b.make_spec(32, 32, 8, 128)
+    for agents, top, layers, most in ((10, 9000, 1, 74), (32, 17900, 2, 68), (512, 131072, 1, 132), (5, 100, 1, 5)):
+        need = b.q4kv_shared_prefix_workspace_bytes(spec, agents, top, layers)
+        assert need <= layers * agents * 32 * most * 130 * 4 + 4 * (5 * agents + 4) + 256

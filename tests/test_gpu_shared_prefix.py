@@ -377,3 +377,13 @@ def test_scores_of_millions(heads, v_scale):
         got = f.call(begin=False).float().cpu().numpy()
         largest = np.abs(got).max()
         assert largest <= 7.5 * v_scale * (1 + 2.0 ** -10), size
+
+
+@pytest.mark.parametrize("heads", [LLAMA, GEMMA, PER_HEAD, NARROW], ids=["128", "256", "192", "64"])
+@pytest.mark.parametrize("prefix,own", [(4032, (4161, 7)), (64, (8000, 8128)), (8064, (1, 128)), (4096, (4096, 4096, 4095))])
+def test_as_many_records_as_there_may_be(heads, prefix, own):
+    """One layer of few KV heads: ranges are as short as they get, and a row's prefix and own records fill what is reserved."""
+    f = Family(1, *heads, [(prefix, own)], seed=prefix)
+    want = f.want()
+    f.check(f.call(), want)
+    f.check(f.call(top=f.table.shape[1] * 256), want)
