@@ -125,6 +125,22 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
                 const int32_t *seq_len_before, int32_t num_agents, int32_t chunk_len, int32_t layer_begin,
                 int32_t layer_end, void *hip_stream);
 
+/* q4kv_append for a batch in which every agent brings a number of tokens of its own: rows of new tokens one behind the other, and
+ * the place of each in the pools (a slot map, as q4kv_resize_tables writes it) instead of a chunk length.
+ *   k_new, v_new  device, [layers of the call][num_tokens] token rows, each token's heads contiguous ([num_kv_heads][dim]);
+ *                 *_stride elements from one token row to the next, so that they may be parts of one fused projection.  Strides
+ *                 are multiples of 8 and no smaller than a row, pointers 16-byte aligned.  v_new must be NULL when
+ *                 spec->v_aliases_k.  in_format: 0 binary16, 1 bfloat16 (of both): a bfloat16 value is rounded once to binary16,
+ *                 and must be inside its range
+ *   slot          device int32 [num_tokens]: block * 256 + place in the block, the same on every layer.  A token whose slot is
+ *                 outside [0, 256 * num_blocks) is skipped (-1 for the tokens that fill a batch up), its rows are not looked at;
+ *                 of two tokens with one slot either may be stored, group by group
+ * The cache gets the bits that q4kv_append makes of the same rows.  num_tokens > Q4KV_MAX_CHUNK_LEN, pools of 2^23 blocks and
+ * more and calls of 2^31 groups and more on a layer -> Q4KV_ERANGE. */
+int q4kv_append_slots(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const void *k_new, const void *v_new,
+                      int32_t in_format, int64_t k_stride, int64_t v_stride, const int32_t *slot, int32_t num_tokens,
+                      int32_t layer_begin, int32_t layer_end, void *hip_stream);
+
 /* What a model does to the heads of Q and K between a layer's projections and the cache (Sec. 3.6 names the models).  For
  * every head row x of k_dim elements:
  *   norm      elements i < norm_dim become x_i * weight[i] / sqrt(mean of x_j^2 over j < norm_dim + eps); the others stay.
@@ -348,6 +364,91 @@ int q4kv_import_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_poo
  * Enqueues on hip_stream, allocates nothing.  At most 65,535 layers. */
 int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const int32_t *src_ids,
                      const int32_t *dst_ids, int32_t num_pairs, void *hip_stream);
+
+/* Block tables that live on the GPU.  q4kv_block_pool_* (below) keeps who owns which block on the host; a serving loop or a beam
+ * search that never waits for the GPU keeps the same in device memory, and the calls behind this struct work on it in stream
+ * order.  A row is an agent (a request, a beam); it lists the ceil(seq_len / 256) blocks of its tokens in token order.
+ *   block_table  device int32 [num_agents][max_blocks], what every attention and append call takes; entries behind a row's blocks
+ *                mean nothing (an entry that a call takes away becomes -1)
+ *   seq_len      device int32 [num_agents], tokens cached (read as 0 below 0, as 256 * max_blocks above that)
+ *   refs         device int32 [num_blocks]: rows that list the block, of this table or of any other with these pools; 0: free.  A
+ *                program that keeps blocks for itself (a prompt's image, say) counts itself in
+ *   refused      device int32 [1] or NULL: set by every call to the number of rows that did not get what they asked for
+ * A block that several rows list is full of tokens that they all have; the block that a row ends in, if it is not full, is its
+ * own.  The calls here keep it so.  Free blocks are handed out lowest id first, to rows in order: results are the same on
+ * every run.  At most Q4KV_MAX_TABLE_ROWS rows and 2^23 - 1 blocks, 2^31 - 1 tokens a row (Q4KV_ERANGE); calls on one table, or on tables
+ * with the same refs, must not overlap in time.  An entry outside [0, num_blocks) is carried along and counted nowhere. */
+#define Q4KV_MAX_TABLE_ROWS 2048
+typedef struct {
+    int32_t *block_table, *seq_len, *refs, *refused;
+    int32_t num_agents, max_blocks, num_blocks;
+} q4kv_tables;
+
+/* The agents' lengths become new_len[], and their tables with them: what q4kv_block_pool_reserve, _truncate and _release do for one
+ * agent on the host, for all of them at once.
+ *   new_len       device int32 [num_agents]: tokens from now on.  0 gives all blocks back, a negative one leaves the row as it is
+ * Rows that get shorter free their blocks first, so that the same call can hand them out.  Rows that get longer are served in
+ * order up to the first whose blocks are not there, or whose tokens do not fit the map; that one and the growing rows behind it
+ * are left as they were (and counted in refused), as is a row whose new length its table cannot list.
+ * A slot map of the tokens that rows got longer by, agent after agent, for q4kv_append_slots:
+ *   max_tokens    places in it; 0: none wanted, and no bound on the tokens
+ *   token_begin   device out, int32 [num_agents + 1]: first token of each agent, and their number
+ *   slot, token_agent, position   device out, int32 [max_tokens]: block * 256 + place, row, and place in the agent's text of each
+ *                 token; -1 behind the last one.  token_agent and position may be NULL
+ * With spec and pools (spec NULL: none), a row that goes on, or is cut, inside a block that others list as well gets a copy of
+ * that block's first tokens, every layer, and goes on in that (of rows that all end there, and with nobody else listing it, the
+ * lowest keeps the block).  Where no block is left for the copy, and without pools, a row that is cut inside a shared block
+ * loses what it has of it: its seq_len becomes the multiple of 256 below, and it counts as refused.  Without pools a row that
+ * goes on is taken to end in a block of its own.
+ *   workspace     device scratch of q4kv_tables_workspace_bytes(num_agents) bytes, 16-byte aligned, contents unspecified; not
+ *                 needed (NULL) without pools
+ * Allocates nothing, never synchronises. */
+int q4kv_resize_tables(const q4kv_tables *tables, const int32_t *new_len, int32_t max_tokens, int32_t *token_begin, int32_t *slot,
+                       int32_t *token_agent, int32_t *position, const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* What a beam search does to the cache once it has chosen: row i of the tables becomes what row parent[i] was before the call
+ * (parent: device int32 [num_agents]; a row whose parent is outside [0, num_agents) becomes empty).  Blocks are listed by one more row
+ * or by one less; nothing is copied but the last block, if it is not full, of a row with several children: the lowest child goes
+ * on in it, the others get free blocks with a copy of its seq_len % 256 tokens, every layer, K and V (what is in the other slots
+ * of such a block is not touched).  A child for which no block is left keeps the full blocks only: its seq_len becomes the
+ * multiple of 256 below, and it counts in refused.  With a parent listed for rows that were empty, this is the fork of an
+ * agent, or of a prompt into its beams.  Workspace as above, needed always. */
+int q4kv_beam_reorder(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const q4kv_tables *tables, const int32_t *parent,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace of the two calls above.  0 on bad arguments. */
+size_t q4kv_tables_workspace_bytes(int32_t num_agents);
+
+/* The choice of a beam search's step.  Rows of logits are grouped (a request's beams); every row's continuations have the totals
+ *     score[row] + x[token] - log(sum over tokens of exp x)
+ * and of all continuations of a group's rows the num_out largest come out, largest first, equal ones in the order of row, then
+ * logit (the larger first), then token.
+ *   logits      device [num_agents][vocab], logits_format 0 binary16, 1 bfloat16 (a q4kv_param_format), 2 binary32; row_stride
+ *               elements from one row to the next, any alignment that the type has.  -inf: a banned token, never chosen.  NaN
+ *               counts as -inf, +inf as the largest finite binary32 number
+ *   score       device binary32 [num_agents]; a row of score -inf (or NaN) has no continuation and is not read: the state before the
+ *               first step is one beam of score 0 beside dead ones
+ *   end_token   device int32 [num_agents] or NULL.  Not negative: the row is finished, its logits are not read, and its one
+ *               continuation is that token, at the row's own score
+ *   group_begin device int32 [num_groups + 1], as for q4kv_shared_prefix_attention: group g is rows group_begin[g] ..
+ *               group_begin[g + 1] - 1 (bounds outside [0, num_agents] are read as the nearest in it; of bounds that fall the group
+ *               is empty)
+ *   num_out     1 .. Q4KV_MAX_BEAM_OUT for every group, whatever its rows.  With the group's number of rows, parent[] is what
+ *               q4kv_beam_reorder takes
+ *   parent, token, total   device out, int32, int32 and binary32 [num_groups][num_out]; where a group has no more continuations:
+ *               -1, -1, -inf
+ *   workspace   device scratch of q4kv_beam_select_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; calls
+ *               that overlap in time need one each
+ * Totals are formed and compared in binary64, from sums that are good to a few 2^-26 of the logarithm, and rounded once to
+ * binary32 on their way out.  Run-to-run identical.  Allocates nothing, never synchronises. */
+#define Q4KV_MAX_BEAM_OUT 64
+int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stride, int32_t vocab, int32_t num_agents, const float *score,
+                     const int32_t *end_token, const int32_t *group_begin, int32_t num_groups, int32_t num_out, int32_t *parent,
+                     int32_t *token, float *total, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace of q4kv_beam_select on the current device.  0 on bad arguments. */
+size_t q4kv_beam_select_workspace_bytes(int32_t logits_format, int32_t vocab, int32_t num_agents, int32_t num_out);
 
 /* Sec. 3.1 "Block Pool with Per-Agent Isolation", host side: which 256-token block of the device pools belongs to
  * which agent.  Pure bookkeeping in HOST memory (no device call): a block id is either free or in exactly one agent's

@@ -20,7 +20,8 @@ EXPORTS = ["q4kv_quantize", "q4kv_dequantize", "q4kv_quantize_fmt", "q4kv_dequan
            "q4kv_block_pool_lru_victim", "q4kv_block_pool_free_blocks", "q4kv_block_pool_owner",
            "q4kv_block_pool_fork", "q4kv_block_pool_truncate", "q4kv_block_pool_compact", "q4kv_block_pool_shares",
            "q4kv_copy_blocks", "q4kv_norm_rope_append", "q4kv_shared_prefix_attention", "q4kv_shared_prefix_workspace_bytes",
-           "q4kv_last_error",
+           "q4kv_append_slots", "q4kv_resize_tables", "q4kv_beam_reorder", "q4kv_tables_workspace_bytes", "q4kv_beam_select",
+           "q4kv_beam_select_workspace_bytes", "q4kv_last_error",
            "q4kv_version"]
 
 
@@ -50,6 +51,12 @@ class _CHeadForm(C.Structure):
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("cos_table", C.c_void_p), ("sin_table", C.c_void_p),
                 ("norm_dim", C.c_int32), ("eps", C.c_float), ("rot_begin", C.c_int32), ("rot_dim", C.c_int32),
                 ("neighbours", C.c_int32), ("table_len", C.c_int32)]
+
+
+class _CTables(C.Structure):
+    """q4kv_tables"""
+    _fields_ = [("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("refs", C.c_void_p), ("refused", C.c_void_p),
+                ("num_agents", C.c_int32), ("max_blocks", C.c_int32), ("num_blocks", C.c_int32)]
 
 
 _lib = None
@@ -117,6 +124,15 @@ def lib():
                                                    i32, i32, C.c_float, i32, i32, vp, C.c_size_t, vp]
         l.q4kv_shared_prefix_workspace_bytes.restype = C.c_size_t
         l.q4kv_shared_prefix_workspace_bytes.argtypes = [C.POINTER(Spec), i32, i32, i32]
+        l.q4kv_append_slots.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), vp, vp, i32, i64, i64, vp, i32, i32, i32, vp]
+        l.q4kv_resize_tables.argtypes = [C.POINTER(_CTables), vp, i32, vp, vp, vp, vp, C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool),
+                                         vp, C.c_size_t, vp]
+        l.q4kv_beam_reorder.argtypes = [C.POINTER(Spec), C.POINTER(_CPool), C.POINTER(_CPool), C.POINTER(_CTables), vp, vp, C.c_size_t, vp]
+        l.q4kv_tables_workspace_bytes.restype = C.c_size_t
+        l.q4kv_tables_workspace_bytes.argtypes = [i32]
+        l.q4kv_beam_select.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, C.c_size_t, vp]
+        l.q4kv_beam_select_workspace_bytes.restype = C.c_size_t
+        l.q4kv_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
         l.q4kv_last_error.restype = C.c_char_p
         l.q4kv_version.restype = C.c_int
         _lib = l
@@ -213,6 +229,51 @@ class HeadForm:
         f32 = torch.float32
         return _CHeadForm(_dev(q_weight, f32, "q_weight"), _dev(k_weight, f32, "k_weight"), _dev(cos, f32, "cos"), _dev(sin, f32, "sin"),
                           self.norm_dim, self.eps, self.rot_begin, self.rot_dim, 1 if self.neighbours else 0, table_len)
+
+
+class BlockTables:
+    """q4kv_tables: block table [agents][max_blocks], lengths [agents] and counts [blocks], int32 on the GPU.  refused: int32 [1], how
+    many rows the last call could not serve."""
+
+    def __init__(self, num_agents, max_blocks, num_blocks, device="cuda"):
+        self._around(torch.full((num_agents, max_blocks), -1, dtype=torch.int32, device=device),
+                     torch.zeros(num_agents, dtype=torch.int32, device=device), torch.zeros(num_blocks, dtype=torch.int32, device=device))
+
+    @classmethod
+    def of(cls, block_table, seq_len, refs):
+        """Around arrays that the caller has."""
+        t = cls.__new__(cls)
+        t._around(block_table, seq_len, refs)
+        return t
+
+    def _around(self, block_table, seq_len, refs):
+        self.block_table, self.seq_len, self.refs = block_table, seq_len, refs
+        self.refused = torch.zeros(1, dtype=torch.int32, device=refs.device)
+
+    def c(self):
+        table, i32 = self.block_table, torch.int32
+        if table.dim() != 2 or self.seq_len.numel() != table.shape[0]:
+            raise ValueError(f"a table of {tuple(table.shape)} for {self.seq_len.numel()} lengths")
+        return _CTables(_dev(table, i32, "block_table"), _dev(self.seq_len, i32, "seq_len"), _dev(self.refs, i32, "refs"),
+                        _dev(self.refused, i32, "refused"), table.shape[0], table.shape[1], self.refs.numel())
+
+
+class TokenMap:
+    """What q4kv_resize_tables writes for the tokens that rows got longer by: begin int32 [agents + 1]; slot, agent and position
+    int32 [max_tokens], -1 behind the last token."""
+
+    def __init__(self, tables, max_tokens):
+        device = tables.refs.device
+        self.begin = torch.zeros(tables.block_table.shape[0] + 1, dtype=torch.int32, device=device)
+        self.slot, self.agent, self.position = (torch.full((max_tokens,), -1, dtype=torch.int32, device=device) for _ in range(3))
+
+
+class BeamChoice:
+    """What q4kv_beam_select writes: parent and token int32, score float32, all [groups][num_out]."""
+
+    def __init__(self, groups, num_out, device="cuda"):
+        self.parent, self.token = (torch.empty((groups, num_out), dtype=torch.int32, device=device) for _ in range(2))
+        self.score = torch.empty((groups, num_out), dtype=torch.float32, device=device)
 
 
 class BlockPool:
@@ -455,6 +516,105 @@ def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table
         _dev(seq_len_before, torch.int32, "seq_len_before"), _dev(positions, torch.int32, "positions"), A, Cn, layer_begin,
         layer_end, _stream()))
     return q_out
+
+
+def q4kv_append_slots(spec, kpool, vpool, k_new, v_new, slot, layer_begin=0, layer_end=None):
+    """k_new / v_new: fp16 or bf16 [layers_in_call][tokens][kv_heads][dim], possibly parts of one fused projection (tokens a fixed
+    stride apart); slot: int32 [tokens] on the GPU, block * 256 + place, outside the pool: the token is skipped."""
+    layer_end = spec.num_layers if layer_end is None else layer_end
+    if k_new.dim() != 4 or (v_new is not None and v_new.dim() != 4):
+        raise TypeError("k_new and v_new: need [layers][tokens][heads][dim]")
+    hkv, kind, lead, v_stride = spec.num_kv_heads, k_new.dtype, k_new.shape[:2], 0
+    k_stride = _token_rows(k_new.unsqueeze(1), hkv, spec.k_dim, "k_new")
+    if v_new is not None:
+        v_stride = _token_rows(v_new.unsqueeze(1), hkv, spec.v_dim, "v_new")
+    if kind not in (torch.float16, torch.bfloat16) or (v_new is not None and v_new.dtype != kind):
+        raise TypeError(f"k_new and v_new: fp16 or bf16, both of one type, got {kind}")
+    if v_new is not None and v_new.shape[:2] != lead:
+        raise TypeError(f"k_new and v_new differ in layers or tokens: {tuple(lead)}, {tuple(v_new.shape[:2])}")
+    if lead[0] != layer_end - layer_begin:
+        raise ValueError(f"{lead[0]} layers of rows for {layer_end - layer_begin} layers")
+    if slot.numel() != lead[1]:
+        raise ValueError(f"{slot.numel()} slots for {lead[1]} tokens")
+    kp, vp = _pools(spec, kpool, vpool)
+    _check(lib().q4kv_append_slots(C.byref(spec), kp, vp, k_new.data_ptr(), None if v_new is None else v_new.data_ptr(),
+                                   1 if kind == torch.bfloat16 else 0, k_stride, v_stride, _dev(slot, torch.int32, "slot"), lead[1],
+                                   layer_begin, layer_end, _stream()))
+
+
+def q4kv_tables_workspace(tables):
+    """The workspace that q4kv_beam_reorder needs, and q4kv_resize_tables with pools."""
+    return torch.empty(lib().q4kv_tables_workspace_bytes(tables.block_table.shape[0]), dtype=torch.uint8, device=tables.refs.device)
+
+
+def q4kv_resize_tables(tables, new_len, out=None, spec=None, kpool=None, vpool=None, workspace=None):
+    """The agents' lengths become new_len (int32 [agents] on the GPU).  out: a TokenMap to fill, or None.  spec and pools: blocks
+    that are shared where a row goes on or is cut are copied; None: see include/q4kv.h."""
+    t, kp, vp = tables.c(), None, None
+    if new_len.numel() != t.num_agents:
+        raise ValueError(f"{new_len.numel()} lengths for {t.num_agents} agents")
+    if spec is not None:
+        kp, vp = _pools(spec, kpool, vpool)
+        if workspace is None:
+            workspace = q4kv_tables_workspace(tables)
+    places, begin, slot, agent, position = 0, None, None, None, None
+    if out is not None:
+        i32 = torch.int32
+        places, begin, slot = out.slot.numel(), _dev(out.begin, i32, "begin"), _dev(out.slot, i32, "slot")
+        agent, position = _dev(out.agent, i32, "agent"), _dev(out.position, i32, "position")
+        if out.begin.numel() != t.num_agents + 1 or any(x is not None and x.numel() != places for x in (out.agent, out.position)):
+            raise ValueError("out: a map of other tables, or of arrays of different lengths")
+    _check(lib().q4kv_resize_tables(C.byref(t), _dev(new_len, torch.int32, "new_len"), places, begin, slot, agent, position,
+                                    None if spec is None else C.byref(spec), kp, vp, _dev(workspace, torch.uint8, "workspace"),
+                                    0 if workspace is None else workspace.numel(), _stream()))
+    return out
+
+
+def q4kv_beam_reorder(spec, kpool, vpool, tables, parent, workspace=None):
+    """Row i of the tables becomes what row parent[i] was (int32 [agents] on the GPU, outside: an empty row)."""
+    t = tables.c()
+    if parent.numel() != t.num_agents:
+        raise ValueError(f"{parent.numel()} parents for {t.num_agents} agents")
+    if workspace is None:
+        workspace = q4kv_tables_workspace(tables)
+    kp, vp = _pools(spec, kpool, vpool)
+    _check(lib().q4kv_beam_reorder(C.byref(spec), kp, vp, C.byref(t), _dev(parent, torch.int32, "parent"),
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+
+
+_LOGITS = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def q4kv_beam_select_workspace(logits, num_out):
+    """The workspace of q4kv_beam_select for rows like these."""
+    rows, vocab = logits.shape
+    need = lib().q4kv_beam_select_workspace_bytes(_LOGITS[logits.dtype], vocab, rows, num_out)
+    if need == 0:
+        raise ValueError(lib().q4kv_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=logits.device)
+
+
+def q4kv_beam_select(logits, score, group_begin, num_out, end_token=None, out=None, workspace=None):
+    """logits: fp16, bf16 or fp32 [agents][vocab], rows any stride apart; score: float32 [agents]; group_begin: int32 [groups + 1];
+    end_token: int32 [agents] or None.  Returns a BeamChoice (out, if given)."""
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError(f"logits: need [agents][vocab] of fp16, bf16 or fp32 with contiguous rows on the GPU, got {logits.dtype} {tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    groups = group_begin.numel() - 1
+    if groups < 0 or score.numel() != rows or (end_token is not None and end_token.numel() != rows):
+        raise ValueError(f"{rows} rows of logits, {score.numel()} scores, {group_begin.numel()} bounds")
+    if out is None:
+        out = BeamChoice(groups, num_out, logits.device)
+    elif out.parent.shape != (groups, num_out) or out.token.shape != (groups, num_out) or out.score.shape != (groups, num_out):
+        raise ValueError(f"out: {tuple(out.parent.shape)} instead of {(groups, num_out)}")
+    if workspace is None:
+        workspace = q4kv_beam_select_workspace(logits, num_out)
+    i32, f32 = torch.int32, torch.float32
+    _check(lib().q4kv_beam_select(logits.data_ptr(), _LOGITS[logits.dtype], logits.stride(0) if rows > 1 else vocab, vocab, rows,
+                                  _dev(score, f32, "score"), _dev(end_token, i32, "end_token"), _dev(group_begin, i32, "group_begin"),
+                                  groups, num_out, _dev(out.parent, i32, "parent"), _dev(out.token, i32, "token"),
+                                  _dev(out.score, f32, "score"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
 
 
 def q4kv_copy_blocks(spec, kpool, vpool, src_ids, dst_ids):

@@ -10,7 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libq4kv.so")
-SOURCES = ["api.hip", "codec.hip", "decode_attention.hip", "chunk_attention.hip", "mla_decode.hip", "read_probe.hip", "persist.hip", "block_pool.hip", "head_append.hip", "prefix_attention.hip"]
+SOURCES = ["api.hip", "codec.hip", "decode_attention.hip", "chunk_attention.hip", "mla_decode.hip", "read_probe.hip", "persist.hip", "block_pool.hip", "head_append.hip", "prefix_attention.hip", "block_tables.hip", "beam_select.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # No fast-math anywhere: the quantizer needs IEEE binary32 division and rounding.
@@ -26,7 +26,7 @@ PARTS = {"chunk_attention.hip": [f"-DQ4KV_CHUNK_WIDTH={width}" for width in (256
 FILE_FLAGS = {"chunk_attention.hip": VGPR_FORM, "mla_decode.hip": VGPR_FORM, "prefix_attention.hip": VGPR_FORM}
 # Files whose kernels must keep everything in vector registers, and the flags that make the compiler say so.  A chunk kernel that
 # spilled gave wild addresses: the spill was behind a divergent loop, where some lanes were still switched off.
-NO_SPILLS = ["chunk_attention.hip", "prefix_attention.hip"]
+NO_SPILLS = ["chunk_attention.hip", "prefix_attention.hip", "beam_select.hip"]
 ACCUMULATORS = ["prefix_attention.hip"]  # may use accumulator registers as well: its waves have a SIMD to themselves
 RESOURCES = ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics"]
 

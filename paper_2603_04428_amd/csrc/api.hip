@@ -56,6 +56,39 @@ int check_pool(const q4kv_pool *p, const char *name)
     return Q4KV_OK;
 }
 
+// The pools of a call whose spec is known to be good.
+int check_pools(const q4kv_spec *s, const q4kv_pool *k, const q4kv_pool *v)
+{
+    int rc = check_pool(k, "K");
+    if (rc) return rc;
+    if (s->v_aliases_k) return v ? fail(Q4KV_EINVAL, "v must be NULL when v_aliases_k") : Q4KV_OK;
+    if ((rc = check_pool(v, "V"))) return rc;
+    return v->num_blocks == k->num_blocks ? Q4KV_OK : fail(Q4KV_EINVAL, "K and V pools differ in num_blocks");
+}
+
+int check_tables(const q4kv_tables *t)
+{
+    if (!t) return fail(Q4KV_EINVAL, "tables is NULL");
+    if (t->num_agents < 0 || t->max_blocks <= 0 || t->num_blocks <= 0) return fail(Q4KV_EINVAL, "negative count");
+    if (t->num_agents > Q4KV_MAX_TABLE_ROWS) return fail(Q4KV_ERANGE, "%d rows, at most %d", t->num_agents, Q4KV_MAX_TABLE_ROWS);
+    if (t->num_blocks >= 1 << 23) return fail(Q4KV_ERANGE, "slots of %d blocks do not fit 31 bits", t->num_blocks);
+    if (t->max_blocks > 1 << 23) return fail(Q4KV_ERANGE, "rows of %d blocks: 2^31 tokens and more", t->max_blocks);
+    if (t->num_agents == 0) return Q4KV_OK;
+    if (!t->block_table || !t->seq_len || !t->refs) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (!aligned16(t->refs)) return fail(Q4KV_EINVAL, "refs must be 16-byte aligned");
+    return Q4KV_OK;
+}
+
+int check_table_pools(const q4kv_tables *t, const q4kv_spec *s, const q4kv_pool *k, const q4kv_pool *v, void *workspace, size_t workspace_bytes)
+{
+    int rc = check_spec(s);
+    if (rc || (rc = check_pools(s, k, v))) return rc;
+    if (k->num_blocks != t->num_blocks) return fail(Q4KV_EINVAL, "tables of %d blocks, pools of %d", t->num_blocks, k->num_blocks);
+    if (!workspace || workspace_bytes < q4kv::tables_workspace_bytes(t->num_agents)) return fail(Q4KV_EWORKSPACE, "workspace too small or missing");
+    if (!aligned16(workspace)) return fail(Q4KV_EINVAL, "workspace must be 16-byte aligned");
+    return Q4KV_OK;
+}
+
 // Compute units of the current device (cached per device); the attention launch is two workgroups per unit.
 int compute_units()
 {
@@ -274,6 +307,36 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
     hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = q4kv::launch_append(*spec, *k, spec->v_aliases_k ? nullptr : v, k_new, v_new, block_table, max_blocks,
                                        seq_len_before, num_agents, chunk_len, layer_begin, layer_end, compute_units(), st);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "append launch: %s", hipGetErrorString(e));
+}
+
+int q4kv_append_slots(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const void *k_new, const void *v_new,
+                      int32_t in_format, int64_t k_stride, int64_t v_stride, const int32_t *slot, int32_t num_tokens,
+                      int32_t layer_begin, int32_t layer_end, void *hip_stream)
+{
+    int rc = check_spec(spec);
+    if (rc) return rc;
+    if ((rc = check_pools(spec, k, v))) return rc;
+    if (spec->v_aliases_k && v_new) return fail(Q4KV_EINVAL, "v_new must be NULL when v_aliases_k");
+    if (in_format != Q4KV_PARAMS_F16 && in_format != Q4KV_PARAMS_BF16)
+        return fail(Q4KV_EINVAL, "in_format %d is neither 0 (binary16) nor 1 (bfloat16)", in_format);
+    if (layer_begin < 0 || layer_end > spec->num_layers || layer_begin > layer_end)
+        return fail(Q4KV_EINVAL, "bad layer range [%d, %d)", layer_begin, layer_end);
+    if (num_tokens < 0) return fail(Q4KV_EINVAL, "negative count");
+    if (num_tokens == 0 || layer_begin == layer_end) return Q4KV_OK;
+    const int64_t k_row = (int64_t)spec->num_kv_heads * spec->k_dim, v_row = (int64_t)spec->num_kv_heads * spec->v_dim;
+    if (num_tokens > Q4KV_MAX_CHUNK_LEN)
+        return fail(Q4KV_ERANGE, "%d tokens are beyond %d: append them in pieces", num_tokens, Q4KV_MAX_CHUNK_LEN);
+    if (k->num_blocks >= 1 << 23) return fail(Q4KV_ERANGE, "slots of %d blocks do not fit 31 bits", k->num_blocks);
+    if ((layer_end - layer_begin) * (v ? 2LL : 1LL) > 65535) return fail(Q4KV_ERANGE, "at most 65,535 layers of K and V in one call");
+    if (num_tokens * (std::max(k_row, v ? v_row : 0) / 64) >= 1LL << 31) return fail(Q4KV_ERANGE, "2^31 groups on a layer: append them in pieces");
+    if (!k_new || (v && !v_new) || !slot) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (!aligned16(k_new) || !aligned16(v_new)) return fail(Q4KV_EINVAL, "k_new/v_new must be 16-byte aligned");
+    if (k_stride < k_row || (v && v_stride < v_row) || k_stride % 8 || (v && v_stride % 8))
+        return fail(Q4KV_ESHAPE, "token strides %lld, %lld: multiples of 8, no smaller than a token's row", (long long)k_stride,
+                    (long long)v_stride);
+    const hipError_t e = q4kv::launch_append_slots(*spec, *k, v, k_new, v_new, in_format == Q4KV_PARAMS_BF16, k_stride, v_stride, slot,
+                                                   num_tokens, layer_begin, layer_end, compute_units(), (hipStream_t)hip_stream);
     return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "append launch: %s", hipGetErrorString(e));
 }
 
@@ -718,6 +781,115 @@ int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool 
     if (spec->num_layers > 65535) return fail(Q4KV_ERANGE, "at most 65,535 layers");
     const hipError_t e = q4kv::launch_block_copy(*spec, *k, v, src_ids, dst_ids, num_pairs, (hipStream_t)hip_stream);
     return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "copy launch: %s", hipGetErrorString(e));
+}
+
+size_t q4kv_tables_workspace_bytes(int32_t num_agents)
+{
+    if (num_agents < 0 || num_agents > Q4KV_MAX_TABLE_ROWS) {
+        fail(Q4KV_ERANGE, "%d rows, at most %d", num_agents, Q4KV_MAX_TABLE_ROWS);
+        return 0;
+    }
+    return q4kv::tables_workspace_bytes(num_agents);
+}
+
+int q4kv_resize_tables(const q4kv_tables *tables, const int32_t *new_len, int32_t max_tokens, int32_t *token_begin, int32_t *slot,
+                       int32_t *token_agent, int32_t *position, const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v,
+                       void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_tables(tables);
+    if (rc) return rc;
+    if (max_tokens < 0) return fail(Q4KV_EINVAL, "negative count");
+    if (spec && (rc = check_table_pools(tables, spec, k, v, workspace, workspace_bytes))) return rc;
+    if (!spec && (k || v)) return fail(Q4KV_EINVAL, "pools without a spec");
+    if (tables->num_agents > 0 && !new_len) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (max_tokens > 0 && (!token_begin || !slot)) return fail(Q4KV_EINVAL, "a slot map without its arrays");
+    q4kv::TablesArgs a = {};
+    a.tables = tables;
+    a.spec = spec;
+    a.k = k;
+    a.v = v;
+    a.new_len = new_len;
+    a.max_tokens = max_tokens;
+    a.token_begin = token_begin;
+    a.slot = slot;
+    a.token_agent = token_agent;
+    a.position = position;
+    a.workspace = workspace;
+    a.compute_units = compute_units();
+    const hipError_t e = q4kv::launch_resize_tables(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "table launch: %s", hipGetErrorString(e));
+}
+
+int q4kv_beam_reorder(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const q4kv_tables *tables, const int32_t *parent,
+                      void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_tables(tables);
+    if (rc || (rc = check_table_pools(tables, spec, k, v, workspace, workspace_bytes))) return rc;
+    if (tables->num_agents == 0) return Q4KV_OK;
+    if (!parent) return fail(Q4KV_EINVAL, "NULL pointer");
+    q4kv::TablesArgs a = {};
+    a.tables = tables;
+    a.spec = spec;
+    a.k = k;
+    a.v = v;
+    a.parent = parent;
+    a.workspace = workspace;
+    a.compute_units = compute_units();
+    const hipError_t e = q4kv::launch_beam_reorder(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "table launch: %s", hipGetErrorString(e));
+}
+
+// what q4kv_beam_select and its workspace query have in common
+static int check_beam_sizes(int32_t format, int32_t vocab, int32_t num_agents, int32_t num_out)
+{
+    if (format < 0 || format > 2) return fail(Q4KV_EINVAL, "logits_format %d is none of 0 (binary16), 1 (bfloat16), 2 (binary32)", format);
+    if (vocab <= 0 || num_agents < 0) return fail(Q4KV_EINVAL, "negative count");
+    if (vocab > 1 << 30) return fail(Q4KV_ERANGE, "a vocabulary of %d tokens, at most 2^30", vocab);
+    if (num_out < 1 || num_out > Q4KV_MAX_BEAM_OUT) return fail(Q4KV_ERANGE, "num_out %d, from 1 to %d", num_out, Q4KV_MAX_BEAM_OUT);
+    if ((int64_t)num_agents * q4kv::beam_select_spans(format, vocab, num_agents, compute_units()) >= 1LL << 31)
+        return fail(Q4KV_ERANGE, "%d rows of %d tokens: choose for fewer groups at a time", num_agents, vocab);
+    return Q4KV_OK;
+}
+
+size_t q4kv_beam_select_workspace_bytes(int32_t logits_format, int32_t vocab, int32_t num_agents, int32_t num_out)
+{
+    if (check_beam_sizes(logits_format, vocab, num_agents, num_out)) return 0;
+    return std::max<size_t>(16, q4kv::beam_select_workspace_bytes(logits_format, vocab, num_agents, num_out, compute_units()));
+}
+
+int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stride, int32_t vocab, int32_t num_agents, const float *score,
+                     const int32_t *end_token, const int32_t *group_begin, int32_t num_groups, int32_t num_out, int32_t *parent,
+                     int32_t *token, float *total, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const int rc = check_beam_sizes(logits_format, vocab, num_agents, num_out);
+    if (rc) return rc;
+    if (num_groups < 0) return fail(Q4KV_EINVAL, "negative count");
+    if (num_groups == 0) return Q4KV_OK;
+    if (row_stride < vocab && num_agents > 1) return fail(Q4KV_ESHAPE, "rows of %d tokens, %lld elements apart", vocab, (long long)row_stride);
+    if ((num_agents > 0 && (!logits || !score)) || !group_begin || !parent || !token || !total) return fail(Q4KV_EINVAL, "NULL pointer");
+    if (reinterpret_cast<uintptr_t>(logits) % (logits_format == 2 ? 4 : 2)) return fail(Q4KV_EINVAL, "logits must be aligned to an element");
+    const int units = compute_units();
+    if (num_agents > 0 && (!workspace || workspace_bytes < q4kv::beam_select_workspace_bytes(logits_format, vocab, num_agents, num_out, units)))
+        return fail(Q4KV_EWORKSPACE, "workspace too small or missing");
+    if (!aligned16(workspace)) return fail(Q4KV_EINVAL, "workspace must be 16-byte aligned");
+    q4kv::BeamSelectArgs a;
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.score = score;
+    a.end_token = end_token;
+    a.group_begin = group_begin;
+    a.parent = parent;
+    a.token = token;
+    a.total = total;
+    a.workspace = workspace;
+    a.format = logits_format;
+    a.vocab = vocab;
+    a.rows = num_agents;
+    a.groups = num_groups;
+    a.num_out = num_out;
+    a.compute_units = units;
+    const hipError_t e = q4kv::launch_beam_select(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "beam launch: %s", hipGetErrorString(e));
 }
 
 int q4kv_read_probe(const void *src, size_t bytes, uint32_t *sink, void *hip_stream)

@@ -1,0 +1,586 @@
+// Block tables that live on the GPU: lengths of many rows changed at once, with the slots of the tokens that came in
+// (q4kv_resize_tables), and rows that become copies of other rows (q4kv_beam_reorder).
+//
+// The state is a count per block: how many rows list it.  A block of count 0 is free; free blocks are handed out lowest id first,
+// to rows in order, so that every result follows from the arguments alone (counts go up and down by atomics, whose order does not
+// show).  The bookkeeping is a chain of prefix sums over at most 2,048 rows with a trip to memory between them: one workgroup,
+// two rows a lane, sums in registers and LDS, no launch in between.  What it has to read beside the rows are the counts, in order until
+// enough free ones are found.  Work of uneven size per row (blocks freed, blocks taken, tokens mapped) is laid out flat and the row
+// of an item found by bisection in the prefix sums.
+//
+// A block in which a row ends and that others list too is copied by a kernel of its own (the pools of all layers; HBM-bound).
+#include "q4_device.h"
+#include "q4kv_internal.h"
+
+namespace q4kv {
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kRows = Q4KV_MAX_TABLE_ROWS;
+constexpr int kPer = kRows / kThreads; // rows of a lane: consecutive ones
+constexpr int kFree = 4096;            // free blocks kept in LDS; a call that takes more reads the counts twice
+constexpr int kHash = 2 * kRows;       // places for the shared blocks that rows end in
+constexpr int kRefs = 16;              // counts a lane reads at a time
+
+// Blocks to copy: counts[0] pairs; then sources, destinations, tokens.
+struct Moves {
+    int32_t *count, *src, *dst, *tokens;
+};
+
+struct TablesParams {
+    int32_t *table, *len, *refs, *refused;
+    int32_t agents, max_blocks, num_blocks;
+    const int32_t *new_len; // resize
+    const int32_t *parent;  // reorder
+    int32_t max_tokens;
+    int32_t *token_begin, *slot, *token_agent, *position;
+    Moves moves;
+    bool copies;  // shared blocks can be copied
+    bool map_here; // the slot map is written by the same workgroup
+};
+
+struct Shared {
+    int32_t before[kRows], after[kRows]; // lengths
+    uint32_t items[kRows + 1];           // first item of a row: blocks freed, then blocks taken
+    uint32_t tokens[kRows + 1];
+    uint8_t copy[kRows];
+    int32_t free[kFree];
+    int32_t key[kHash], lowest[kHash], rows[kHash];
+    uint32_t wave[2][kThreads / kWave];
+    int32_t first_refused, moves, refused;
+};
+
+__device__ __forceinline__ int blocks_of(int tokens) { return (tokens >> 8) + ((tokens & 255) != 0); }
+__device__ __forceinline__ uint32_t sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Exclusive prefix sums of two numbers over the lanes of the workgroup, and their totals; sums that pass 32 bits stay at the top.
+__device__ __forceinline__ void scan(Shared &s, uint32_t a, uint32_t b, uint32_t &ex_a, uint32_t &ex_b, uint32_t &all_a, uint32_t &all_b)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t ia = a, ib = b;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const uint32_t ua = __shfl_up(ia, off), ub = __shfl_up(ib, off);
+        if (lane >= off) {
+            ia = sat(ia, ua);
+            ib = sat(ib, ub);
+        }
+    }
+    __syncthreads();
+    if (lane == 63) {
+        s.wave[0][wave] = ia;
+        s.wave[1][wave] = ib;
+    }
+    __syncthreads();
+    uint32_t la = __shfl_up(ia, 1), lb = __shfl_up(ib, 1); // what the lanes below have
+    if (lane == 0) la = lb = 0;
+    ex_a = ex_b = all_a = all_b = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) {
+        if (w == wave) {
+            ex_a = all_a;
+            ex_b = all_b;
+        }
+        all_a = sat(all_a, s.wave[0][w]);
+        all_b = sat(all_b, s.wave[1][w]);
+    }
+    ex_a = sat(ex_a, la);
+    ex_b = sat(ex_b, lb);
+}
+
+// The row that item i belongs to: the last whose first item is not behind i.
+__device__ __forceinline__ int row_of(const uint32_t *first, int rows, uint32_t i)
+{
+    int lo = 0, hi = rows;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// What one thread reads of the counts: kRefs from `at` on, bit i set where count i is 0.
+__device__ __forceinline__ uint32_t free_bits(const TablesParams &p, int64_t at)
+{
+    uint32_t bits = 0;
+    if (at + kRefs <= p.num_blocks) {
+        int4 c[kRefs / 4];
+#pragma unroll
+        for (int i = 0; i < kRefs / 4; ++i) c[i] = reinterpret_cast<const int4 *>(p.refs + at)[i];
+#pragma unroll
+        for (int i = 0; i < kRefs / 4; ++i)
+            bits |= (uint32_t)(c[i].x == 0) << (4 * i) | (uint32_t)(c[i].y == 0) << (4 * i + 1) | (uint32_t)(c[i].z == 0) << (4 * i + 2) |
+                    (uint32_t)(c[i].w == 0) << (4 * i + 3);
+    } else {
+        for (int i = 0; i < kRefs; ++i)
+            if (at + i < p.num_blocks && p.refs[at + i] == 0) bits |= 1u << i;
+    }
+    return bits;
+}
+
+// A free block becomes item i of the rows' items.
+__device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uint32_t i, int32_t id)
+{
+    const int r = row_of(s.items, p.agents, i), at = min(s.before[r], s.after[r]);
+    const int k = (int)(i - s.items[r]);
+    int32_t *row = p.table + (int64_t)r * p.max_blocks;
+    p.refs[id] = 1;
+    if (s.copy[r] && k == 0) {
+        const int32_t src = row[at >> 8];
+        atomicSub(&p.refs[src], 1);
+        row[at >> 8] = id;
+        const int m = atomicAdd(&s.moves, 1);
+        p.moves.src[m] = src;
+        p.moves.dst[m] = id;
+        p.moves.tokens[m] = at & 255;
+    } else {
+        row[blocks_of(s.before[r]) + k - s.copy[r]] = id;
+    }
+}
+
+// Lane's rows kPer t .. : lengths from `before` (blocks up to there are listed) to `after`; rows that get shorter have given their
+// blocks back.  Finds the blocks that rows end in and share, takes free blocks, writes lengths and the map's bounds.
+__device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const int (&before)[kPer], int (&after)[kPer], int refused)
+{
+    const int t = threadIdx.x;
+    bool shared[kPer], copy[kPer];
+    int32_t last[kPer];
+    int32_t listed[kPer];
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = kPer * t + i, at = min(before[i], after[i]);
+        shared[i] = copy[i] = false;
+        last[i] = -1;
+        if (r < p.agents && (at & 255) && (p.copies || after[i] < before[i])) {
+            last[i] = p.table[(int64_t)r * p.max_blocks + (at >> 8)];
+            if ((uint32_t)last[i] < (uint32_t)p.num_blocks) {
+                listed[i] = p.refs[last[i]];
+                shared[i] = listed[i] > 1;
+            }
+        }
+        any |= shared[i];
+    }
+    if (t == 0) {
+        s.moves = 0;
+        s.refused = 0;
+        s.first_refused = p.agents;
+    }
+    if (__syncthreads_or(any)) {
+        for (int i = t; i < kHash; i += kThreads) {
+            s.key[i] = -1;
+            s.lowest[i] = kRows;
+            s.rows[i] = 0;
+        }
+        __syncthreads();
+        int place[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (!shared[i]) continue;
+            int h = (int)(((uint32_t)last[i] * 2654435769u) >> 20) & (kHash - 1);
+            while (true) { // at most kRows keys in twice as many places
+                const int32_t was = atomicCAS(&s.key[h], -1, last[i]);
+                if (was == -1 || was == last[i]) break;
+                h = (h + 1) & (kHash - 1);
+            }
+            atomicMin(&s.lowest[h], kPer * t + i);
+            atomicAdd(&s.rows[h], 1);
+            place[i] = h;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (shared[i]) copy[i] = !(s.lowest[place[i]] == kPer * t + i && s.rows[place[i]] == listed[i]);
+    }
+    uint32_t need[kPer], more[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (copy[i] && !p.copies) { // cut inside a shared block, and nothing to copy it with
+            const int r = kPer * t + i;
+            atomicSub(&p.refs[last[i]], 1);
+            p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
+            after[i] &= ~255;
+            copy[i] = false;
+            ++refused;
+        }
+        need[i] = (uint32_t)copy[i] + (uint32_t)max(0, blocks_of(after[i]) - blocks_of(before[i]));
+        more[i] = p.max_tokens > 0 ? (uint32_t)max(0, after[i] - before[i]) : 0u;
+    }
+    uint32_t ex_need, ex_more, all_need, all_more;
+    scan(s, sat(need[0], need[1]), sat(more[0], more[1]), ex_need, ex_more, all_need, all_more);
+    const uint32_t first_need[kPer] = {ex_need, sat(ex_need, need[0])}, first_more[kPer] = {ex_more, sat(ex_more, more[0])};
+    // free blocks, lowest first, as far as they are needed
+    uint32_t found = 0;
+    for (int64_t base = 0; base < p.num_blocks && found < all_need; base += kThreads * kRefs) {
+        const uint32_t bits = free_bits(p, base + (int64_t)t * kRefs);
+        uint32_t ex, none, all, none_all;
+        scan(s, __popc(bits), 0, ex, none, all, none_all);
+        uint32_t rank = found + ex;
+        for (uint32_t b = bits; b && rank < kFree; b &= b - 1, ++rank) s.free[rank] = (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1);
+        found += all;
+    }
+    // rows are served in order up to the first that cannot be
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const bool fails = (need[i] || more[i]) &&
+                           (sat(first_need[i], need[i]) > found || (p.max_tokens > 0 && sat(first_more[i], more[i]) > (uint32_t)p.max_tokens));
+        if (fails) atomicMin(&s.first_refused, kPer * t + i);
+    }
+    __syncthreads();
+    const int first_refused = s.first_refused;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = kPer * t + i;
+        if (r < p.agents) {
+            if (r >= first_refused && (need[i] || after[i] > before[i])) {
+                ++refused;
+                if (after[i] > before[i]) { // stays as it was
+                    after[i] = before[i];
+                } else {
+                    atomicSub(&p.refs[last[i]], 1);
+                    p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
+                    after[i] &= ~255;
+                }
+                copy[i] = false;
+            }
+            p.len[r] = after[i];
+            s.before[r] = before[i];
+            s.after[r] = after[i];
+            s.items[r] = first_need[i];
+            s.tokens[r] = first_more[i];
+            s.copy[r] = copy[i];
+        }
+        if (r == first_refused) { // the items and tokens of the rows in front of it
+            s.items[p.agents] = first_need[i];
+            s.tokens[p.agents] = first_more[i];
+        }
+    }
+    if (t == 0 && first_refused == p.agents) {
+        s.items[p.agents] = all_need;
+        s.tokens[p.agents] = all_more;
+    }
+    if (refused) atomicAdd(&s.refused, refused);
+    __syncthreads();
+    const uint32_t taken = s.items[p.agents], mapped = s.tokens[p.agents];
+    if (taken > kFree) {
+        // more than LDS holds: those behind are taken while the counts are read once more (before any of them changes)
+        uint32_t seen = 0;
+        for (int64_t base = 0; base < p.num_blocks && seen < taken; base += kThreads * kRefs) {
+            const uint32_t bits = free_bits(p, base + (int64_t)t * kRefs);
+            uint32_t ex, none, all, none_all;
+            scan(s, __popc(bits), 0, ex, none, all, none_all);
+            uint32_t rank = seen + ex;
+            for (uint32_t b = bits; b && rank < taken; b &= b - 1, ++rank)
+                if (rank >= kFree) take_block(p, s, rank, (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1));
+            seen += all;
+        }
+        __syncthreads();
+    }
+    for (uint32_t i = t; i < min(taken, (uint32_t)kFree); i += kThreads) take_block(p, s, i, s.free[i]);
+    if (p.max_tokens > 0) {
+        for (int r = t; r < p.agents; r += kThreads) p.token_begin[r] = (int32_t)min(s.tokens[r], mapped);
+        if (t == 0) p.token_begin[p.agents] = (int32_t)mapped;
+    }
+    __syncthreads();
+    if (t == 0) {
+        if (p.refused) *p.refused = s.refused;
+        if (p.copies) *p.moves.count = s.moves;
+    }
+    if (p.max_tokens > 0 && p.map_here) {
+        for (int i = t; i < p.max_tokens; i += kThreads) {
+            int32_t slot = -1, agent = -1, position = -1;
+            if ((uint32_t)i < mapped) {
+                agent = row_of(s.tokens, p.agents, i);
+                position = s.before[agent] + (int)(i - s.tokens[agent]);
+                const int32_t id = p.table[(int64_t)agent * p.max_blocks + (position >> 8)];
+                if ((uint32_t)id < (uint32_t)p.num_blocks) slot = id * kBlockTokens + (position & 255);
+            }
+            p.slot[i] = slot;
+            if (p.token_agent) p.token_agent[i] = agent;
+            if (p.position) p.position[i] = position;
+        }
+    }
+}
+
+__device__ __forceinline__ int length_of(const TablesParams &p, int r)
+{
+    const int64_t most = min((int64_t)p.max_blocks * kBlockTokens, (int64_t)0x7fffffff);
+    return (int)min((int64_t)max(p.len[r], 0), most);
+}
+
+__global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
+{
+    __shared__ Shared s;
+    const int t = threadIdx.x;
+    int before[kPer], after[kPer], refused = 0;
+    uint32_t gone[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = kPer * t + i;
+        before[i] = after[i] = 0;
+        if (r < p.agents) {
+            before[i] = after[i] = length_of(p, r);
+            const int32_t wanted = p.new_len[r];
+            if (wanted > (int64_t)p.max_blocks * kBlockTokens) ++refused;
+            else if (wanted >= 0) after[i] = wanted;
+        }
+        gone[i] = (uint32_t)max(0, blocks_of(before[i]) - blocks_of(after[i]));
+    }
+    uint32_t ex, none, all, none_all;
+    scan(s, sat(gone[0], gone[1]), 0, ex, none, all, none_all);
+    if (all > 0) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = kPer * t + i;
+            if (r >= p.agents) continue;
+            s.items[r] = i == 0 ? ex : sat(ex, gone[0]);
+            s.after[r] = after[i];
+        }
+        __syncthreads();
+        for (uint32_t i = t; i < all; i += kThreads) {
+            const int r = row_of(s.items, p.agents, i);
+            int32_t *entry = p.table + (int64_t)r * p.max_blocks + blocks_of(s.after[r]) + (i - s.items[r]);
+            const int32_t id = *entry;
+            if ((uint32_t)id < (uint32_t)p.num_blocks) atomicSub(&p.refs[id], 1);
+            *entry = -1;
+        }
+        __threadfence(); // the counts are read from here on
+        __syncthreads();
+    }
+    settle(p, s, before, after, refused);
+}
+
+// The map of a call with many tokens, behind resize_kernel.
+__global__ __launch_bounds__(256) void slot_map_kernel(TablesParams p)
+{
+    __shared__ uint32_t s_first[kRows + 1];
+    for (int r = threadIdx.x; r <= p.agents; r += 256) s_first[r] = (uint32_t)p.token_begin[r];
+    __syncthreads();
+    const uint32_t mapped = s_first[p.agents];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.max_tokens; i += (int64_t)gridDim.x * 256) {
+        int32_t slot = -1, agent = -1, position = -1;
+        if (i < mapped) {
+            agent = row_of(s_first, p.agents, (uint32_t)i);
+            position = p.len[agent] - (int32_t)(s_first[agent + 1] - (uint32_t)i);
+            const int32_t id = p.table[(int64_t)agent * p.max_blocks + (position >> 8)];
+            if ((uint32_t)id < (uint32_t)p.num_blocks) slot = id * kBlockTokens + (position & 255);
+        }
+        p.slot[i] = slot;
+        if (p.token_agent) p.token_agent[i] = agent;
+        if (p.position) p.position[i] = position;
+    }
+}
+
+// Rows' entries of a slab of columns become those of their parents.  All of a slab's entries are read before the first is
+// written, kHeld a lane; columns have nothing to do with each other, so that any number of workgroups shares the table.
+constexpr int kHeld = 8;
+__device__ __forceinline__ void gather_rows(const TablesParams &p, Shared &s, int first_slab, int slabs)
+{
+    const int t = threadIdx.x;
+    for (int r = t; r < p.agents; r += kThreads) {
+        const int32_t from = p.parent[r];
+        const bool has = from >= 0 && from < p.agents;
+        s.key[r] = has ? from : -1;
+        s.before[r] = blocks_of(length_of(p, r));
+        s.after[r] = has ? blocks_of(length_of(p, from)) : 0;
+    }
+    __syncthreads();
+    const int cols = max(1, kThreads * kHeld / p.agents); // at least kHeld / kPer
+    for (int64_t c0 = (int64_t)first_slab * cols; c0 < p.max_blocks; c0 += (int64_t)slabs * cols) {
+        int32_t was[kHeld], is[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int i = k * kThreads + t, r = i / cols;
+            const int64_t c = c0 + i % cols;
+            was[k] = is[k] = -1;
+            if (r >= p.agents || c >= p.max_blocks) continue;
+            if (c < s.before[r]) was[k] = p.table[(int64_t)r * p.max_blocks + c];
+            if (c < s.after[r]) is[k] = p.table[(int64_t)s.key[r] * p.max_blocks + c];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int i = k * kThreads + t, r = i / cols;
+            const int64_t c = c0 + i % cols;
+            if (r >= p.agents || c >= p.max_blocks || s.key[r] == r || c >= max(s.before[r], s.after[r])) continue;
+            if (was[k] == is[k] && c < s.before[r]) continue; // the prefix that rows share
+            if ((uint32_t)was[k] < (uint32_t)p.num_blocks) atomicSub(&p.refs[was[k]], 1);
+            if ((uint32_t)is[k] < (uint32_t)p.num_blocks) atomicAdd(&p.refs[is[k]], 1);
+            p.table[(int64_t)r * p.max_blocks + c] = is[k];
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void gather_kernel(TablesParams p)
+{
+    __shared__ Shared s;
+    gather_rows(p, s, blockIdx.x, gridDim.x);
+}
+
+template <bool ALONE>
+__global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
+{
+    __shared__ Shared s;
+    if (ALONE) {
+        gather_rows(p, s, 0, 1);
+        __threadfence();
+        __syncthreads();
+    }
+    int before[kPer], after[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = kPer * (int)threadIdx.x + i;
+        int32_t from = -1;
+        if (r < p.agents) from = p.parent[r];
+        before[i] = after[i] = from >= 0 && from < p.agents ? length_of(p, from) : 0;
+    }
+    __syncthreads(); // lengths are read before the first is written
+    settle(p, s, before, after, 0);
+}
+
+// The first tokens of blocks copied to other blocks, on every layer.  A unit is one head's plane of a (pair, layer): K codes,
+// scale, bias and the same of V, each a run of tokens * (bytes per token) bytes that begins on a multiple of 16 bytes; taken as one
+// list of 16-byte granules, kCopyUnit of them per step of a workgroup, every load in front of the first store.
+constexpr int kCopyThreads = 256, kCopyLoads = 4, kCopyUnit = kCopyThreads * kCopyLoads;
+struct TailParams {
+    unsigned char *pool[6];
+    int32_t token_bytes[6];
+    int32_t pieces, heads, layers, num_blocks, chunks; // chunks: steps of a unit of 256 tokens
+    Moves moves;
+};
+
+__global__ __launch_bounds__(kCopyThreads) void tail_copy_kernel(TailParams p)
+{
+    typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+    const int pairs = *p.moves.count;
+    const int64_t per_pair = (int64_t)p.layers * p.heads * p.chunks, items = pairs * per_pair;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int pair = (int)(item / per_pair);
+        const int64_t in_pair = item - pair * per_pair;
+        const int plane = (int)(in_pair / p.chunks), chunk = (int)(in_pair - (int64_t)plane * p.chunks);
+        const int layer = plane / p.heads, head = plane - layer * p.heads;
+        const int src = p.moves.src[pair], dst = p.moves.dst[pair], tokens = p.moves.tokens[pair];
+        const int64_t from = ((int64_t)layer * p.num_blocks + src) * p.heads + head, to = ((int64_t)layer * p.num_blocks + dst) * p.heads + head;
+        u4_t data[kCopyLoads];
+        unsigned char *out[kCopyLoads];
+        int bytes[kCopyLoads];
+#pragma unroll
+        for (int j = 0; j < kCopyLoads; ++j) {
+            int g = chunk * kCopyUnit + j * kCopyThreads + (int)threadIdx.x;
+            out[j] = nullptr;
+            bytes[j] = 0;
+#pragma unroll
+            for (int k = 0; k < 6; ++k) {
+                if (k >= p.pieces || out[j]) continue;
+                const int run = tokens * p.token_bytes[k], granules = (run + 15) >> 4;
+                if (g < granules) {
+                    const int64_t plane_bytes = (int64_t)p.token_bytes[k] * kBlockTokens;
+                    bytes[j] = min(16, run - 16 * g);
+                    data[j] = *reinterpret_cast<const u4_t *>(p.pool[k] + from * plane_bytes + 16 * g); // inside the plane: a multiple of 512 bytes
+                    out[j] = p.pool[k] + to * plane_bytes + 16 * g;
+                } else {
+                    g -= granules;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kCopyLoads; ++j) {
+            if (bytes[j] == 16) {
+                *reinterpret_cast<u4_t *>(out[j]) = data[j];
+            } else { // the last parameters of a run: pairs of bytes, what is behind them stays
+                for (int i = 0; i < bytes[j] / 2; ++i)
+                    reinterpret_cast<uint16_t *>(out[j])[i] = (uint16_t)(data[j][i >> 1] >> (16 * (i & 1)));
+            }
+        }
+    }
+}
+
+TablesParams params_of(const TablesArgs &a)
+{
+    TablesParams p = {};
+    p.table = a.tables->block_table;
+    p.len = a.tables->seq_len;
+    p.refs = a.tables->refs;
+    p.refused = a.tables->refused;
+    p.agents = a.tables->num_agents;
+    p.max_blocks = a.tables->max_blocks;
+    p.num_blocks = a.tables->num_blocks;
+    p.copies = a.spec != nullptr;
+    if (p.copies) {
+        int32_t *w = static_cast<int32_t *>(a.workspace);
+        p.moves = Moves{w, w + 64, w + 64 + p.agents, w + 64 + 2 * p.agents};
+    }
+    return p;
+}
+
+hipError_t launch_tail_copy(const TablesArgs &a, const Moves &moves, hipStream_t stream)
+{
+    TailParams p = {};
+    const q4kv_pool *const pools[2] = {a.k, a.v};
+    const int dims[2] = {a.spec->k_dim, a.spec->v_dim};
+    int granules = 0;
+    for (int i = 0; i < (a.v ? 6 : 3); ++i) {
+        const q4kv_pool &pool = *pools[i / 3];
+        const int dim = dims[i / 3];
+        p.pool[i] = i % 3 == 0 ? reinterpret_cast<unsigned char *>(pool.codes) : reinterpret_cast<unsigned char *>(i % 3 == 1 ? pool.scale : pool.bias);
+        p.token_bytes[i] = i % 3 == 0 ? dim / 2 : dim / kGroup * 2;
+        granules += p.token_bytes[i] * kBlockTokens / 16;
+    }
+    p.pieces = a.v ? 6 : 3;
+    p.heads = a.spec->num_kv_heads;
+    p.layers = a.spec->num_layers;
+    p.num_blocks = a.k->num_blocks;
+    p.chunks = (granules + kCopyUnit - 1) / kCopyUnit;
+    p.moves = moves;
+    const int64_t most = (int64_t)a.tables->num_agents * p.layers * p.heads * p.chunks, cap = 8LL * a.compute_units;
+    hipLaunchKernelGGL(tail_copy_kernel, dim3((unsigned)(most < cap ? most : cap)), dim3(kCopyThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+} // namespace
+
+size_t tables_workspace_bytes(int num_agents) { return (size_t)(64 + 3 * (size_t)num_agents) * sizeof(int32_t); }
+
+hipError_t launch_resize_tables(const TablesArgs &a, hipStream_t stream)
+{
+    TablesParams p = params_of(a);
+    p.new_len = a.new_len;
+    p.max_tokens = a.max_tokens;
+    p.token_begin = a.token_begin;
+    p.slot = a.slot;
+    p.token_agent = a.token_agent;
+    p.position = a.position;
+    p.map_here = a.max_tokens <= 4096;
+    hipLaunchKernelGGL(resize_kernel, dim3(1), dim3(kThreads), 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && p.max_tokens > 0 && !p.map_here) {
+        const int64_t blocks = ((int64_t)p.max_tokens + 255) / 256, cap = 8LL * a.compute_units;
+        hipLaunchKernelGGL(slot_map_kernel, dim3((unsigned)(blocks < cap ? blocks : cap)), dim3(256), 0, stream, p);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && p.copies && p.agents > 0) e = launch_tail_copy(a, p.moves, stream);
+    return e;
+}
+
+hipError_t launch_beam_reorder(const TablesArgs &a, hipStream_t stream)
+{
+    TablesParams p = params_of(a);
+    p.parent = a.parent;
+    const int64_t entries = (int64_t)p.agents * p.max_blocks;
+    hipError_t e = hipSuccess;
+    if (entries <= 4 * kThreads * kHeld) {
+        hipLaunchKernelGGL(reorder_kernel<true>, dim3(1), dim3(kThreads), 0, stream, p);
+    } else {
+        const int cols = kThreads * kHeld / p.agents;
+        const int64_t slabs = ((int64_t)p.max_blocks + cols - 1) / cols, cap = 2LL * a.compute_units;
+        hipLaunchKernelGGL(gather_kernel, dim3((unsigned)(slabs < cap ? slabs : cap)), dim3(kThreads), 0, stream, p);
+        e = hipGetLastError();
+        if (e == hipSuccess) hipLaunchKernelGGL(reorder_kernel<false>, dim3(1), dim3(kThreads), 0, stream, p);
+    }
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e == hipSuccess) e = launch_tail_copy(a, p.moves, stream);
+    return e;
+}
+
+} // namespace q4kv

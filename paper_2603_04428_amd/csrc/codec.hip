@@ -6,6 +6,9 @@
 // Work layout: one group of 64 elements is handled by 8 consecutive lanes; each lane moves
 // 16 bytes of binary16 input (8 elements) and one 32-bit word of codes, so both the loads and
 // the stores of a wavefront are contiguous.
+#include <algorithm>
+#include <type_traits>
+
 #include "q4_device.h"
 #include "q4kv_internal.h"
 #include "quantize_octet.h"
@@ -92,15 +95,34 @@ struct AppendPool {
     uint32_t *codes;
     uint16_t *scale, *bias;
     int groups_per_row;
+    int64_t token_stride; // slots: elements from a token's row to the next one's
 };
 struct AppendParams {
     AppendPool pool[2];
     const int32_t *block_table;
     const int32_t *seq_len_before;
     int max_blocks, chunk_len, heads, layer_begin, num_blocks, layers;
+    const int32_t *slot;
 };
 
-template <bool BF>
+// How the rows of a call lie and where they go.  kAgents: [layer][agent][chunk token][head], behind the agents' cached tokens.
+// kSlots: [layer][token], a fixed stride apart, each into its slot; kSlotsBf: the same with bfloat16 rows, rounded once to binary16.
+// A call with slots is one agent's to the kernels, whose chunk is all of its tokens.
+enum AppendRows { kAgents, kSlots, kSlotsBf };
+
+// eight bfloat16 values as binary16
+__device__ __forceinline__ uint4 halves_of(uint4 raw)
+{
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        h[i] = (uint32_t)float_to_half_bits(__builtin_bit_cast(float, w[i] << 16)) |
+               (uint32_t)float_to_half_bits(__builtin_bit_cast(float, w[i] & 0xffff0000u)) << 16;
+    return make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+template <bool BF, AppendRows ROWS>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 {
     // a wave's round is 64 groups in four steps: whole lines of scales and biases (long chunks on many agents: the kernel is
@@ -119,8 +141,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
     uint16_t *__restrict__ scale = pp.pool[which].scale, *__restrict__ bias = pp.pool[which].bias;
     const uint32_t per_unit = (uint32_t)p.chunk_len * p.heads * p.groups_per_row; // groups of one (layer, agent)
     const int64_t src0 = ((int64_t)li * agents + a) * per_unit;
-    const int n0 = p.seq_len_before[a];
-    const int32_t *table = p.block_table + (int64_t)a * p.max_blocks;
+    const int64_t stride = pp.pool[which].token_stride;
+    const int n0 = ROWS == kAgents ? p.seq_len_before[a] : 0;
+    const int32_t *table = ROWS == kAgents ? p.block_table + (int64_t)a * p.max_blocks : pp.slot;
     // generations of the launch: workgroups in launch order (x fastest), about 256 of them per generation
     const uint32_t linear = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
     const int generation = linear / max(1u, gridDim.x * gridDim.y * gridDim.z / kWorkgroupsPerCu);
@@ -131,7 +154,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
     // by those (the vector ALUs were busy nine tenths of its time).
     __shared__ uint16_t s_par[kThreads / 64][2][64];
     __shared__ int64_t s_dst[kThreads / 64][64];  // group index in the pool, -1: skipped
-    __shared__ uint32_t s_src[kThreads / 64][64]; // group index in this (layer, agent)'s source rows
+    // group index in this (layer, agent)'s source rows; with slots the distance from this layer's first row, in 8 elements
+    typedef std::conditional_t<ROWS == kAgents, uint32_t, int64_t> src_t;
+    __shared__ src_t s_src[kThreads / 64][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool words_ok = ((reinterpret_cast<uintptr_t>(scale) | reinterpret_cast<uintptr_t>(bias)) & 3u) == 0;
     const float inv_gpr = 1.0f / (float)p.groups_per_row, inv_chunk = 1.0f / (float)p.chunk_len;
@@ -153,8 +178,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const uint32_t l = step * 16 + 8 * j + (lane >> 3);
-                raw[j] = c0 + l < per_unit ? *reinterpret_cast<const uint4 *>(x + (src0 + s_src[wave][l]) * kGroup + sub * 8)
-                                           : make_uint4(0, 0, 0, 0);
+                const int64_t at = ROWS == kAgents ? (src0 + s_src[wave][l]) * kGroup + sub * 8
+                                                   : (int64_t)li * p.chunk_len * stride + (s_src[wave][l] + sub) * 8;
+                raw[j] = c0 + l < per_unit ? *reinterpret_cast<const uint4 *>(x + at) : make_uint4(0, 0, 0, 0);
+                if (ROWS == kSlotsBf) raw[j] = halves_of(raw[j]);
             }
         };
         {
@@ -165,13 +192,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
             const uint32_t heads = (uint32_t)(((float)cl + 0.5f) * inv_chunk);
             const uint32_t h = h0 + heads, c = cl - heads * p.chunk_len;
             const bool mine = lane < ROUND && c0 + lane < per_unit;
-            if (lane < ROUND) s_src[wave][lane] = (c * p.heads + h) * p.groups_per_row + g;
+            if (lane < ROUND) {
+                if constexpr (ROWS == kAgents) s_src[wave][lane] = (c * p.heads + h) * p.groups_per_row + g;
+                else s_src[wave][lane] = c * (stride / 8) + (h * p.groups_per_row + g) * 8;
+            }
             int64_t dgrp = -1;
             if (mine) {
-                const int t = n0 + (int)c;
+                const int t = ROWS == kAgents ? n0 + (int)c : table[c];
                 const int bi = t / kBlockTokens;
-                if (t >= 0 && bi < p.max_blocks) {
-                    const int blk = table[bi];
+                if (t >= 0 && (ROWS != kAgents || bi < p.max_blocks)) {
+                    const int blk = ROWS == kAgents ? table[bi] : bi;
                     if (blk >= 0 && blk < p.num_blocks) {
                         const int64_t drow = (((int64_t)(p.layer_begin + li) * p.num_blocks + blk) * p.heads + h) * kBlockTokens +
                                              (t % kBlockTokens);
@@ -228,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 // and of instructions that each wave runs once.  An octet of lanes takes one group, everything stays in registers, and the
 // row is asked for before the length and the table.  Twelve 256-wide layers of ten agents, a plan, an append and a call each
 // 435 -> 426 us, nine 192 + 128-wide ones of three agents 205 -> 195 (rounds of 16 groups per wave before).
-template <bool BF>
+template <bool BF, AppendRows ROWS>
 __global__ __launch_bounds__(kThreads) void append_few_kernel(AppendParams p)
 {
     const int sub = threadIdx.x & 7;
@@ -237,15 +267,18 @@ __global__ __launch_bounds__(kThreads) void append_few_kernel(AppendParams p)
     const uint32_t per_row = p.pool[which].groups_per_row, chunk = p.chunk_len;
     const uint32_t i = blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3); // group in the order of the pool: head, token, group
     if (i >= chunk * p.heads * per_row) return;
-    const int n0 = p.seq_len_before[a];
+    const int n0 = ROWS == kAgents ? p.seq_len_before[a] : 0;
     // quotients of numbers below 2^21 as in the kernel above
     const uint32_t row = (uint32_t)(((float)i + 0.5f) * (1.0f / (float)per_row)), g = i - row * per_row;
     const uint32_t h = (uint32_t)(((float)row + 0.5f) * (1.0f / (float)chunk)), c = row - h * chunk;
-    const int64_t src = ((((int64_t)li * gridDim.y + a) * chunk + c) * p.heads + h) * per_row + g;
-    const uint4 raw = *reinterpret_cast<const uint4 *>(p.pool[which].x + src * kGroup + sub * 8);
-    const int t = n0 + (int)c, bi = t / kBlockTokens;
+    int64_t src = (((((int64_t)li * gridDim.y + a) * chunk + c) * p.heads + h) * per_row + g) * kGroup;
+    if (ROWS != kAgents) src = ((int64_t)li * chunk + c) * p.pool[which].token_stride + (h * per_row + g) * kGroup;
+    uint4 raw = *reinterpret_cast<const uint4 *>(p.pool[which].x + src + sub * 8);
+    if (ROWS == kSlotsBf) raw = halves_of(raw);
+    const int t = ROWS == kAgents ? n0 + (int)c : p.slot[c], bi = t / kBlockTokens;
     int blk = -1;
-    if (t >= 0 && bi < p.max_blocks) blk = p.block_table[(int64_t)a * p.max_blocks + bi];
+    if (ROWS != kAgents) blk = t >= 0 ? bi : -1;
+    else if (t >= 0 && bi < p.max_blocks) blk = p.block_table[(int64_t)a * p.max_blocks + bi];
     uint16_t sb, bb;
     const uint32_t word = quantize_octet<BF>(raw, sub, &sb, &bb);
     if (blk < 0 || blk >= p.num_blocks) return;
@@ -337,6 +370,42 @@ hipError_t launch_dequantize(const uint32_t *codes, const uint16_t *scale, const
     return hipGetLastError();
 }
 
+namespace {
+
+template <AppendRows ROWS>
+hipError_t launch_append_rows(const q4kv_spec &spec, const AppendParams &p, bool two_pools, int num_agents, int compute_units, hipStream_t stream)
+{
+    const int layers = p.layers, pools = two_pools ? 2 : 1;
+    const int64_t per_unit = (int64_t)p.chunk_len * spec.num_kv_heads * std::max(p.pool[0].groups_per_row, p.pool[1].groups_per_row); // of the wider pool
+    // workgroups per (pool, layer, agent): enough for the chunk, and at most 8 per compute unit over the whole
+    // launch (rounded down: a launch of 1.2 rounds takes as long as one of 2)
+    const int64_t units = (int64_t)pools * layers * num_agents, slots = (int64_t)compute_units * kWorkgroupsPerCu;
+    // An octet per group while there are at most 96 groups per workgroup slot of the chip (196,608).  Measured (us, rounds of
+    // 64 groups per wave / an octet each): one token of ten agents, 256-wide heads 4.6 / 2.6, of three agents, sixteen 192 +
+    // 128-wide heads 5.3 / 2.6; 70 tokens of four agents, 128-wide 6.8 / 2.8; 512 tokens of one agent, 256-wide 6.8 / 3.5; by
+    // groups: 128,000 8.2 / 7.5, 164,000 9.4 / 8.3, 192,000 10.3 / 10.1, 320,000 13.8 / 14.8, 800,000 29.2 / 31.9.
+    if (units * per_unit <= 96 * slots) {
+        const dim3 grid((unsigned)((per_unit + kThreads / 8 - 1) / (kThreads / 8)), (unsigned)num_agents, (unsigned)(pools * layers));
+        if (spec.param_format == Q4KV_PARAMS_BF16)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_few_kernel<true, ROWS>), grid, dim3(kThreads), 0, stream, p);
+        else
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_few_kernel<false, ROWS>), grid, dim3(kThreads), 0, stream, p);
+        return hipGetLastError();
+    }
+    int64_t gx = (per_unit + kThreads - 1) / kThreads;
+    const int64_t cap = slots / units;
+    if (gx > cap) gx = cap;
+    if (gx < 1) gx = 1;
+    const dim3 grid((unsigned)gx, (unsigned)num_agents, (unsigned)(pools * layers)), block(kThreads);
+    if (spec.param_format == Q4KV_PARAMS_BF16)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(append_kernel<true, ROWS>), grid, block, 0, stream, p);
+    else
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(append_kernel<false, ROWS>), grid, block, 0, stream, p);
+    return hipGetLastError();
+}
+
+} // namespace
+
 hipError_t launch_append(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_pool *v, const uint16_t *k_new,
                          const uint16_t *v_new, const int32_t *block_table, int max_blocks,
                          const int32_t *seq_len_before, int num_agents, int chunk_len, int layer_begin, int layer_end,
@@ -350,8 +419,8 @@ hipError_t launch_append(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_p
     if (per_unit > 0x7fffffffLL || num_agents > 65535 || pools * layers > 65535 || chunk_len > Q4KV_MAX_CHUNK_LEN)
         return hipErrorInvalidValue;
     AppendParams p;
-    p.pool[0] = AppendPool{k_new, k.codes, k.scale, k.bias, gk};
-    p.pool[1] = v ? AppendPool{v_new, v->codes, v->scale, v->bias, gv} : p.pool[0];
+    p.pool[0] = AppendPool{k_new, k.codes, k.scale, k.bias, gk, 0};
+    p.pool[1] = v ? AppendPool{v_new, v->codes, v->scale, v->bias, gv, 0} : p.pool[0];
     p.block_table = block_table;
     p.seq_len_before = seq_len_before;
     p.max_blocks = max_blocks;
@@ -360,31 +429,28 @@ hipError_t launch_append(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_p
     p.layer_begin = layer_begin;
     p.num_blocks = k.num_blocks;
     p.layers = layers;
-    // workgroups per (pool, layer, agent): enough for the chunk, and at most 8 per compute unit over the whole
-    // launch (rounded down: a launch of 1.2 rounds takes as long as one of 2)
-    const int64_t units = (int64_t)pools * layers * num_agents, slots = (int64_t)compute_units * kWorkgroupsPerCu;
-    // An octet per group while there are at most 96 groups per workgroup slot of the chip (196,608).  Measured (us, rounds of
-    // 64 groups per wave / an octet each): one token of ten agents, 256-wide heads 4.6 / 2.6, of three agents, sixteen 192 +
-    // 128-wide heads 5.3 / 2.6; 70 tokens of four agents, 128-wide 6.8 / 2.8; 512 tokens of one agent, 256-wide 6.8 / 3.5; by
-    // groups: 128,000 8.2 / 7.5, 164,000 9.4 / 8.3, 192,000 10.3 / 10.1, 320,000 13.8 / 14.8, 800,000 29.2 / 31.9.
-    if (units * per_unit <= 96 * slots) {
-        const dim3 grid((unsigned)((per_unit + kThreads / 8 - 1) / (kThreads / 8)), (unsigned)num_agents, (unsigned)(pools * layers));
-        if (spec.param_format == Q4KV_PARAMS_BF16)
-            hipLaunchKernelGGL(append_few_kernel<true>, grid, dim3(kThreads), 0, stream, p);
-        else
-            hipLaunchKernelGGL(append_few_kernel<false>, grid, dim3(kThreads), 0, stream, p);
-        return hipGetLastError();
-    }
-    int64_t gx = (per_unit + kThreads - 1) / kThreads;
-    const int64_t cap = slots / units;
-    if (gx > cap) gx = cap;
-    if (gx < 1) gx = 1;
-    const dim3 grid((unsigned)gx, (unsigned)num_agents, (unsigned)(pools * layers)), block(kThreads);
-    if (spec.param_format == Q4KV_PARAMS_BF16)
-        hipLaunchKernelGGL(append_kernel<true>, grid, block, 0, stream, p);
-    else
-        hipLaunchKernelGGL(append_kernel<false>, grid, block, 0, stream, p);
-    return hipGetLastError();
+    p.slot = nullptr;
+    return launch_append_rows<kAgents>(spec, p, v != nullptr, num_agents, compute_units, stream);
+}
+
+hipError_t launch_append_slots(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_pool *v, const void *k_new, const void *v_new,
+                               bool in_bf16, int64_t k_stride, int64_t v_stride, const int32_t *slot, int num_tokens, int layer_begin,
+                               int layer_end, int compute_units, hipStream_t stream)
+{
+    AppendParams p;
+    p.pool[0] = AppendPool{static_cast<const uint16_t *>(k_new), k.codes, k.scale, k.bias, spec.k_dim / kGroup, k_stride};
+    p.pool[1] = v ? AppendPool{static_cast<const uint16_t *>(v_new), v->codes, v->scale, v->bias, spec.v_dim / kGroup, v_stride} : p.pool[0];
+    p.block_table = nullptr;
+    p.seq_len_before = nullptr;
+    p.max_blocks = 0;
+    p.chunk_len = num_tokens;
+    p.heads = spec.num_kv_heads;
+    p.layer_begin = layer_begin;
+    p.num_blocks = k.num_blocks;
+    p.layers = layer_end - layer_begin;
+    p.slot = slot;
+    return in_bf16 ? launch_append_rows<kSlotsBf>(spec, p, v != nullptr, 1, compute_units, stream)
+                   : launch_append_rows<kSlots>(spec, p, v != nullptr, 1, compute_units, stream);
 }
 
 } // namespace q4kv

@@ -19,6 +19,11 @@ hipError_t launch_append(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_p
                          const int32_t *seq_len_before, int num_agents, int chunk_len, int layer_begin, int layer_end,
                          int compute_units, hipStream_t stream);
 
+// q4kv_append_slots (v, v_new: null when the V rows alias the K rows)
+hipError_t launch_append_slots(const q4kv_spec &spec, const q4kv_pool &k, const q4kv_pool *v, const void *k_new, const void *v_new,
+                               bool in_bf16, int64_t k_stride, int64_t v_stride, const int32_t *slot, int num_tokens, int layer_begin,
+                               int layer_end, int compute_units, hipStream_t stream);
+
 // head_append.hip: the arguments of q4kv_norm_rope_append (v, v_new: null when the V rows alias the K rows)
 struct HeadAppendArgs {
     const q4kv_spec *spec;
@@ -122,6 +127,37 @@ hipError_t launch_image_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_
 // below 2^31 bytes, at most 65,535 layers
 hipError_t launch_block_copy(const q4kv_spec &s, const q4kv_pool &k, const q4kv_pool *v, const int32_t *src_ids,
                              const int32_t *dst_ids, int num_pairs, hipStream_t stream);
+
+// block_tables.hip: q4kv_resize_tables (spec, k, v, workspace: null where nothing can be copied; v: null when V aliases K) and
+// q4kv_beam_reorder
+struct TablesArgs {
+    const q4kv_tables *tables;
+    const q4kv_spec *spec;
+    const q4kv_pool *k, *v;
+    const int32_t *new_len, *parent;
+    int max_tokens;
+    int32_t *token_begin, *slot, *token_agent, *position;
+    void *workspace;
+    int compute_units;
+};
+size_t tables_workspace_bytes(int num_agents);
+hipError_t launch_resize_tables(const TablesArgs &a, hipStream_t stream);
+hipError_t launch_beam_reorder(const TablesArgs &a, hipStream_t stream);
+
+// beam_select.hip: q4kv_beam_select (num_groups > 0)
+struct BeamSelectArgs {
+    const void *logits;
+    int64_t row_stride;
+    const float *score;
+    const int32_t *end_token, *group_begin;
+    int32_t *parent, *token;
+    float *total;
+    void *workspace;
+    int format, vocab, rows, groups, num_out, compute_units;
+};
+int beam_select_spans(int format, int vocab, int rows, int compute_units);
+size_t beam_select_workspace_bytes(int format, int vocab, int rows, int num_out, int compute_units);
+hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream);
 
 // read_probe.hip: reads bytes / 16,384 * 16,384 bytes of `src` once; `sink` is one device word that may be written
 hipError_t launch_read_probe(const void *src, size_t bytes, uint32_t *sink, int workgroups, hipStream_t stream);

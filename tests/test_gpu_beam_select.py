@@ -1,0 +1,182 @@
+"""q4kv_beam_select against a plain selection in extended precision.  Which continuations come out has to be equal wherever the
+logarithm's error cannot decide it; ties inside a row, where it has no say, go to the lower token always.
+
+The bound: a term exp(x - ref) of a row's sum has a relative error of at most |x - ref| 2^-24 (its argument, rounded) + 2^-22 (the
+exponential, the sums of up to 32 in binary32).  |x - ref| weighted by the terms is at most ln(vocab) + 1 behind the reference, which
+lies at most 40 below the maximum, where the terms count e^40 times more than all that is in front: LOG = (ln(vocab) + 5) 2^-23."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_04428_amd import binding as b
+from tests.gpu_util import DEV
+from tests.table_model import choose
+
+pytestmark = pytest.mark.gpu
+
+KINDS = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def check(logits, score, bounds, num_out, end=None, pad=0, shift=0):
+    """logits: a CPU tensor of any of the three types."""
+    rows, vocab = logits.shape
+    wide = torch.full((rows * (vocab + pad) + shift + 8,), float("nan"), dtype=logits.dtype, device=DEV)
+    view = wide[shift:shift + rows * (vocab + pad)].view(rows, vocab + pad)[:, :vocab]
+    view.copy_(logits)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    out = b.BeamChoice(len(bounds) - 1, num_out)
+    for t in (out.parent, out.token):
+        t.fill_(-99)
+    b.q4kv_beam_select(view, torch.tensor(score, dtype=torch.float32, device=DEV), ints(bounds), num_out,
+                       end_token=None if end is None else ints(end), out=out)
+    torch.cuda.synchronize()
+    parent, token, total = out.parent.cpu().numpy(), out.token.cpu().numpy(), out.score.cpu().numpy().astype(np.float64)
+    wp, wt, ws, every = choose(logits.double().numpy(), np.array(score, np.float32).astype(np.float64), bounds, num_out, end)
+    log = (np.log(vocab) + 5) * 2.0 ** -23
+    for g in range(len(bounds) - 1):
+        n = int((wp[g] >= 0).sum())
+        assert (parent[g, n:] == -1).all() and (token[g, n:] == -1).all() and (total[g, n:] == -np.inf).all()
+        chosen = list(zip(parent[g, :n].tolist(), token[g, :n].tolist()))
+        assert len(set(chosen)) == n
+        for i, c in enumerate(chosen):
+            exact = every[g][c]
+            with np.errstate(over="ignore"):
+                rounded = np.float64(np.float32(exact))
+            assert total[g, i] == rounded or abs(total[g, i] - exact) <= 2.0 ** -24 * abs(exact) + log, (g, i)
+            if c != (wp[g, i], wt[g, i]):       # only where two rows' totals are within their errors
+                assert abs(exact - ws[g, i]) <= 2 * log and c[0] != wp[g, i], (g, i, c, (wp[g, i], wt[g, i]), exact - ws[g, i])
+        for r in set(parent[g, :n].tolist()):   # a row's own continuations are the first of its order, without exception
+            mine = [t for p, t in chosen if p == r]
+            x = logits[r].double().numpy()
+            x = np.where(np.isnan(x), -np.inf, np.minimum(x, float(np.finfo(np.float32).max)))
+            if end is None or end[r] < 0:
+                assert mine == np.argsort(-x, kind="stable")[:len(mine)].tolist()
+    return out
+
+
+def random_rows(seed, rows, vocab, kind, peak=3.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(rows, vocab, generator=g) * peak).to(KINDS[kind])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [1, 2, 7, 63, 64, 65, 1000, 1023, 1025, 2047, 2048, 2049, 32001, 100003])
+def test_sizes(kind, vocab):
+    rng = np.random.default_rng(vocab)
+    for num_out in (1, 4, 17, 64):
+        check(random_rows(vocab + num_out, 5, vocab, kind), (-rng.random(5) * 3).tolist(), [0, 3, 5], num_out)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 3), (7, 5), (64, 2)])
+def test_rows_any_distance_apart_and_at_any_element(kind, pad, shift):
+    check(random_rows(pad, 6, 5003, kind), [-1.0, 0.0, -0.5, -2.0, -0.1, -3.0], [0, 2, 6], 8, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("rows,groups,num_out", [(1, 1, 1), (70, 1, 64), (256, 64, 4), (300, 7, 33), (1000, 500, 2)])
+def test_many_rows(rows, groups, num_out):
+    rng = np.random.default_rng(rows)
+    bounds = [0] + sorted(rng.integers(0, rows + 1, groups - 1).tolist()) + [rows]   # groups of all sizes, empty ones among them
+    check(random_rows(rows, rows, 3001, "f16"), (-rng.random(rows) * 8).tolist(), bounds, num_out)
+
+
+def test_bounds_outside_the_rows_and_falling_ones():
+    check(random_rows(0, 6, 300, "bf16"), [0.0] * 6, [-4, 2, 1, 4, 99, 100], 5)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_dead_and_finished_rows(kind):
+    inf = float("inf")
+    x = random_rows(4, 8, 4000, kind)
+    check(x, [0.0] + [-inf] * 7, [0, 8], 8)                                     # the first step
+    check(x, [-inf] * 8, [0, 4, 8], 3)                                          # nobody left
+    check(x, [0.0, float("nan"), -1.0, -inf, -2.0, -1.0, -0.5, 0.0], [0, 4, 8], 9)
+    check(x, [-1.0, -2.0, -0.25, -9.0, -1.0, -1.0, -0.5, 0.0], [0, 4, 8], 9, end=[-1, 3, 2, 2, -1, 0, 3999, -1])
+    check(x, [-1.0] * 8, [0, 8], 10, end=[7] * 8)                               # all finished, at one score: in order of rows
+    check(x, [-1.0, -inf] * 4, [0, 8], 10, end=[7, 7, -1, -1] * 2)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_masks(kind):
+    """Banned tokens, whole rows of them, one token left, masks of the type's lowest value."""
+    inf, lowest = float("inf"), torch.finfo(KINDS[kind]).min
+    x = random_rows(9, 7, 6001, kind)
+    x[0] = -inf
+    x[1] = -inf
+    x[1, 5000] = -3.0
+    x[2, torch.rand(6001, generator=torch.Generator().manual_seed(3)) < 0.99] = -inf
+    x[3] = lowest
+    x[4] = lowest
+    x[4, 17] = 2.0
+    x[5, :2100] = -inf                                                          # a wave's first steps see nothing
+    x[6, 100:] = lowest
+    for num_out in (3, 20, 64):
+        check(x, [-1.0] * 7, [0, 7], num_out)
+        check(x, [-1.0] * 7, [0, 1, 2, 3, 4, 5, 6, 7], num_out)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_values_that_are_no_numbers_or_very_large(kind):
+    x = random_rows(2, 6, 3000, kind)
+    big = torch.finfo(KINDS[kind]).max
+    x[0, ::7] = float("nan")
+    x[1] = float("nan")
+    x[2, 1234] = float("inf")
+    x[3, [5, 2999]] = float("inf")
+    x[4, 77] = big
+    x[4, 99] = -big
+    x[5] = big
+    for num_out in (2, 30):
+        check(x, [-1.0] * 6, [0, 1, 2, 3, 4, 5, 6], num_out)
+        check(x, [-1.0] * 6, [0, 6], num_out)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", ["equal", "rising", "falling", "few", "zeros", "late", "steps"])
+def test_ties_and_orders(kind, form):
+    """Rows where a threshold from the first values lets everything through, or all that follows equals it."""
+    n = 20000
+    i = torch.arange(n)
+    x = {"equal": torch.full((n,), 1.5), "rising": i / 1000.0 - 9, "falling": 9 - i / 1000.0, "few": (i * 7919 % 5).float(),
+         "zeros": torch.where(i % 3 == 0, -0.0, 0.0), "late": torch.where(i >= n - 300, 8.0, -8.0),
+         "steps": (i // 2048).float() * 45}[form].to(KINDS[kind])
+    rows = torch.stack([x, x, x.flip(0)])
+    for num_out in (1, 5, 64):
+        check(rows, [-1.0, -1.0, -2.0], [0, 2, 3], num_out)
+        check(rows, [-1.0, -1.0, -1.0], [0, 3], num_out)
+
+
+def test_large_vocabulary_and_peaked_rows():
+    x = random_rows(11, 8, 262144, "bf16", peak=1.0) * torch.linspace(0.01, 9, 8)[:, None].bfloat16()
+    check(x, (-np.arange(8.0)).tolist(), [0, 4, 8], 16)
+
+
+def test_repeats_bit_for_bit_and_in_a_graph():
+    x = random_rows(12, 12, 50001, "f16").to(DEV)
+    score, bounds = -torch.arange(12, dtype=torch.float32, device=DEV), torch.tensor([0, 6, 12], dtype=torch.int32, device=DEV)
+    first = b.q4kv_beam_select(x, score, bounds, 9)
+    want = [t.clone() for t in (first.parent, first.token, first.score)]
+    out, ws = b.BeamChoice(2, 9), b.q4kv_beam_select_workspace(x, 9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        b.q4kv_beam_select(x, score, bounds, 9, out=out, workspace=ws)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            b.q4kv_beam_select(x, score, bounds, 9, out=out, workspace=ws)
+    for step in range(4):
+        for t in (out.parent, out.token, out.score):
+            t.zero_()
+        ws.fill_(255 - step)                                                    # its contents mean nothing
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((out.parent, out.token, out.score), want):
+            assert torch.equal(got, w)
+        x.copy_(x.flip(1))
+        graph.replay()
+        eager = b.q4kv_beam_select(x, score, bounds, 9)
+        torch.cuda.synchronize()
+        for got, w in zip((out.parent, out.token, out.score), (eager.parent, eager.token, eager.score)):
+            assert torch.equal(got, w)
+        x.copy_(x.flip(1))
