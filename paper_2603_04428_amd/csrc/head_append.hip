@@ -66,38 +66,6 @@ __device__ __forceinline__ void widen(const uint4 &raw, float (&x)[8])
     }
 }
 
-// Sum over the LPR lanes of a row, in all of them: exchanges inside 16 lanes as data-parallel-primitive moves, the rest as swaps
-// of half rows.
-template <int CTRL>
-__device__ __forceinline__ double dpp_add(double v)
-{
-    const uint64_t u = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xF, 0xF, true);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
-    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-template <int LPR>
-__device__ __forceinline__ double row_sum(double v)
-{
-    v = dpp_add<0xB1>(v);  // quad_perm [1,0,3,2]
-    v = dpp_add<0x4E>(v);  // quad_perm [2,3,0,1]
-    v = dpp_add<0x141>(v); // row_half_mirror
-    if constexpr (LPR >= 16) v = dpp_add<0x140>(v); // row_mirror
-    if constexpr (LPR >= 32) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, v);
-        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-        v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
-    }
-    if constexpr (LPR >= 64) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, v);
-        const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
-        const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-        v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
-    }
-    return v;
-}
-
 // 1 / sqrt(v): the instruction is good to 2^-23 or better, two Newton steps to a few 2^-53.  A row of zeros without an eps stays zeros.
 __device__ __forceinline__ double inverse_root(double v)
 {
