@@ -846,7 +846,7 @@ static int check_beam_sizes(int32_t format, int32_t vocab, int32_t num_agents, i
     if (vocab <= 0 || num_agents < 0) return fail(Q4KV_EINVAL, "negative count");
     if (vocab > 1 << 30) return fail(Q4KV_ERANGE, "a vocabulary of %d tokens, at most 2^30", vocab);
     if (num_out < 1 || num_out > Q4KV_MAX_BEAM_OUT) return fail(Q4KV_ERANGE, "num_out %d, from 1 to %d", num_out, Q4KV_MAX_BEAM_OUT);
-    if ((int64_t)num_agents * q4kv::beam_select_spans(format, vocab, num_agents, compute_units()) >= 1LL << 31)
+    if ((int64_t)num_agents * q4kv::beam_select_spans(vocab, num_agents, compute_units()) >= 1LL << 31)
         return fail(Q4KV_ERANGE, "%d rows of %d tokens: choose for fewer groups at a time", num_agents, vocab);
     return Q4KV_OK;
 }
@@ -854,7 +854,7 @@ static int check_beam_sizes(int32_t format, int32_t vocab, int32_t num_agents, i
 size_t q4kv_beam_select_workspace_bytes(int32_t logits_format, int32_t vocab, int32_t num_agents, int32_t num_out)
 {
     if (check_beam_sizes(logits_format, vocab, num_agents, num_out)) return 0;
-    return std::max<size_t>(16, q4kv::beam_select_workspace_bytes(logits_format, vocab, num_agents, num_out, compute_units()));
+    return std::max<size_t>(16, q4kv::beam_select_workspace_bytes(vocab, num_agents, num_out, compute_units()));
 }
 
 int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stride, int32_t vocab, int32_t num_agents, const float *score,
@@ -869,7 +869,7 @@ int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stri
     if ((num_agents > 0 && (!logits || !score)) || !group_begin || !parent || !token || !total) return fail(Q4KV_EINVAL, "NULL pointer");
     if (reinterpret_cast<uintptr_t>(logits) % (logits_format == 2 ? 4 : 2)) return fail(Q4KV_EINVAL, "logits must be aligned to an element");
     const int units = compute_units();
-    if (num_agents > 0 && (!workspace || workspace_bytes < q4kv::beam_select_workspace_bytes(logits_format, vocab, num_agents, num_out, units)))
+    if (num_agents > 0 && (!workspace || workspace_bytes < q4kv::beam_select_workspace_bytes(vocab, num_agents, num_out, units)))
         return fail(Q4KV_EWORKSPACE, "workspace too small or missing");
     if (!aligned16(workspace)) return fail(Q4KV_EINVAL, "workspace must be 16-byte aligned");
     q4kv::BeamSelectArgs a;

@@ -19,7 +19,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kList = 192;     // candidates a wave can hold: what it keeps (64 at most) and two appends of up to 64
 constexpr int kMergeList = 1536;
-constexpr int kUnroll = 4;     // 16-byte loads per lane in flight
+constexpr int kRowLogs = 64; // rows of a group whose logarithms are kept in LDS
+constexpr int kHeld = 32;      // elements of a step per lane
 
 struct SpanRecord {
     double sum; // of exp(x - ref) over the span; ref
@@ -115,13 +116,60 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
-// exp(x - ref): the difference first (exact for neighbouring values of 16-bit types), then log2 e in two terms, so that the
-// constant's own rounding (1.3e-8 of the exponent) does not shift every term of a sum the same way
-__device__ __forceinline__ float exp_from(float x, float ref)
+// exp(x - ref) as 2^(x c - ref c), one fused multiply-add in front of the exponential.  log2 e in binary32 is 1.93e-8 too small,
+// which would shift every term of a sum the same way (15 below the reference by 2e-7): in 5 of 32 places the next larger number
+// stands for it, 1e-7 too large, so that what is left on average is 6e-10.  ref c is rounded; the terms are 2^-shift too large
+// then, the same for all places of one constant.
+constexpr float kLog2e[2] = {1.442695022f, 1.442695141f};
+constexpr double kLog2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
+
+// exp r for |r| <= 0.35 to 3e-13: the first eleven terms of its series
+__device__ __forceinline__ double exp_series(double r)
 {
-    const float d = x - ref;
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(d, 1.925963033500e-8f, d * 1.442695022f));
+    double y = 1.0 / 3628800.0;
+#pragma unroll
+    for (int n = 9; n >= 0; --n) {
+        constexpr double inverse[10] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880};
+        y = __builtin_fma(y, r, inverse[n]);
+    }
+    return y;
 }
+// exp d for d <= 1, -inf as well, to 1e-12: 2^n times the series of what is left of d
+__device__ __forceinline__ double exp_wide(double d)
+{
+    d = fmax(d, -1000.0);
+    const double n = __builtin_rint(d * kLog2);
+    return __builtin_amdgcn_ldexp(exp_series(__builtin_fma(-n, kLn2, d)), (int)n);
+}
+// log v, v > 0: the instruction's binary32 logarithm, and one step of Newton's method on exp
+__device__ __forceinline__ double log_wide(double v)
+{
+    const int e = __builtin_amdgcn_frexp_exp(v);
+    const double m = __builtin_amdgcn_ldexp(v, -e); // [0.5, 1)
+    const double y = (double)(__builtin_amdgcn_logf((float)m) * 0.693147181f); // -0.7 .. 0, to 1e-7
+    return (y + __builtin_fma(m, exp_wide(-y), -1.0)) + e * kLn2;
+}
+struct Reference {
+    float ref, minus[2]; // -ref c
+    __device__ __forceinline__ void set(float r)
+    {
+        ref = r;
+        minus[0] = -(r * kLog2e[0]);
+        minus[1] = -(r * kLog2e[1]);
+    }
+    template <int WHICH>
+    __device__ __forceinline__ float exp(float x) const
+    {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e[WHICH], minus[WHICH]));
+    }
+    // what the sum of such terms has to be multiplied with
+    __device__ __forceinline__ double unshift(int which) const
+    {
+        return exp_series(-kLn2 * ((double)ref * (double)kLog2e[which] + (double)minus[which]));
+    }
+    // the rounding of ref c is a small part of one: below 2^20 it is 2^-4 or less
+    __device__ __forceinline__ bool usable() const { return fabsf(minus[0]) < 0x1p20f; }
+};
 
 // The `keep` largest of n <= kList candidates in LDS, in order, at the front of the list (one wave; every lane calls).
 __device__ __forceinline__ int keep_best(uint64_t *list, int n, int keep)
@@ -137,10 +185,11 @@ __device__ __forceinline__ int keep_best(uint64_t *list, int n, int keep)
         rank[i] = 0;
     }
     if (n <= kWave) {
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) rank[0] += list[j] > mine[0];
+        const int lo = (int)(uint32_t)mine[0], hi = (int)(mine[0] >> 32);
+        for (int j = 0; j < n; ++j)
+            rank[0] += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j)) > mine[0];
     } else {
-#pragma unroll 2
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const uint64_t other = list[j];
 #pragma unroll
@@ -155,12 +204,25 @@ __device__ __forceinline__ int keep_best(uint64_t *list, int n, int keep)
     return min(n, keep);
 }
 
-// A value above `floor` that at least `keep` lanes reach with their `mine`, and few more do: halving of the range between the
-// lanes' extremes until the count is between keep and twice that.  At least `keep` lanes are above the floor.
-__device__ __forceinline__ float reached_by(float mine, float floor, float top, int keep)
+// A value that at least `keep` lanes reach with their `mine`, and few more do.  For up to eight the lanes are cut into eight (four)
+// groups: every group has a lane that reaches the lowest of the groups' maxima.  Where that lets many lanes through, and for more
+// than eight, by halving the range up to the largest until the count is between keep and twice that.
+__device__ __forceinline__ float reached_by(float mine, int keep)
 {
-    const float lowest = -wave_max(-mine);
-    uint32_t lo = max(ordered(floor) + 1, ordered(lowest)), hi = ordered(top); // enough lanes reach lo, none is above hi
+    float low;
+    if (keep <= 8) {
+        float v = mine;
+        v = fmaxf(v, Q4KV_DPP(v, v, 0xB1, 0xF));                 // quad_perm [1,0,3,2]
+        v = fmaxf(v, Q4KV_DPP(v, v, 0x4E, 0xF));                 // quad_perm [2,3,0,1]
+        v = fmaxf(v, Q4KV_DPP(v, v, 0x141, 0xF));                // row_half_mirror: groups of eight lanes
+        const float w = Q4KV_DPP(v, v, 0x140, 0xF);              // row_mirror: the other eight of a row
+        v = keep <= 4 ? fmaxf(v, w) : fminf(v, w);
+        low = -xor32_max(xor16_max(-v));
+        if (__popcll(__ballot(mine >= low)) <= 2 * keep + 8) return low;
+    } else {
+        low = -wave_max(-mine);
+    }
+    uint32_t lo = ordered(low), hi = ordered(wave_max(mine)); // enough lanes reach lo, none is above hi
     while (lo < hi) { // 32 rounds at most
         const uint32_t mid = lo + (hi - lo + 1) / 2;
         const int n = __popcll(__ballot(mine >= unordered(mid)));
@@ -186,118 +248,182 @@ __device__ __forceinline__ float element(const float *x, int at)
     }
 }
 
-// A span of a row: its candidates, in order, in `list`; the sum of exp(x - ref) and ref.  clean: NaN and +inf are replaced while
-// reading.  Without it they show in the maximum and the sum, and the answer is false: the span is to be done again.
-template <int FORMAT>
-__device__ __forceinline__ bool scan_span(const char *row, int begin, int end, int keep, bool clean, uint64_t *list, int &listed,
-                                          double &sum_out, float &ref_out)
+__device__ __forceinline__ bool dead(float score) { return !(score > -kInf); }
+
+// A span of a row: its candidates, in order, in `list`; the sum of exp(x - ref) and ref.  A lane has UNROLL loads of a step.
+// CLEAN: NaN and +inf are replaced while reading.  Without it they show in the maximum and the sum, and the answer is false: the
+// span is to be done again (so it is where the largest logit is beyond 700,000 on either side of zero).
+template <int FORMAT, bool CLEAN, int UNROLL, typename Skip>
+__device__ __forceinline__ bool scan_span(const char *row, int begin, int end, int keep, Skip skip, uint64_t *list, int &listed, double &sum_out,
+                                          float &ref_out)
 {
     typedef Logits<FORMAT> L;
-    constexpr int PER = L::kPer, HELD = kUnroll * PER, STEP = kWave * HELD;
+    constexpr int PER = L::kPer, STEP = kWave * UNROLL * PER;
+    // places of the larger constant: 5 of a lane's 32
+    constexpr auto upper = [](int u, int e) { return PER == 8 ? e == 0 || (u == 0 && e == 4) : e == 0 && u < 5; };
+    static_assert(CLEAN || UNROLL * PER == 32, "places of the larger constant");
     const int lane = threadIdx.x & 63;
-    float ref = kLowest, threshold = kLowest; // candidates are at or above the threshold
-    double sum = 0.0;
+    Reference at_ref;
+    at_ref.set(0.0f);
+    float threshold = kLowest; // candidates are at or above the threshold
+    double sum[2] = {0.0, 0.0};
     int n = 0;
-    words_t next[kUnroll] = {};
+    bool unset = true;
+    auto widen = [](const words_t &w, float (&x)[PER]) {
+        L::widen(w, x);
+        if constexpr (CLEAN) {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[e] = x[e] != x[e] ? -kInf : fminf(x[e], -kLowest);
+        }
+    };
+    words_t next[UNROLL] = {};
     for (int at = begin - STEP; at < end; at += STEP) {
         // the values that were asked for a step ago, and the next ones asked for
-        float x[HELD];
+        words_t now[UNROLL];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) L::widen(next[u], x + u * PER);
+        for (int u = 0; u < UNROLL; ++u) now[u] = next[u];
         const int ahead = at + STEP + lane * PER;
         if (at + 2 * STEP <= end) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) next[u] = L::load(row, ahead + u * kWave * PER);
+            for (int u = 0; u < UNROLL; ++u) next[u] = L::load(row, ahead + u * kWave * PER);
         } else if (at + STEP < end) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) next[u] = L::load_to(row, ahead + u * kWave * PER, end);
+            for (int u = 0; u < UNROLL; ++u) next[u] = L::load_to(row, ahead + u * kWave * PER, end);
         }
-        if (at < begin) continue;
-        if (clean) {
-#pragma unroll
-            for (int i = 0; i < HELD; ++i) x[i] = x[i] != x[i] ? -kInf : fminf(x[i], -kLowest);
+        if (at < begin) {
+            if (skip()) break; // asked for while the first values are on their way
+            continue;
         }
-        float mine = x[0];
+        float top[UNROLL];
 #pragma unroll
-        for (int i = 1; i + 1 < HELD; i += 2) mine = max3(x[i], x[i + 1], mine);
-        mine = fmaxf(mine, x[HELD - 1]);
-        // The reference is the maximum of the first step; it moves only where an exponential could grow large.
-        float highest = 0.0f;
-        if (at == begin || __any(mine > ref + 40.0f)) {
-            highest = fmaxf(wave_max(mine), kLowest);
-            if (at != begin) sum *= __builtin_amdgcn_exp2f((ref - highest) * 1.442695022f);
-            ref = highest;
+        for (int u = 0; u < UNROLL; ++u) {
+            if constexpr (FORMAT == 0 && !CLEAN) {
+                const half2_t h = bits_to_half2(pk_max(pk_max(now[u][0], now[u][1]), pk_max(now[u][2], now[u][3])));
+                top[u] = fmaxf((float)h.x, (float)h.y);
+            } else {
+                float x[PER];
+                widen(now[u], x);
+                top[u] = max3(x[0], x[1], x[2]);
+#pragma unroll
+                for (int e = 3; e + 1 < PER; e += 2) top[u] = max3(x[e], x[e + 1], top[u]);
+                top[u] = fmaxf(top[u], x[PER - 1]);
+            }
+        }
+        float mine = top[0];
+#pragma unroll
+        for (int u = 1; u < UNROLL; ++u) mine = fmaxf(mine, top[u]);
+        // The reference is the maximum of the first step that has a value; it moves only where an exponential could grow large.
+        if (unset || __any(mine > at_ref.ref + 40.0f)) {
+            const float highest = wave_max(mine);
+            if (highest > -kInf) {
+                const float scale = unset ? 0.0f : __builtin_amdgcn_exp2f((at_ref.ref - highest) * kLog2e[0]);
+                sum[0] *= scale;
+                sum[1] *= scale;
+                at_ref.set(highest);
+                unset = false;
+            }
         }
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) part[i & 3] += exp_from(x[i], ref);
-        sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
+        for (int u = 0; u < UNROLL; ++u) {
+            float x[PER];
+            widen(now[u], x);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (CLEAN) part[1] += __builtin_amdgcn_exp2f((x[e] - at_ref.ref) * kLog2e[0]);
+                else if (upper(u, e)) part[0] += at_ref.exp<1>(x[e]);
+                else part[1 + (u * PER + e) % 3] += at_ref.exp<0>(x[e]);
+            }
+        }
+        sum[0] += (double)(part[1] + part[2] + part[3]);
+        if (!CLEAN) sum[1] += (double)part[0];
         const uint64_t over = __ballot(mine >= threshold);
         if (over == 0) continue;
         // `keep` lanes and more with a candidate: this step alone has so many elements at or above what `keep` of its lanes reach
-        if (__popcll(over) >= keep) threshold = reached_by(mine, unordered(ordered(threshold) - 1), wave_max(mine), keep);
-        // bit i: x[i] is no less than the threshold, by the sign of the difference (either zero less -0 is +0)
-        if (threshold == 0.0f) threshold = -0.0f;
-        uint32_t bits = 0;
+        if (__popcll(over) >= keep) threshold = fmaxf(threshold, reached_by(mine, keep));
+        uint32_t granules = 0;
 #pragma unroll
-        for (int i = HELD - 1; i >= 0; --i) bits = __builtin_amdgcn_alignbit(bits, __builtin_bit_cast(uint32_t, x[i] - threshold), 31);
-        bits = ~bits & (uint32_t)((1ull << HELD) - 1);
-        while (true) {
-            const uint64_t mask = __ballot(bits != 0);
-            if (mask == 0) break;
-            if (n > kList - kWave) {
-                n = keep_best(list, n, keep);
-                if (n == keep) threshold = fmaxf(threshold, unordered((uint32_t)(list[keep - 1] >> 32)));
+        for (int u = 0; u < UNROLL; ++u) granules |= __any(top[u] >= threshold) ? 1u << u : 0u;
+        while (granules) {
+            const int u = __ffs(granules) - 1;
+            granules &= granules - 1;
+            words_t w = now[0];
+#pragma unroll
+            for (int k = 1; k < UNROLL; ++k)
+                if (u == k) w = now[k];
+            float x[PER];
+            widen(w, x);
+            // bit e: x[e] is no less than the threshold, by the sign of the difference (either zero less -0 is +0)
+            if (threshold == 0.0f) threshold = -0.0f;
+            uint32_t bits = 0;
+#pragma unroll
+            for (int e = PER - 1; e >= 0; --e) bits = __builtin_amdgcn_alignbit(bits, __builtin_bit_cast(uint32_t, x[e] - threshold), 31);
+            bits = ~bits & ((1u << PER) - 1);
+            while (true) {
+                const uint64_t mask = __ballot(bits != 0);
+                if (mask == 0) break;
+                if (n > kList - kWave) {
+                    n = keep_best(list, n, keep);
+                    if (n == keep) threshold = fmaxf(threshold, unordered((uint32_t)(list[keep - 1] >> 32)));
+                }
+                const int e = bits ? __ffs(bits) - 1 : 0;
+                const float v = element<PER>(x, e);
+                const bool take = bits && v >= threshold;
+                const uint64_t taken = __ballot(take);
+                if (take) {
+                    const int place = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0));
+                    list[place] = candidate(v, at + (u * kWave + lane) * PER + e);
+                }
+                n += __popcll(taken);
+                bits &= bits - 1;
             }
-            const int i = bits ? __ffs(bits) - 1 : 0;
-            const float v = element<HELD>(x, i);
-            const bool take = bits && v >= threshold;
-            const uint64_t taken = __ballot(take);
-            if (take) {
-                const int place = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0));
-                list[place] = candidate(v, at + (i / PER * kWave + lane) * PER + i % PER);
-            }
-            n += __popcll(taken);
-            bits &= bits - 1;
         }
-        // later steps have higher tokens: what only equals the last one kept does not come in any more
-        if (at + STEP < end && n >= keep) {
+        // Later steps have higher tokens: what only equals the last one kept does not come in any more.  The list is put in order
+        // for that after the first of them, and then whenever it has grown to twice what is kept.
+        if (at + STEP < end && n >= keep && (at == begin || n >= 2 * keep)) {
             n = keep_best(list, n, keep);
             threshold = fmaxf(threshold, unordered((uint32_t)(list[keep - 1] >> 32) + 1));
         }
     }
     listed = keep_best(list, n, keep);
-    ref_out = ref;
-    sum = row_sum<kWave>(sum);
-    if (!clean && !(sum < (double)kInf && ref < kInf)) return false; // a NaN or +inf among them
+    ref_out = unset ? kLowest : at_ref.ref;
+    const double shift[2] = {CLEAN ? 1.0 : at_ref.unshift(0), CLEAN ? 1.0 : at_ref.unshift(1)};
+    const double all = row_sum<kWave>(sum[0] * shift[0] + sum[1] * shift[1]);
+    if (!CLEAN && !(all < (double)kInf && at_ref.usable())) return false; // a NaN or +inf among them, or a far reference
     // The largest elements dominate the sum of a peaked row: theirs are taken again in binary64.
     double fix = 0.0;
     if (lane < listed) {
         const float v = unordered((uint32_t)(list[lane] >> 32));
-        fix = exp((double)v - (double)ref) - (double)exp_from(v, ref);
+        const int o = ((int)~(uint32_t)list[lane] - begin) % STEP;
+        fix = exp_wide((double)v - (double)at_ref.ref);
+        if (CLEAN) fix -= (double)__builtin_amdgcn_exp2f((v - at_ref.ref) * kLog2e[0]);
+        else if (upper(o / (kWave * PER), o % PER)) fix -= (double)at_ref.exp<1>(v) * shift[1];
+        else fix -= (double)at_ref.exp<0>(v) * shift[0];
     }
-    sum_out = sum + row_sum<kWave>(fix);
+    sum_out = unset ? 0.0 : all + row_sum<kWave>(fix);
     return true;
 }
 
-__device__ __forceinline__ bool dead(float score) { return !(score > -kInf); }
-
 template <int FORMAT>
-__global__ __launch_bounds__(kThreads, 4) void beam_scan_kernel(SelectParams p)
+__global__ __launch_bounds__(kThreads, FORMAT == 2 ? 3 : 4) void beam_scan_kernel(SelectParams p)
 {
     __shared__ uint64_t s_list[kWaves][kList];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * kWaves + wave; // waves are on their own: no barrier
     const int r = (int)(unit / p.spans), span = (int)(unit - (int64_t)r * p.spans);
     if (r >= p.rows) return;
-    if (dead(p.score[r]) || (p.end_token && p.end_token[r] >= 0)) return;
     const int begin = span * p.span_len, end = p.vocab - begin < p.span_len ? p.vocab : begin + p.span_len;
     const char *row = static_cast<const char *>(p.logits) + (int64_t)r * p.row_stride * Logits<FORMAT>::kBytes;
     uint64_t *list = s_list[wave];
     int n;
     double sum;
     float ref;
-    for (bool clean = false; !scan_span<FORMAT>(row, begin, end, p.num_out, clean, list, n, sum, ref);) clean = true; // twice at most
+    const float score = p.score[r];
+    const int32_t finished = p.end_token ? p.end_token[r] : -1;
+    const auto skip = [=] { return dead(score) || finished >= 0; }; // a row that is not read: its records are not looked at
+    if (!scan_span<FORMAT, false, FORMAT == 2 ? 8 : 4>(row, begin, end, p.num_out, skip, list, n, sum, ref))
+        scan_span<FORMAT, true, 1>(row, begin, end, p.num_out, skip, list, n, sum, ref);
+    if (skip()) return;
     if (lane == 0) p.records[unit] = SpanRecord{sum, ref, 0};
     if (lane < p.num_out) p.keys[unit * p.num_out + lane] = lane < n ? list[lane] : 0;
 }
@@ -397,6 +523,7 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
 {
     __shared__ MergeList s_list;
     __shared__ Choice s_room[Q4KV_MAX_BEAM_OUT];
+    __shared__ double s_log[kRowLogs];
     __shared__ int s_n;
     __shared__ float s_reached[kWaves];
     const int g = blockIdx.x, t = threadIdx.x, keep = p.num_out;
@@ -404,30 +531,36 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
     const int64_t records = (int64_t)max(hi - lo, 0) * p.spans;
     Walk w = walk_at(p, lo, t, records); // of the first records; asked for ahead of the rows' sums
     if (t == 0) s_n = 0;
-    // logarithms of the rows' sums: as many lanes to a row as it has spans, up to a wave
+    // logarithms of the rows' sums: as many lanes to a row as it has spans, up to a wave.  Records of rows that were not read hold
+    // anything; what comes of them is never used.
     int lanes = 1;
     while (lanes < p.spans && lanes < kWave) lanes <<= 1;
+    const int first = t & (lanes - 1);
     for (int r = lo + t / lanes; r - t / lanes < hi; r += kThreads / lanes) {
         const SpanRecord *rec = p.records + (int64_t)r * p.spans;
-        const bool on = r < hi && !dead(p.score[r]) && !(p.end_token && p.end_token[r] >= 0);
-        const int first = t & (lanes - 1);
-        float ref = kLowest;
-        if (on)
-            for (int i = first; i < p.spans; i += lanes) ref = fmaxf(ref, rec[i].ref);
+        const SpanRecord mine = r < hi && first < p.spans ? rec[first] : SpanRecord{0.0, kLowest, 0};
+        float ref = mine.ref;
+        if (r < hi)
+            for (int i = first + lanes; i < p.spans; i += lanes) ref = fmaxf(ref, rec[i].ref);
         for (int off = 1; off < lanes; off <<= 1) ref = fmaxf(ref, __shfl_xor(ref, off));
-        double sum = 0.0;
-        if (on)
-            for (int i = first; i < p.spans; i += lanes) sum += rec[i].sum * exp((double)rec[i].ref - (double)ref);
+        double sum = mine.sum * exp_wide((double)mine.ref - (double)ref);
+        if (r < hi)
+            for (int i = first + lanes; i < p.spans; i += lanes) sum += rec[i].sum * exp_wide((double)rec[i].ref - (double)ref);
         for (int off = 1; off < lanes; off <<= 1) sum += __shfl_xor(sum, off);
-        if (on && first == 0) p.row_log[r] = (double)ref + log(sum); // -inf for a row without any, which is never used
+        if (r < hi && first == 0) {
+            const double row_log = (double)ref + log_wide(sum);
+            if (r - lo < kRowLogs) s_log[r - lo] = row_log;
+            else p.row_log[r] = row_log;
+        }
     }
     __syncthreads();
-    if (w.on && w.end < 0) w.row_log = p.row_log[w.row];
+    auto log_of = [&](int r) { return r - lo < kRowLogs ? s_log[r - lo] : p.row_log[r]; };
+    if (w.on && w.end < 0) w.row_log = log_of(w.row);
     // What `keep` lanes of a wave reach with the first element of their records is reached by the group's best `keep`.
     float reached = -kInf;
     {
         float mine = w.on && w.ahead[0] ? (float)unordered64(choice_of(w, w.ahead[0]).total) : -kInf;
-        if (__popcll(__ballot(mine > -kInf)) >= keep) reached = reached_by(mine, -kInf, wave_max(mine), keep);
+        reached = reached_by(mine, keep);
         if ((t & 63) == 0) s_reached[t >> 6] = reached;
     }
     __syncthreads();
@@ -440,7 +573,7 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
     for (int64_t base = 0; base < records; base += kThreads) {
         if (base > 0) {
             w = walk_at(p, lo, base + t, records);
-            if (w.on && w.end < 0) w.row_log = p.row_log[w.row];
+            if (w.on && w.end < 0) w.row_log = log_of(w.row);
         }
         for (int next = 0;; next += kAhead) {
 #pragma unroll
@@ -477,9 +610,9 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
 
 // Elements of a span: whole steps of a wave, so many that about kWavesPerCu waves per compute unit share the call's rows.
 constexpr int kWavesPerCu = 8, kMaxSteps = 8;
-int span_length(int format, int vocab, int rows, int compute_units)
+int span_length(int vocab, int rows, int compute_units)
 {
-    const int64_t step = (int64_t)kWave * kUnroll * (format == 2 ? 4 : 8);
+    const int64_t step = (int64_t)kWave * kHeld;
     const int64_t steps = ((int64_t)vocab + step - 1) / step * rows / ((int64_t)compute_units * kWavesPerCu);
     return (int)(step * (steps < 1 ? 1 : steps > kMaxSteps ? kMaxSteps : steps));
 }
@@ -488,15 +621,15 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 } // namespace
 
-int beam_select_spans(int format, int vocab, int rows, int compute_units)
+int beam_select_spans(int vocab, int rows, int compute_units)
 {
-    const int len = span_length(format, vocab, rows, compute_units);
+    const int len = span_length(vocab, rows, compute_units);
     return (int)(((int64_t)vocab + len - 1) / len);
 }
 
-size_t beam_select_workspace_bytes(int format, int vocab, int rows, int num_out, int compute_units)
+size_t beam_select_workspace_bytes(int vocab, int rows, int num_out, int compute_units)
 {
-    const size_t units = (size_t)rows * beam_select_spans(format, vocab, rows, compute_units);
+    const size_t units = (size_t)rows * beam_select_spans(vocab, rows, compute_units);
     return up(units * sizeof(SpanRecord)) + up((size_t)rows * sizeof(double)) + up(units * num_out * sizeof(uint64_t));
 }
 
@@ -510,8 +643,8 @@ hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream)
     p.group_begin = a.group_begin;
     p.rows = a.rows;
     p.vocab = a.vocab;
-    p.span_len = span_length(a.format, a.vocab, a.rows, a.compute_units);
-    p.spans = beam_select_spans(a.format, a.vocab, a.rows, a.compute_units);
+    p.span_len = span_length(a.vocab, a.rows, a.compute_units);
+    p.spans = beam_select_spans(a.vocab, a.rows, a.compute_units);
     p.groups = a.groups;
     p.num_out = a.num_out;
     p.parent = a.parent;

@@ -24,6 +24,21 @@ __device__ __forceinline__ uint16_t float_to_half_bits(float f)
     return __builtin_bit_cast(uint16_t, (half_t)f); // v_cvt_f16_f32, round to nearest even
 }
 
+// Packed binary16 minimum / maximum as single instructions.  (The generic element-wise builtins first quiet a
+// signalling NaN in each operand, one more instruction per operand; a cache row holds no NaN.)
+__device__ __forceinline__ uint32_t pk_min(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
 // bfloat16 (the upper half of a binary32): the other type scale and bias may be stored in (Sec. 3.1, Sec. 3.2).
 __device__ __forceinline__ float bf16_bits_to_float(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
 __device__ __forceinline__ uint16_t float_to_bf16_bits(float f) // finite f, round to nearest even

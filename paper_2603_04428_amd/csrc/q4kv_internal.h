@@ -155,8 +155,8 @@ struct BeamSelectArgs {
     void *workspace;
     int format, vocab, rows, groups, num_out, compute_units;
 };
-int beam_select_spans(int format, int vocab, int rows, int compute_units);
-size_t beam_select_workspace_bytes(int format, int vocab, int rows, int num_out, int compute_units);
+int beam_select_spans(int vocab, int rows, int compute_units);
+size_t beam_select_workspace_bytes(int vocab, int rows, int num_out, int compute_units);
 hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream);
 
 // read_probe.hip: reads bytes / 16,384 * 16,384 bytes of `src` once; `sink` is one device word that may be written

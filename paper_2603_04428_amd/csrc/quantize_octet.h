@@ -8,21 +8,6 @@ namespace {
 
 #pragma clang fp contract(off)
 
-// Packed binary16 minimum / maximum as single instructions.  (The generic element-wise builtins first quiet a
-// signalling NaN in each operand, one more instruction per operand; a cache row holds no NaN.)
-__device__ __forceinline__ uint32_t pk_min(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
-
 // fl(h + a) in binary32 for the low / the high binary16 half h of a word: the mixed-precision fused multiply-add
 // h * 1.0 + a converts and adds in one instruction (the product is exact, so the one rounding is that of the sum)
 __device__ __forceinline__ float half_lo_plus(uint32_t pair, float a)
