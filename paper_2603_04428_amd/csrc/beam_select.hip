@@ -6,9 +6,10 @@
 // num_out largest elements in order.  A second kernel, one workgroup per group, adds the sums up, forms the totals of what the
 // records list and takes the best.  Two launches, no atomics on memory, and the same order of every sum on every run.
 //
-// What bounds it is memory for large batches (every logit is read once) and the trips to memory of two launches for small ones.
-#include <type_traits>
-
+// While a wave streams its span it does no more than a maximum and an exponential per element (7.5 instruction slots of a
+// bfloat16 one, four of them the exponential's) and notes each lane's maximum of every step.  Those maxima then say how large an
+// element has to be to count, and which lanes of which steps have one: their 64 bytes are read again.  Candidates kept while
+// streaming cost a step in two some 150 instructions more.
 #include "q4_device.h"
 #include "q4kv_internal.h"
 
@@ -18,9 +19,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kList = 192;     // candidates a wave can hold: what it keeps (64 at most) and two appends of up to 64
-constexpr int kMergeList = 1536;
+constexpr int kMergeList = 1024;
 constexpr int kRowLogs = 64; // rows of a group whose logarithms are kept in LDS
 constexpr int kHeld = 32;      // elements of a step per lane
+constexpr int kMaxSteps = 8;   // steps of a span
 
 struct SpanRecord {
     double sum; // of exp(x - ref) over the span; ref
@@ -34,7 +36,7 @@ struct SelectParams {
     const float *score;
     const int32_t *end_token, *group_begin;
     SpanRecord *records;  // [rows][spans]
-    uint64_t *keys;       // [rows][spans][num_out]: value and place, largest first, 0 where there are no more
+    uint64_t *keys;       // [rows][num_out][spans]: value and place, a span's largest first, 0 where there are no more
     double *row_log;      // [rows]: logarithm of the row's sum of exponentials
     int32_t *parent, *token;
     float *total;
@@ -74,19 +76,17 @@ struct Logits {
     static constexpr int kPer = FORMAT == 2 ? 4 : 8, kBytes = 16 / kPer;
     struct __attribute__((packed, aligned(kBytes))) Loose { words_t w; }; // rows may begin at any element
     static __device__ __forceinline__ words_t load(const char *row, int i) { return reinterpret_cast<const Loose *>(row + (int64_t)i * kBytes)->w; }
-    // the same where the row may end inside: -inf from `end` on (end > 0)
+    static constexpr uint32_t kBanned = FORMAT == 2 ? 0xff800000u : FORMAT == 1 ? 0xff80ff80u : 0xfc00fc00u;
+    // the same, -inf where that would read beyond `end`
     static __device__ __forceinline__ words_t load_to(const char *row, int i, int end)
     {
-        typedef std::conditional_t<FORMAT == 2, uint32_t, uint16_t> bits_t;
-        constexpr uint32_t banned = FORMAT == 2 ? 0xff800000u : FORMAT == 1 ? 0xff80u : 0xfc00u;
-        uint32_t e[kPer];
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            e[j] = reinterpret_cast<const bits_t *>(row)[min(i + j, end - 1)];
-            if (i + j >= end) e[j] = banned;
-        }
-        if constexpr (FORMAT == 2) return words_t{e[0], e[1], e[2], e[3]};
-        else return words_t{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+        return i + kPer <= end ? load(row, i) : words_t{kBanned, kBanned, kBanned, kBanned};
+    }
+    static __device__ __forceinline__ float one(const char *row, int i)
+    {
+        if constexpr (FORMAT == 2) return reinterpret_cast<const float *>(row)[i];
+        const uint16_t b = reinterpret_cast<const uint16_t *>(row)[i];
+        return FORMAT == 1 ? bf16_bits_to_float(b) : half_bits_to_float(b);
     }
     static __device__ __forceinline__ void widen(const words_t &w, float *x)
     {
@@ -204,28 +204,32 @@ __device__ __forceinline__ int keep_best(uint64_t *list, int n, int keep)
     return min(n, keep);
 }
 
-// A value that at least `keep` lanes reach with their `mine`, and few more do.  For up to eight the lanes are cut into eight (four)
-// groups: every group has a lane that reaches the lowest of the groups' maxima.  Where that lets many lanes through, and for more
-// than eight, by halving the range up to the largest until the count is between keep and twice that.
-__device__ __forceinline__ float reached_by(float mine, int keep)
+// A value that at least `keep` (up to eight) lanes reach with their `mine`: the lanes are cut into eight (four) groups, and every group
+// has a lane that reaches the lowest of the groups' maxima.
+__device__ __forceinline__ float reached_by_groups(float mine, int keep)
 {
-    float low;
-    if (keep <= 8) {
-        float v = mine;
-        v = fmaxf(v, Q4KV_DPP(v, v, 0xB1, 0xF));                 // quad_perm [1,0,3,2]
-        v = fmaxf(v, Q4KV_DPP(v, v, 0x4E, 0xF));                 // quad_perm [2,3,0,1]
-        v = fmaxf(v, Q4KV_DPP(v, v, 0x141, 0xF));                // row_half_mirror: groups of eight lanes
-        const float w = Q4KV_DPP(v, v, 0x140, 0xF);              // row_mirror: the other eight of a row
-        v = keep <= 4 ? fmaxf(v, w) : fminf(v, w);
-        low = -xor32_max(xor16_max(-v));
-        if (__popcll(__ballot(mine >= low)) <= 2 * keep + 8) return low;
-    } else {
-        low = -wave_max(-mine);
-    }
-    uint32_t lo = ordered(low), hi = ordered(wave_max(mine)); // enough lanes reach lo, none is above hi
+    float v = mine;
+    v = fmaxf(v, Q4KV_DPP(v, v, 0xB1, 0xF));                 // quad_perm [1,0,3,2]
+    v = fmaxf(v, Q4KV_DPP(v, v, 0x4E, 0xF));                 // quad_perm [2,3,0,1]
+    v = fmaxf(v, Q4KV_DPP(v, v, 0x141, 0xF));                // row_half_mirror: groups of eight lanes
+    const float w = Q4KV_DPP(v, v, 0x140, 0xF);              // row_mirror: the other eight of a row
+    v = keep <= 4 ? fmaxf(v, w) : fminf(v, w);
+    return -xor32_max(xor16_max(-v));
+}
+
+// A value that at least `keep` of the wave's N * 64 values reach, and few more do: halving of the range from `low` (which so many
+// reach, or which is -inf) to their largest until the count is between keep and twice that.
+template <int N>
+__device__ __forceinline__ float reached_by_halving(const float (&v)[N], float low, float high, int keep)
+{
+    uint32_t lo = ordered(low), hi = ordered(high);
+#pragma unroll 1
     while (lo < hi) { // 32 rounds at most
         const uint32_t mid = lo + (hi - lo + 1) / 2;
-        const int n = __popcll(__ballot(mine >= unordered(mid)));
+        const float m = unordered(mid);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot(v[i] >= m));
         if (n >= keep) {
             lo = mid;
             if (n <= 2 * keep) break;
@@ -236,82 +240,77 @@ __device__ __forceinline__ float reached_by(float mine, int keep)
     return unordered(lo);
 }
 
-// Element `at` of N values in registers (N a power of two).
+// Word `at` of N words in registers (N a power of two).
 template <int N>
-__device__ __forceinline__ float element(const float *x, int at)
+__device__ __forceinline__ uint32_t word_of(const uint32_t *x, int at)
 {
     if constexpr (N == 1) {
         return x[0];
     } else {
-        const float a = element<N / 2>(x, at), b = element<N / 2>(x + N / 2, at);
+        const uint32_t a = word_of<N / 2>(x, at), b = word_of<N / 2>(x + N / 2, at);
         return at & (N / 2) ? b : a;
     }
 }
 
 __device__ __forceinline__ bool dead(float score) { return !(score > -kInf); }
 
-// A span of a row: its candidates, in order, in `list`; the sum of exp(x - ref) and ref.  A lane has UNROLL loads of a step.
+// A span of a row: its candidates, in order, in `list`; the sum of exp(x - ref) and ref.  tops: LDS, [kMaxSteps][64].
 // CLEAN: NaN and +inf are replaced while reading.  Without it they show in the maximum and the sum, and the answer is false: the
 // span is to be done again (so it is where the largest logit is beyond 700,000 on either side of zero).
-template <int FORMAT, bool CLEAN, int UNROLL, typename Skip>
-__device__ __forceinline__ bool scan_span(const char *row, int begin, int end, int keep, Skip skip, uint64_t *list, int &listed, double &sum_out,
-                                          float &ref_out)
+template <int FORMAT, bool CLEAN, typename Skip>
+__device__ __forceinline__ bool scan_span(const char *row, int begin, int end, int keep, Skip skip, float *tops, uint64_t *list, int &listed,
+                                          double &sum_out, float &ref_out)
 {
     typedef Logits<FORMAT> L;
-    constexpr int PER = L::kPer, STEP = kWave * UNROLL * PER;
+    constexpr int PER = L::kPer, UNROLL = kHeld / PER, STEP = kWave * kHeld;
     // places of the larger constant: 5 of a lane's 32
     constexpr auto upper = [](int u, int e) { return PER == 8 ? e == 0 || (u == 0 && e == 4) : e == 0 && u < 5; };
-    static_assert(CLEAN || UNROLL * PER == 32, "places of the larger constant");
     const int lane = threadIdx.x & 63;
+    auto clean = [](float x) { return !CLEAN ? x : x != x ? -kInf : fminf(x, -kLowest); };
+    auto widen = [&](const words_t &w, float (&x)[PER]) {
+        L::widen(w, x);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = clean(x[e]);
+    };
     Reference at_ref;
     at_ref.set(0.0f);
-    float threshold = kLowest; // candidates are at or above the threshold
-    double sum[2] = {0.0, 0.0};
-    int n = 0;
     bool unset = true;
-    auto widen = [](const words_t &w, float (&x)[PER]) {
-        L::widen(w, x);
-        if constexpr (CLEAN) {
-#pragma unroll
-            for (int e = 0; e < PER; ++e) x[e] = x[e] != x[e] ? -kInf : fminf(x[e], -kLowest);
-        }
-    };
-    words_t next[UNROLL] = {};
+    double sum[2] = {0.0, 0.0};
+    const int left = (end - begin) % PER, whole = end - left; // what does not fill a load is one element of `left` lanes more, in the first step
+    words_t now[UNROLL] = {}, next[UNROLL] = {};
+    float largest = -kInf, rest = -kInf;
     for (int at = begin - STEP; at < end; at += STEP) {
         // the values that were asked for a step ago, and the next ones asked for
-        words_t now[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) now[u] = next[u];
         const int ahead = at + STEP + lane * PER;
-        if (at + 2 * STEP <= end) {
+        if (at + 2 * STEP <= whole) {
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) next[u] = L::load(row, ahead + u * kWave * PER);
-        } else if (at + STEP < end) {
+        } else {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) next[u] = L::load_to(row, ahead + u * kWave * PER, end);
+            for (int u = 0; u < UNROLL; ++u) next[u] = L::load_to(row, ahead + u * kWave * PER, whole);
         }
         if (at < begin) {
-            if (skip()) break; // asked for while the first values are on their way
+            if (lane < left) rest = clean(L::one(row, whole + lane));
+            if (skip()) return true; // asked for while the first values are on their way
             continue;
         }
-        float top[UNROLL];
+        float extra = at == begin ? rest : -kInf, mine = extra;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             if constexpr (FORMAT == 0 && !CLEAN) {
                 const half2_t h = bits_to_half2(pk_max(pk_max(now[u][0], now[u][1]), pk_max(now[u][2], now[u][3])));
-                top[u] = fmaxf((float)h.x, (float)h.y);
+                mine = max3(mine, (float)h.x, (float)h.y);
             } else {
                 float x[PER];
                 widen(now[u], x);
-                top[u] = max3(x[0], x[1], x[2]);
 #pragma unroll
-                for (int e = 3; e + 1 < PER; e += 2) top[u] = max3(x[e], x[e + 1], top[u]);
-                top[u] = fmaxf(top[u], x[PER - 1]);
+                for (int e = 0; e < PER; e += 2) mine = max3(x[e], x[e + 1], mine);
             }
         }
-        float mine = top[0];
-#pragma unroll
-        for (int u = 1; u < UNROLL; ++u) mine = fmaxf(mine, top[u]);
+        tops[(at - begin) / STEP * kWave + lane] = mine;
+        largest = fmaxf(largest, mine);
         // The reference is the maximum of the first step that has a value; it moves only where an exponential could grow large.
         if (unset || __any(mine > at_ref.ref + 40.0f)) {
             const float highest = wave_max(mine);
@@ -323,82 +322,102 @@ __device__ __forceinline__ bool scan_span(const char *row, int begin, int end, i
                 unset = false;
             }
         }
-        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto term = [&](float x) { return CLEAN ? __builtin_amdgcn_exp2f((x - at_ref.ref) * kLog2e[0]) : at_ref.exp<0>(x); };
+        float part[4] = {0.0f, term(extra), 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             float x[PER];
             widen(now[u], x);
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
-                if (CLEAN) part[1] += __builtin_amdgcn_exp2f((x[e] - at_ref.ref) * kLog2e[0]);
-                else if (upper(u, e)) part[0] += at_ref.exp<1>(x[e]);
-                else part[1 + (u * PER + e) % 3] += at_ref.exp<0>(x[e]);
+                if (!CLEAN && upper(u, e)) part[0] += at_ref.exp<1>(x[e]);
+                else part[1 + (u * PER + e) % 3] += term(x[e]);
             }
         }
         sum[0] += (double)(part[1] + part[2] + part[3]);
         if (!CLEAN) sum[1] += (double)part[0];
-        const uint64_t over = __ballot(mine >= threshold);
-        if (over == 0) continue;
-        // `keep` lanes and more with a candidate: this step alone has so many elements at or above what `keep` of its lanes reach
-        if (__popcll(over) >= keep) threshold = fmaxf(threshold, reached_by(mine, keep));
-        uint32_t granules = 0;
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) granules |= __any(top[u] >= threshold) ? 1u << u : 0u;
-        while (granules) {
-            const int u = __ffs(granules) - 1;
-            granules &= granules - 1;
-            words_t w = now[0];
-#pragma unroll
-            for (int k = 1; k < UNROLL; ++k)
-                if (u == k) w = now[k];
-            float x[PER];
-            widen(w, x);
-            // bit e: x[e] is no less than the threshold, by the sign of the difference (either zero less -0 is +0)
-            if (threshold == 0.0f) threshold = -0.0f;
-            uint32_t bits = 0;
-#pragma unroll
-            for (int e = PER - 1; e >= 0; --e) bits = __builtin_amdgcn_alignbit(bits, __builtin_bit_cast(uint32_t, x[e] - threshold), 31);
-            bits = ~bits & ((1u << PER) - 1);
-            while (true) {
-                const uint64_t mask = __ballot(bits != 0);
-                if (mask == 0) break;
-                if (n > kList - kWave) {
-                    n = keep_best(list, n, keep);
-                    if (n == keep) threshold = fmaxf(threshold, unordered((uint32_t)(list[keep - 1] >> 32)));
-                }
-                const int e = bits ? __ffs(bits) - 1 : 0;
-                const float v = element<PER>(x, e);
-                const bool take = bits && v >= threshold;
-                const uint64_t taken = __ballot(take);
-                if (take) {
-                    const int place = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0));
-                    list[place] = candidate(v, at + (u * kWave + lane) * PER + e);
-                }
-                n += __popcll(taken);
-                bits &= bits - 1;
-            }
-        }
-        // Later steps have higher tokens: what only equals the last one kept does not come in any more.  The list is put in order
-        // for that after the first of them, and then whenever it has grown to twice what is kept.
-        if (at + STEP < end && n >= keep && (at == begin || n >= 2 * keep)) {
-            n = keep_best(list, n, keep);
-            threshold = fmaxf(threshold, unordered((uint32_t)(list[keep - 1] >> 32) + 1));
-        }
     }
-    listed = keep_best(list, n, keep);
     ref_out = unset ? kLowest : at_ref.ref;
     const double shift[2] = {CLEAN ? 1.0 : at_ref.unshift(0), CLEAN ? 1.0 : at_ref.unshift(1)};
     const double all = row_sum<kWave>(sum[0] * shift[0] + sum[1] * shift[1]);
     if (!CLEAN && !(all < (double)kInf && at_ref.usable())) return false; // a NaN or +inf among them, or a far reference
+    // Elements below `threshold` are not among the best: as many lanes (or steps of lanes) have a larger one.
+    const int steps = (end - begin + STEP - 1) / STEP;
+    wave_lds_sync();
+    float top[kMaxSteps];
+#pragma unroll
+    for (int k = 0; k < kMaxSteps; ++k) top[k] = k < steps ? tops[k * kWave + lane] : -kInf;
+    float threshold = keep <= 8 ? reached_by_groups(largest, keep) : -wave_max(-largest);
+    if (keep > 8 || __popcll(__ballot(largest >= threshold)) > 2 * keep + 8)
+        threshold = reached_by_halving(top, threshold, wave_max(largest), keep);
+    threshold = fmaxf(threshold, kLowest);
+    uint32_t flagged = 0; // steps in which the lane has an element to look at
+#pragma unroll
+    for (int k = 0; k < kMaxSteps; ++k) flagged |= (uint32_t)(top[k] >= threshold) << k;
+    int n = 0;
+    uint64_t worst = 0; // of the list once it has been full
+    auto push = [&](bool take, float v, int token) {
+        if (n > kList - kWave) {
+            n = keep_best(list, n, keep);
+            if (n == keep) worst = list[keep - 1];
+        }
+        const uint64_t key = candidate(v, token);
+        take = take && key > worst;
+        const uint64_t taken = __ballot(take);
+        if (take) list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0))] = key;
+        n += __popcll(taken);
+    };
+    float v = rest;
+    int token = whole + lane, step = 0;
+    uint32_t bits = 0;
+    bool take = rest >= threshold;
+    while (true) {
+        if (__any(take)) push(take, v, token);
+        // the next element of the lane, in this step or the next flagged one
+        if (!__any(bits != 0)) {
+            if (!__any(flagged != 0)) break;
+            const bool mine = flagged != 0;
+            step = mine ? __ffs(flagged) - 1 : 0;
+            flagged &= flagged - 1;
+            const int at = begin + step * STEP + lane * PER;
+            if (steps > 1 && mine) {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) now[u] = L::load_to(row, at + u * kWave * PER, whole);
+            }
+            // bit u * PER + e: the element is no less than the threshold, by the sign of the difference (either zero less -0 is +0)
+            const float less = threshold == 0.0f ? -0.0f : threshold;
+#pragma unroll
+            for (int u = UNROLL - 1; u >= 0; --u) {
+                float x[PER];
+                widen(now[u], x);
+#pragma unroll
+                for (int e = PER - 1; e >= 0; --e) bits = __builtin_amdgcn_alignbit(bits, __builtin_bit_cast(uint32_t, x[e] - less), 31);
+            }
+            bits = mine ? ~bits : 0u;
+        }
+        take = bits != 0;
+        const int i = take ? __ffs(bits) - 1 : 0, u = i / PER;
+        bits &= bits - 1;
+        uint32_t words[kHeld * 4 / PER];
+#pragma unroll
+        for (int k = 0; k < UNROLL * 4; ++k) words[k] = now[k / 4][k % 4];
+        const uint32_t word = word_of<UNROLL * 4>(words, FORMAT == 2 ? i : i >> 1);
+        if constexpr (FORMAT == 2) v = __builtin_bit_cast(float, word);
+        else if constexpr (FORMAT == 1) v = __builtin_bit_cast(float, i & 1 ? word & 0xffff0000u : word << 16);
+        else v = half_bits_to_float((uint16_t)(i & 1 ? word >> 16 : word & 0xffffu));
+        v = clean(v);
+        token = begin + step * STEP + (u * kWave + lane) * PER + i % PER;
+    }
+    listed = keep_best(list, n, keep);
     // The largest elements dominate the sum of a peaked row: theirs are taken again in binary64.
     double fix = 0.0;
     if (lane < listed) {
-        const float v = unordered((uint32_t)(list[lane] >> 32));
-        const int o = ((int)~(uint32_t)list[lane] - begin) % STEP;
-        fix = exp_wide((double)v - (double)at_ref.ref);
-        if (CLEAN) fix -= (double)__builtin_amdgcn_exp2f((v - at_ref.ref) * kLog2e[0]);
-        else if (upper(o / (kWave * PER), o % PER)) fix -= (double)at_ref.exp<1>(v) * shift[1];
-        else fix -= (double)at_ref.exp<0>(v) * shift[0];
+        const float x = unordered((uint32_t)(list[lane] >> 32));
+        const int t = (int)~(uint32_t)list[lane], o = (t - begin) % STEP;
+        fix = exp_wide((double)x - (double)at_ref.ref);
+        if (CLEAN) fix -= (double)__builtin_amdgcn_exp2f((x - at_ref.ref) * kLog2e[0]);
+        else if (t < whole && upper(o / (kWave * PER), o % PER)) fix -= (double)at_ref.exp<1>(x) * shift[1];
+        else fix -= (double)at_ref.exp<0>(x) * shift[0];
     }
     sum_out = unset ? 0.0 : all + row_sum<kWave>(fix);
     return true;
@@ -408,6 +427,7 @@ template <int FORMAT>
 __global__ __launch_bounds__(kThreads, FORMAT == 2 ? 3 : 4) void beam_scan_kernel(SelectParams p)
 {
     __shared__ uint64_t s_list[kWaves][kList];
+    __shared__ float s_tops[kWaves][kMaxSteps * kWave];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * kWaves + wave; // waves are on their own: no barrier
     const int r = (int)(unit / p.spans), span = (int)(unit - (int64_t)r * p.spans);
@@ -415,17 +435,17 @@ __global__ __launch_bounds__(kThreads, FORMAT == 2 ? 3 : 4) void beam_scan_kerne
     const int begin = span * p.span_len, end = p.vocab - begin < p.span_len ? p.vocab : begin + p.span_len;
     const char *row = static_cast<const char *>(p.logits) + (int64_t)r * p.row_stride * Logits<FORMAT>::kBytes;
     uint64_t *list = s_list[wave];
-    int n;
-    double sum;
-    float ref;
+    int n = 0;
+    double sum = 0.0;
+    float ref = kLowest;
     const float score = p.score[r];
     const int32_t finished = p.end_token ? p.end_token[r] : -1;
     const auto skip = [=] { return dead(score) || finished >= 0; }; // a row that is not read: its records are not looked at
-    if (!scan_span<FORMAT, false, FORMAT == 2 ? 8 : 4>(row, begin, end, p.num_out, skip, list, n, sum, ref))
-        scan_span<FORMAT, true, 1>(row, begin, end, p.num_out, skip, list, n, sum, ref);
+    if (!scan_span<FORMAT, false>(row, begin, end, p.num_out, skip, s_tops[wave], list, n, sum, ref))
+        scan_span<FORMAT, true>(row, begin, end, p.num_out, skip, s_tops[wave], list, n, sum, ref);
     if (skip()) return;
     if (lane == 0) p.records[unit] = SpanRecord{sum, ref, 0};
-    if (lane < p.num_out) p.keys[unit * p.num_out + lane] = lane < n ? list[lane] : 0;
+    if (lane < p.num_out) p.keys[((int64_t)r * p.num_out + lane) * p.spans + span] = lane < n ? list[lane] : 0;
 }
 
 // A continuation in the merge: its total, then the lower row, then the row's own order (where a logit is so large that totals
@@ -458,16 +478,12 @@ __device__ __forceinline__ int keep_best_choices(MergeList &list, Choice *room, 
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const Choice mine = list.at(i);
-        int ahead = 0, equal = 0;
-#pragma unroll 8
+        int ahead = 0;
+#pragma unroll 2
         for (int j = 0; j < n; ++j) {
             const uint64_t other = list.total[j];
-            ahead += other > mine.total;
-            equal += other == mine.total;
+            ahead += other > mine.total || (other == mine.total && better(list.at(j), mine));
         }
-        if (equal > 1)
-#pragma unroll 1
-            for (int j = 0; j < n; ++j) ahead += list.total[j] == mine.total && better(list.at(j), mine);
         if (ahead < keep) room[ahead] = mine;
     }
     __syncthreads();
@@ -477,46 +493,13 @@ __device__ __forceinline__ int keep_best_choices(MergeList &list, Choice *room, 
     return kept;
 }
 
-// Where a thread is in the merge: a record (a span's elements in order, the next kAhead of them in registers), or a finished row.
-constexpr int kAhead = 4;
-struct Walk {
-    const uint64_t *keys;
-    uint64_t ahead[kAhead];
-    double score, row_log;
-    int32_t row, end;
-    bool on;
-};
-
-__device__ __forceinline__ Walk walk_at(const SelectParams &p, int lo, int64_t i, int64_t records)
+// maximum over the 16 lanes of a row, in all of them
+__device__ __forceinline__ float row16_max(float v)
 {
-    Walk w;
-    w.on = i < records;
-    w.keys = nullptr;
-    w.score = w.row_log = 0.0;
-    w.row = lo;
-    w.end = -1;
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) w.ahead[j] = 0;
-    if (w.on) {
-        const int span = (int)(i % p.spans);
-        w.row = lo + (int)(i / p.spans);
-        w.keys = p.keys + ((int64_t)w.row * p.spans + span) * p.num_out;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (j < p.num_out) w.ahead[j] = w.keys[j];
-        const float score = p.score[w.row];
-        if (p.end_token) w.end = p.end_token[w.row];
-        w.score = (double)score;
-        w.on = !dead(score) && (w.end < 0 || span == 0);
-        if (w.end >= 0) w.ahead[0] = (uint32_t)~w.end; // its one continuation; the rest is never looked at
-    }
-    return w;
-}
-
-__device__ __forceinline__ Choice choice_of(const Walk &w, uint64_t key)
-{
-    const double total = w.end >= 0 ? w.score : w.score + ((double)unordered((uint32_t)(key >> 32)) - w.row_log);
-    return Choice{ordered64(total), key, (uint32_t)w.row};
+    v = fmaxf(v, Q4KV_DPP(v, v, 0xB1, 0xF));  // quad_perm [1,0,3,2]
+    v = fmaxf(v, Q4KV_DPP(v, v, 0x4E, 0xF));  // quad_perm [2,3,0,1]
+    v = fmaxf(v, Q4KV_DPP(v, v, 0x141, 0xF)); // row_half_mirror
+    return fmaxf(v, Q4KV_DPP(v, v, 0x140, 0xF)); // row_mirror
 }
 
 __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
@@ -526,67 +509,87 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
     __shared__ double s_log[kRowLogs];
     __shared__ int s_n;
     __shared__ float s_reached[kWaves];
-    const int g = blockIdx.x, t = threadIdx.x, keep = p.num_out;
+    const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, keep = p.num_out;
     const int lo = min(max(p.group_begin[g], 0), p.rows), hi = min(max(p.group_begin[g + 1], 0), p.rows);
     const int64_t records = (int64_t)max(hi - lo, 0) * p.spans;
-    Walk w = walk_at(p, lo, t, records); // of the first records; asked for ahead of the rows' sums
+    // A thread walks down a record, a span's elements in order; a finished row has one in its first span.
+    struct Walk {
+        const uint64_t *keys;
+        uint64_t key;
+        double score, row_log;
+        int32_t row, end;
+    } w;
+    auto start = [&](int64_t i) {
+        w = Walk{nullptr, 0, 0.0, 0.0, lo, -1};
+        if (i >= records) return;
+        const int r = (int)(i / p.spans), span = (int)(i - (int64_t)r * p.spans);
+        w.row = lo + r;
+        w.keys = p.keys + (int64_t)w.row * keep * p.spans + span;
+        w.key = w.keys[0];
+        const float score = p.score[w.row];
+        if (p.end_token) w.end = p.end_token[w.row];
+        w.score = (double)score;
+        if (w.end >= 0) w.key = span == 0 ? (uint32_t)~w.end : 0;
+        if (dead(score)) w.key = 0;
+    };
+    start(t); // the first records are asked for ahead of the rows' sums
     if (t == 0) s_n = 0;
-    // logarithms of the rows' sums: as many lanes to a row as it has spans, up to a wave.  Records of rows that were not read hold
-    // anything; what comes of them is never used.
-    int lanes = 1;
-    while (lanes < p.spans && lanes < kWave) lanes <<= 1;
-    const int first = t & (lanes - 1);
-    for (int r = lo + t / lanes; r - t / lanes < hi; r += kThreads / lanes) {
+    // Logarithms of the rows' sums, 16 lanes to a row.  Records of rows that were not read hold anything; what comes of them is
+    // never used.
+    for (int r = lo + t / 16; r - t / 16 < hi; r += kThreads / 16) {
         const SpanRecord *rec = p.records + (int64_t)r * p.spans;
-        const SpanRecord mine = r < hi && first < p.spans ? rec[first] : SpanRecord{0.0, kLowest, 0};
-        float ref = mine.ref;
-        if (r < hi)
-            for (int i = first + lanes; i < p.spans; i += lanes) ref = fmaxf(ref, rec[i].ref);
-        for (int off = 1; off < lanes; off <<= 1) ref = fmaxf(ref, __shfl_xor(ref, off));
-        double sum = mine.sum * exp_wide((double)mine.ref - (double)ref);
-        if (r < hi)
-            for (int i = first + lanes; i < p.spans; i += lanes) sum += rec[i].sum * exp_wide((double)rec[i].ref - (double)ref);
-        for (int off = 1; off < lanes; off <<= 1) sum += __shfl_xor(sum, off);
-        if (r < hi && first == 0) {
-            const double row_log = (double)ref + log_wide(sum);
+        const int spans = r < hi ? p.spans : 0;
+        float ref = kLowest;
+#pragma unroll 4
+        for (int i = t & 15; i < spans; i += 16) ref = fmaxf(ref, rec[i].ref);
+        ref = row16_max(ref);
+        double sum = 0.0;
+#pragma unroll 1
+        for (int i = t & 15; i < spans; i += 16) sum += rec[i].sum * exp_wide((double)rec[i].ref - (double)ref);
+        sum = row_sum<16>(sum);
+        const double row_log = (double)ref + log_wide(sum);
+        if (spans && (t & 15) == 0) {
             if (r - lo < kRowLogs) s_log[r - lo] = row_log;
             else p.row_log[r] = row_log;
         }
     }
     __syncthreads();
-    auto log_of = [&](int r) { return r - lo < kRowLogs ? s_log[r - lo] : p.row_log[r]; };
-    if (w.on && w.end < 0) w.row_log = log_of(w.row);
+    auto choice = [&] {
+        const double total = w.end >= 0 ? w.score : w.score + ((double)unordered((uint32_t)(w.key >> 32)) - w.row_log);
+        return Choice{ordered64(total), w.key, (uint32_t)w.row};
+    };
+    auto with_log = [&] {
+        if (w.key && w.end < 0) w.row_log = w.row - lo < kRowLogs ? s_log[w.row - lo] : p.row_log[w.row];
+    };
+    with_log();
     // What `keep` lanes of a wave reach with the first element of their records is reached by the group's best `keep`.
+    const float mine[1] = {w.key ? (float)unordered64(choice().total) : -kInf};
+    const float most = wave_max(mine[0]);
     float reached = -kInf;
-    {
-        float mine = w.on && w.ahead[0] ? (float)unordered64(choice_of(w, w.ahead[0]).total) : -kInf;
-        reached = reached_by(mine, keep);
-        if ((t & 63) == 0) s_reached[t >> 6] = reached;
-    }
+    if (__popcll(__ballot(w.key != 0)) >= keep) reached = reached_by_halving(mine, -wave_max(w.key ? -mine[0] : -kInf), most, keep);
+    if (lane == 0) s_reached[t >> 6] = reached;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) reached = fmaxf(reached, s_reached[i]);
-    // Every thread walks down its record until its next element is no better than the worst kept.
     int n = 0;
     Choice worst = {};
     bool full = false;
     for (int64_t base = 0; base < records; base += kThreads) {
         if (base > 0) {
-            w = walk_at(p, lo, base + t, records);
-            if (w.on && w.end < 0) w.row_log = log_of(w.row);
+            start(base + t);
+            with_log();
         }
-        for (int next = 0;; next += kAhead) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) { // at most kAhead * kThreads in a round
-                const Choice c = choice_of(w, w.ahead[j]);
-                w.on = w.on && w.ahead[j] != 0 && (float)unordered64(c.total) >= reached && !(full && !better(c, worst));
-                if (w.on) s_list.set(atomicAdd(&s_n, 1), c);
-                if (w.end >= 0) w.on = false;
-            }
-            const bool more = __syncthreads_or(w.on && next + kAhead < keep);
+        for (int next = 1;; ++next) {
+            // one element of every record that is still looked at, and the one behind it asked for
+            const uint64_t ahead = w.key && w.end < 0 && next < keep ? w.keys[(int64_t)next * p.spans] : 0;
+            const Choice c = choice();
+            const bool on = w.key != 0 && (float)unordered64(c.total) >= reached && !(full && !better(c, worst));
+            if (on) s_list.set(atomicAdd(&s_n, 1), c); // at most kThreads in a round
+            w.key = on ? ahead : 0;
+            const bool more = __syncthreads_or(w.key != 0);
             n = s_n;
             __syncthreads(); // everybody has the same n before the next push
-            if (n > kMergeList - kAhead * kThreads || (more && !full && n >= keep)) {
+            if (n > kMergeList - kThreads || (more && !full && n >= keep)) {
                 n = keep_best_choices(s_list, s_room, n, keep);
                 if (t == 0) s_n = n;
                 full = n == keep;
@@ -594,22 +597,28 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
                 __syncthreads();
             }
             if (!more) break;
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) w.ahead[j] = w.on && next + kAhead + j < keep ? w.keys[next + kAhead + j] : 0;
         }
     }
-    n = keep_best_choices(s_list, s_room, n, keep);
-    for (int i = t; i < keep; i += kThreads) {
-        const int64_t at = (int64_t)g * keep + i;
-        const bool in = i < n;
-        p.parent[at] = in ? (int32_t)s_list.row[i] : -1;
-        p.token[at] = in ? (int32_t)~(uint32_t)s_list.key[i] : -1;
-        p.total[at] = in ? (float)unordered64(s_list.total[i]) : -kInf;
+    if (n > kWave) n = keep_best_choices(s_list, s_room, n, keep);
+    if (t >= kWave) return;
+    // the last ones, a lane each
+    Choice c = {};
+    int rank = lane;
+    if (lane < n) {
+        c = s_list.at(lane);
+        rank = 0;
+        for (int j = 0; j < n; ++j) rank += better(s_list.at(j), c);
+    }
+    if (rank < keep) {
+        const int64_t at = (int64_t)g * keep + rank;
+        p.parent[at] = lane < n ? (int32_t)c.row : -1;
+        p.token[at] = lane < n ? (int32_t)~(uint32_t)c.key : -1;
+        p.total[at] = lane < n ? (float)unordered64(c.total) : -kInf;
     }
 }
 
 // Elements of a span: whole steps of a wave, so many that about kWavesPerCu waves per compute unit share the call's rows.
-constexpr int kWavesPerCu = 8, kMaxSteps = 8;
+constexpr int kWavesPerCu = 8;
 int span_length(int vocab, int rows, int compute_units)
 {
     const int64_t step = (int64_t)kWave * kHeld;
