@@ -19,8 +19,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kList = 192;     // candidates a wave can hold: what it keeps (64 at most) and two appends of up to 64
-constexpr int kMergeList = 1024;
-constexpr int kRowLogs = 64; // rows of a group whose logarithms are kept in LDS
+constexpr int kMergeList = 2048;
+constexpr int kRowsHeld = 64; // rows of a group that the merge keeps in LDS
 constexpr int kHeld = 32;      // elements of a step per lane
 constexpr int kMaxSteps = 8;   // steps of a span
 
@@ -469,6 +469,19 @@ struct MergeList {
         key[i] = c.key;
         row[i] = c.row;
     }
+    // how many of n are better than entry i
+    __device__ __forceinline__ int rank(int i, int n) const
+    {
+        const Choice mine = at(i);
+        int ahead = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) { // no branch: the reads of several entries overlap
+            const Choice other = at(j);
+            ahead += (other.total > mine.total) |
+                     ((other.total == mine.total) & ((other.row < mine.row) | ((other.row == mine.row) & (other.key > mine.key))));
+        }
+        return ahead;
+    }
 };
 
 // As keep_best, for a workgroup's list; `room`: LDS for what is kept.
@@ -477,14 +490,8 @@ __device__ __forceinline__ int keep_best_choices(MergeList &list, Choice *room, 
     __syncthreads();
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += kThreads) {
-        const Choice mine = list.at(i);
-        int ahead = 0;
-#pragma unroll 2
-        for (int j = 0; j < n; ++j) {
-            const uint64_t other = list.total[j];
-            ahead += other > mine.total || (other == mine.total && better(list.at(j), mine));
-        }
-        if (ahead < keep) room[ahead] = mine;
+        const int rank = list.rank(i, n);
+        if (rank < keep) room[rank] = list.at(i);
     }
     __syncthreads();
     const int kept = min(n, keep);
@@ -502,45 +509,42 @@ __device__ __forceinline__ float row16_max(float v)
     return fmaxf(v, Q4KV_DPP(v, v, 0x140, 0xF)); // row_mirror
 }
 
+// One group's choice out of what its rows' records list: chunks of kThreads * kTaken elements, of which those come into a list
+// that reach what `keep` of the chunk reach.  A chain of trips to memory (bounds, records, outputs) and of instructions
+// that every wave runs once; hence no loop is unrolled that does not have to be.
+constexpr int kTaken = 4;
 __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
 {
+    struct Row {
+        double score, log; // of the sum of its exponentials
+        int32_t end;       // its end token, or kOpen, or kDead
+    };
+    constexpr int32_t kOpen = -1, kDead = -2;
     __shared__ MergeList s_list;
     __shared__ Choice s_room[Q4KV_MAX_BEAM_OUT];
-    __shared__ double s_log[kRowLogs];
+    __shared__ Row s_row[kRowsHeld];
     __shared__ int s_n;
-    __shared__ float s_reached[kWaves];
-    const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, keep = p.num_out;
+    __shared__ float s_low[kWaves], s_most[kWaves];
+    __shared__ int s_count[3][kWaves];
+    const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6, keep = p.num_out;
     const int lo = min(max(p.group_begin[g], 0), p.rows), hi = min(max(p.group_begin[g + 1], 0), p.rows);
-    const int64_t records = (int64_t)max(hi - lo, 0) * p.spans;
-    // A thread walks down a record, a span's elements in order; a finished row has one in its first span.
-    struct Walk {
-        const uint64_t *keys;
-        uint64_t key;
-        double score, row_log;
-        int32_t row, end;
-    } w;
-    auto start = [&](int64_t i) {
-        w = Walk{nullptr, 0, 0.0, 0.0, lo, -1};
-        if (i >= records) return;
-        const int r = (int)(i / p.spans), span = (int)(i - (int64_t)r * p.spans);
-        w.row = lo + r;
-        w.keys = p.keys + (int64_t)w.row * keep * p.spans + span;
-        w.key = w.keys[0];
-        const float score = p.score[w.row];
-        if (p.end_token) w.end = p.end_token[w.row];
-        w.score = (double)score;
-        if (w.end >= 0) w.key = span == 0 ? (uint32_t)~w.end : 0;
-        if (dead(score)) w.key = 0;
-    };
-    start(t); // the first records are asked for ahead of the rows' sums
+    const int per_row = p.spans * keep; // elements of a row's records: at most 2^20 spans
+    const int64_t elements = (int64_t)max(hi - lo, 0) * per_row;
+    const uint64_t *keys = p.keys + (int64_t)lo * per_row;
+    uint64_t key[kTaken];
+#pragma unroll
+    for (int e = 0; e < kTaken; ++e) key[e] = e * kThreads + t < elements ? keys[e * kThreads + t] : 0; // asked for ahead of the rows' sums
     if (t == 0) s_n = 0;
     // Logarithms of the rows' sums, 16 lanes to a row.  Records of rows that were not read hold anything; what comes of them is
     // never used.
+#pragma unroll 1
     for (int r = lo + t / 16; r - t / 16 < hi; r += kThreads / 16) {
         const SpanRecord *rec = p.records + (int64_t)r * p.spans;
         const int spans = r < hi ? p.spans : 0;
+        const float score = spans ? p.score[r] : 0.0f;
+        const int32_t end = spans && p.end_token ? p.end_token[r] : -1;
         float ref = kLowest;
-#pragma unroll 4
+#pragma unroll 2
         for (int i = t & 15; i < spans; i += 16) ref = fmaxf(ref, rec[i].ref);
         ref = row16_max(ref);
         double sum = 0.0;
@@ -549,96 +553,164 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
         sum = row_sum<16>(sum);
         const double row_log = (double)ref + log_wide(sum);
         if (spans && (t & 15) == 0) {
-            if (r - lo < kRowLogs) s_log[r - lo] = row_log;
+            if (r - lo < kRowsHeld) s_row[r - lo] = Row{(double)score, row_log, dead(score) ? kDead : end >= 0 ? end : kOpen};
             else p.row_log[r] = row_log;
         }
     }
     __syncthreads();
-    auto choice = [&] {
-        const double total = w.end >= 0 ? w.score : w.score + ((double)unordered((uint32_t)(w.key >> 32)) - w.row_log);
-        return Choice{ordered64(total), w.key, (uint32_t)w.row};
+    auto row_at = [&](int r) {
+        if (r - lo < kRowsHeld) return s_row[r - lo];
+        const float score = p.score[r];
+        const int32_t end = p.end_token ? p.end_token[r] : -1;
+        return Row{(double)score, p.row_log[r], dead(score) ? kDead : end >= 0 ? end : kOpen};
     };
-    auto with_log = [&] {
-        if (w.key && w.end < 0) w.row_log = w.row - lo < kRowLogs ? s_log[w.row - lo] : p.row_log[w.row];
-    };
-    with_log();
-    // What `keep` lanes of a wave reach with the first element of their records is reached by the group's best `keep`.
-    const float mine[1] = {w.key ? (float)unordered64(choice().total) : -kInf};
-    const float most = wave_max(mine[0]);
-    float reached = -kInf;
-    if (__popcll(__ballot(w.key != 0)) >= keep) reached = reached_by_halving(mine, -wave_max(w.key ? -mine[0] : -kInf), most, keep);
-    if (lane == 0) s_reached[t >> 6] = reached;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) reached = fmaxf(reached, s_reached[i]);
     int n = 0;
+    float reached = -kInf;
     Choice worst = {};
     bool full = false;
-    for (int64_t base = 0; base < records; base += kThreads) {
-        if (base > 0) {
-            start(base + t);
-            with_log();
-        }
-        for (int next = 1;; ++next) {
-            // one element of every record that is still looked at, and the one behind it asked for
-            const uint64_t ahead = w.key && w.end < 0 && next < keep ? w.keys[(int64_t)next * p.spans] : 0;
-            const Choice c = choice();
-            const bool on = w.key != 0 && (float)unordered64(c.total) >= reached && !(full && !better(c, worst));
-            if (on) s_list.set(atomicAdd(&s_n, 1), c); // at most kThreads in a round
-            w.key = on ? ahead : 0;
-            const bool more = __syncthreads_or(w.key != 0);
-            n = s_n;
-            __syncthreads(); // everybody has the same n before the next push
-            if (n > kMergeList - kThreads || (more && !full && n >= keep)) {
-                n = keep_best_choices(s_list, s_room, n, keep);
-                if (t == 0) s_n = n;
-                full = n == keep;
-                if (full) worst = s_list.at(keep - 1);
-                __syncthreads();
+    const float one_row = 1.0f / (float)per_row;
+#pragma unroll 1
+    for (int64_t base = 0; base < elements; base += kThreads * kTaken) {
+        const int first_row = lo + (int)(base / per_row);
+        const uint32_t offset = (uint32_t)(base % per_row) + t;
+        Choice c[kTaken];
+        float total[kTaken], low = kInf, most = -kInf;
+        int valid = 0;
+#pragma unroll
+        for (int e = 0; e < kTaken; ++e) {
+            // at most 1,025 rows further on: the quotient is one off at most
+            const uint32_t at = offset + e * kThreads;
+            uint32_t row = (uint32_t)((float)at * one_row);
+            if (at < row * per_row) --row;
+            else if (at - row * per_row >= (uint32_t)per_row) ++row;
+            const bool first = at == row * per_row, in = base + e * kThreads + t < elements;
+            total[e] = -kInf;
+            c[e] = Choice{0, key[e], (uint32_t)first_row + row};
+            if (in && (key[e] != 0 || first)) {
+                const Row r = row_at(first_row + (int)row);
+                double v = r.score + ((double)unordered((uint32_t)(key[e] >> 32)) - r.log);
+                bool on = r.end == kOpen && key[e] != 0;
+                if (r.end >= 0) { // finished: its one continuation, in the place of the first element
+                    on = first;
+                    c[e].key = (uint32_t)~r.end;
+                    v = r.score;
+                }
+                c[e].total = ordered64(v);
+                if (on) total[e] = fmaxf((float)v, kLowest);
             }
-            if (!more) break;
+            valid += __popcll(__ballot(total[e] > -kInf));
+            most = fmaxf(most, total[e]);
+            if (total[e] > -kInf) low = fminf(low, total[e]);
+        }
+        // the next chunk's are on their way while this one's are looked at
+#pragma unroll
+        for (int e = 0; e < kTaken; ++e) {
+            const int64_t at = base + (kTaken + e) * kThreads + t;
+            key[e] = at < elements ? keys[at] : 0;
+        }
+        low = -wave_max(-low);
+        most = wave_max(most);
+        if (lane == 0) {
+            s_low[wave] = low;
+            s_most[wave] = most;
+            s_count[2][wave] = valid;
+        }
+        __syncthreads();
+        valid = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            low = fminf(low, s_low[i]);
+            most = fmaxf(most, s_most[i]);
+            valid += s_count[2][i];
+        }
+        if (valid >= keep) { // halving as in reached_by_halving, by all waves together
+            uint32_t under = ordered(low), above = ordered(most);
+            int slot = 0;
+#pragma unroll 1
+            while (under < above) {
+                const uint32_t mid = under + (above - under + 1) / 2;
+                const float m = unordered(mid);
+                int count = 0;
+#pragma unroll
+                for (int e = 0; e < kTaken; ++e) count += __popcll(__ballot(total[e] >= m));
+                if (lane == 0) s_count[slot][wave] = count;
+                __syncthreads(); // the other slot's counts have been read by all when this one's are written again
+                count = 0;
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) count += s_count[slot][i];
+                slot ^= 1;
+                if (count >= keep) {
+                    under = mid;
+                    if (count <= 2 * keep) break;
+                } else {
+                    above = mid - 1;
+                }
+            }
+            reached = fmaxf(reached, unordered(under));
+        }
+        int mine = 0, place[kTaken];
+#pragma unroll
+        for (int e = 0; e < kTaken; ++e) {
+            const bool on = total[e] > -kInf && total[e] >= reached && !(full && !better(c[e], worst));
+            const uint64_t mask = __ballot(on);
+            place[e] = on ? mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)) : -1;
+            mine += __popcll(mask);
+        }
+        if (mine > 0) {
+            int first = 0;
+            if (lane == 0) first = atomicAdd(&s_n, mine);
+            first = __builtin_amdgcn_readfirstlane(first);
+#pragma unroll
+            for (int e = 0; e < kTaken; ++e)
+                if (place[e] >= 0) s_list.set(first + place[e], c[e]);
+        }
+        __syncthreads();
+        n = s_n;
+        __syncthreads(); // everybody has the same n before the next append
+        if (n > kMergeList - kTaken * kThreads || (n > 2 * keep + kWave && base + kThreads * kTaken < elements)) {
+            n = keep_best_choices(s_list, s_room, n, keep);
+            if (t == 0) s_n = n;
+            full = n == keep;
+            if (full) worst = s_list.at(keep - 1);
+            __syncthreads();
         }
     }
     if (n > kWave) n = keep_best_choices(s_list, s_room, n, keep);
     if (t >= kWave) return;
     // the last ones, a lane each
-    Choice c = {};
-    int rank = lane;
-    if (lane < n) {
-        c = s_list.at(lane);
-        rank = 0;
-        for (int j = 0; j < n; ++j) rank += better(s_list.at(j), c);
-    }
+    const int rank = lane < n ? s_list.rank(lane, n) : lane;
     if (rank < keep) {
         const int64_t at = (int64_t)g * keep + rank;
-        p.parent[at] = lane < n ? (int32_t)c.row : -1;
-        p.token[at] = lane < n ? (int32_t)~(uint32_t)c.key : -1;
-        p.total[at] = lane < n ? (float)unordered64(c.total) : -kInf;
+        p.parent[at] = lane < n ? (int32_t)s_list.row[lane] : -1;
+        p.token[at] = lane < n ? (int32_t)~(uint32_t)s_list.key[lane] : -1;
+        p.total[at] = lane < n ? (float)unordered64(s_list.total[lane]) : -kInf;
     }
 }
 
-// Elements of a span: whole steps of a wave, so many that about kWavesPerCu waves per compute unit share the call's rows.
+// Elements of a span: whole steps of a wave, so many that about kWavesPerCu waves per compute unit share the call's rows, and that
+// a wave has four times as many maxima as it keeps elements.
 constexpr int kWavesPerCu = 8;
-int span_length(int vocab, int rows, int compute_units)
+int span_length(int vocab, int rows, int num_out, int compute_units)
 {
     const int64_t step = (int64_t)kWave * kHeld;
     const int64_t steps = ((int64_t)vocab + step - 1) / step * rows / ((int64_t)compute_units * kWavesPerCu);
-    return (int)(step * (steps < 1 ? 1 : steps > kMaxSteps ? kMaxSteps : steps));
+    const int64_t least = (num_out + 15) / 16;
+    return (int)(step * (steps < least ? least : steps > kMaxSteps ? kMaxSteps : steps));
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 } // namespace
 
-int beam_select_spans(int vocab, int rows, int compute_units)
+int beam_select_spans(int vocab, int rows, int num_out, int compute_units)
 {
-    const int len = span_length(vocab, rows, compute_units);
+    const int len = span_length(vocab, rows, num_out, compute_units);
     return (int)(((int64_t)vocab + len - 1) / len);
 }
 
 size_t beam_select_workspace_bytes(int vocab, int rows, int num_out, int compute_units)
 {
-    const size_t units = (size_t)rows * beam_select_spans(vocab, rows, compute_units);
+    const size_t units = (size_t)rows * beam_select_spans(vocab, rows, num_out, compute_units);
     return up(units * sizeof(SpanRecord)) + up((size_t)rows * sizeof(double)) + up(units * num_out * sizeof(uint64_t));
 }
 
@@ -652,8 +724,8 @@ hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream)
     p.group_begin = a.group_begin;
     p.rows = a.rows;
     p.vocab = a.vocab;
-    p.span_len = span_length(a.vocab, a.rows, a.compute_units);
-    p.spans = beam_select_spans(a.vocab, a.rows, a.compute_units);
+    p.span_len = span_length(a.vocab, a.rows, a.num_out, a.compute_units);
+    p.spans = beam_select_spans(a.vocab, a.rows, a.num_out, a.compute_units);
     p.groups = a.groups;
     p.num_out = a.num_out;
     p.parent = a.parent;

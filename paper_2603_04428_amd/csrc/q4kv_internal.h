@@ -155,7 +155,7 @@ struct BeamSelectArgs {
     void *workspace;
     int format, vocab, rows, groups, num_out, compute_units;
 };
-int beam_select_spans(int vocab, int rows, int compute_units);
+int beam_select_spans(int vocab, int rows, int num_out, int compute_units);
 size_t beam_select_workspace_bytes(int vocab, int rows, int num_out, int compute_units);
 hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream);
 
