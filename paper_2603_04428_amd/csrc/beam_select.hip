@@ -19,7 +19,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kList = 192;     // candidates a wave can hold: what it keeps (64 at most) and two appends of up to 64
-constexpr int kMergeList = 2048;
 constexpr int kRowsHeld = 64; // rows of a group that the merge keeps in LDS
 constexpr int kHeld = 32;      // elements of a step per lane
 constexpr int kMaxSteps = 8;   // steps of a span
@@ -459,9 +458,10 @@ __device__ __forceinline__ bool better(const Choice &a, const Choice &b)
     return a.total > b.total || (a.total == b.total && (a.row < b.row || (a.row == b.row && a.key > b.key)));
 }
 
+template <int SIZE>
 struct MergeList {
-    uint64_t total[kMergeList], key[kMergeList];
-    uint32_t row[kMergeList];
+    uint64_t total[SIZE], key[SIZE];
+    uint32_t row[SIZE];
     __device__ __forceinline__ Choice at(int i) const { return Choice{total[i], key[i], row[i]}; }
     __device__ __forceinline__ void set(int i, const Choice &c)
     {
@@ -485,11 +485,12 @@ struct MergeList {
 };
 
 // As keep_best, for a workgroup's list; `room`: LDS for what is kept.
-__device__ __forceinline__ int keep_best_choices(MergeList &list, Choice *room, int n, int keep)
+template <int THREADS, int SIZE>
+__device__ __forceinline__ int keep_best_choices(MergeList<SIZE> &list, Choice *room, int n, int keep)
 {
     __syncthreads();
 #pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const int rank = list.rank(i, n);
         if (rank < keep) room[rank] = list.at(i);
     }
@@ -513,14 +514,16 @@ __device__ __forceinline__ float row16_max(float v)
 // that reach what `keep` of the chunk reach.  A chain of trips to memory (bounds, records, outputs) and of instructions
 // that every wave runs once; hence no loop is unrolled that does not have to be.
 constexpr int kTaken = 4;
-__global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
 {
+    constexpr int kThreads = THREADS, kWaves = THREADS / kWave, kSize = (kTaken + 2) * THREADS;
     struct Row {
         double score, log; // of the sum of its exponentials
         int32_t end;       // its end token, or kOpen, or kDead
     };
     constexpr int32_t kOpen = -1, kDead = -2;
-    __shared__ MergeList s_list;
+    __shared__ MergeList<kSize> s_list;
     __shared__ Choice s_room[Q4KV_MAX_BEAM_OUT];
     __shared__ Row s_row[kRowsHeld];
     __shared__ int s_n;
@@ -667,15 +670,15 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectParams p)
         __syncthreads();
         n = s_n;
         __syncthreads(); // everybody has the same n before the next append
-        if (n > kMergeList - kTaken * kThreads || (n > 2 * keep + kWave && base + kThreads * kTaken < elements)) {
-            n = keep_best_choices(s_list, s_room, n, keep);
+        if (n > kSize - kTaken * kThreads || (n > 2 * keep + kWave && base + kThreads * kTaken < elements)) {
+            n = keep_best_choices<kThreads>(s_list, s_room, n, keep);
             if (t == 0) s_n = n;
             full = n == keep;
             if (full) worst = s_list.at(keep - 1);
             __syncthreads();
         }
     }
-    if (n > kWave) n = keep_best_choices(s_list, s_room, n, keep);
+    if (n > kWave) n = keep_best_choices<kThreads>(s_list, s_room, n, keep);
     if (t >= kWave) return;
     // the last ones, a lane each
     const int rank = lane < n ? s_list.rank(lane, n) : lane;
@@ -749,7 +752,11 @@ hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(beam_merge_kernel, dim3((unsigned)p.groups), dim3(kThreads), 0, stream, p);
+    // A workgroup of 1,024 where a group's records list more than a chunk of 256 threads
+    if (units * p.num_out > (int64_t)p.groups * kThreads * kTaken)
+        hipLaunchKernelGGL(beam_merge_kernel<1024>, dim3((unsigned)p.groups), dim3(1024), 0, stream, p);
+    else
+        hipLaunchKernelGGL(beam_merge_kernel<kThreads>, dim3((unsigned)p.groups), dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
