@@ -84,6 +84,8 @@ int check_table_pools(const q4kv_tables *t, const q4kv_spec *s, const q4kv_pool 
     int rc = check_spec(s);
     if (rc || (rc = check_pools(s, k, v))) return rc;
     if (k->num_blocks != t->num_blocks) return fail(Q4KV_EINVAL, "tables of %d blocks, pools of %d", t->num_blocks, k->num_blocks);
+    if (q4kv::image_record_bytes(*s) >= (1u << 31)) return fail(Q4KV_ESHAPE, "a block of one layer must be below 2^31 bytes");
+    if ((int64_t)s->num_layers * s->num_kv_heads >= 1LL << 31) return fail(Q4KV_ERANGE, "2^31 planes of layers and heads and more");
     if (!workspace || workspace_bytes < q4kv::tables_workspace_bytes(t->num_agents)) return fail(Q4KV_EWORKSPACE, "workspace too small or missing");
     if (!aligned16(workspace)) return fail(Q4KV_EINVAL, "workspace must be 16-byte aligned");
     return Q4KV_OK;

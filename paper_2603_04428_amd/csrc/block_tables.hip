@@ -439,59 +439,70 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
     settle(p, s, before, after, 0);
 }
 
-// The first tokens of blocks copied to other blocks, on every layer.  A unit is one head's plane of a (pair, layer): K codes,
-// scale, bias and the same of V, each a run of tokens * (bytes per token) bytes that begins on a multiple of 16 bytes; taken as one
-// list of 16-byte granules, kCopyUnit of them per step of a workgroup, every load in front of the first store.
-constexpr int kCopyThreads = 256, kCopyLoads = 4, kCopyUnit = kCopyThreads * kCopyLoads;
+// The first tokens of blocks copied to other blocks, on every layer.  In every (layer, head) plane of a block the tokens of each of
+// the six arrays are one run that begins on a multiple of 16 bytes.  A workgroup has a plane and takes pairs in turn, or, where
+// there are fewer pairs than workgroups to a plane, a part of a pair; kCopyLoads 16-byte loads per lane of K's and as many of
+// V's codes are in flight in front of the first store, and a wave takes one of the four arrays of parameters.
+constexpr int kCopyThreads = 256, kCopyLoads = 4;
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 struct TailParams {
-    unsigned char *pool[6];
-    int32_t token_bytes[6];
-    int32_t pieces, heads, layers, num_blocks, chunks; // chunks: steps of a unit of 256 tokens
+    unsigned char *codes[2], *params[4];
+    int32_t code_bytes[2], param_bytes[2]; // of a token in a plane; 0 where there is no V
+    int32_t heads, num_blocks;
     Moves moves;
 };
 
 __global__ __launch_bounds__(kCopyThreads) void tail_copy_kernel(TailParams p)
 {
-    typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
-    const int pairs = *p.moves.count;
-    const int64_t per_pair = (int64_t)p.layers * p.heads * p.chunks, items = pairs * per_pair;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int pair = (int)(item / per_pair);
-        const int64_t in_pair = item - pair * per_pair;
-        const int plane = (int)(in_pair / p.chunks), chunk = (int)(in_pair - (int64_t)plane * p.chunks);
-        const int layer = plane / p.heads, head = plane - layer * p.heads;
-        const int src = p.moves.src[pair], dst = p.moves.dst[pair], tokens = p.moves.tokens[pair];
-        const int64_t from = ((int64_t)layer * p.num_blocks + src) * p.heads + head, to = ((int64_t)layer * p.num_blocks + dst) * p.heads + head;
-        u4_t data[kCopyLoads];
-        unsigned char *out[kCopyLoads];
-        int bytes[kCopyLoads];
+    const int pairs = *p.moves.count, t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    if (pairs == 0) return;
+    const int layer = blockIdx.x / p.heads, head = blockIdx.x - layer * p.heads;
+    const int workers = gridDim.y, parts = max(1, workers / pairs), part = blockIdx.y / pairs;
+    if (part >= parts) return;
+    const int step = pairs < workers ? pairs : workers;
+    for (int pair = blockIdx.y % pairs; pair < pairs; pair += step) {
+        const int tokens = p.moves.tokens[pair];
+        const int64_t from = ((int64_t)layer * p.num_blocks + p.moves.src[pair]) * p.heads + head;
+        const int64_t to = ((int64_t)layer * p.num_blocks + p.moves.dst[pair]) * p.heads + head;
+        const u4_t *in[2];
+        u4_t *out[2];
+        int first[2], end[2]; // granules of 16 bytes
 #pragma unroll
-        for (int j = 0; j < kCopyLoads; ++j) {
-            int g = chunk * kCopyUnit + j * kCopyThreads + (int)threadIdx.x;
-            out[j] = nullptr;
-            bytes[j] = 0;
-#pragma unroll
-            for (int k = 0; k < 6; ++k) {
-                if (k >= p.pieces || out[j]) continue;
-                const int run = tokens * p.token_bytes[k], granules = (run + 15) >> 4;
-                if (g < granules) {
-                    const int64_t plane_bytes = (int64_t)p.token_bytes[k] * kBlockTokens;
-                    bytes[j] = min(16, run - 16 * g);
-                    data[j] = *reinterpret_cast<const u4_t *>(p.pool[k] + from * plane_bytes + 16 * g); // inside the plane: a multiple of 512 bytes
-                    out[j] = p.pool[k] + to * plane_bytes + 16 * g;
-                } else {
-                    g -= granules;
-                }
-            }
+        for (int k = 0; k < 2; ++k) {
+            const int64_t plane = (int64_t)p.code_bytes[k] * kBlockTokens;
+            const int granules = tokens * (p.code_bytes[k] / 16);
+            in[k] = reinterpret_cast<const u4_t *>(p.codes[k] + from * plane);
+            out[k] = reinterpret_cast<u4_t *>(p.codes[k] + to * plane);
+            first[k] = (int)((int64_t)granules * part / parts);
+            end[k] = (int)((int64_t)granules * (part + 1) / parts);
         }
+        const int rounds = (max(end[0] - first[0], end[1] - first[1]) + kCopyThreads * kCopyLoads - 1) / (kCopyThreads * kCopyLoads);
+        for (int r = 0; r < rounds; ++r) {
+            u4_t data[2][kCopyLoads];
 #pragma unroll
-        for (int j = 0; j < kCopyLoads; ++j) {
-            if (bytes[j] == 16) {
-                *reinterpret_cast<u4_t *>(out[j]) = data[j];
-            } else { // the last parameters of a run: pairs of bytes, what is behind them stays
-                for (int i = 0; i < bytes[j] / 2; ++i)
-                    reinterpret_cast<uint16_t *>(out[j])[i] = (uint16_t)(data[j][i >> 1] >> (16 * (i & 1)));
-            }
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < kCopyLoads; ++j) {
+                    const int i = first[k] + (r * kCopyLoads + j) * kCopyThreads + t;
+                    if (i < end[k]) data[k][j] = in[k][i];
+                }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < kCopyLoads; ++j) {
+                    const int i = first[k] + (r * kCopyLoads + j) * kCopyThreads + t;
+                    if (i < end[k]) out[k][i] = data[k][j];
+                }
+        }
+        const int bytes = tokens * p.param_bytes[wave >> 1];
+        if (part == 0 && bytes > 0) {
+            const int64_t plane = (int64_t)p.param_bytes[wave >> 1] * kBlockTokens;
+            const unsigned char *src = p.params[wave] + from * plane;
+            unsigned char *dst = p.params[wave] + to * plane;
+            for (int at = lane * 16; at + 16 <= bytes; at += kWave * 16)
+                *reinterpret_cast<u4_t *>(dst + at) = *reinterpret_cast<const u4_t *>(src + at);
+            const int rest = (bytes & ~15) + lane * 2; // what does not fill a granule, two bytes a lane: what is behind it stays
+            if (rest < bytes) *reinterpret_cast<uint16_t *>(dst + rest) = *reinterpret_cast<const uint16_t *>(src + rest);
         }
     }
 }
@@ -517,24 +528,23 @@ TablesParams params_of(const TablesArgs &a)
 hipError_t launch_tail_copy(const TablesArgs &a, const Moves &moves, hipStream_t stream)
 {
     TailParams p = {};
-    const q4kv_pool *const pools[2] = {a.k, a.v};
-    const int dims[2] = {a.spec->k_dim, a.spec->v_dim};
-    int granules = 0;
-    for (int i = 0; i < (a.v ? 6 : 3); ++i) {
-        const q4kv_pool &pool = *pools[i / 3];
-        const int dim = dims[i / 3];
-        p.pool[i] = i % 3 == 0 ? reinterpret_cast<unsigned char *>(pool.codes) : reinterpret_cast<unsigned char *>(i % 3 == 1 ? pool.scale : pool.bias);
-        p.token_bytes[i] = i % 3 == 0 ? dim / 2 : dim / kGroup * 2;
-        granules += p.token_bytes[i] * kBlockTokens / 16;
+    for (int i = 0; i < (a.v ? 2 : 1); ++i) {
+        const q4kv_pool &pool = i ? *a.v : *a.k;
+        const int dim = i ? a.spec->v_dim : a.spec->k_dim;
+        p.codes[i] = reinterpret_cast<unsigned char *>(pool.codes);
+        p.params[2 * i] = reinterpret_cast<unsigned char *>(pool.scale);
+        p.params[2 * i + 1] = reinterpret_cast<unsigned char *>(pool.bias);
+        p.code_bytes[i] = dim / 2;
+        p.param_bytes[i] = dim / kGroup * 2;
     }
-    p.pieces = a.v ? 6 : 3;
     p.heads = a.spec->num_kv_heads;
-    p.layers = a.spec->num_layers;
     p.num_blocks = a.k->num_blocks;
-    p.chunks = (granules + kCopyUnit - 1) / kCopyUnit;
     p.moves = moves;
-    const int64_t most = (int64_t)a.tables->num_agents * p.layers * p.heads * p.chunks, cap = 8LL * a.compute_units;
-    hipLaunchKernelGGL(tail_copy_kernel, dim3((unsigned)(most < cap ? most : cap)), dim3(kCopyThreads), 0, stream, p);
+    // the planes of all layers side by side, and workgroups to a plane so that eight or so stand on every compute unit
+    const int64_t planes = (int64_t)a.spec->num_layers * p.heads, wanted = 8LL * a.compute_units / planes;
+    const int most = a.tables->num_agents > 16 ? a.tables->num_agents : 16;
+    const int workers = (int)(wanted < 1 ? 1 : wanted > most ? most : wanted);
+    hipLaunchKernelGGL(tail_copy_kernel, dim3((unsigned)planes, (unsigned)workers), dim3(kCopyThreads), 0, stream, p);
     return hipGetLastError();
 }
 
