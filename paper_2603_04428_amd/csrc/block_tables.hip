@@ -20,7 +20,7 @@ constexpr int kRows = Q4KV_MAX_TABLE_ROWS;
 constexpr int kPer = kRows / kThreads; // rows of a lane: consecutive ones
 constexpr int kFree = 4096;            // free blocks kept in LDS; a call that takes more reads the counts twice
 constexpr int kHash = 2 * kRows;       // places for the shared blocks that rows end in
-constexpr int kRefs = 16;              // counts a lane reads at a time
+constexpr int kRefs = 4;               // counts a lane reads at a time: 16 bytes, consecutive lanes consecutive ones
 
 // Blocks to copy: counts[0] pairs; then sources, destinations, tokens.
 struct Moves {
@@ -46,46 +46,65 @@ struct Shared {
     uint8_t copy[kRows];
     int32_t free[kFree];
     int32_t key[kHash], lowest[kHash], rows[kHash];
-    uint32_t wave[2][kThreads / kWave];
+    uint32_t wave[8][kThreads / kWave]; // what the waves tell each other, by the place that asks: one barrier each
     int32_t first_refused, moves, refused;
 };
+enum Place { kGone, kGoneSum, kWidest, kShared, kNeed, kMore, kFound }; // kFound and the one behind it in turns
 
 __device__ __forceinline__ int blocks_of(int tokens) { return (tokens >> 8) + ((tokens & 255) != 0); }
 __device__ __forceinline__ uint32_t sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
-// Exclusive prefix sums of two numbers over the lanes of the workgroup, and their totals; sums that pass 32 bits stay at the top.
-__device__ __forceinline__ void scan(Shared &s, uint32_t a, uint32_t b, uint32_t &ex_a, uint32_t &ex_b, uint32_t &all_a, uint32_t &all_b)
+// Counts of blocks.  A kernel of one workgroup has them to itself; where several share a table's columns they meet in memory.
+template <bool ALONE>
+__device__ __forceinline__ void count(int32_t *ref, int32_t by)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t ia = a, ib = b;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const uint32_t ua = __shfl_up(ia, off), ub = __shfl_up(ib, off);
-        if (lane >= off) {
-            ia = sat(ia, ua);
-            ib = sat(ib, ub);
-        }
-    }
+    (void)__hip_atomic_fetch_add(ref, by, __ATOMIC_RELAXED, ALONE ? __HIP_MEMORY_SCOPE_WORKGROUP : __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// v and the sum of v over the lanes below, in steps of the data-parallel-primitive moves; sums that pass 32 bits stay at the top
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
+{
+#define Q4KV_SCAN_STEP(CTRL, ROWS) v = sat(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, (CTRL), (ROWS), 0xF, false))
+    Q4KV_SCAN_STEP(0x111, 0xF); // row_shr 1, 2, 4, 8
+    Q4KV_SCAN_STEP(0x112, 0xF);
+    Q4KV_SCAN_STEP(0x114, 0xF);
+    Q4KV_SCAN_STEP(0x118, 0xF);
+    Q4KV_SCAN_STEP(0x142, 0xA); // row_bcast15 into rows 1 and 3
+    Q4KV_SCAN_STEP(0x143, 0xC); // row_bcast31 into rows 2 and 3
+#undef Q4KV_SCAN_STEP
+    return v;
+}
+
+// Exclusive prefix sum of a number over the lanes of the workgroup out of its sum within the wave, and its total; behind a barrier
+// between the waves' writing of s.wave[place] and here.
+__device__ __forceinline__ void tell(Shared &s, int place, uint32_t v) { s.wave[place][threadIdx.x >> 6] = v; }
+__device__ __forceinline__ uint32_t told(const Shared &s, int place)
+{
+    const int lane = threadIdx.x & 63;
+    return lane < kThreads / kWave ? s.wave[place][lane] : 0u;
+}
+__device__ __forceinline__ uint32_t prefix(const Shared &s, int place, uint32_t inclusive, uint32_t &all)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t totals = wave_scan(told(s, place)); // the waves' totals in the lanes of every wave
+    all = (uint32_t)__builtin_amdgcn_readlane((int)totals, kThreads / kWave - 1);
+    const uint32_t below = wave ? (uint32_t)__builtin_amdgcn_readlane((int)totals, wave - 1) : 0u;
+    return sat(below, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)inclusive, 0x138, 0xF, 0xF, false)); // wave_shr 1
+}
+__device__ __forceinline__ uint32_t scan(Shared &s, int place, uint32_t v, uint32_t &all)
+{
+    const uint32_t inclusive = wave_scan(v);
+    if ((threadIdx.x & 63) == 63) tell(s, place, inclusive);
     __syncthreads();
-    if (lane == 63) {
-        s.wave[0][wave] = ia;
-        s.wave[1][wave] = ib;
-    }
+    return prefix(s, place, inclusive, all);
+}
+// Whether any lane of the workgroup says so.
+__device__ __forceinline__ bool any_of(Shared &s, int place, bool v)
+{
+    const bool here = __any(v);
+    if ((threadIdx.x & 63) == 0) tell(s, place, here);
     __syncthreads();
-    uint32_t la = __shfl_up(ia, 1), lb = __shfl_up(ib, 1); // what the lanes below have
-    if (lane == 0) la = lb = 0;
-    ex_a = ex_b = all_a = all_b = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) {
-        if (w == wave) {
-            ex_a = all_a;
-            ex_b = all_b;
-        }
-        all_a = sat(all_a, s.wave[0][w]);
-        all_b = sat(all_b, s.wave[1][w]);
-    }
-    ex_a = sat(ex_a, la);
-    ex_b = sat(ex_b, lb);
+    return __any(told(s, place) != 0);
 }
 
 // The row that item i belongs to: the last whose first item is not behind i.
@@ -100,23 +119,24 @@ __device__ __forceinline__ int row_of(const uint32_t *first, int rows, uint32_t 
     return lo;
 }
 
-// What one thread reads of the counts: kRefs from `at` on, bit i set where count i is 0.
-__device__ __forceinline__ uint32_t free_bits(const TablesParams &p, int64_t at)
+// What a lane reads of the counts: kRefs from `at` on, and bit i set where count i is 0.
+struct Counts {
+    int4 c;
+};
+__device__ __forceinline__ Counts counts_at(const TablesParams &p, int64_t at)
 {
-    uint32_t bits = 0;
-    if (at + kRefs <= p.num_blocks) {
-        int4 c[kRefs / 4];
-#pragma unroll
-        for (int i = 0; i < kRefs / 4; ++i) c[i] = reinterpret_cast<const int4 *>(p.refs + at)[i];
-#pragma unroll
-        for (int i = 0; i < kRefs / 4; ++i)
-            bits |= (uint32_t)(c[i].x == 0) << (4 * i) | (uint32_t)(c[i].y == 0) << (4 * i + 1) | (uint32_t)(c[i].z == 0) << (4 * i + 2) |
-                    (uint32_t)(c[i].w == 0) << (4 * i + 3);
+    Counts k;
+    if (__builtin_expect(at + kRefs <= p.num_blocks, 1)) {
+        k.c = *reinterpret_cast<const int4 *>(p.refs + at);
     } else {
-        for (int i = 0; i < kRefs; ++i)
-            if (at + i < p.num_blocks && p.refs[at + i] == 0) bits |= 1u << i;
+        auto one = [&](int64_t i) { return i < p.num_blocks ? p.refs[i] : 1; }; // behind the last: taken
+        k.c = make_int4(one(at), one(at + 1), one(at + 2), one(at + 3));
     }
-    return bits;
+    return k;
+}
+__device__ __forceinline__ uint32_t free_bits(const Counts &k)
+{
+    return (uint32_t)(k.c.x == 0) | (uint32_t)(k.c.y == 0) << 1 | (uint32_t)(k.c.z == 0) << 2 | (uint32_t)(k.c.w == 0) << 3;
 }
 
 // A free block becomes item i of the rows' items.
@@ -128,7 +148,7 @@ __device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uin
     p.refs[id] = 1;
     if (s.copy[r] && k == 0) {
         const int32_t src = row[at >> 8];
-        atomicSub(&p.refs[src], 1);
+        count<true>(&p.refs[src], -1);
         row[at >> 8] = id;
         const int m = atomicAdd(&s.moves, 1);
         p.moves.src[m] = src;
@@ -144,6 +164,7 @@ __device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uin
 __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const int (&before)[kPer], int (&after)[kPer], int refused)
 {
     const int t = threadIdx.x;
+    Counts counts = counts_at(p, (int64_t)t * kRefs); // on their way while rows are looked at
     bool shared[kPer], copy[kPer];
     int32_t last[kPer];
     int32_t listed[kPer];
@@ -167,8 +188,10 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         s.refused = 0;
         s.first_refused = p.agents;
     }
-    if (__syncthreads_or(any)) {
-        for (int i = t; i < kHash; i += kThreads) {
+    if (__builtin_expect(any_of(s, kShared, any), 0)) {
+        int places = 64; // twice as many as rows
+        while (places < 2 * p.agents) places <<= 1;
+        for (int i = t; i < places; i += kThreads) {
             s.key[i] = -1;
             s.lowest[i] = kRows;
             s.rows[i] = 0;
@@ -178,11 +201,11 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (!shared[i]) continue;
-            int h = (int)(((uint32_t)last[i] * 2654435769u) >> 20) & (kHash - 1);
-            while (true) { // at most kRows keys in twice as many places
+            int h = (int)(((uint32_t)last[i] * 2654435769u) >> 20) & (places - 1);
+            while (true) { // at most as many keys as rows
                 const int32_t was = atomicCAS(&s.key[h], -1, last[i]);
                 if (was == -1 || was == last[i]) break;
-                h = (h + 1) & (kHash - 1);
+                h = (h + 1) & (places - 1);
             }
             atomicMin(&s.lowest[h], kPer * t + i);
             atomicAdd(&s.rows[h], 1);
@@ -198,7 +221,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
     for (int i = 0; i < kPer; ++i) {
         if (copy[i] && !p.copies) { // cut inside a shared block, and nothing to copy it with
             const int r = kPer * t + i;
-            atomicSub(&p.refs[last[i]], 1);
+            count<true>(&p.refs[last[i]], -1);
             p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
             after[i] &= ~255;
             copy[i] = false;
@@ -207,16 +230,26 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         need[i] = (uint32_t)copy[i] + (uint32_t)max(0, blocks_of(after[i]) - blocks_of(before[i]));
         more[i] = p.max_tokens > 0 ? (uint32_t)max(0, after[i] - before[i]) : 0u;
     }
-    uint32_t ex_need, ex_more, all_need, all_more;
-    scan(s, sat(need[0], need[1]), sat(more[0], more[1]), ex_need, ex_more, all_need, all_more);
+    const uint32_t in_need = wave_scan(sat(need[0], need[1])), in_more = wave_scan(sat(more[0], more[1]));
+    if ((t & 63) == 63) {
+        tell(s, kNeed, in_need);
+        tell(s, kMore, in_more);
+    }
+    __syncthreads();
+    uint32_t all_need, all_more;
+    const uint32_t ex_need = prefix(s, kNeed, in_need, all_need), ex_more = prefix(s, kMore, in_more, all_more);
     const uint32_t first_need[kPer] = {ex_need, sat(ex_need, need[0])}, first_more[kPer] = {ex_more, sat(ex_more, more[0])};
     // free blocks, lowest first, as far as they are needed
     uint32_t found = 0;
+    int turn = 0;
+#pragma unroll 1
     for (int64_t base = 0; base < p.num_blocks && found < all_need; base += kThreads * kRefs) {
-        const uint32_t bits = free_bits(p, base + (int64_t)t * kRefs);
-        uint32_t ex, none, all, none_all;
-        scan(s, __popc(bits), 0, ex, none, all, none_all);
-        uint32_t rank = found + ex;
+        const uint32_t bits = free_bits(counts);
+        counts = counts_at(p, base + kThreads * kRefs + (int64_t)t * kRefs);
+        uint32_t all;
+        uint32_t rank = found + scan(s, kFound + turn, __popc(bits), all);
+        turn ^= 1;
+#pragma unroll 1
         for (uint32_t b = bits; b && rank < kFree; b &= b - 1, ++rank) s.free[rank] = (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1);
         found += all;
     }
@@ -238,7 +271,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
                 if (after[i] > before[i]) { // stays as it was
                     after[i] = before[i];
                 } else {
-                    atomicSub(&p.refs[last[i]], 1);
+                    count<true>(&p.refs[last[i]], -1);
                     p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
                     after[i] &= ~255;
                 }
@@ -263,14 +296,16 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
     if (refused) atomicAdd(&s.refused, refused);
     __syncthreads();
     const uint32_t taken = s.items[p.agents], mapped = s.tokens[p.agents];
-    if (taken > kFree) {
+    uint32_t seen = 0;
+    if (__builtin_expect(taken > kFree, 0)) {
         // more than LDS holds: those behind are taken while the counts are read once more (before any of them changes)
-        uint32_t seen = 0;
+#pragma unroll 1
         for (int64_t base = 0; base < p.num_blocks && seen < taken; base += kThreads * kRefs) {
-            const uint32_t bits = free_bits(p, base + (int64_t)t * kRefs);
-            uint32_t ex, none, all, none_all;
-            scan(s, __popc(bits), 0, ex, none, all, none_all);
-            uint32_t rank = seen + ex;
+            const uint32_t bits = free_bits(counts_at(p, base + (int64_t)t * kRefs));
+            uint32_t all;
+            uint32_t rank = seen + scan(s, kFound + turn, __popc(bits), all);
+            turn ^= 1;
+#pragma unroll 1
             for (uint32_t b = bits; b && rank < taken; b &= b - 1, ++rank)
                 if (rank >= kFree) take_block(p, s, rank, (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1));
             seen += all;
@@ -327,9 +362,9 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
         }
         gone[i] = (uint32_t)max(0, blocks_of(before[i]) - blocks_of(after[i]));
     }
-    uint32_t ex, none, all, none_all;
-    scan(s, sat(gone[0], gone[1]), 0, ex, none, all, none_all);
-    if (all > 0) {
+    if (any_of(s, kGone, (gone[0] | gone[1]) != 0)) {
+        uint32_t all;
+        const uint32_t ex = scan(s, kGoneSum, sat(gone[0], gone[1]), all);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int r = kPer * t + i;
@@ -338,15 +373,15 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
             s.after[r] = after[i];
         }
         __syncthreads();
+#pragma unroll 1
         for (uint32_t i = t; i < all; i += kThreads) {
             const int r = row_of(s.items, p.agents, i);
             int32_t *entry = p.table + (int64_t)r * p.max_blocks + blocks_of(s.after[r]) + (i - s.items[r]);
             const int32_t id = *entry;
-            if ((uint32_t)id < (uint32_t)p.num_blocks) atomicSub(&p.refs[id], 1);
+            if ((uint32_t)id < (uint32_t)p.num_blocks) count<true>(&p.refs[id], -1);
             *entry = -1;
         }
-        __threadfence(); // the counts are read from here on
-        __syncthreads();
+        __syncthreads(); // the counts are read from here on
     }
     settle(p, s, before, after, refused);
 }
@@ -375,67 +410,97 @@ __global__ __launch_bounds__(256) void slot_map_kernel(TablesParams p)
 // Rows' entries of a slab of columns become those of their parents.  All of a slab's entries are read before the first is
 // written, kHeld a lane; columns have nothing to do with each other, so that any number of workgroups shares the table.
 constexpr int kHeld = 8;
-__device__ __forceinline__ void gather_rows(const TablesParams &p, Shared &s, int first_slab, int slabs)
+template <bool ALONE, int HELD>
+__device__ __forceinline__ void gather_slabs(const TablesParams &p, Shared &s, int first_slab, int slabs, int widest, int cols)
 {
     const int t = threadIdx.x;
-    for (int r = t; r < p.agents; r += kThreads) {
-        const int32_t from = p.parent[r];
-        const bool has = from >= 0 && from < p.agents;
-        s.key[r] = has ? from : -1;
-        s.before[r] = blocks_of(length_of(p, r));
-        s.after[r] = has ? blocks_of(length_of(p, from)) : 0;
-    }
-    __syncthreads();
-    const int cols = max(1, kThreads * kHeld / p.agents); // at least kHeld / kPer
-    for (int64_t c0 = (int64_t)first_slab * cols; c0 < p.max_blocks; c0 += (int64_t)slabs * cols) {
-        int32_t was[kHeld], is[kHeld];
+    const int r0 = t / cols, c0 = t - r0 * cols, r_step = kThreads / cols, c_step = kThreads - r_step * cols;
+#pragma unroll 1
+    for (int64_t slab = (int64_t)first_slab * cols; slab < widest; slab += (int64_t)slabs * cols) {
+        int32_t was[HELD], is[HELD], row[HELD], col[HELD];
+        int r = r0, c = c0;
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            const int i = k * kThreads + t, r = i / cols;
-            const int64_t c = c0 + i % cols;
-            was[k] = is[k] = -1;
-            if (r >= p.agents || c >= p.max_blocks) continue;
-            if (c < s.before[r]) was[k] = p.table[(int64_t)r * p.max_blocks + c];
-            if (c < s.after[r]) is[k] = p.table[(int64_t)s.key[r] * p.max_blocks + c];
+        for (int k = 0; k < HELD; ++k) {
+            const int64_t at = slab + c;
+            was[k] = is[k] = row[k] = -1;
+            col[k] = (int)at;
+            if (r < p.agents && s.key[r] != r) {
+                const int64_t from = s.key[r];
+                row[k] = at < max(s.before[r], s.after[r]) ? r : -1;
+                if (at < s.before[r]) was[k] = p.table[(int64_t)r * p.max_blocks + at];
+                if (at < s.after[r]) is[k] = p.table[from * p.max_blocks + at];
+            }
+            r += r_step;
+            c += c_step;
+            if (c >= cols) {
+                c -= cols;
+                ++r;
+            }
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            const int i = k * kThreads + t, r = i / cols;
-            const int64_t c = c0 + i % cols;
-            if (r >= p.agents || c >= p.max_blocks || s.key[r] == r || c >= max(s.before[r], s.after[r])) continue;
-            if (was[k] == is[k] && c < s.before[r]) continue; // the prefix that rows share
-            if ((uint32_t)was[k] < (uint32_t)p.num_blocks) atomicSub(&p.refs[was[k]], 1);
-            if ((uint32_t)is[k] < (uint32_t)p.num_blocks) atomicAdd(&p.refs[is[k]], 1);
-            p.table[(int64_t)r * p.max_blocks + c] = is[k];
+        for (int k = 0; k < HELD; ++k) {
+            if (row[k] < 0 || (was[k] == is[k] && col[k] < s.before[row[k]])) continue; // equal: the prefix that rows share
+            if ((uint32_t)was[k] < (uint32_t)p.num_blocks) count<ALONE>(&p.refs[was[k]], -1);
+            if ((uint32_t)is[k] < (uint32_t)p.num_blocks) count<ALONE>(&p.refs[is[k]], 1);
+            p.table[(int64_t)row[k] * p.max_blocks + col[k]] = is[k];
         }
     }
+}
+
+// Leaves the rows' new lengths in s.items.
+template <bool ALONE>
+__device__ __forceinline__ void gather_rows(const TablesParams &p, Shared &s, int first_slab, int slabs)
+{
+    const int t = threadIdx.x;
+    int widest = 0; // no row lists more blocks, before or after
+    for (int r = t; r < p.agents; r += kThreads) {
+        const int32_t from = p.parent[r];
+        const bool has = from >= 0 && from < p.agents;
+        const int length = has ? length_of(p, from) : 0, before = blocks_of(length_of(p, r)), after = blocks_of(length);
+        s.key[r] = has ? from : -1;
+        s.before[r] = before;
+        s.after[r] = after;
+        s.items[r] = (uint32_t)length;
+        widest = max(widest, max(before, after));
+    }
+    // (as binary32: at most 2^23 blocks)
+    const float here = wave_max((float)widest);
+    if ((t & 63) == 0) tell(s, kWidest, (uint32_t)here);
+    __syncthreads();
+    widest = (int)wave_max((float)told(s, kWidest));
+    const int most = max(1, kThreads * kHeld / p.agents); // columns that fit: at least kHeld / kPer
+    const int cols = ALONE ? min(most, max(widest, 1)) : most;
+    if ((int64_t)p.agents * cols <= kThreads) gather_slabs<ALONE, 1>(p, s, first_slab, slabs, widest, cols);
+    else gather_slabs<ALONE, kHeld>(p, s, first_slab, slabs, widest, cols);
 }
 
 __global__ __launch_bounds__(kThreads) void gather_kernel(TablesParams p)
 {
     __shared__ Shared s;
-    gather_rows(p, s, blockIdx.x, gridDim.x);
+    gather_rows<false>(p, s, blockIdx.x, gridDim.x);
 }
 
 template <bool ALONE>
 __global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
 {
     __shared__ Shared s;
-    if (ALONE) {
-        gather_rows(p, s, 0, 1);
-        __threadfence();
-        __syncthreads();
-    }
     int before[kPer], after[kPer];
+    if (ALONE) gather_rows<true>(p, s, 0, 1);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = kPer * (int)threadIdx.x + i;
-        int32_t from = -1;
-        if (r < p.agents) from = p.parent[r];
-        before[i] = after[i] = from >= 0 && from < p.agents ? length_of(p, from) : 0;
+        int length = 0;
+        if (ALONE) {
+            if (r < p.agents) length = (int)s.items[r];
+        } else {
+            int32_t from = -1;
+            if (r < p.agents) from = p.parent[r];
+            if (from >= 0 && from < p.agents) length = length_of(p, from);
+        }
+        before[i] = after[i] = length;
     }
-    __syncthreads(); // lengths are read before the first is written
+    __syncthreads(); // lengths are read before the first is written, and counts from here on
     settle(p, s, before, after, 0);
 }
 
