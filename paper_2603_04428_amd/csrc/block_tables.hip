@@ -15,9 +15,9 @@
 namespace q4kv {
 namespace {
 
-constexpr int kThreads = 1024;
 constexpr int kRows = Q4KV_MAX_TABLE_ROWS;
-constexpr int kPer = kRows / kThreads; // rows of a lane: consecutive ones
+constexpr int kWide = 1024, kNarrow = 256; // threads of a workgroup: kThreads of the functions below
+constexpr int kPer = kRows / kWide;         // rows of a lane: consecutive ones
 constexpr int kFree = 4096;            // free blocks kept in LDS; a call that takes more reads the counts twice
 constexpr int kHash = 2 * kRows;       // places for the shared blocks that rows end in
 constexpr int kRefs = 4;               // counts a lane reads at a time: 16 bytes, consecutive lanes consecutive ones
@@ -46,7 +46,7 @@ struct Shared {
     uint8_t copy[kRows];
     int32_t free[kFree];
     int32_t key[kHash], lowest[kHash], rows[kHash];
-    uint32_t wave[8][kThreads / kWave]; // what the waves tell each other, by the place that asks: one barrier each
+    uint32_t wave[8][kWide / kWave]; // what the waves tell each other, by the place that asks: one barrier each
     int32_t first_refused, moves, refused;
 };
 enum Place { kGone, kGoneSum, kWidest, kShared, kNeed, kMore, kFound }; // kFound and the one behind it in turns
@@ -78,33 +78,37 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v)
 // Exclusive prefix sum of a number over the lanes of the workgroup out of its sum within the wave, and its total; behind a barrier
 // between the waves' writing of s.wave[place] and here.
 __device__ __forceinline__ void tell(Shared &s, int place, uint32_t v) { s.wave[place][threadIdx.x >> 6] = v; }
+template <int kThreads>
 __device__ __forceinline__ uint32_t told(const Shared &s, int place)
 {
     const int lane = threadIdx.x & 63;
     return lane < kThreads / kWave ? s.wave[place][lane] : 0u;
 }
+template <int kThreads>
 __device__ __forceinline__ uint32_t prefix(const Shared &s, int place, uint32_t inclusive, uint32_t &all)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t totals = wave_scan(told(s, place)); // the waves' totals in the lanes of every wave
+    const uint32_t totals = wave_scan(told<kThreads>(s, place)); // the waves' totals in the lanes of every wave
     all = (uint32_t)__builtin_amdgcn_readlane((int)totals, kThreads / kWave - 1);
     const uint32_t below = wave ? (uint32_t)__builtin_amdgcn_readlane((int)totals, wave - 1) : 0u;
     return sat(below, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)inclusive, 0x138, 0xF, 0xF, false)); // wave_shr 1
 }
+template <int kThreads>
 __device__ __forceinline__ uint32_t scan(Shared &s, int place, uint32_t v, uint32_t &all)
 {
     const uint32_t inclusive = wave_scan(v);
     if ((threadIdx.x & 63) == 63) tell(s, place, inclusive);
     __syncthreads();
-    return prefix(s, place, inclusive, all);
+    return prefix<kThreads>(s, place, inclusive, all);
 }
 // Whether any lane of the workgroup says so.
+template <int kThreads>
 __device__ __forceinline__ bool any_of(Shared &s, int place, bool v)
 {
     const bool here = __any(v);
     if ((threadIdx.x & 63) == 0) tell(s, place, here);
     __syncthreads();
-    return __any(told(s, place) != 0);
+    return __any(told<kThreads>(s, place) != 0);
 }
 
 // The row that item i belongs to: the last whose first item is not behind i.
@@ -161,6 +165,7 @@ __device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uin
 
 // Lane's rows kPer t .. : lengths from `before` (blocks up to there are listed) to `after`; rows that get shorter have given their
 // blocks back.  Finds the blocks that rows end in and share, takes free blocks, writes lengths and the map's bounds.
+template <int kThreads>
 __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const int (&before)[kPer], int (&after)[kPer], int refused)
 {
     const int t = threadIdx.x;
@@ -188,7 +193,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         s.refused = 0;
         s.first_refused = p.agents;
     }
-    if (__builtin_expect(any_of(s, kShared, any), 0)) {
+    if (__builtin_expect(any_of<kThreads>(s, kShared, any), 0)) {
         int places = 64; // twice as many as rows
         while (places < 2 * p.agents) places <<= 1;
         for (int i = t; i < places; i += kThreads) {
@@ -237,7 +242,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
     }
     __syncthreads();
     uint32_t all_need, all_more;
-    const uint32_t ex_need = prefix(s, kNeed, in_need, all_need), ex_more = prefix(s, kMore, in_more, all_more);
+    const uint32_t ex_need = prefix<kThreads>(s, kNeed, in_need, all_need), ex_more = prefix<kThreads>(s, kMore, in_more, all_more);
     const uint32_t first_need[kPer] = {ex_need, sat(ex_need, need[0])}, first_more[kPer] = {ex_more, sat(ex_more, more[0])};
     // free blocks, lowest first, as far as they are needed
     uint32_t found = 0;
@@ -247,55 +252,64 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         const uint32_t bits = free_bits(counts);
         counts = counts_at(p, base + kThreads * kRefs + (int64_t)t * kRefs);
         uint32_t all;
-        uint32_t rank = found + scan(s, kFound + turn, __popc(bits), all);
+        uint32_t rank = found + scan<kThreads>(s, kFound + turn, __popc(bits), all);
         turn ^= 1;
 #pragma unroll 1
         for (uint32_t b = bits; b && rank < kFree; b &= b - 1, ++rank) s.free[rank] = (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1);
         found += all;
     }
-    // rows are served in order up to the first that cannot be
+    uint32_t taken = 0, mapped = 0; // blocks and places that are given out
+    if (all_need | all_more) {
+        // rows are served in order up to the first that cannot be
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const bool fails = (need[i] || more[i]) &&
-                           (sat(first_need[i], need[i]) > found || (p.max_tokens > 0 && sat(first_more[i], more[i]) > (uint32_t)p.max_tokens));
-        if (fails) atomicMin(&s.first_refused, kPer * t + i);
-    }
-    __syncthreads();
-    const int first_refused = s.first_refused;
+        for (int i = 0; i < kPer; ++i) {
+            const bool fails = (need[i] || more[i]) &&
+                               (sat(first_need[i], need[i]) > found || (p.max_tokens > 0 && sat(first_more[i], more[i]) > (uint32_t)p.max_tokens));
+            if (fails) atomicMin(&s.first_refused, kPer * t + i);
+        }
+        __syncthreads();
+        const int first_refused = s.first_refused;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int r = kPer * t + i;
-        if (r < p.agents) {
-            if (r >= first_refused && (need[i] || after[i] > before[i])) {
-                ++refused;
-                if (after[i] > before[i]) { // stays as it was
-                    after[i] = before[i];
-                } else {
-                    count<true>(&p.refs[last[i]], -1);
-                    p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
-                    after[i] &= ~255;
+        for (int i = 0; i < kPer; ++i) {
+            const int r = kPer * t + i;
+            if (r < p.agents) {
+                if (r >= first_refused && (need[i] || after[i] > before[i])) {
+                    ++refused;
+                    if (after[i] > before[i]) { // stays as it was
+                        after[i] = before[i];
+                    } else {
+                        count<true>(&p.refs[last[i]], -1);
+                        p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
+                        after[i] &= ~255;
+                    }
+                    copy[i] = false;
                 }
-                copy[i] = false;
+                p.len[r] = after[i];
+                s.before[r] = before[i];
+                s.after[r] = after[i];
+                s.items[r] = first_need[i];
+                s.tokens[r] = first_more[i];
+                s.copy[r] = copy[i];
             }
-            p.len[r] = after[i];
-            s.before[r] = before[i];
-            s.after[r] = after[i];
-            s.items[r] = first_need[i];
-            s.tokens[r] = first_more[i];
-            s.copy[r] = copy[i];
+            if (r == first_refused) { // the items and tokens of the rows in front of it
+                s.items[p.agents] = first_need[i];
+                s.tokens[p.agents] = first_more[i];
+            }
         }
-        if (r == first_refused) { // the items and tokens of the rows in front of it
-            s.items[p.agents] = first_need[i];
-            s.tokens[p.agents] = first_more[i];
+        if (t == 0 && first_refused == p.agents) {
+            s.items[p.agents] = all_need;
+            s.tokens[p.agents] = all_more;
         }
+        if (refused) atomicAdd(&s.refused, refused);
+        __syncthreads();
+        taken = s.items[p.agents];
+        mapped = s.tokens[p.agents];
+    } else { // nobody wants anything
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (kPer * t + i < p.agents) p.len[kPer * t + i] = after[i];
+        if (refused) atomicAdd(&s.refused, refused);
     }
-    if (t == 0 && first_refused == p.agents) {
-        s.items[p.agents] = all_need;
-        s.tokens[p.agents] = all_more;
-    }
-    if (refused) atomicAdd(&s.refused, refused);
-    __syncthreads();
-    const uint32_t taken = s.items[p.agents], mapped = s.tokens[p.agents];
     uint32_t seen = 0;
     if (__builtin_expect(taken > kFree, 0)) {
         // more than LDS holds: those behind are taken while the counts are read once more (before any of them changes)
@@ -303,7 +317,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         for (int64_t base = 0; base < p.num_blocks && seen < taken; base += kThreads * kRefs) {
             const uint32_t bits = free_bits(counts_at(p, base + (int64_t)t * kRefs));
             uint32_t all;
-            uint32_t rank = seen + scan(s, kFound + turn, __popc(bits), all);
+            uint32_t rank = seen + scan<kThreads>(s, kFound + turn, __popc(bits), all);
             turn ^= 1;
 #pragma unroll 1
             for (uint32_t b = bits; b && rank < taken; b &= b - 1, ++rank)
@@ -314,7 +328,7 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
     }
     for (uint32_t i = t; i < min(taken, (uint32_t)kFree); i += kThreads) take_block(p, s, i, s.free[i]);
     if (p.max_tokens > 0) {
-        for (int r = t; r < p.agents; r += kThreads) p.token_begin[r] = (int32_t)min(s.tokens[r], mapped);
+        for (int r = t; r < p.agents; r += kThreads) p.token_begin[r] = mapped ? (int32_t)min(s.tokens[r], mapped) : 0;
         if (t == 0) p.token_begin[p.agents] = (int32_t)mapped;
     }
     __syncthreads();
@@ -344,6 +358,7 @@ __device__ __forceinline__ int length_of(const TablesParams &p, int r)
     return (int)min((int64_t)max(p.len[r], 0), most);
 }
 
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
 {
     __shared__ Shared s;
@@ -362,9 +377,9 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
         }
         gone[i] = (uint32_t)max(0, blocks_of(before[i]) - blocks_of(after[i]));
     }
-    if (any_of(s, kGone, (gone[0] | gone[1]) != 0)) {
+    if (any_of<kThreads>(s, kGone, (gone[0] | gone[1]) != 0)) {
         uint32_t all;
-        const uint32_t ex = scan(s, kGoneSum, sat(gone[0], gone[1]), all);
+        const uint32_t ex = scan<kThreads>(s, kGoneSum, sat(gone[0], gone[1]), all);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int r = kPer * t + i;
@@ -383,7 +398,7 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
         }
         __syncthreads(); // the counts are read from here on
     }
-    settle(p, s, before, after, refused);
+    settle<kThreads>(p, s, before, after, refused);
 }
 
 // The map of a call with many tokens, behind resize_kernel.
@@ -410,7 +425,7 @@ __global__ __launch_bounds__(256) void slot_map_kernel(TablesParams p)
 // Rows' entries of a slab of columns become those of their parents.  All of a slab's entries are read before the first is
 // written, kHeld a lane; columns have nothing to do with each other, so that any number of workgroups shares the table.
 constexpr int kHeld = 8;
-template <bool ALONE, int HELD>
+template <int kThreads, bool ALONE, int HELD>
 __device__ __forceinline__ void gather_slabs(const TablesParams &p, Shared &s, int first_slab, int slabs, int widest, int cols)
 {
     const int t = threadIdx.x;
@@ -449,7 +464,7 @@ __device__ __forceinline__ void gather_slabs(const TablesParams &p, Shared &s, i
 }
 
 // Leaves the rows' new lengths in s.items.
-template <bool ALONE>
+template <int kThreads, bool ALONE>
 __device__ __forceinline__ void gather_rows(const TablesParams &p, Shared &s, int first_slab, int slabs)
 {
     const int t = threadIdx.x;
@@ -468,25 +483,25 @@ __device__ __forceinline__ void gather_rows(const TablesParams &p, Shared &s, in
     const float here = wave_max((float)widest);
     if ((t & 63) == 0) tell(s, kWidest, (uint32_t)here);
     __syncthreads();
-    widest = (int)wave_max((float)told(s, kWidest));
+    widest = (int)wave_max((float)told<kThreads>(s, kWidest));
     const int most = max(1, kThreads * kHeld / p.agents); // columns that fit: at least kHeld / kPer
     const int cols = ALONE ? min(most, max(widest, 1)) : most;
-    if ((int64_t)p.agents * cols <= kThreads) gather_slabs<ALONE, 1>(p, s, first_slab, slabs, widest, cols);
-    else gather_slabs<ALONE, kHeld>(p, s, first_slab, slabs, widest, cols);
+    if ((int64_t)p.agents * cols <= kThreads) gather_slabs<kThreads, ALONE, 1>(p, s, first_slab, slabs, widest, cols);
+    else gather_slabs<kThreads, ALONE, kHeld>(p, s, first_slab, slabs, widest, cols);
 }
 
-__global__ __launch_bounds__(kThreads) void gather_kernel(TablesParams p)
+__global__ __launch_bounds__(kWide) void gather_kernel(TablesParams p)
 {
     __shared__ Shared s;
-    gather_rows<false>(p, s, blockIdx.x, gridDim.x);
+    gather_rows<kWide, false>(p, s, blockIdx.x, gridDim.x);
 }
 
-template <bool ALONE>
+template <int kThreads, bool ALONE>
 __global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
 {
     __shared__ Shared s;
     int before[kPer], after[kPer];
-    if (ALONE) gather_rows<true>(p, s, 0, 1);
+    if (ALONE) gather_rows<kThreads, true>(p, s, 0, 1);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = kPer * (int)threadIdx.x + i;
@@ -501,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
         before[i] = after[i] = length;
     }
     __syncthreads(); // lengths are read before the first is written, and counts from here on
-    settle(p, s, before, after, 0);
+    settle<kThreads>(p, s, before, after, 0);
 }
 
 // The first tokens of blocks copied to other blocks, on every layer.  In every (layer, head) plane of a block the tokens of each of
@@ -590,6 +605,15 @@ TablesParams params_of(const TablesArgs &a)
     return p;
 }
 
+// Whether a workgroup of 256 does: its four waves have a SIMD each, the sixteen of a wide one share them, which shows where a call is
+// a chain of instructions (resize, 40 rows a token longer: 4.2 us for 4.4, and back 3.2 for 3.8).  Many rows, counts to read or tokens
+// to map want more lanes (500 rows, 2,800 tokens: 13.2 for 8.0), and so do more entries to gather than lanes (64 rows of 17 blocks:
+// 10.6 for 8.2).
+bool narrow(const TablesParams &p)
+{
+    return p.agents <= kPer * kNarrow && p.num_blocks <= 16 * kNarrow * kRefs && (!p.map_here || p.max_tokens <= 4 * kNarrow);
+}
+
 hipError_t launch_tail_copy(const TablesArgs &a, const Moves &moves, hipStream_t stream)
 {
     TailParams p = {};
@@ -626,8 +650,9 @@ hipError_t launch_resize_tables(const TablesArgs &a, hipStream_t stream)
     p.slot = a.slot;
     p.token_agent = a.token_agent;
     p.position = a.position;
-    p.map_here = a.max_tokens <= 4096;
-    hipLaunchKernelGGL(resize_kernel, dim3(1), dim3(kThreads), 0, stream, p);
+    p.map_here = a.max_tokens <= 4 * kWide; // four rounds of the workgroup's lanes: less than another launch
+    if (narrow(p)) hipLaunchKernelGGL(resize_kernel<kNarrow>, dim3(1), dim3(kNarrow), 0, stream, p);
+    else hipLaunchKernelGGL(resize_kernel<kWide>, dim3(1), dim3(kWide), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.max_tokens > 0 && !p.map_here) {
         const int64_t blocks = ((int64_t)p.max_tokens + 255) / 256, cap = 8LL * a.compute_units;
@@ -644,14 +669,16 @@ hipError_t launch_beam_reorder(const TablesArgs &a, hipStream_t stream)
     p.parent = a.parent;
     const int64_t entries = (int64_t)p.agents * p.max_blocks;
     hipError_t e = hipSuccess;
-    if (entries <= 4 * kThreads * kHeld) {
-        hipLaunchKernelGGL(reorder_kernel<true>, dim3(1), dim3(kThreads), 0, stream, p);
+    if (narrow(p) && entries <= kNarrow) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(reorder_kernel<kNarrow, true>), dim3(1), dim3(kNarrow), 0, stream, p);
+    } else if (entries <= 4 * kWide * kHeld) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(reorder_kernel<kWide, true>), dim3(1), dim3(kWide), 0, stream, p);
     } else {
-        const int cols = kThreads * kHeld / p.agents;
+        const int cols = kWide * kHeld / p.agents;
         const int64_t slabs = ((int64_t)p.max_blocks + cols - 1) / cols, cap = 2LL * a.compute_units;
-        hipLaunchKernelGGL(gather_kernel, dim3((unsigned)(slabs < cap ? slabs : cap)), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL(gather_kernel, dim3((unsigned)(slabs < cap ? slabs : cap)), dim3(kWide), 0, stream, p);
         e = hipGetLastError();
-        if (e == hipSuccess) hipLaunchKernelGGL(reorder_kernel<false>, dim3(1), dim3(kThreads), 0, stream, p);
+        if (e == hipSuccess) hipLaunchKernelGGL(HIP_KERNEL_NAME(reorder_kernel<kWide, false>), dim3(1), dim3(kWide), 0, stream, p);
     }
     if (e == hipSuccess) e = hipGetLastError();
     if (e == hipSuccess) e = launch_tail_copy(a, p.moves, stream);
