@@ -7,7 +7,6 @@
 // 16 bytes of binary16 input (8 elements) and one 32-bit word of codes, so both the loads and
 // the stores of a wavefront are contiguous.
 #include <algorithm>
-#include <type_traits>
 
 #include "q4_device.h"
 #include "q4kv_internal.h"
@@ -107,22 +106,24 @@ struct AppendParams {
 
 // How the rows of a call lie and where they go.  kAgents: [layer][agent][chunk token][head], behind the agents' cached tokens.
 // kSlots: [layer][token], a fixed stride apart, each into its slot; kSlotsBf: the same with bfloat16 rows, rounded once to binary16.
-// A call with slots is one agent's to the kernels, whose chunk is all of its tokens.
+// A call with slots is one agent's, whose chunk is all of its tokens.
 enum AppendRows { kAgents, kSlots, kSlotsBf };
 
-// eight bfloat16 values as binary16
+// eight bfloat16 values as binary16, each rounded once
 __device__ __forceinline__ uint4 halves_of(uint4 raw)
 {
+    typedef float float2_t __attribute__((ext_vector_type(2)));
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
     uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        h[i] = (uint32_t)float_to_half_bits(__builtin_bit_cast(float, w[i] << 16)) |
-               (uint32_t)float_to_half_bits(__builtin_bit_cast(float, w[i] & 0xffff0000u)) << 16;
+    for (int i = 0; i < 4; ++i) {
+        const float2_t two = {__builtin_bit_cast(float, w[i] << 16), __builtin_bit_cast(float, w[i] & 0xffff0000u)};
+        h[i] = half2_to_bits(__builtin_convertvector(two, half2_t));
+    }
     return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
-template <bool BF, AppendRows ROWS>
+template <bool BF>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 {
     // a wave's round is 64 groups in four steps: whole lines of scales and biases (long chunks on many agents: the kernel is
@@ -141,9 +142,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
     uint16_t *__restrict__ scale = pp.pool[which].scale, *__restrict__ bias = pp.pool[which].bias;
     const uint32_t per_unit = (uint32_t)p.chunk_len * p.heads * p.groups_per_row; // groups of one (layer, agent)
     const int64_t src0 = ((int64_t)li * agents + a) * per_unit;
-    const int64_t stride = pp.pool[which].token_stride;
-    const int n0 = ROWS == kAgents ? p.seq_len_before[a] : 0;
-    const int32_t *table = ROWS == kAgents ? p.block_table + (int64_t)a * p.max_blocks : pp.slot;
+    const int n0 = p.seq_len_before[a];
+    const int32_t *table = p.block_table + (int64_t)a * p.max_blocks;
     // generations of the launch: workgroups in launch order (x fastest), about 256 of them per generation
     const uint32_t linear = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
     const int generation = linear / max(1u, gridDim.x * gridDim.y * gridDim.z / kWorkgroupsPerCu);
@@ -154,9 +154,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
     // by those (the vector ALUs were busy nine tenths of its time).
     __shared__ uint16_t s_par[kThreads / 64][2][64];
     __shared__ int64_t s_dst[kThreads / 64][64];  // group index in the pool, -1: skipped
-    // group index in this (layer, agent)'s source rows; with slots the distance from this layer's first row, in 8 elements
-    typedef std::conditional_t<ROWS == kAgents, uint32_t, int64_t> src_t;
-    __shared__ src_t s_src[kThreads / 64][64];
+    __shared__ uint32_t s_src[kThreads / 64][64]; // group index in this (layer, agent)'s source rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool words_ok = ((reinterpret_cast<uintptr_t>(scale) | reinterpret_cast<uintptr_t>(bias)) & 3u) == 0;
     const float inv_gpr = 1.0f / (float)p.groups_per_row, inv_chunk = 1.0f / (float)p.chunk_len;
@@ -178,10 +176,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const uint32_t l = step * 16 + 8 * j + (lane >> 3);
-                const int64_t at = ROWS == kAgents ? (src0 + s_src[wave][l]) * kGroup + sub * 8
-                                                   : (int64_t)li * p.chunk_len * stride + (s_src[wave][l] + sub) * 8;
-                raw[j] = c0 + l < per_unit ? *reinterpret_cast<const uint4 *>(x + at) : make_uint4(0, 0, 0, 0);
-                if (ROWS == kSlotsBf) raw[j] = halves_of(raw[j]);
+                raw[j] = c0 + l < per_unit ? *reinterpret_cast<const uint4 *>(x + (src0 + s_src[wave][l]) * kGroup + sub * 8)
+                                           : make_uint4(0, 0, 0, 0);
             }
         };
         {
@@ -192,16 +188,13 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
             const uint32_t heads = (uint32_t)(((float)cl + 0.5f) * inv_chunk);
             const uint32_t h = h0 + heads, c = cl - heads * p.chunk_len;
             const bool mine = lane < ROUND && c0 + lane < per_unit;
-            if (lane < ROUND) {
-                if constexpr (ROWS == kAgents) s_src[wave][lane] = (c * p.heads + h) * p.groups_per_row + g;
-                else s_src[wave][lane] = c * (stride / 8) + (h * p.groups_per_row + g) * 8;
-            }
+            if (lane < ROUND) s_src[wave][lane] = (c * p.heads + h) * p.groups_per_row + g;
             int64_t dgrp = -1;
             if (mine) {
-                const int t = ROWS == kAgents ? n0 + (int)c : table[c];
+                const int t = n0 + (int)c;
                 const int bi = t / kBlockTokens;
-                if (t >= 0 && (ROWS != kAgents || bi < p.max_blocks)) {
-                    const int blk = ROWS == kAgents ? table[bi] : bi;
+                if (t >= 0 && bi < p.max_blocks) {
+                    const int blk = table[bi];
                     if (blk >= 0 && blk < p.num_blocks) {
                         const int64_t drow = (((int64_t)(p.layer_begin + li) * p.num_blocks + blk) * p.heads + h) * kBlockTokens +
                                              (t % kBlockTokens);
@@ -251,6 +244,83 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// By slots: a round of a wave is one head's rows of as many consecutive tokens as make up 64 groups, and consecutive waves take the
+// heads of the same tokens.  So the tokens' rows, which a fused projection sets far apart, are read whole at about one time, and
+// what is written is a run of one head's plane wherever tokens have consecutive slots.  In the order of the kernel above, one head
+// of all tokens after the other, 8,400 rows of 16 128-wide heads that lie 12 KB apart, four layers, took 75 us.
+template <bool BF, bool IN_BF>
+__global__ __launch_bounds__(kThreads) void append_slots_kernel(AppendParams p)
+{
+    const int which = blockIdx.z >= (unsigned)p.layers ? 1 : 0, li = blockIdx.z - which * p.layers;
+    const AppendPool &pool = p.pool[which];
+    const int per_row = pool.groups_per_row, sub = threadIdx.x & 7, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = per_row < 64 ? 64 / per_row : 1, groups = min(64, tile * per_row); // (a row of more than 64 groups: several rounds)
+    const int pieces = (per_row + 63) / 64;
+    const uint32_t linear = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+    const int generation = linear / max(1u, gridDim.x * gridDim.y * gridDim.z / kWorkgroupsPerCu);
+    __shared__ uint16_t s_par[kThreads / 64][2][64];
+    __shared__ int64_t s_dst[kThreads / 64][64]; // group index in the pool, -1: skipped
+    __shared__ int64_t s_src[kThreads / 64][64]; // elements from the layer's first row
+    const uint16_t *__restrict__ x = pool.x + (int64_t)li * p.chunk_len * pool.token_stride + sub * 8;
+    const float one_row = 1.0f / (float)per_row;
+    const int64_t rounds = ((int64_t)p.chunk_len + tile - 1) / tile * pieces * p.heads;
+    for (int64_t round = (int64_t)blockIdx.x * (kThreads / 64) + wave; round < rounds; round += (int64_t)gridDim.x * (kThreads / 64)) {
+        rotate_wave_priority(generation);
+        const uint32_t tile_piece = (uint32_t)(round / p.heads), h = (uint32_t)(round - (int64_t)tile_piece * p.heads);
+        const uint32_t t0 = tile_piece / (uint32_t)pieces * tile, g0 = tile_piece % (uint32_t)pieces * 64;
+        {
+            // lane l's place: quotients of numbers below 64 as in the kernel above
+            const uint32_t c = pieces > 1 ? 0u : (uint32_t)(((float)lane + 0.5f) * one_row), g = g0 + lane - c * per_row, token = t0 + c;
+            int64_t dst = -1;
+            if (lane < groups && g < (uint32_t)per_row && token < (uint32_t)p.chunk_len) {
+                const int slot = p.slot[token], blk = slot / kBlockTokens;
+                if (slot >= 0 && blk < p.num_blocks)
+                    dst = ((((int64_t)(p.layer_begin + li) * p.num_blocks + blk) * p.heads + h) * kBlockTokens + slot % kBlockTokens) * per_row + g;
+            }
+            s_dst[wave][lane] = dst;
+            s_src[wave][lane] = (int64_t)token * pool.token_stride + ((int64_t)h * per_row + g) * kGroup;
+        }
+        wave_lds_sync();
+#pragma unroll 1
+        for (int step = 0; step < 4; ++step) {
+            uint4 raw[2];
+            int64_t dst[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int l = step * 16 + 8 * j + (lane >> 3);
+                dst[j] = s_dst[wave][l];
+                raw[j] = dst[j] >= 0 ? *reinterpret_cast<const uint4 *>(x + s_src[wave][l]) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint16_t sb, bb;
+                const uint32_t word = quantize_octet<BF>(IN_BF ? halves_of(raw[j]) : raw[j], sub, &sb, &bb);
+                if (dst[j] >= 0) pool.codes[dst[j] * 8 + sub] = word;
+                if (sub == 0) {
+                    s_par[wave][0][step * 16 + 8 * j + (lane >> 3)] = sb;
+                    s_par[wave][1][step * 16 + 8 * j + (lane >> 3)] = bb;
+                }
+            }
+        }
+        wave_lds_sync();
+        {
+            // two scales (lanes 0 to 31) or biases a lane, together where they are neighbours
+            const int pair = lane & 31;
+            const int64_t d0 = s_dst[wave][2 * pair], d1 = s_dst[wave][2 * pair + 1];
+            const uint32_t two = *reinterpret_cast<const uint32_t *>(&s_par[wave][lane >> 5][2 * pair]);
+            uint16_t *arr = lane >> 5 ? pool.bias : pool.scale;
+            if (d0 >= 0 && d1 == d0 + 1 && (d0 & 1) == 0) {
+                *reinterpret_cast<uint32_t *>(arr + d0) = two;
+            } else {
+                if (d0 >= 0) arr[d0] = (uint16_t)(two & 0xffffu);
+                if (d1 >= 0) arr[d1] = (uint16_t)(two >> 16);
+            }
+        }
+        wave_lds_sync();
     }
 }
 
@@ -397,10 +467,14 @@ hipError_t launch_append_rows(const q4kv_spec &spec, const AppendParams &p, bool
     if (gx > cap) gx = cap;
     if (gx < 1) gx = 1;
     const dim3 grid((unsigned)gx, (unsigned)num_agents, (unsigned)(pools * layers)), block(kThreads);
-    if (spec.param_format == Q4KV_PARAMS_BF16)
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(append_kernel<true, ROWS>), grid, block, 0, stream, p);
-    else
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(append_kernel<false, ROWS>), grid, block, 0, stream, p);
+    const bool bf16 = spec.param_format == Q4KV_PARAMS_BF16;
+    if constexpr (ROWS == kAgents) {
+        if (bf16) hipLaunchKernelGGL(append_kernel<true>, grid, block, 0, stream, p);
+        else hipLaunchKernelGGL(append_kernel<false>, grid, block, 0, stream, p);
+    } else {
+        if (bf16) hipLaunchKernelGGL(HIP_KERNEL_NAME(append_slots_kernel<true, ROWS == kSlotsBf>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(append_slots_kernel<false, ROWS == kSlotsBf>), grid, block, 0, stream, p);
+    }
     return hipGetLastError();
 }
 
