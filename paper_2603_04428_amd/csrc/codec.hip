@@ -454,7 +454,9 @@ hipError_t launch_append_rows(const q4kv_spec &spec, const AppendParams &p, bool
     // 64 groups per wave / an octet each): one token of ten agents, 256-wide heads 4.6 / 2.6, of three agents, sixteen 192 +
     // 128-wide heads 5.3 / 2.6; 70 tokens of four agents, 128-wide 6.8 / 2.8; 512 tokens of one agent, 256-wide 6.8 / 3.5; by
     // groups: 128,000 8.2 / 7.5, 164,000 9.4 / 8.3, 192,000 10.3 / 10.1, 320,000 13.8 / 14.8, 800,000 29.2 / 31.9.
-    if (units * per_unit <= 96 * slots) {
+    // By slots, up to 128 (262,144 groups): 64,000 11.0 / 5.0, 128,000 8.5 / 7.5, 192,000 12.8 / 10.2, 256,000 12.6 / 12.8, 384,000
+    // 16.3 / 17.4.
+    if (units * per_unit <= (ROWS == kAgents ? 96 : 128) * slots) {
         const dim3 grid((unsigned)((per_unit + kThreads / 8 - 1) / (kThreads / 8)), (unsigned)num_agents, (unsigned)(pools * layers));
         if (spec.param_format == Q4KV_PARAMS_BF16)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(append_few_kernel<true, ROWS>), grid, dim3(kThreads), 0, stream, p);
