@@ -518,16 +518,25 @@ def q4kv_norm_rope_append(spec, kpool, vpool, form, q, k_new, v_new, block_table
     return q_out
 
 
+def _slot_rows(t, heads, dim, name):
+    """[layers][tokens][heads][dim] -> the stride of its tokens, as _token_rows; most tensors are told by their strides alone."""
+    if t.dim() != 4:
+        raise TypeError(f"{name}: need [layers][tokens][{heads}][{dim}], got {tuple(t.shape)}")
+    layers, tokens, h, d = t.shape
+    s0, s1, s2, s3 = t.stride()
+    if h == heads and d == dim and s3 == 1 and s2 == dim and tokens > 1 and (layers == 1 or s0 == s1 * tokens) and t.is_cuda:
+        return s1
+    return _token_rows(t.unsqueeze(1), heads, dim, name)
+
+
 def q4kv_append_slots(spec, kpool, vpool, k_new, v_new, slot, layer_begin=0, layer_end=None):
     """k_new / v_new: fp16 or bf16 [layers_in_call][tokens][kv_heads][dim], possibly parts of one fused projection (tokens a fixed
     stride apart); slot: int32 [tokens] on the GPU, block * 256 + place, outside the pool: the token is skipped."""
     layer_end = spec.num_layers if layer_end is None else layer_end
-    if k_new.dim() != 4 or (v_new is not None and v_new.dim() != 4):
-        raise TypeError("k_new and v_new: need [layers][tokens][heads][dim]")
     hkv, kind, lead, v_stride = spec.num_kv_heads, k_new.dtype, k_new.shape[:2], 0
-    k_stride = _token_rows(k_new.unsqueeze(1), hkv, spec.k_dim, "k_new")
+    k_stride = _slot_rows(k_new, hkv, spec.k_dim, "k_new")
     if v_new is not None:
-        v_stride = _token_rows(v_new.unsqueeze(1), hkv, spec.v_dim, "v_new")
+        v_stride = _slot_rows(v_new, hkv, spec.v_dim, "v_new")
     if kind not in (torch.float16, torch.bfloat16) or (v_new is not None and v_new.dtype != kind):
         raise TypeError(f"k_new and v_new: fp16 or bf16, both of one type, got {kind}")
     if v_new is not None and v_new.shape[:2] != lead:
