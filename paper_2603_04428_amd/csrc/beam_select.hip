@@ -471,30 +471,42 @@ struct MergeList {
         key[i] = c.key;
         row[i] = c.row;
     }
-    // how many of n are better than entry i
-    __device__ __forceinline__ int rank(int i, int n) const
-    {
-        const Choice mine = at(i);
-        int ahead = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) { // no branch: the reads of several entries overlap
-            const Choice other = at(j);
-            ahead += (other.total > mine.total) |
-                     ((other.total == mine.total) & ((other.row < mine.row) | ((other.row == mine.row) & (other.key > mine.key))));
-        }
-        return ahead;
-    }
 };
+
+// How many of the list's n entries are better than one, counted by THREADS / 64 neighbouring lanes per entry, 64 entries at a time.
+template <int THREADS, int SIZE>
+__device__ __forceinline__ int rank_of(const MergeList<SIZE> &list, int n, const Choice &mine)
+{
+    constexpr int SHARE = THREADS / kWave;
+    static_assert(SHARE == 4 || SHARE == 16, "lanes of a quad or a row");
+    int ahead = 0;
+#pragma unroll 2
+    for (int j = threadIdx.x % SHARE; j < n; j += SHARE) { // no branch: the reads of several entries overlap
+        const Choice other = list.at(j);
+        ahead += (other.total > mine.total) |
+                 ((other.total == mine.total) & ((other.row < mine.row) | ((other.row == mine.row) & (other.key > mine.key))));
+    }
+    ahead += __builtin_amdgcn_mov_dpp(ahead, 0xB1, 0xF, 0xF, true); // quad_perm [1,0,3,2]
+    ahead += __builtin_amdgcn_mov_dpp(ahead, 0x4E, 0xF, 0xF, true); // quad_perm [2,3,0,1]
+    if constexpr (SHARE == 16) {
+        ahead += __builtin_amdgcn_mov_dpp(ahead, 0x141, 0xF, 0xF, true); // row_half_mirror
+        ahead += __builtin_amdgcn_mov_dpp(ahead, 0x140, 0xF, 0xF, true); // row_mirror
+    }
+    return ahead;
+}
 
 // As keep_best, for a workgroup's list; `room`: LDS for what is kept.
 template <int THREADS, int SIZE>
 __device__ __forceinline__ int keep_best_choices(MergeList<SIZE> &list, Choice *room, int n, int keep)
 {
+    constexpr int SHARE = THREADS / kWave;
     __syncthreads();
 #pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const int rank = list.rank(i, n);
-        if (rank < keep) room[rank] = list.at(i);
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+        const int i = i0 + threadIdx.x / SHARE;
+        const Choice mine = list.at(min(i, n - 1));
+        const int rank = rank_of<THREADS>(list, n, mine);
+        if (i < n && rank < keep && threadIdx.x % SHARE == 0) room[rank] = mine;
     }
     __syncthreads();
     const int kept = min(n, keep);
@@ -515,7 +527,7 @@ __device__ __forceinline__ float row16_max(float v)
 // One group's choice out of what its rows' records list: chunks of kThreads * kTaken elements, of which those come into a list
 // that reach what `keep` of the chunk reach.  A chain of trips to memory (bounds, records, outputs) and of instructions
 // that every wave runs once; hence no loop is unrolled that does not have to be.
-constexpr int kTaken = 4;
+constexpr int kTaken = 4, kRecordsHeld = 4;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
 {
@@ -548,15 +560,21 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
         const int spans = r < hi ? p.spans : 0;
         const float score = spans ? p.score[r] : 0.0f;
         const int32_t end = spans && p.end_token ? p.end_token[r] : -1;
+        SpanRecord held[kRecordsHeld];
+#pragma unroll
+        for (int k = 0; k < kRecordsHeld; ++k) held[k] = (t & 15) + 16 * k < spans ? rec[(t & 15) + 16 * k] : SpanRecord{0.0, kLowest, 0};
         float ref = kLowest;
-#pragma unroll 2
-        for (int i = t & 15; i < spans; i += 16) ref = fmaxf(ref, rec[i].ref);
+#pragma unroll
+        for (int k = 0; k < kRecordsHeld; ++k) ref = fmaxf(ref, held[k].ref);
+#pragma unroll 1
+        for (int i = (t & 15) + 16 * kRecordsHeld; i < spans; i += 16) ref = fmaxf(ref, rec[i].ref);
         ref = row16_max(ref);
         double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < kRecordsHeld; ++k) sum += held[k].sum * exp_wide((double)held[k].ref - (double)ref);
 #pragma unroll 1
-        for (int i = t & 15; i < spans; i += 16) sum += rec[i].sum * exp_wide((double)rec[i].ref - (double)ref);
-        sum = row_sum<16>(sum);
-        const double row_log = (double)ref + log_wide(sum);
+        for (int i = (t & 15) + 16 * kRecordsHeld; i < spans; i += 16) sum += rec[i].sum * exp_wide((double)rec[i].ref - (double)ref);
+        const double row_log = (double)ref + log_wide(row_sum<16>(sum));
         if (spans && (t & 15) == 0) {
             if (r - lo < kRowsHeld) s_row[r - lo] = Row{(double)score, row_log, dead(score) ? kDead : end >= 0 ? end : kOpen};
             else p.row_log[r] = row_log;
@@ -681,14 +699,16 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
         }
     }
     if (n > kWave) n = keep_best_choices<kThreads>(s_list, s_room, n, keep);
-    if (t >= kWave) return;
-    // the last ones, a lane each
-    const int rank = lane < n ? s_list.rank(lane, n) : lane;
-    if (rank < keep) {
-        const int64_t at = (int64_t)g * keep + rank;
-        p.parent[at] = lane < n ? (int32_t)s_list.row[lane] : -1;
-        p.token[at] = lane < n ? (int32_t)~(uint32_t)s_list.key[lane] : -1;
-        p.total[at] = lane < n ? (float)unordered64(s_list.total[lane]) : -kInf;
+    // the last ones, and behind them the places that stay empty
+    constexpr int SHARE = kThreads / kWave;
+    const int i = t / SHARE;
+    const Choice c = s_list.at(i);
+    const int rank = rank_of<kThreads>(s_list, n, c), place = i < n ? rank : i;
+    if (place < keep && t % SHARE == 0) {
+        const int64_t at = (int64_t)g * keep + place;
+        p.parent[at] = i < n ? (int32_t)c.row : -1;
+        p.token[at] = i < n ? (int32_t)~(uint32_t)c.key : -1;
+        p.total[at] = i < n ? (float)unordered64(c.total) : -kInf;
     }
 }
 
