@@ -85,7 +85,7 @@ int check_table_pools(const q4kv_tables *t, const q4kv_spec *s, const q4kv_pool 
     if (rc || (rc = check_pools(s, k, v))) return rc;
     if (k->num_blocks != t->num_blocks) return fail(Q4KV_EINVAL, "tables of %d blocks, pools of %d", t->num_blocks, k->num_blocks);
     if (q4kv::image_record_bytes(*s) >= (1u << 31)) return fail(Q4KV_ESHAPE, "a block of one layer must be below 2^31 bytes");
-    if ((int64_t)s->num_layers * s->num_kv_heads >= 1LL << 31) return fail(Q4KV_ERANGE, "2^31 planes of layers and heads and more");
+    if ((int64_t)s->num_layers * s->num_kv_heads >= 1LL << 24) return fail(Q4KV_ERANGE, "2^24 planes of layers and heads and more");
     if (!workspace || workspace_bytes < q4kv::tables_workspace_bytes(t->num_agents)) return fail(Q4KV_EWORKSPACE, "workspace too small or missing");
     if (!aligned16(workspace)) return fail(Q4KV_EINVAL, "workspace must be 16-byte aligned");
     return Q4KV_OK;
@@ -848,7 +848,7 @@ static int check_beam_sizes(int32_t format, int32_t vocab, int32_t num_agents, i
     if (vocab <= 0 || num_agents < 0) return fail(Q4KV_EINVAL, "negative count");
     if (vocab > 1 << 30) return fail(Q4KV_ERANGE, "a vocabulary of %d tokens, at most 2^30", vocab);
     if (num_out < 1 || num_out > Q4KV_MAX_BEAM_OUT) return fail(Q4KV_ERANGE, "num_out %d, from 1 to %d", num_out, Q4KV_MAX_BEAM_OUT);
-    if ((int64_t)num_agents * q4kv::beam_select_spans(vocab, num_agents, num_out, compute_units()) >= 1LL << 31)
+    if ((int64_t)num_agents * q4kv::beam_select_spans(vocab, num_agents, num_out, compute_units()) >= 1LL << 26)
         return fail(Q4KV_ERANGE, "%d rows of %d tokens: choose for fewer groups at a time", num_agents, vocab);
     return Q4KV_OK;
 }
@@ -867,6 +867,7 @@ int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stri
     if (rc) return rc;
     if (num_groups < 0) return fail(Q4KV_EINVAL, "negative count");
     if (num_groups == 0) return Q4KV_OK;
+    if (num_groups >= 1 << 22) return fail(Q4KV_ERANGE, "%d groups: choose for fewer at a time", num_groups);
     if (row_stride < vocab && num_agents > 1) return fail(Q4KV_ESHAPE, "rows of %d tokens, %lld elements apart", vocab, (long long)row_stride);
     if ((num_agents > 0 && (!logits || !score)) || !group_begin || !parent || !token || !total) return fail(Q4KV_EINVAL, "NULL pointer");
     if (reinterpret_cast<uintptr_t>(logits) % (logits_format == 2 ? 4 : 2)) return fail(Q4KV_EINVAL, "logits must be aligned to an element");

@@ -311,8 +311,9 @@ __device__ __forceinline__ bool scan_span(const char *row, int begin, int end, i
         }
         tops[(at - begin) / STEP * kWave + lane] = mine;
         largest = fmaxf(largest, mine);
-        // The reference is the maximum of the first step that has a value; it moves only where an exponential could grow large.
-        if (unset || __any(mine > at_ref.ref + 40.0f)) {
+        // The reference is the maximum of the first step that has a value; it moves where a step's is well above it (exponents are
+        // good to 2^-24 of their size).
+        if (unset || __any(mine > at_ref.ref + 8.0f)) {
             const float highest = wave_max(mine);
             if (highest > -kInf) {
                 const float scale = unset ? 0.0f : __builtin_amdgcn_exp2f((at_ref.ref - highest) * kLog2e[0]);

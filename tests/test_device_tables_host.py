@@ -106,7 +106,7 @@ def select(**kw):
 
 @pytest.mark.parametrize("code,text,kw", [
     (-1, "logits_format", dict(fmt=3)), (-1, "logits_format", dict(fmt=-1)), (-1, "negative", dict(vocab=0)), (-1, "negative", dict(rows=-1)),
-    (-1, "negative", dict(groups=-1)), (-3, "vocabulary", dict(vocab=(1 << 30) + 1, stride=1 << 40)), (-3, "num_out", dict(out=0)), (-3, "num_out", dict(out=65)),
+    (-1, "negative", dict(groups=-1)), (-3, "groups", dict(groups=1 << 22)), (-3, "fewer groups", dict(rows=1 << 23, vocab=1 << 18, stride=1 << 18)), (-3, "vocabulary", dict(vocab=(1 << 30) + 1, stride=1 << 40)), (-3, "num_out", dict(out=0)), (-3, "num_out", dict(out=65)),
     (-3, "fewer groups", dict(rows=2 ** 31 - 1, vocab=1 << 20, stride=1 << 20)), (-2, "apart", dict(stride=999)), (-1, "NULL", dict(logits=None)),
     (-1, "NULL", dict(score=None)), (-1, "NULL", dict(bounds=None)), (-1, "NULL", dict(parent=None)), (-1, "NULL", dict(token=None)),
     (-1, "NULL", dict(total=None)), (-1, "element", dict(logits=0x4001)), (-1, "element", dict(logits=0x4002, fmt=2)), (-4, "workspace", dict(ws=None)),
