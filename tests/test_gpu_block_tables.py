@@ -68,13 +68,15 @@ class Both:
             out = b.TokenMap(self.t, max_tokens + slack)
             for x in (out.begin, out.slot, out.agent, out.position):
                 x.fill_(-77)
-            out.slot, out.agent, out.position = (x[:max_tokens] for x in (out.slot, out.agent, out.position))
+            whole = out.slot, out.agent, out.position
+            out.slot, out.agent, out.position = (x[:max_tokens] for x in whole)
         want = self.model.resize(new_len, max_tokens)
         b.q4kv_resize_tables(self.t, torch.tensor(new_len, dtype=torch.int32, device=DEV), out=out, **self.args())
         self.check()
         if max_tokens:
             for got, w in zip((out.begin, out.slot, out.agent, out.position), want):
                 assert got.tolist() == list(w)
+            assert all((x[max_tokens:] == -77).all() for x in whole)
 
     def reorder(self, parent):
         self.model.reorder(parent)
