@@ -87,8 +87,8 @@ __device__ __forceinline__ uint32_t quantize_octet(uint4 raw, int lane_in_octet,
         // here (d <= max - min, and s is (max - min) / 15 rounded to binary16, at worst halved when it is a binary16
         // subnormal), so |t - fl(d / s)| <= 32 * (2^-23 + 2^-24 + 2^-24) = 2^-17.  rint(t) can differ from
         // rint(fl(d / s)) only if a half-integer lies within that distance of t; such octets (about one element in
-        // 2^15) redo all eight codes with the true division.  v_cvt_pk_u8_f32 rounds to nearest even and saturates
-        // at 0 (checked on the device); quotients reach 15.5 only in the careful path, which clamps them first.
+        // 2^15, and exact ties) look closer, and divide where that does not settle it.  v_cvt_pk_u8_f32 rounds to nearest
+        // even and saturates at 0 (checked on the device); quotients reach 15.5 only where they are divided and clamped.
         // With bfloat16 parameters the bias may lie above the minimum or far below it (|d / s| is then unbounded):
         // groups whose quotients leave [-0.4, 15.4] take the careful path as well.
         const float inv = __builtin_amdgcn_rcpf(s);
@@ -105,8 +105,21 @@ __device__ __forceinline__ uint32_t quantize_octet(uint4 raw, int lane_in_octet,
             careful |= fabsf(__builtin_amdgcn_fractf(t[i]) - 0.5f) <= 0x1p-16f;
         }
         if (careful) {
+            // Most of these are exact ties: inputs and parameters of few bits, with bfloat16 parameters or inputs in nearly every
+            // wave.  One Newton step brings t within 2^-21 of d / s (half an ulp below 16, and an error of 2^-17 times inv's 2^-22); so
+            // where t is more than 2^-17 from a half-integer fl(d / s) rounds to the same integer, and where t s = d without a
+            // remainder (one fused operation, zero only if exact) t is the quotient.  The rest is divided.  9,000 rows of 16 128-wide
+            // heads, four layers, with bfloat16 parameters 66 -> 51 us, with bfloat16 inputs 58 -> 51, with both 70 -> 56.
+            bool divide = (mx - b) * inv >= 15.4f || (BF && (mn - b) * inv <= -0.4f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = fminf(BF ? fmaxf(d[i] / s, 0.0f) : d[i] / s, 15.0f);
+            for (int i = 0; i < 8; ++i) {
+                t[i] = __builtin_fmaf(__builtin_fmaf(-t[i], s, d[i]), inv, t[i]);
+                divide |= fabsf(__builtin_amdgcn_fractf(t[i]) - 0.5f) <= 0x1p-17f && __builtin_fmaf(-t[i], s, d[i]) != 0.0f;
+            }
+            if (divide) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = fminf(BF ? fmaxf(d[i] / s, 0.0f) : d[i] / s, 15.0f);
+            }
         }
         uint32_t even = 0, odd = 0; // codes 0,2,4,6 and 1,3,5,7 as bytes
 #pragma unroll
