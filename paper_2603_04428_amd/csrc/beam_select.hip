@@ -9,10 +9,10 @@
 // While a wave streams its span it does no more than a maximum and an exponential per element (7.5 instruction slots of a
 // bfloat16 one, four of them the exponential's) and notes each lane's maximum of every step.  Those maxima then say how large an
 // element has to be to count, and which lanes of which steps have one: their 64 bytes are read again.  Candidates kept while
-// streaming cost a step in two some 150 instructions more.
+// streaming took 373 vector instructions a step of 2,048 elements, this takes 259 (256 rows of 262,144, the spans' ends included).
 //
 // What bounds it: memory for large batches, where the scan of 256 rows of 262,144 bfloat16 logits (134 MB) takes 28 us, 4.7 TB/s (a
-// kernel that only reads 134 MB: 6.2 to 6.3; waves stream at that rate, but all begin and end at one time); elsewhere the chain of each
+// kernel that only reads 134 MB: 6.2 to 6.3; waves begin within 0.4 us of each other and end between 16 and 29); elsewhere the chain of each
 // wave (a trip to memory, 32 elements a lane, the best of them: 4 us) and of the merge (three trips, logarithms, threshold, ranks: 4
 // us), both of them with instruction fetch in them, and two launches.  Four rows of 32,000 binary16 5.3 + 4.6 us, 72 rows of 50,001 binary32 in 16
 // groups with 16 out 10.1 + 8.8, ten live rows of 80 of 128,000 with 8 out 10.8 + 7.0.
@@ -722,8 +722,8 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
 // Elements of a span: whole steps of a wave, so many that about kWavesPerCu waves per compute unit share the call's rows, and that
 // a wave has four times as many maxima as it keeps elements.  Measured, a call of 256 rows of 262,144 with at most 4 / 8 / 16 steps a
 // span 40.9 / 39.2 / 39.9 us, 64 rows of 128,000 19.3 / 19.4 / 19.7; with 16 waves wanted per compute unit spans are shorter and the merge has more
-// records: ten of 80 rows of 128,000 alive 10.1 + 8.9 us for 11.0 + 7.3.  24 rows of 32,000 with 64 out: a step a span 80 us, four (and
-// a merge of 1,024 threads) 30.
+// records: ten of 80 rows of 128,000 alive 10.1 + 8.9 us for 11.0 + 7.3.  24 rows of 32,000 with 64 out take as long with
+// one step a span as with four, 80 us; what helps there is the wider merge below.
 constexpr int kWavesPerCu = 8;
 int span_length(int vocab, int rows, int num_out, int compute_units)
 {
@@ -785,7 +785,7 @@ hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     // A workgroup of 1,024 where a group's records list more than a chunk of 256 threads: 8 rows of 63 spans with 8 out 8.0 us for
-    // 7.3, of 25 with 16 out 15.9 for 9.8, 24 rows with 64 out 77 for 37 (whole calls).
+    // 7.3, of 25 with 16 out 15.9 for 9.8, 24 rows with 64 out 77 for 37 (these two the whole call).
     if (units * p.num_out > (int64_t)p.groups * kThreads * kTaken)
         hipLaunchKernelGGL(beam_merge_kernel<1024>, dim3((unsigned)p.groups), dim3(1024), 0, stream, p);
     else
