@@ -133,8 +133,9 @@ int q4kv_append(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, c
  *                 spec->v_aliases_k.  in_format: 0 binary16, 1 bfloat16 (of both): a bfloat16 value is rounded once to binary16,
  *                 and must be inside its range
  *   slot          device int32 [num_tokens]: block * 256 + place in the block, the same on every layer.  A token whose slot is
- *                 outside [0, 256 * num_blocks) is skipped (-1 for the tokens that fill a batch up), its rows are not looked at;
- *                 of two tokens with one slot either may be stored, group by group
+ *                 outside [0, 256 * num_blocks) is skipped (-1 for the tokens that fill a batch up): its rows may hold anything, and
+ *                 may be read.  Tokens with one slot are not put in order: each word of codes, scale and bias there is one of
+ *                 theirs, but a group's codes may stand beside another token's scale, so the slot's value means nothing
  * The cache gets the bits that q4kv_append makes of the same rows.  num_tokens > Q4KV_MAX_CHUNK_LEN, pools of 2^23 blocks and
  * more and calls of 2^31 groups and more on a layer -> Q4KV_ERANGE. */
 int q4kv_append_slots(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool *v, const void *k_new, const void *v_new,

@@ -91,3 +91,31 @@ def test_no_tokens():
     b.q4kv_append_slots(spec, kp, vp, none[:0], none[:0], torch.empty(0, dtype=torch.int32, device=DEV), layer_begin=1, layer_end=1)
     torch.cuda.synchronize()
     assert torch.equal(kp.codes, before)
+
+
+@pytest.mark.parametrize("tokens", [40, 9000])                                    # an octet per group; rounds of 64 groups per wave
+def test_one_slot_twice(tokens):
+    """Every word in a slot that two tokens have is one of theirs; all other slots hold what they would hold otherwise."""
+    spec = b.make_spec(1, 8, 8, 128)
+    blocks = tokens // 256 + 2
+    g = torch.Generator(device=DEV).manual_seed(tokens)
+    k, v = (torch.randn((1, tokens, 8, 128), generator=g, device=DEV, dtype=torch.float16) for _ in range(2))
+    first = torch.arange(tokens, dtype=torch.int32, device=DEV)
+    both, last = first.clone(), first.clone()
+    twice = tokens // 4
+    both[-twice:] = first[:twice]                                                 # the last tokens have the first ones' slots
+    last[-twice:] = first[:twice]
+    last[:twice] = -1
+    first[-twice:] = -1
+    held = []
+    for slot in (both, first, last):
+        pools = pools_of(spec, blocks, False, 4)
+        b.q4kv_append_slots(spec, *pools, k, v, slot)
+        held.append(pools)
+    torch.cuda.synchronize()
+    for got, one, other in zip(*held):
+        for name in ("codes", "scale", "bias"):
+            x, y, z = (bits(getattr(p, name)) for p in (got, one, other))
+            assert np.all((x == y) | (x == z))
+            same = y == z                                                         # slots of one token, and of none
+            assert np.array_equal(x[same], y[same]) and not same.all()
