@@ -785,7 +785,7 @@ hipError_t launch_beam_select(const BeamSelectArgs &a, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     // A workgroup of 1,024 where a group's records list more than a chunk of 256 threads: 8 rows of 63 spans with 8 out 8.0 us for
-    // 7.3, of 25 with 16 out 15.9 for 9.8, 24 rows with 64 out 77 for 37 (these two the whole call).
+    // 7.3, of 25 with 16 out 15.9 for 9.8; a whole call of 24 rows with 64 out 77 for 37.
     if (units * p.num_out > (int64_t)p.groups * kThreads * kTaken)
         hipLaunchKernelGGL(beam_merge_kernel<1024>, dim3((unsigned)p.groups), dim3(1024), 0, stream, p);
     else
