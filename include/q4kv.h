@@ -378,7 +378,8 @@ int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool 
  * A block that several rows list is full of tokens that they all have; the block that a row ends in, if it is not full, is its
  * own.  The calls here keep it so.  Free blocks are handed out lowest id first, to rows in order: results are the same on
  * every run.  At most Q4KV_MAX_TABLE_ROWS rows and 2^23 - 1 blocks, 2^31 - 1 tokens a row (Q4KV_ERANGE); calls on one table, or on tables
- * with the same refs, must not overlap in time.  An entry outside [0, num_blocks) is carried along and counted nowhere. */
+ * with the same refs, must not overlap in time.  An entry outside [0, num_blocks) is carried along and counted nowhere.  Tables of no
+ * rows need none of the first three arrays (NULL). */
 #define Q4KV_MAX_TABLE_ROWS 2048
 typedef struct {
     int32_t *block_table, *seq_len, *refs, *refused;

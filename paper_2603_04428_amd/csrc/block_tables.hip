@@ -600,7 +600,7 @@ TablesParams params_of(const TablesArgs &a)
     p.refused = a.tables->refused;
     p.agents = a.tables->num_agents;
     p.max_blocks = a.tables->max_blocks;
-    p.num_blocks = a.tables->num_blocks;
+    p.num_blocks = p.agents > 0 ? a.tables->num_blocks : 0; // a table of no rows may come without counts: none is read
     p.copies = a.spec != nullptr;
     if (p.copies) {
         int32_t *w = static_cast<int32_t *>(a.workspace);

@@ -1,0 +1,28 @@
+"""What include/q4kv.h promises of q4kv_resize_tables and q4kv_beam_reorder where blocks, places or rows are missing."""
+import ctypes as C
+
+import torch
+import pytest
+
+from paper_2603_04428_amd import binding as b
+from tests.gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("blocks", [1, 4, 1024, 1 << 20])
+@pytest.mark.parametrize("places", [0, 3, 5000])
+def test_a_table_of_no_rows_needs_no_arrays(blocks, places):
+    """Neither table nor lengths nor counts: the map says that there are no tokens, and nobody was refused."""
+    refused, begin, slot, agent = ints([77]), ints([77]), torch.full((places + 1,), 77, dtype=torch.int32, device=DEV), ints([77] * (places + 1))
+    t = b._CTables(None, None, None, refused.data_ptr(), 0, 7, blocks)
+    rc = b.lib().q4kv_resize_tables(C.byref(t), None, places, begin.data_ptr(), slot.data_ptr(), agent.data_ptr(), None, None, None, None, None, 0, b._stream())
+    torch.cuda.synchronize()
+    assert rc == 0 and refused.item() == 0
+    assert begin.item() == (0 if places else 77)
+    for x in (slot, agent):
+        assert (x[:places] == -1).all() and x[places] == 77
