@@ -827,10 +827,14 @@ int q4kv_beam_reorder(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool
 {
     int rc = check_tables(tables);
     if (rc || (rc = check_table_pools(tables, spec, k, v, workspace, workspace_bytes))) return rc;
-    if (tables->num_agents == 0) return Q4KV_OK;
-    if (!parent) return fail(Q4KV_EINVAL, "NULL pointer");
     q4kv::TablesArgs a = {};
     a.tables = tables;
+    if (tables->num_agents == 0) { // nobody was refused: what a resize of no rows says, too
+        if (!tables->refused) return Q4KV_OK;
+        const hipError_t e = q4kv::launch_resize_tables(a, (hipStream_t)hip_stream);
+        return e == hipSuccess ? Q4KV_OK : fail(Q4KV_EHIP, "table launch: %s", hipGetErrorString(e));
+    }
+    if (!parent) return fail(Q4KV_EINVAL, "NULL pointer");
     a.spec = spec;
     a.k = k;
     a.v = v;

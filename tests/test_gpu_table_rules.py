@@ -26,3 +26,13 @@ def test_a_table_of_no_rows_needs_no_arrays(blocks, places):
     assert begin.item() == (0 if places else 77)
     for x in (slot, agent):
         assert (x[:places] == -1).all() and x[places] == 77
+
+
+def test_a_reorder_of_no_rows_says_that_nobody_was_refused():
+    spec = b.make_spec(1, 1, 1, 64)
+    kpool, vpool = b.Pool(spec, 64, 4, DEV), b.Pool(spec, 64, 4, DEV)
+    t = b.BlockTables(0, 7, 4, DEV)
+    t.refused.fill_(77)
+    b.q4kv_beam_reorder(spec, kpool, vpool, t, ints([]))
+    torch.cuda.synchronize()
+    assert t.refused.item() == 0
