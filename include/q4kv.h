@@ -376,7 +376,7 @@ int q4kv_copy_blocks(const q4kv_spec *spec, const q4kv_pool *k, const q4kv_pool 
  *                program that keeps blocks for itself (a prompt's image, say) counts itself in
  *   refused      device int32 [1] or NULL: set by every call to the number of rows that did not get what they asked for
  * A block that several rows list is full of tokens that they all have; the block that a row ends in, if it is not full, is its
- * own.  The calls here keep it so.  Free blocks are handed out lowest id first, to rows in order: results are the same on
+ * own.  The calls here keep it so, as far as blocks last.  Free blocks are handed out lowest id first, to rows in order: results are the same on
  * every run.  At most Q4KV_MAX_TABLE_ROWS rows and 2^23 - 1 blocks, 2^31 - 1 tokens a row (Q4KV_ERANGE); calls on one table, or on tables
  * with the same refs, must not overlap in time.  An entry outside [0, num_blocks) is carried along and counted nowhere.  Tables of no
  * rows need none of the first three arrays (NULL). */
@@ -389,19 +389,21 @@ typedef struct {
 /* The agents' lengths become new_len[], and their tables with them: what q4kv_block_pool_reserve, _truncate and _release do for one
  * agent on the host, for all of them at once.
  *   new_len       device int32 [num_agents]: tokens from now on.  0 gives all blocks back, a negative one leaves the row as it is
- * Rows that get shorter free their blocks first, so that the same call can hand them out.  Rows that get longer are served in
- * order up to the first whose blocks are not there, or whose tokens do not fit the map; that one and the growing rows behind it
- * are left as they were (and counted in refused), as is a row whose new length its table cannot list.
+ * Rows that get shorter free their blocks first, so that the same call can hand them out.  Free blocks go to rows in order.  Rows
+ * that get longer are served up to the first whose blocks are not there, or whose tokens do not fit the map; that one and
+ * the growing rows behind it are left as they were (and counted in refused) and take no blocks, as is a row whose new length its table
+ * cannot list.
  * A slot map of the tokens that rows got longer by, agent after agent, for q4kv_append_slots:
  *   max_tokens    places in it; 0: none wanted, and no bound on the tokens
  *   token_begin   device out, int32 [num_agents + 1]: first token of each agent, and their number
  *   slot, token_agent, position   device out, int32 [max_tokens]: block * 256 + place, row, and place in the agent's text of each
  *                 token; -1 behind the last one.  token_agent and position may be NULL
- * With spec and pools (spec NULL: none), a row that goes on, or is cut, inside a block that others list as well gets a copy of
- * that block's first tokens, every layer, and goes on in that (of rows that all end there, and with nobody else listing it, the
- * lowest keeps the block).  Where no block is left for the copy, and without pools, a row that is cut inside a shared block
- * loses what it has of it: its seq_len becomes the multiple of 256 below, and it counts as refused.  Without pools a row that
- * goes on is taken to end in a block of its own.
+ * With spec and pools (spec NULL: none), a row that goes on, or is cut, or stays, inside a block that others list as well gets a copy
+ * of that block's first tokens, every layer, and goes on in that (of rows that all end there, and with nobody else listing it, the
+ * lowest keeps the block; but it gets a copy too where it grows and a row that has more tokens there gets none).  Where no block is
+ * left for the copy, a row that is cut loses what it has of the shared block: its seq_len becomes the multiple of 256 below, and it
+ * counts as refused; a row that stays, or was refused, keeps it, shared as it is.  Without pools all but that lowest row lose what
+ * they have of a shared block that they are cut inside, and a row that goes on is taken to end in a block of its own.
  *   workspace     device scratch of q4kv_tables_workspace_bytes(num_agents) bytes, 16-byte aligned, contents unspecified; not
  *                 needed (NULL) without pools
  * Allocates nothing, never synchronises. */

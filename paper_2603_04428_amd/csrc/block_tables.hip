@@ -49,11 +49,11 @@ struct Shared {
     uint32_t tokens[kRows + 1];
     uint8_t copy[kRows];
     int32_t free[kFree];
-    int32_t key[kHash], lowest[kHash], rows[kHash];
-    uint32_t wave[8][kWide / kWave]; // what the waves tell each other, by the place that asks: one barrier each
+    int32_t key[kHash], lowest[kHash], rows[kHash], left[kHash];
+    uint32_t wave[10][kWide / kWave]; // what the waves tell each other, by the place that asks: one barrier each
     int32_t first_refused, moves, refused;
 };
-enum Place { kGone, kGoneSum, kWidest, kShared, kNeed, kMore, kFound }; // kFound and the one behind it in turns
+enum Place { kGone, kGoneSum, kWidest, kShared, kNeed, kMore, kBehind, kOver, kFound }; // kFound and the one behind it in turns
 
 __device__ __forceinline__ int blocks_of(int tokens) { return (tokens >> 8) + ((tokens & 255) != 0); }
 __device__ __forceinline__ uint32_t sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
@@ -156,7 +156,6 @@ __device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uin
     p.refs[id] = 1;
     if (s.copy[r] && k == 0) {
         const int32_t src = row[at >> 8];
-        count<true>(&p.refs[src], -1);
         row[at >> 8] = id;
         const int m = atomicAdd(&s.moves, 1);
         p.moves.src[m] = src;
@@ -169,20 +168,27 @@ __device__ __forceinline__ void take_block(const TablesParams &p, Shared &s, uin
 
 // Lane's rows kPer t .. : lengths from `before` (blocks up to there are listed) to `after`; rows that get shorter have given their
 // blocks back.  Finds the blocks that rows end in and share, takes free blocks, writes lengths and the map's bounds.
-template <int kThreads>
+//
+// Rows are served in order.  The first growing row that finds too few blocks or places in the map ends that for growing rows; what
+// it and those behind it would have taken is there for the copies of rows that do not grow, as long as blocks last.  Of those
+// a row that was cut, or that a reorder made, loses what it has of a block for which there is no copy, and any other stays in it.
+// GROWS: of a resize; a reorder's rows have their lengths, before and after are the same.
+template <int kThreads, bool GROWS>
 __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const int (&before)[kPer], int (&after)[kPer], int refused)
 {
     const int t = threadIdx.x;
     Counts counts = counts_at(p, (int64_t)t * kRefs); // on their way while rows are looked at
-    bool shared[kPer], copy[kPer];
+    bool shared[kPer], copy[kPer], keeps[kPer]; // keeps: grows, and is the row that goes on in a block of several
     int32_t last[kPer];
     int32_t listed[kPer];
+    int place[kPer];
     bool any = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = kPer * t + i, at = min(before[i], after[i]);
-        shared[i] = copy[i] = false;
+        shared[i] = copy[i] = keeps[i] = false;
         last[i] = -1;
+        place[i] = 0;
         if (r < p.agents && (at & 255) && (p.copies || after[i] < before[i])) {
             last[i] = p.table[(int64_t)r * p.max_blocks + (at >> 8)];
             if ((uint32_t)last[i] < (uint32_t)p.num_blocks) {
@@ -197,16 +203,16 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         s.refused = 0;
         s.first_refused = p.agents;
     }
-    if (__builtin_expect(any_of<kThreads>(s, kShared, any), 0)) {
+    const bool sharing = any_of<kThreads>(s, kShared, any);
+    if (__builtin_expect(sharing, 0)) {
         int places = 64; // twice as many as rows
         while (places < 2 * p.agents) places <<= 1;
         for (int i = t; i < places; i += kThreads) {
             s.key[i] = -1;
             s.lowest[i] = kRows;
-            s.rows[i] = 0;
+            s.rows[i] = s.left[i] = 0;
         }
         __syncthreads();
-        int place[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (!shared[i]) continue;
@@ -222,8 +228,11 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (shared[i]) copy[i] = !(s.lowest[place[i]] == kPer * t + i && s.rows[place[i]] == listed[i]);
+        for (int i = 0; i < kPer; ++i) {
+            if (!shared[i]) continue;
+            copy[i] = !(s.lowest[place[i]] == kPer * t + i && s.rows[place[i]] == listed[i]);
+            keeps[i] = !copy[i] && after[i] > before[i];
+        }
     }
     uint32_t need[kPer], more[kPer];
 #pragma unroll
@@ -239,81 +248,130 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         need[i] = (uint32_t)copy[i] + (uint32_t)max(0, blocks_of(after[i]) - blocks_of(before[i]));
         more[i] = p.max_tokens > 0 ? (uint32_t)max(0, after[i] - before[i]) : 0u;
     }
-    const uint32_t in_need = wave_scan(sat(need[0], need[1])), in_more = wave_scan(sat(more[0], more[1]));
-    if ((t & 63) == 63) {
-        tell(s, kNeed, in_need);
-        tell(s, kMore, in_more);
-    }
-    __syncthreads();
-    uint32_t all_need, all_more;
-    const uint32_t ex_need = prefix<kThreads>(s, kNeed, in_need, all_need), ex_more = prefix<kThreads>(s, kMore, in_more, all_more);
-    const uint32_t first_need[kPer] = {ex_need, sat(ex_need, need[0])}, first_more[kPer] = {ex_more, sat(ex_more, more[0])};
-    // free blocks, lowest first, as far as they are needed
-    uint32_t found = 0;
+    uint32_t found = 0, all_need, all_more;
+    uint32_t first_need[kPer], first_more[kPer];
+    int64_t base = 0; // counts read up to here
     int turn = 0;
+    // Sums of what rows need; free blocks, lowest first, as far as they are needed; the first growing row that cannot be served.
+    auto serve = [&]() __attribute__((always_inline)) {
+        const uint32_t in_need = wave_scan(sat(need[0], need[1])), in_more = wave_scan(sat(more[0], more[1]));
+        if ((t & 63) == 63) {
+            tell(s, kNeed, in_need);
+            tell(s, kMore, in_more);
+        }
+        __syncthreads();
+        first_need[0] = prefix<kThreads>(s, kNeed, in_need, all_need);
+        first_more[0] = prefix<kThreads>(s, kMore, in_more, all_more);
+        first_need[1] = sat(first_need[0], need[0]);
+        first_more[1] = sat(first_more[0], more[0]);
+        if (!(all_need | all_more)) return p.agents; // nobody wants anything
 #pragma unroll 1
-    for (int64_t base = 0; base < p.num_blocks && found < all_need; base += kThreads * kRefs) {
-        const uint32_t bits = free_bits(counts);
-        counts = counts_at(p, base + kThreads * kRefs + (int64_t)t * kRefs);
-        uint32_t all;
-        uint32_t rank = found + scan<kThreads>(s, kFound + turn, __popc(bits), all);
-        turn ^= 1;
+        for (; base < p.num_blocks && found < all_need; base += kThreads * kRefs) {
+            const uint32_t bits = free_bits(counts);
+            counts = counts_at(p, base + kThreads * kRefs + (int64_t)t * kRefs);
+            uint32_t all;
+            uint32_t rank = found + scan<kThreads>(s, kFound + turn, __popc(bits), all);
+            turn ^= 1;
 #pragma unroll 1
-        for (uint32_t b = bits; b && rank < kFree; b &= b - 1, ++rank) s.free[rank] = (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1);
-        found += all;
-    }
-    uint32_t taken = 0, mapped = 0; // blocks and places that are given out
-    if (all_need | all_more) {
-        // rows are served in order up to the first that cannot be
+            for (uint32_t b = bits; b && rank < kFree; b &= b - 1, ++rank) s.free[rank] = (int32_t)(base + (int64_t)t * kRefs + __ffs(b) - 1);
+            found += all;
+        }
+        if (!GROWS) return p.agents;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const bool fails = (need[i] || more[i]) &&
-                               (sat(first_need[i], need[i]) > found || (p.max_tokens > 0 && sat(first_more[i], more[i]) > (uint32_t)p.max_tokens));
+            const bool fails = after[i] > before[i] && ((need[i] && sat(first_need[i], need[i]) > found) ||
+                                                        (p.max_tokens > 0 && sat(first_more[i], more[i]) > (uint32_t)p.max_tokens));
             if (fails) atomicMin(&s.first_refused, kPer * t + i);
         }
         __syncthreads();
-        const int first_refused = s.first_refused;
+        return s.first_refused;
+    };
+    int stop = serve();
+    const bool wanted = (all_need | all_more) != 0;
+    uint32_t taken = min(all_need, found), mapped = all_more; // blocks and places that are given out
+    if (GROWS && __builtin_expect(stop < p.agents || (sharing && wanted), 0)) {
+#pragma unroll 1
+        while (true) {
+            // the items and tokens of the rows in front of the refused one, and behind them the copies of rows that do not grow
+            uint32_t behind[kPer], all_behind;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = kPer * t + i;
+                behind[i] = r > stop && after[i] <= before[i] ? need[i] : 0u;
+                if (r == stop) {
+                    s.items[p.agents] = min(first_need[i], found);
+                    s.tokens[p.agents] = first_more[i];
+                }
+            }
+            const uint32_t ex = scan<kThreads>(s, kBehind, behind[0] + behind[1], all_behind);
+            if (stop < p.agents) {
+                const uint32_t used = s.items[p.agents];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (kPer * t + i >= stop) first_need[i] = used + ex + (i ? behind[0] : 0u);
+                taken = min(used + all_behind, found);
+                mapped = s.tokens[p.agents];
+            }
+            if (!sharing) break;
+            // A row goes on in a block of several only if nobody stays there who has more tokens in it: else it gets a copy as well.
+            bool over = false;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const bool served = after[i] > before[i] ? kPer * t + i < stop : first_need[i] < found;
+                if (copy[i] && !served && after[i] >= before[i]) atomicMax(&s.left[place[i]], before[i] & 255);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (!keeps[i] || kPer * t + i >= stop || s.left[place[i]] <= (before[i] & 255)) continue;
+                keeps[i] = false;
+                copy[i] = over = true;
+                ++need[i];
+            }
+            if (!any_of<kThreads>(s, kOver, over)) break;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (shared[i]) s.left[place[i]] = 0;
+            if (t == 0) s.first_refused = p.agents;
+            stop = serve();
+            taken = min(all_need, found);
+            mapped = all_more;
+        }
+    }
+    bool leaves[kPer] = {}; // the block it shared
+    if (__builtin_expect(sharing, 0)) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int r = kPer * t + i;
-            if (r < p.agents) {
-                if (r >= first_refused && (need[i] || after[i] > before[i])) {
-                    ++refused;
-                    if (after[i] > before[i]) { // stays as it was
-                        after[i] = before[i];
-                    } else {
-                        count<true>(&p.refs[last[i]], -1);
-                        p.table[(int64_t)r * p.max_blocks + (after[i] >> 8)] = -1;
-                        after[i] &= ~255;
-                    }
-                    copy[i] = false;
-                }
-                p.len[r] = after[i];
-                s.before[r] = before[i];
-                s.after[r] = after[i];
-                s.items[r] = first_need[i];
-                s.tokens[r] = first_more[i];
-                s.copy[r] = copy[i];
-            }
-            if (r == first_refused) { // the items and tokens of the rows in front of it
-                s.items[p.agents] = first_need[i];
-                s.tokens[p.agents] = first_more[i];
+            if (!copy[i]) continue;
+            const bool served = GROWS && after[i] > before[i] ? kPer * t + i < stop : first_need[i] < found;
+            leaves[i] = served || !GROWS || after[i] < before[i];
+            copy[i] = served;
+            if (leaves[i] && !served) {
+                p.table[(int64_t)(kPer * t + i) * p.max_blocks + (after[i] >> 8)] = -1;
+                after[i] &= ~255;
+                ++refused;
             }
         }
-        if (t == 0 && first_refused == p.agents) {
-            s.items[p.agents] = all_need;
-            s.tokens[p.agents] = all_more;
-        }
-        if (refused) atomicAdd(&s.refused, refused);
-        __syncthreads();
-        taken = s.items[p.agents];
-        mapped = s.tokens[p.agents];
-    } else { // nobody wants anything
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (kPer * t + i < p.agents) p.len[kPer * t + i] = after[i];
-        if (refused) atomicAdd(&s.refused, refused);
     }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = kPer * t + i;
+        if (r >= p.agents) continue;
+        if (GROWS && r >= stop && after[i] > before[i]) { // stays as it was
+            ++refused;
+            after[i] = before[i];
+        }
+        p.len[r] = after[i];
+        if (wanted) {
+            s.before[r] = before[i];
+            s.after[r] = after[i];
+            s.items[r] = min(first_need[i], taken);
+            s.tokens[r] = min(first_more[i], mapped);
+            s.copy[r] = copy[i];
+        }
+    }
+    if (refused) atomicAdd(&s.refused, refused);
+    if (wanted) __syncthreads();
     uint32_t seen = 0;
     if (__builtin_expect(taken > kFree, 0)) {
         // more than LDS holds: those behind are taken while the counts are read once more (before any of them changes)
@@ -331,8 +389,13 @@ __device__ __forceinline__ void settle(const TablesParams &p, Shared &s, const i
         __syncthreads();
     }
     for (uint32_t i = t; i < min(taken, (uint32_t)kFree); i += kThreads) take_block(p, s, i, s.free[i]);
+    if (__builtin_expect(sharing, 0)) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (leaves[i]) count<true>(&p.refs[last[i]], -1); // behind the last look at the counts: such a block may be free from here on
+    }
     if (p.max_tokens > 0) {
-        for (int r = t; r < p.agents; r += kThreads) p.token_begin[r] = mapped ? (int32_t)min(s.tokens[r], mapped) : 0;
+        for (int r = t; r < p.agents; r += kThreads) p.token_begin[r] = mapped ? (int32_t)s.tokens[r] : 0;
         if (t == 0) p.token_begin[p.agents] = (int32_t)mapped;
     }
     __syncthreads();
@@ -402,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(TablesParams p)
         }
         __syncthreads(); // the counts are read from here on
     }
-    settle<kThreads>(p, s, before, after, refused);
+    settle<kThreads, true>(p, s, before, after, refused);
 }
 
 // The map of a call with many tokens, behind resize_kernel.
@@ -520,7 +583,7 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(TablesParams p)
         before[i] = after[i] = length;
     }
     __syncthreads(); // lengths are read before the first is written, and counts from here on
-    settle<kThreads>(p, s, before, after, 0);
+    settle<kThreads, false>(p, s, before, after, 0);
 }
 
 // The first tokens of blocks copied to other blocks, on every layer.  In every (layer, head) plane of a block the tokens of each of
