@@ -154,6 +154,12 @@ __device__ __forceinline__ double log_wide(double v)
     const double y = (double)(__builtin_amdgcn_logf((float)m) * 0.693147181f); // -0.7 .. 0, to 1e-7
     return (y + __builtin_fma(m, exp_wide(-y), -1.0)) + e * kLn2;
 }
+__device__ __forceinline__ double lane_value(double v, int lane)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 struct Reference {
     float ref, minus[2]; // -ref c
     __device__ __forceinline__ void set(float r)
@@ -282,6 +288,7 @@ __device__ __forceinline__ bool scan_span(const char *row, int begin, int end, i
     Reference at_ref;
     at_ref.set(0.0f);
     bool unset = true;
+    int set_at = begin; // the step whose maximum the reference is
     double sum[2] = {0.0, 0.0};
     const int left = (end - begin) % PER, whole = end - left; // what does not fill a load is one element of `left` lanes more, in the first step
     words_t now[UNROLL] = {}, next[UNROLL] = {};
@@ -322,11 +329,19 @@ __device__ __forceinline__ bool scan_span(const char *row, int begin, int end, i
         if (unset || __any(mine > at_ref.ref + 8.0f)) {
             const float highest = wave_max(mine);
             if (highest > -kInf) {
-                const float scale = unset ? 0.0f : __builtin_amdgcn_exp2f((at_ref.ref - highest) * kLog2e[0]);
-                sum[0] *= scale;
-                sum[1] *= scale;
+                const Reference was = at_ref;
                 at_ref.set(highest);
+                if (__builtin_expect(!unset, 0)) {
+                    // What is there may be nearly all of the sum (many elements just below the limit).  Terms 2^(x c - was c) become
+                    // terms 2^(x c - ref c) with the products as they are rounded: so one factor at the end is right for all of them.
+                    // Odd lanes look at the second constant.
+                    const double moved = lane & 1 ? (double)at_ref.minus[1] - (double)was.minus[1] : (double)at_ref.minus[0] - (double)was.minus[0];
+                    const double scale = exp_wide(CLEAN ? (double)was.ref - (double)highest : kLn2 * moved);
+                    sum[0] *= lane_value(scale, 0);
+                    sum[1] *= lane_value(scale, 1);
+                }
                 unset = false;
+                set_at = at;
             }
         }
         auto term = [&](float x) { return CLEAN ? __builtin_amdgcn_exp2f((x - at_ref.ref) * kLog2e[0]) : at_ref.exp<0>(x); };
@@ -416,11 +431,13 @@ __device__ __forceinline__ bool scan_span(const char *row, int begin, int end, i
         token = begin + step * STEP + (u * kWave + lane) * PER + i % PER;
     }
     listed = keep_best(list, n, keep);
-    // The largest elements dominate the sum of a peaked row: theirs are taken again in binary64.
+    // The largest elements dominate the sum of a peaked row: theirs are taken again in binary64, in the place of the terms that
+    // they were summed as.  (Those that an earlier reference made are not these terms, and stay.)
     double fix = 0.0;
-    if (lane < listed) {
+    const int t = lane < listed ? (int)~(uint32_t)list[lane] : 0;
+    if (lane < listed && (t < whole ? t : begin) >= set_at) {
         const float x = unordered((uint32_t)(list[lane] >> 32));
-        const int t = (int)~(uint32_t)list[lane], o = (t - begin) % STEP;
+        const int o = (t - begin) % STEP;
         fix = exp_wide((double)x - (double)at_ref.ref);
         if (CLEAN) fix -= (double)__builtin_amdgcn_exp2f((x - at_ref.ref) * kLog2e[0]);
         else if (t < whole && upper(o / (kWave * PER), o % PER)) fix -= (double)at_ref.exp<1>(x) * shift[1];
