@@ -446,7 +446,7 @@ size_t q4kv_tables_workspace_bytes(int32_t num_agents);
  *               that overlap in time need one each
  * Totals are formed and compared in binary64, from logarithms that are within (1.1 ln(vocab) + 18) 2^-23 of the true ones, and rounded
  * once to binary32 on their way out; the order within a row is that of its logits, exactly.  Run-to-run identical.  Rows times spans of
- * vocab (of 2,048 tokens at least) below 2^26, at most 2^22 - 1 groups, vocab at most 2^30 (Q4KV_ERANGE).  Allocates nothing, never
+ * vocab (of 2,048 tokens at least) at most 2^26 - 4, at most 2^22 - 1 groups, vocab at most 2^30 (Q4KV_ERANGE).  Allocates nothing, never
  * synchronises. */
 #define Q4KV_MAX_BEAM_OUT 64
 int q4kv_beam_select(const void *logits, int32_t logits_format, int64_t row_stride, int32_t vocab, int32_t num_agents, const float *score,

@@ -852,7 +852,8 @@ static int check_beam_sizes(int32_t format, int32_t vocab, int32_t num_agents, i
     if (vocab <= 0 || num_agents < 0) return fail(Q4KV_EINVAL, "negative count");
     if (vocab > 1 << 30) return fail(Q4KV_ERANGE, "a vocabulary of %d tokens, at most 2^30", vocab);
     if (num_out < 1 || num_out > Q4KV_MAX_BEAM_OUT) return fail(Q4KV_ERANGE, "num_out %d, from 1 to %d", num_out, Q4KV_MAX_BEAM_OUT);
-    if ((int64_t)num_agents * q4kv::beam_select_spans(vocab, num_agents, num_out, compute_units()) >= 1LL << 26)
+    // four spans to a workgroup of 256, and a grid has less than 2^32 threads
+    if ((int64_t)num_agents * q4kv::beam_select_spans(vocab, num_agents, num_out, compute_units()) > (1LL << 26) - 4)
         return fail(Q4KV_ERANGE, "%d rows of %d tokens: choose for fewer groups at a time", num_agents, vocab);
     return Q4KV_OK;
 }
