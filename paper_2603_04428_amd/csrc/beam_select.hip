@@ -139,7 +139,7 @@ __device__ __forceinline__ double exp_series(double r)
     }
     return y;
 }
-// exp d for d <= 1, -inf as well, to 1e-12: 2^n times the series of what is left of d
+// exp d for d up to some 9 (an element over its span's reference), -inf as well, to 1e-12: 2^n times the series of what is left of d
 __device__ __forceinline__ double exp_wide(double d)
 {
     d = fmax(d, -1000.0);
@@ -625,7 +625,8 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(SelectParams p)
         int valid = 0;
 #pragma unroll
         for (int e = 0; e < kTaken; ++e) {
-            // at most 1,025 rows further on: the quotient is one off at most
+            // `at` is below per_row + kTaken * THREADS, so at most that many rows further on, 4,096: a quotient of that size is off by
+            // less than 2^-10 in binary32, and one off at most as an integer
             const uint32_t at = offset + e * kThreads;
             uint32_t row = (uint32_t)((float)at * one_row);
             if (at < row * per_row) --row;
