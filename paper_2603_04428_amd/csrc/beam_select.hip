@@ -6,16 +6,19 @@
 // num_out largest elements in order.  A second kernel, one workgroup per group, adds the sums up, forms the totals of what the
 // records list and takes the best.  Two launches, no atomics on memory, and the same order of every sum on every run.
 //
-// While a wave streams its span it does no more than a maximum and an exponential per element (7.5 instruction slots of a
-// bfloat16 one, four of them the exponential's) and notes each lane's maximum of every step.  Those maxima then say how large an
-// element has to be to count, and which lanes of which steps have one: their 64 bytes are read again.  Candidates kept while
-// streaming took 373 vector instructions a step of 2,048 elements, this takes 259 (256 rows of 262,144, the spans' ends included).
+// While a wave streams its span it does no more than a maximum and an exponential per element (5.2 instructions of a
+// bfloat16 one, and by the counters one slot more for the exponential) and notes each lane's maximum of every step.  Those maxima
+// then say how large an element has to be to count, and which lanes of which steps have one: their 64 bytes are read again.
+// Candidates kept while streaming took 1.4 times the vector instructions, the spans' ends included.
 //
-// What bounds it: memory for large batches, where the scan of 256 rows of 262,144 bfloat16 logits (134 MB) takes 28 us, 4.7 TB/s (a
-// kernel that only reads 134 MB: 6.2 to 6.3; waves begin within 0.4 us of each other and end between 16 and 29); elsewhere the chain of each
-// wave (a trip to memory, 32 elements a lane, the best of them: 4 us) and of the merge (three trips, logarithms, threshold, ranks: 4
-// us), both of them with instruction fetch in them, and two launches.  Four rows of 32,000 binary16 5.3 + 4.6 us, 72 rows of 50,001 binary32 in 16
-// groups with 16 out 10.1 + 8.8, ten live rows of 80 of 128,000 with 8 out 10.8 + 7.0.
+// What bounds it, for large batches: 247 live rows of 262,144 bfloat16 logits (129 MB) take 28 us, 4.6 TB/s.  Reading alone is 21 us of
+// that (a kernel that only reads: 6.2 to 6.3 TB/s), issue 16 (9.8 million quad-cycles of the vector units), and neither is behind the
+// other: all waves are on the chip at once (they begin within 0.4 us of each other and end between 16 and 29), stream at the same time,
+// and then are at their ends at the same time, with 106 of their 272 vector instructions a step and a trip to memory for each step
+// that is read again.  Elsewhere it is the chain of each wave (a trip to memory, 32 elements a lane, the best of them: 4 us) and of the
+// merge (three trips, logarithms, threshold, ranks: 4 us), both of them with instruction fetch in them, and two launches.  Four rows
+// of 32,000 binary16 5.4 + 4.6 us, 72 rows of 50,001 binary32 in 16 groups with 16 out 10.5 + 8.4, ten live rows of 80 of 128,000 with 8 out
+// 11.0 + 7.0.
 #include "q4_device.h"
 #include "q4kv_internal.h"
 

@@ -8,9 +8,11 @@
 // enough free ones are found.  Work of uneven size per row (blocks freed, blocks taken, tokens mapped) is laid out flat and the row
 // of an item found by bisection in the prefix sums.
 //
-// Measured (kernel times): 40 rows a token longer 4.1 us, back 3.2; 500 rows of 15,500 blocks with 2,800 tokens mapped 8.2, back 4.6; 400
-// prompts of 299,000 tokens admitted 6.5 and their map 4.4, released 5.4; rows of 4, 40 and 64 beams gathered 7.3, 8.6 and 8.6.  A wide call's
+// Measured (kernel times): 40 rows a token longer 4.1 us, back 3.3; 500 rows of 15,500 blocks with 2,800 tokens mapped 8.1, back 4.7; 400
+// prompts of 299,000 tokens admitted 6.2 and their map 4.4, released 5.5; rows of 4, 40 and 64 beams gathered 6.7, 8.2 and 8.2.  A wide call's
 // time stamps (10,700 clocks) lie 600 to 2,100 clocks apart: no step of it is long, and none can begin before the one in front of it has ended.
+// What is done where rows are refused or share their last blocks stands beside the straight path, not in a loop around it: in a loop
+// the same calls took 0.2 us longer.
 //
 // A block in which a row ends and that others list too is copied by a kernel of its own (the pools of all layers; HBM-bound).
 #include "q4_device.h"

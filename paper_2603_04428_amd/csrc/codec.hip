@@ -251,8 +251,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams pp)
 // heads of the same tokens.  So the tokens' rows, which a fused projection sets far apart, are read whole at about one time, and
 // what is written is a run of one head's plane wherever tokens have consecutive slots.  9,000 tokens, four layers of 8 + 8 heads, us by
 // this kernel / the one above on the same rows: 128-wide binary16 46 / 51 (out of a fused projection 49), 256-wide 82 / 97, 64-wide
-// (16 + 16) 45 / 45, 128-wide with bfloat16 parameters 52 / 52, with bfloat16 rows 52; the bytes at a copy's rate 37, 74, 37.  Vector
-// instructions, 160 of them for 8 groups of bfloat16 rows, take what memory leaves.
+// (16 + 16) 45 / 45, 128-wide with bfloat16 parameters 52 / 52, with bfloat16 rows 52; the bytes at a copy's rate 37, 74, 37.  Bfloat16
+// rows and parameters together take 58 for 37 of bytes: 160 vector instructions for 8 groups are 38 us of issue, and as a step
+// waits for its own two loads with nothing asked for ahead, the two are side by side for some 17 us only.
 template <bool BF, bool IN_BF>
 __global__ __launch_bounds__(kThreads) void append_slots_kernel(AppendParams p)
 {
