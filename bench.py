@@ -37,23 +37,23 @@ CODEC_FILES = ("codec.hip", "quantize_octet.h", "q4_device.h", "q4kv_internal.h"
 CHUNK_FILES = ("chunk_attention.hip", "chunk_rules.h", "q4_device.h", "q4kv_internal.h")
 MEASURED_TRAFFIC = {
     "gemma12b_10agents_48layers_ragged_1k_8k_decode": {
-        "read": 4786221758, "written": 20898816, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": DECODE_FILES, "sources": "f7aec25374b9"},
+        "read": 4786592232, "written": 20898816, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": DECODE_FILES, "sources": "72e53ce4ae27"},
     "llama8b_5agents_32layers_4k_decode": {
-        "read": 767855100, "written": 8134656, "file": "profiles/decode_attention_llama8b_5x4k.md",
-        "files": DECODE_FILES, "sources": "f7aec25374b9"},
+        "read": 767903656, "written": 8134656, "file": "profiles/decode_attention_llama8b_5x4k.md",
+        "files": DECODE_FILES, "sources": "72e53ce4ae27"},
     "dsv2lite_mla_per_head_5agents_27layers_8k_decode": {
-        "read": 3190043027, "written": 2958848, "file": "profiles/decode_attention_mla_per_head_5x8k.md",
-        "files": DECODE_FILES, "sources": "f7aec25374b9"},
+        "read": 3190092750, "written": 2958848, "file": "profiles/decode_attention_mla_per_head_5x8k.md",
+        "files": DECODE_FILES, "sources": "72e53ce4ae27"},
     "dsv2lite_mla_latent_5agents_27layers_32k_decode": {
-        "read": 1442821165, "written": 37889439, "file": "profiles/mla_decode_dsv2lite_5x32k.md",
-        "files": LATENT_FILES, "sources": "3998b41874f3"},
+        "read": 1442839654, "written": 37894570, "file": "profiles/mla_decode_dsv2lite_5x32k.md",
+        "files": LATENT_FILES, "sources": "4c2ee7b5a0d4"},
     "quantize_4k_cache": {
-        "read": 1610806109, "written": 452984832, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": CODEC_FILES, "sources": "3ae135dcacab"},
+        "read": 1610878452, "written": 452984832, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": CODEC_FILES, "sources": "5c70ef093bf6"},
     "dequantize_4k_cache": {
-        "read": 453040946, "written": 1610613219, "file": "profiles/decode_attention_gemma10_ragged.md",
-        "files": CODEC_FILES, "sources": "3ae135dcacab"},
+        "read": 453048432, "written": 1610616189, "file": "profiles/decode_attention_gemma10_ragged.md",
+        "files": CODEC_FILES, "sources": "5c70ef093bf6"},
 }
 
 
